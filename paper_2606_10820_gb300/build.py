@@ -45,7 +45,7 @@ def _digest(nvcc: str) -> str:
     h.update(nvcc.encode())
     h.update(os.uname().machine.encode())
     for f in _sources() + sorted(glob.glob(os.path.join(CSRC, "*.cuh"))) + \
-            [os.path.join(ROOT, "include", "kforcing.h"), os.path.join(ROOT, "include", "kforcing_ops.h")]:
+            sorted(glob.glob(os.path.join(ROOT, "include", "*.h"))):
         if os.path.exists(f):
             h.update(f.encode())
             with open(f, "rb") as fh:

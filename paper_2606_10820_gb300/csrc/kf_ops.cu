@@ -4,6 +4,7 @@
 
 #include "../../include/kforcing_ops.h"
 #include "kf_internal.cuh"
+#include "kf_serving.cuh"
 
 using namespace kf;
 
@@ -209,9 +210,35 @@ extern "C" int kf_op_head_tokens_noalloc(int32_t rows, int32_t V, int32_t d, con
   return head_tokens(rows, V, d, x, w_head, noise, tau, map_kind, tokens, sc.rec, sc.err, s);
 }
 
+// ------------------------------------------------------ serving operators
+static __device__ __align__(256) int g_serving_err;
+
+namespace {
+int* g_serving_word[kMaxDevices];
+std::mutex g_serving_mu;
+}  // namespace
+
+namespace kf {
+int* serving_error_word() {
+  int dev = 0;
+  if (current_device(&dev) != KF_OK) return nullptr;
+  std::lock_guard<std::mutex> lock(g_serving_mu);
+  if (!g_serving_word[dev]) {
+    void* e = nullptr;
+    if (cudaGetSymbolAddress(&e, g_serving_err) != cudaSuccess) {
+      cudaGetLastError();
+      return nullptr;
+    }
+    g_serving_word[dev] = static_cast<int*>(e);
+  }
+  return g_serving_word[dev];
+}
+}  // namespace kf
+
 // Reads and clears the error words of the op entry points on the current
 // device after `stream` finishes: the allocating entries' word (if one of
-// them has run on this device) and the no-allocation entry's static word.
+// them has run on this device), the no-allocation entry's static word and the
+// serving operators'.
 // Allocates nothing.
 extern "C" int kf_op_status(void* stream) {
   int dev = 0;
@@ -238,6 +265,12 @@ extern "C" int kf_op_status(void* stream) {
   const int zero = 0;
   if (cudaMemcpyFromSymbol(&v, g_noalloc_err, sizeof(int)) != cudaSuccess ||
       cudaMemcpyToSymbol(g_noalloc_err, &zero, sizeof(int)) != cudaSuccess) {
+    cudaGetLastError();
+    return KF_E_CUDA;
+  }
+  bits |= v;
+  if (cudaMemcpyFromSymbol(&v, g_serving_err, sizeof(int)) != cudaSuccess ||
+      (v && cudaMemcpyToSymbol(g_serving_err, &zero, sizeof(int)) != cudaSuccess)) {
     cudaGetLastError();
     return KF_E_CUDA;
   }

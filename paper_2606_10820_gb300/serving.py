@@ -1,0 +1,123 @@
+"""Serving operators of libkforcing.so on torch tensors (include/kforcing_serving.h).
+
+Argument checks and marshalling only: every operator runs in the CUDA library, on the
+current torch stream of its tensors' device, without synchronising.  What a call
+refuses raises ``KfError`` (the library's own checks) or ``ValueError`` (shapes,
+types, devices); what only the device can see is reported by ``status()``.
+Outputs and scratch come from torch's allocator, so they belong to the current
+stream; tensors that are made on another stream need that stream's work
+to be waited for, as with any torch operator.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import torch
+
+from . import kforcing as kf
+
+DEV_BAD_TOKEN, DEV_BAD_PAGE, DEV_TIMEOUT, DEV_BAD_ROW, DEV_NO_PAGES = 1, 2, 4, 8, 32
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_I32, _I64, _F32, _VP = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
+_SIGNATURES = {
+    "kf_op_token_scores": (ctypes.c_int, [_I32, _I64, _I32, _VP, _I64, _VP, _F32, _I32] + [_VP] * 6),
+    "kf_op_token_scores_grad": (ctypes.c_int, [_I32, _I64, _I32, _VP, _I64, _VP, _F32] + [_VP] * 6 + [_I64, _VP]),
+    "kf_op_status": (ctypes.c_int, [_VP]),
+}
+_lib = None
+
+
+def _library():
+    global _lib
+    if _lib is None:
+        lib = kf.load_library()
+        for name, (res, args) in _SIGNATURES.items():
+            f = getattr(lib, name)
+            f.restype, f.argtypes = res, args
+        _lib = lib
+    return _lib
+
+
+def _stream(t):
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _run(name, device, *args):
+    """One call of the library with `device` current (argument checks come first)."""
+    f = getattr(_lib or _library(), name)
+    if torch.cuda.current_device() == device.index:
+        rc = f(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = f(*args)
+    if rc:
+        kf._check(rc)
+
+
+def _on(t, device, dtype, shape, what):
+    if t.dtype != dtype or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} tensor {tuple(shape)} on {device} is wanted, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def status(device=None):
+    """Waits for the current stream; raises KfError (KF_E_DEVICE) if an operator has flagged
+    an error on this device since the last call."""
+    with torch.cuda.device(device if device is not None else torch.cuda.current_device()):
+        kf._check(_library().kf_op_status(torch.cuda.current_stream().cuda_stream))
+
+
+# ------------------------------------------------------------------ scores
+
+def _score_args(logits, tokens, tau):
+    _need(logits.is_cuda and logits.dim() == 2 and logits.dtype in _TYPES, "logits: a 2-D fp32, bf16 or fp16 CUDA tensor")
+    R, V = logits.shape
+    _need(V > 0 and (logits.stride(1) == 1 or V == 1), "logits: rows of contiguous elements")
+    stride = logits.stride(0) if R > 1 else V
+    _need(stride >= V, "logits: rows that do not overlap")
+    return R, V, stride, _on(tokens, logits.device, torch.int64, (R,), "tokens")
+
+
+def token_scores(logits, tokens, top=0, tau=1.0):
+    """Scores of ``tokens`` [R] (int64; negative: padding) under ``logits`` [R, V] / tau: a dict of
+    ``logp``, ``entropy`` and ``lse`` [R] fp32 and, with top > 0, ``top_ids`` [R, top] int32 and
+    ``top_logp`` [R, top] fp32 of the likeliest tokens (ties: the lowest id first)."""
+    R, V, stride, tok = _score_args(logits, tokens, tau)
+    _need(0 <= top <= min(64, V), "top: 0 to 64, and at most the vocabulary")
+    dev = logits.device
+    nums = torch.empty((3, R), dtype=torch.float32, device=dev)
+    out = {"logp": nums[0], "entropy": nums[1], "lse": nums[2]}
+    p = nums.data_ptr()
+    ids = lps = None
+    if top:
+        out["top_ids"] = ids = torch.empty((R, top), dtype=torch.int32, device=dev)
+        out["top_logp"] = lps = torch.empty((R, top), dtype=torch.float32, device=dev)
+        ids, lps = ids.data_ptr(), lps.data_ptr()
+    _run("kf_op_token_scores", dev, _TYPES[logits.dtype], R, V, logits.data_ptr(), stride, tok, tau, top, p, p + 4 * R,
+         p + 8 * R, ids, lps, _stream(logits))
+    return out
+
+
+def token_scores_grad(logits, tokens, g_logp=None, g_entropy=None, tau=1.0, out=None):
+    """The scores and the gradient of ``sum(g_logp * logp + g_entropy * entropy)``: a dict of
+    ``logp``, ``entropy``, ``lse`` [R] fp32 and ``grad`` [R, V] in the logits' type (``out``, which may be
+    the logits themselves, where it is given)."""
+    R, V, stride, tok = _score_args(logits, tokens, tau)
+    dev = logits.device
+    gl, gh = (None if g is None else _on(g, dev, torch.float32, (R,), n) for g, n in ((g_logp, "g_logp"), (g_entropy, "g_entropy")))
+    grad = torch.empty((R, V), dtype=logits.dtype, device=dev) if out is None else out
+    if out is not None:
+        _need(out.dtype == logits.dtype and out.device == dev and out.shape == logits.shape and (out.stride(1) == 1 or V == 1),
+              "out: a tensor like the logits")
+    nums = torch.empty((3, R), dtype=torch.float32, device=dev)
+    p = nums.data_ptr()
+    _run("kf_op_token_scores_grad", dev, _TYPES[logits.dtype], R, V, logits.data_ptr(), stride, tok, tau, gl, gh, p, p + 4 * R,
+         p + 8 * R, grad.data_ptr(), grad.stride(0) if R > 1 else V, _stream(logits))
+    return {"logp": nums[0], "entropy": nums[1], "lse": nums[2], "grad": grad}
