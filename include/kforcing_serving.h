@@ -1,6 +1,7 @@
 /*
- * kforcing_serving.h - serving operators of libkforcing.so: scores of tokens
- * with their gradient.
+ * kforcing_serving.h - serving operators of libkforcing.so for models with
+ * grouped heads over a paged cache: attention of the newest rows, and scores
+ * of tokens with their gradient.
  *
  * Device pointers only, caller-owned; work is enqueued on `stream`
  * (cudaStream_t, NULL = legacy default) and nothing is allocated or
@@ -36,6 +37,30 @@ extern "C" {
 #define KF_DEV_TIMEOUT 4       /* a bounded wait ran out                         */
 #define KF_DEV_BAD_ROW 8       /* a slot, length or start out of range           */
 #define KF_DEV_NO_PAGES 32     /* not enough free pages                          */
+
+/*
+ * Attention of the newest `rows` rows of each of B sequences over a paged
+ * cache that already holds their own K and V: with len = lens[b], row i of
+ * sequence b is token len - rows + i and sees keys 0 .. len - rows + i.  A row
+ * that sees no key (len < rows) is zeros.  rows = 1 is the ordinary decode
+ * step, rows = P + k a joint one.
+ * type: KF_TYPE_BF16 or KF_TYPE_FP16; hd: 64 or 128; Hq a multiple of Hkv.
+ * q [B][rows][Hq][hd] with strides q_seq / q_row / q_head (multiples of 8
+ * elements); out [B][rows][Hq][hd] contiguous.
+ * pool: one layer's pages [n_pages][2: K, V][Hkv][page][hd], contiguous, page a
+ * multiple of 16; table: int32 [B][width] page ids; lens: int32 [B], 0 ..
+ * width * page.  Scores, maxima, sums and the accumulation are fp32.
+ * KV beyond a sequence's length is never used, whatever it holds.
+ * A page id outside the pool: KF_DEV_BAD_PAGE, its keys count as unseen.
+ * A length outside 0 .. width * page: KF_DEV_BAD_ROW, clamped.
+ * The same lengths give the same bits, whatever the pages' order.
+ * Errors: KF_E_ARG, KF_E_CUDA.
+ */
+int64_t kf_op_paged_attention_work(int32_t hd);
+int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd,
+                          const void* q, int64_t q_seq, int64_t q_row, int64_t q_head, const void* pool,
+                          int64_t n_pages, int32_t page, const int32_t* table, int32_t width,
+                          const int32_t* lens, float scale, void* out, void* work, void* stream);
 
 /*
  * Scores of R rows of logits [R][V] (type fp32, bf16 or fp16; rows `stride`

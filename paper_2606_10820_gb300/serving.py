@@ -23,6 +23,8 @@ _I32, _I64, _F32, _VP = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c
 _SIGNATURES = {
     "kf_op_token_scores": (ctypes.c_int, [_I32, _I64, _I32, _VP, _I64, _VP, _F32, _I32] + [_VP] * 6),
     "kf_op_token_scores_grad": (ctypes.c_int, [_I32, _I64, _I32, _VP, _I64, _VP, _F32] + [_VP] * 6 + [_I64, _VP]),
+    "kf_op_paged_attention_work": (_I64, [_I32]),
+    "kf_op_paged_attention": (ctypes.c_int, [_I32] * 6 + [_VP] + [_I64] * 3 + [_VP, _I64, _I32, _VP, _I32, _VP, _F32] + [_VP] * 3),
     "kf_op_status": (ctypes.c_int, [_VP]),
 }
 _lib = None
@@ -72,6 +74,45 @@ def status(device=None):
     an error on this device since the last call."""
     with torch.cuda.device(device if device is not None else torch.cuda.current_device()):
         kf._check(_library().kf_op_status(torch.cuda.current_stream().cuda_stream))
+
+
+# --------------------------------------------------------------- attention
+
+_HALF = {torch.bfloat16: 1, torch.float16: 2}
+_work_bytes = {}
+
+
+def _scratch(name, device, *args):
+    """Scratch of a call, from torch's allocator (one tensor per call: calls on several streams may overlap)."""
+    key = (name, device.index, args)
+    n = _work_bytes.get(key)
+    if n is None:
+        with torch.cuda.device(device):
+            n = _work_bytes[key] = max(16, getattr(_lib or _library(), name)(*args))
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def paged_attention(q, pool, table, lens, scale=None, out=None):
+    """Attention of the newest rows of each sequence over a paged cache that holds their K and V.
+
+    q [B, rows, Hq, hd] (bf16 or fp16; any strides but the last); pool [pages, 2, Hkv, page, hd],
+    one layer's K and V; table [B, width] int32; lens [B] int32, the tokens of each sequence with the
+    new rows.  Row i sees keys 0 .. lens - rows + i; a row that sees none is zeros.  scale: 1 / sqrt(hd)."""
+    _need(q.is_cuda and q.dim() == 4 and pool.dim() == 5 and table.dim() == 2 and q.dtype in _HALF,
+          "q: [B, rows, Hq, hd], pool: [pages, 2, Hkv, page, hd], table: [B, width], bf16 or fp16 on a GPU")
+    B, rows, Hq, hd = q.shape
+    n_pages, two, Hkv, page, _ = pool.shape
+    dev = q.device
+    _need(two == 2 and q.stride(3) == 1, "pool: K and V of each page; q: heads of contiguous elements")
+    if out is None:
+        out = torch.empty((B, rows, Hq, hd), dtype=q.dtype, device=dev)
+    work = _scratch("kf_op_paged_attention_work", dev, hd)
+    width = table.shape[1]
+    _run("kf_op_paged_attention", dev, _HALF[q.dtype], B, rows, Hq, Hkv, hd, q.data_ptr(), q.stride(0), q.stride(1), q.stride(2),
+         _on(pool, dev, q.dtype, (n_pages, 2, Hkv, page, hd), "pool"), n_pages, page,
+         _on(table, dev, torch.int32, (B, width), "table"), width, _on(lens, dev, torch.int32, (B,), "lens"),
+         1.0 / math.sqrt(hd) if scale is None else scale, _on(out, dev, q.dtype, q.shape, "out"), work.data_ptr(), _stream(q))
+    return out
 
 
 # ------------------------------------------------------------------ scores
