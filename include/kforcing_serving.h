@@ -1,7 +1,8 @@
 /*
  * kforcing_serving.h - serving operators of libkforcing.so for models with
- * grouped heads over a paged cache: attention of the newest rows, and scores
- * of tokens with their gradient.
+ * grouped heads over a paged cache: attention of the newest rows, the
+ * cache's pages (room, append, fork, free, compact, copy), and scores of tokens
+ * with their gradient.
  *
  * Device pointers only, caller-owned; work is enqueued on `stream`
  * (cudaStream_t, NULL = legacy default) and nothing is allocated or
@@ -61,6 +62,65 @@ int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int
                           const void* q, int64_t q_seq, int64_t q_row, int64_t q_head, const void* pool,
                           int64_t n_pages, int32_t page, const int32_t* table, int32_t width,
                           const int32_t* lens, float scale, void* out, void* work, void* stream);
+
+/*
+ * The book of a cache: ref int32 [n_pages], the references to each page (0:
+ * free); table int32 [slots][width], the pages of each sequence in order (-1:
+ * none); lens int32 [slots], its tokens.  A sequence of len tokens has
+ * ceil(len / page) pages.  Calls change it in place, in stream order.  Pages
+ * are handed out lowest id first, in the order of the call's list and then of
+ * the table's columns, so a book and a call give one result.
+ * A call that cannot be done as a whole (a slot out of range or twice in a
+ * list, a length past width * page, pages run out, a table that contradicts the
+ * references) sets KF_DEV_BAD_ROW, KF_DEV_NO_PAGES or KF_DEV_BAD_PAGE and
+ * leaves book and pool as they were.
+ *
+ * kf_op_pages_grow: slot slots[i] (i < n, all different) gets pages for
+ *   new_lens[i] >= lens tokens, and that length.
+ * kf_op_pages_free: the listed slots (all different) give up their pages:
+ *   each reference count falls by one, the table row becomes -1, the length 0.
+ * kf_op_pages_fork: the sequence of slot src[i] continues in slot dst[i] too (all
+ *   dst different, empty and no src): full pages are shared (one reference more), a
+ *   last page that is not full is copied to a page of its own, in every layer of the pool,
+ *   so appending to either never touches the other.
+ * kf_op_pages_compact: with L live pages, the i-th lowest live page at or above L moves to
+ *   the i-th lowest free page below L, in every layer; tables and references
+ *   follow, and live (int32, device, or NULL) receives L.  Page ids >= L are free afterwards.
+ * kf_op_pages_copy: page src[i] to page dst[i], in every layer; the dst pages are
+ *   different from each other and from every src.  Ids outside the pool: KF_DEV_BAD_PAGE, that copy is
+ *   left out.
+ * pool: [layers][n_pages][page_bytes], page_bytes a multiple of 16.
+ * Errors: KF_E_ARG, KF_E_CUDA.
+ */
+int64_t kf_op_pages_work(int32_t n_pages, int32_t slots, int32_t n);
+int kf_op_pages_grow(int32_t n, const int32_t* which, const int32_t* new_lens, int32_t* ref, int32_t n_pages,
+                     int32_t* table, int32_t slots, int32_t width, int32_t* lens, int32_t page, void* work,
+                     void* stream);
+int kf_op_pages_free(int32_t n, const int32_t* which, int32_t* ref, int32_t n_pages, int32_t* table,
+                     int32_t slots, int32_t width, int32_t* lens, int32_t page, void* work, void* stream);
+int kf_op_pages_fork(int32_t n, const int32_t* src, const int32_t* dst, int32_t* ref, int32_t n_pages,
+                     int32_t* table, int32_t slots, int32_t width, int32_t* lens, int32_t page, void* pool,
+                     int32_t layers, int64_t page_bytes, void* work, void* stream);
+int kf_op_pages_compact(int32_t* ref, int32_t n_pages, int32_t* table, int32_t slots, int32_t width,
+                        void* pool, int32_t layers, int64_t page_bytes, int32_t* live, void* work,
+                        void* stream);
+int kf_op_pages_copy(int32_t n, const int32_t* src, const int32_t* dst, void* pool, int32_t layers,
+                     int32_t n_pages, int64_t page_bytes, void* stream);
+
+/*
+ * K and V rows of new tokens into their pages of one layer: rows starts[i] ..
+ * starts[i+1]-1 of k and v (T rows of Hkv heads, strides in elements, multiples of
+ * 8; 16-bit elements) are the last tokens of slot which[i], at positions lens[slot]
+ * - count .. lens[slot] - 1.  pool: that layer's [n_pages][2][Hkv][page][hd], hd a
+ * multiple of 8.  The pages must not be shared (kf_op_pages_fork leaves none of them so).
+ * A token whose slot, position or page is out of range: KF_DEV_BAD_ROW or
+ * KF_DEV_BAD_PAGE, and it is not written.
+ * Errors: KF_E_ARG, KF_E_CUDA.
+ */
+int kf_op_pages_append(int32_t n, const int32_t* which, const int32_t* starts, int64_t T, int32_t Hkv,
+                       int32_t hd, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row,
+                       int64_t v_head, void* pool, int32_t n_pages, int32_t page, const int32_t* table,
+                       int32_t slots, int32_t width, const int32_t* lens, void* stream);
 
 /*
  * Scores of R rows of logits [R][V] (type fp32, bf16 or fp16; rows `stride`

@@ -1,0 +1,570 @@
+// The pages of a paged cache: room, fork, free, compact, copy and append
+// (kf_op_pages_*).
+//
+// The book (references of each page, page table, lengths) lives on the device, so
+// that a scheduler's calls need no readback and can be captured.  One team of 1024 threads,
+// or of a cluster of 8 x 1024 where the book is large, does a call's whole bookkeeping in one
+// launch: it checks everything first and writes only when all of it can be
+// done.  Free pages are found by counting: each warp counts its stretch of the
+// references by ballots, the counts before it give the rank of its first one, so
+// the i-th lowest free page goes to the i-th request whatever the team's size.
+// Page contents are moved by a second, dependent launch over all SMs that
+// reads the list of moves (its bound: HBM, each moved byte read and written once).
+#include <algorithm>
+#include <cooperative_groups.h>
+
+#include "kf_serving.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace kf {
+namespace {
+
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kTeam = 8;                  // CTAs of a large book's team
+constexpr int kCopyThreads = 256, kCopyUnit = kCopyThreads * 4 * 16;   // bytes that a CTA copies at a time
+
+struct Book {
+  int32_t *ref, *table, *lens;
+  int n_pages, slots, width, page;
+};
+// the scratch of a call: a stamp per slot, an offset per request, lists of
+// pages, and where a moved page went
+struct Work {
+  int32_t *count, *mark, *off, *src, *dst, *to;
+};
+
+struct Shared {
+  int flag;
+  int warp[2][kWarps];
+  int scan[kWarps];
+};
+
+template <int C>
+struct Team {
+  Shared& sh;
+  int t, lane, warp, rank, id;
+  __device__ __forceinline__ explicit Team(Shared& s) : sh(s) {
+    t = threadIdx.x;
+    lane = t & 31;
+    warp = t >> 5;
+    rank = C > 1 ? blockIdx.x : 0;
+    id = rank * kThreads + t;
+    if (t == 0) sh.flag = 0;
+    sync();
+  }
+  static constexpr int size = C * kThreads;
+  __device__ __forceinline__ void sync() const {
+    if constexpr (C > 1) cg::this_cluster().sync();
+    else __syncthreads();
+  }
+  __device__ __forceinline__ const Shared* of(int c) const {
+    if constexpr (C > 1) return cg::this_cluster().map_shared_rank(&sh, c);
+    else return &sh;
+  }
+  // all threads' bits so far (also orders their memory accesses)
+  __device__ __forceinline__ int any(int bits) const {
+    if (bits) atomicOr(&sh.flag, bits);
+    sync();
+    int all = 0;
+    for (int c = 0; c < C; ++c) all |= of(c)->flag;
+    sync();
+    return all;
+  }
+  // this warp's stretch of the pages
+  __device__ __forceinline__ int per_warp(int n_pages) const { return round_up(ceil_div(n_pages, C * kWarps), 32); }
+  __device__ __forceinline__ int begin(int n_pages) const { return min(n_pages, (rank * kWarps + warp) * per_warp(n_pages)); }
+  // f(id, ballots of a and b) over 32 pages at a time; A and B: predicates of (id, references)
+  template <typename A, typename B, typename F>
+  __device__ __forceinline__ void walk(const Book& k, A a, B b, F f) const {
+    const int lo = begin(k.n_pages), hi = min(k.n_pages, lo + per_warp(k.n_pages));
+#pragma unroll 4
+    for (int p = lo; p < hi; p += 32) {
+      const int i = p + lane;
+      const bool in = i < hi;
+      const int r = in ? __ldcg(k.ref + i) : -1;
+      f(i, __ballot_sync(~0u, in && a(i, r)), __ballot_sync(~0u, in && b(i, r)));
+    }
+  }
+  // the counts of a and b before this warp's stretch, and all of them
+  template <typename A, typename B>
+  __device__ __forceinline__ void count(const Book& k, A a, B b, int2* before, int2* all) const {
+    int na = 0, nb = 0;
+    walk(k, a, b, [&](int, uint32_t x, uint32_t y) {
+      na += __popc(x);
+      nb += __popc(y);
+    });
+    if (lane == 0) {
+      sh.warp[0][warp] = na;
+      sh.warp[1][warp] = nb;
+    }
+    sync();
+    int2 pre = make_int2(0, 0), tot = make_int2(0, 0);
+    for (int c = 0; c < C; ++c) {
+      const Shared* s = of(c);
+      const int x = s->warp[0][lane], y = s->warp[1][lane];
+      tot.x += x;
+      tot.y += y;
+      if (c < rank || (c == rank && lane < warp)) {
+        pre.x += x;
+        pre.y += y;
+      }
+    }
+    before->x = __reduce_add_sync(~0u, pre.x);
+    before->y = __reduce_add_sync(~0u, pre.y);
+    all->x = __reduce_add_sync(~0u, tot.x);
+    all->y = __reduce_add_sync(~0u, tot.y);
+    sync();
+  }
+  // the n lowest free pages to list; false if there are fewer
+  __device__ bool free_pages(const Book& k, int n, int32_t* list) const {
+    auto is_free = [](int, int r) { return r == 0; };
+    auto no = [](int, int) { return false; };
+    int2 at, all;
+    count(k, is_free, no, &at, &all);
+    if (all.x < n) return false;
+    int base = at.x;
+    walk(k, is_free, no, [&](int i, uint32_t x, uint32_t) {
+      const int rk = base + __popc(x & ((1u << lane) - 1));
+      if (((x >> lane) & 1u) && rk < n) list[rk] = i;
+      base += __popc(x);
+    });
+    return true;
+  }
+  // off[i] = sum of f(0 .. i-1) for i < n, by the first CTA; the sum (to every thread)
+  template <typename F>
+  __device__ int offsets(int n, int32_t* off, int32_t* total, F f) const {
+    if (rank == 0) {
+      int run = 0;
+      for (int i0 = 0; i0 < n; i0 += kThreads) {
+        const int i = i0 + t, v = i < n ? f(i) : 0;
+        int incl = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int u = __shfl_up_sync(~0u, incl, o);
+          if (lane >= o) incl += u;
+        }
+        if (lane == 31) sh.scan[warp] = incl;
+        __syncthreads();
+        const int w = sh.scan[lane];
+        const int before = __reduce_add_sync(~0u, lane < warp ? w : 0), all = __reduce_add_sync(~0u, w);
+        if (i < n) off[i] = run + before + incl - v;
+        run += all;
+        __syncthreads();
+      }
+      if (t == 0) *total = run;
+    }
+    sync();
+    return __ldcg(total);
+  }
+};
+
+__device__ __forceinline__ int pages_of(int len, int page) { return (len + page - 1) / page; }
+
+// which[i] in range and listed once (mark needs no clearing: a slot listed twice holds
+// the stamp of one of the two)
+template <int C>
+__device__ int check_slots(const Team<C>& team, const Book& k, const int32_t* which, int n, int32_t* mark) {
+  int bad = 0;
+  for (int i = team.id; i < n; i += team.size) {
+    const int s = which[i];
+    if (s < 0 || s >= k.slots) bad |= KF_DEV_BAD_ROW;
+    else mark[s] = i;
+  }
+  bad = team.any(bad);
+  if (bad) return bad;
+  for (int i = team.id; i < n; i += team.size)
+    if (__ldcg(mark + which[i]) != i) bad |= KF_DEV_BAD_ROW;
+  return team.any(bad);
+}
+template <int C>
+__device__ __forceinline__ bool refused(const Team<C>& team, int bad, int* err) {
+  if (bad && team.id == 0) atomicOr(err, bad);
+  return bad != 0;
+}
+
+template <int C>
+__global__ void __launch_bounds__(kThreads) k_grow(const Book k, int n, const int32_t* which, const int32_t* new_lens, const Work w, int* err) {
+  __shared__ Shared sh;
+  const Team<C> team(sh);
+  int bad = check_slots(team, k, which, n, w.mark);
+  if (refused(team, bad, err)) return;
+  for (int i = team.id; i < n; i += team.size) {
+    const int was = k.lens[which[i]], now = new_lens[i];
+    if (was < 0 || now < was || now > (int64_t)k.width * k.page) bad |= KF_DEV_BAD_ROW;
+  }
+  bad = team.any(bad);
+  if (refused(team, bad, err)) return;
+  const int total = team.offsets(n, w.off, w.count, [&](int i) { return pages_of(new_lens[i], k.page) - pages_of(k.lens[which[i]], k.page); });
+  if (!team.free_pages(k, total, w.src)) {
+    refused(team, KF_DEV_NO_PAGES, err);
+    return;
+  }
+  team.sync();
+  // a warp per request
+  for (int i = team.id >> 5; i < n; i += team.size >> 5) {
+    const int s = which[i], have = pages_of(k.lens[s], k.page), need = pages_of(new_lens[i], k.page), off = __ldcg(w.off + i);
+    __syncwarp();
+    for (int c = have + team.lane; c < need; c += 32) {
+      const int p = __ldcg(w.src + off + c - have);
+      k.table[(int64_t)s * k.width + c] = p;
+      k.ref[p] = 1;
+    }
+    if (team.lane == 0) k.lens[s] = new_lens[i];
+  }
+}
+
+template <int C>
+__global__ void __launch_bounds__(kThreads) k_free(const Book k, int n, const int32_t* which, const Work w, int* err) {
+  __shared__ Shared sh;
+  const Team<C> team(sh);
+  int bad = check_slots(team, k, which, n, w.mark);
+  if (refused(team, bad, err)) return;
+  const uint32_t all = (uint32_t)n * k.width, width = k.width;
+  for (uint32_t e = team.id; e < all; e += team.size) {
+    const int p = k.table[(int64_t)which[e / width] * k.width + e % width];
+    if (p == -1) continue;
+    if (p < 0 || p >= k.n_pages || atomicSub(k.ref + p, 1) <= 0) bad |= KF_DEV_BAD_PAGE;
+  }
+  bad = team.any(bad);
+  for (uint32_t e = team.id; e < all; e += team.size) {
+    int32_t* at = k.table + (int64_t)which[e / width] * k.width + e % width;
+    const int p = *at;
+    if (!bad) *at = -1;
+    else if (p >= 0 && p < k.n_pages) atomicAdd(k.ref + p, 1);      // as it was
+  }
+  if (refused(team, bad, err)) return;
+  for (int i = team.id; i < n; i += team.size) k.lens[which[i]] = 0;
+}
+
+template <int C>
+__global__ void __launch_bounds__(kThreads) k_fork(const Book k, int n, const int32_t* src, const int32_t* dst, const Work w, int* err) {
+  __shared__ Shared sh;
+  const Team<C> team(sh);
+  if (team.id == 0) *w.count = 0;            // (a refused call copies nothing)
+  int bad = check_slots(team, k, dst, n, w.mark);
+  if (refused(team, bad, err)) return;
+  for (int i = team.id; i < n; i += team.size) {
+    const int s = src[i];
+    if (s < 0 || s >= k.slots) {
+      bad |= KF_DEV_BAD_ROW;
+      continue;
+    }
+    const int m = __ldcg(w.mark + s), len = k.lens[s];
+    if ((m >= 0 && m < n && dst[m] == s) || len < 0 || len > (int64_t)k.width * k.page || k.lens[dst[i]] != 0) bad |= KF_DEV_BAD_ROW;
+  }
+  bad = team.any(bad);
+  if (refused(team, bad, err)) return;
+  const uint32_t all = (uint32_t)n * k.width, width = k.width;
+  for (uint32_t e = team.id; e < all; e += team.size) {
+    const int i = (int)(e / width), c = (int)(e % width);
+    if (k.table[(int64_t)dst[i] * k.width + c] != -1) bad |= KF_DEV_BAD_PAGE;      // not empty
+    if (c >= pages_of(k.lens[src[i]], k.page)) continue;
+    const int p = k.table[(int64_t)src[i] * k.width + c];
+    if (p < 0 || p >= k.n_pages || __ldcg(k.ref + p) <= 0) bad |= KF_DEV_BAD_PAGE;
+  }
+  bad = team.any(bad);
+  if (refused(team, bad, err)) return;
+  const int total = team.offsets(n, w.off, w.to, [&](int i) { return k.lens[src[i]] % k.page != 0; });
+  if (!team.free_pages(k, total, w.dst)) {
+    refused(team, KF_DEV_NO_PAGES, err);
+    return;
+  }
+  team.sync();
+  for (uint32_t e = team.id; e < all; e += team.size) {
+    const int i = (int)(e / width), c = (int)(e % width), len = k.lens[src[i]], full = len / k.page;
+    int p = -1;
+    if (c < full) {
+      p = k.table[(int64_t)src[i] * k.width + c];
+      atomicAdd(k.ref + p, 1);
+    } else if (c == full && len % k.page) {
+      const int off = __ldcg(w.off + i);
+      w.src[off] = k.table[(int64_t)src[i] * k.width + c];
+      p = __ldcg(w.dst + off);
+      k.ref[p] = 1;
+    }
+    k.table[(int64_t)dst[i] * k.width + c] = p;
+    if (c == 0) k.lens[dst[i]] = len;
+  }
+  if (k.width == 0)
+    for (int i = team.id; i < n; i += team.size) k.lens[dst[i]] = 0;
+  if (team.id == 0) *w.count = total;
+}
+
+template <int C>
+__global__ void __launch_bounds__(kThreads) k_compact(const Book k, const Work w, int32_t* live, int* err) {
+  __shared__ Shared sh;
+  const Team<C> team(sh);
+  if (team.id == 0) *w.count = 0;
+  auto is_live = [](int, int r) { return r > 0; };
+  auto is_bad = [](int, int r) { return r < 0; };
+  int2 at, all;
+  team.count(k, is_live, is_bad, &at, &all);
+  const int L = all.x;
+  int bad = all.y ? KF_DEV_BAD_PAGE : 0;
+  const uint32_t entries = (uint32_t)k.slots * k.width;
+  for (uint32_t e = team.id; e < entries; e += team.size) {
+    const int p = k.table[e];
+    if (p != -1 && (p < 0 || p >= k.n_pages || __ldcg(k.ref + p) <= 0)) bad |= KF_DEV_BAD_PAGE;
+  }
+  bad = team.any(bad);
+  if (refused(team, bad, err)) return;
+  auto high = [L](int i, int r) { return r > 0 && i >= L; };
+  auto hole = [L](int i, int r) { return r == 0 && i < L; };
+  team.count(k, high, hole, &at, &all);
+  team.walk(k, high, hole, [&](int i, uint32_t x, uint32_t y) {
+    const uint32_t below = (1u << team.lane) - 1;
+    if ((x >> team.lane) & 1u) w.src[at.x + __popc(x & below)] = i;
+    if ((y >> team.lane) & 1u) w.dst[at.y + __popc(y & below)] = i;
+    at.x += __popc(x);
+    at.y += __popc(y);
+  });
+  team.sync();
+  // (as many live pages above as holes below)
+  for (int i = team.id; i < all.x; i += team.size) {
+    const int s = __ldcg(w.src + i), d = __ldcg(w.dst + i);
+    k.ref[d] = __ldcg(k.ref + s);
+    k.ref[s] = 0;
+    w.to[s] = d;
+  }
+  team.sync();
+  for (uint32_t e = team.id; e < entries; e += team.size) {
+    const int p = k.table[e];
+    if (p >= L) k.table[e] = __ldcg(w.to + p);
+  }
+  if (team.id == 0) {
+    *w.count = all.x;
+    if (live) *live = L;
+  }
+}
+
+// page src[i] to dst[i] in every layer; the list's length is n, or *count
+__global__ void __launch_bounds__(kCopyThreads) k_move(uint8_t* pool, int layers, int n_pages, int64_t page_bytes, const int32_t* src,
+                                                     const int32_t* dst, int n, const int32_t* count, int* err) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (count) n = __ldcg(count);
+  const int chunks = (int)((page_bytes + kCopyUnit - 1) / kCopyUnit);
+  const int64_t units = (int64_t)n * layers * chunks;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    const int64_t m = u / chunks;
+    const int i = (int)(m / layers), layer = (int)(m % layers);
+    const int s = __ldcg(src + i), d = __ldcg(dst + i);
+    if (s < 0 || d < 0 || s >= n_pages || d >= n_pages) {
+      if (threadIdx.x == 0) atomicOr(err, KF_DEV_BAD_PAGE);
+      continue;
+    }
+    const int64_t at = (u - m * chunks) * kCopyUnit + threadIdx.x * 16;
+    const uint8_t* from = pool + ((int64_t)layer * n_pages + s) * page_bytes + at;
+    uint8_t* to = pool + ((int64_t)layer * n_pages + d) * page_bytes + at;
+    uint4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (at + j * kCopyThreads * 16 < page_bytes) v[j] = *reinterpret_cast<const uint4*>(from + j * kCopyThreads * 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (at + j * kCopyThreads * 16 < page_bytes) *reinterpret_cast<uint4*>(to + j * kCopyThreads * 16) = v[j];
+  }
+}
+
+// K and V rows into their pages: a CTA takes kTokens tokens; a thread copies 16 bytes at a time
+constexpr int kTokens = 16;
+struct Append {
+  const int32_t *which, *starts, *table, *lens;
+  const uint8_t *k, *v;
+  uint8_t* pool;
+  int64_t T, k_row, k_head, v_row, v_head;       // strides in bytes
+  int n, Hkv, chunks, n_pages, page, slots, width;   // chunks: 16-byte pieces of a head
+};
+__global__ void __launch_bounds__(kCopyThreads) k_append(const Append a, int* err) {
+  __shared__ int64_t row[kTokens];               // K's first piece in the pool, or -1
+  const int64_t t0 = (int64_t)blockIdx.x * kTokens;
+  if (threadIdx.x < kTokens && t0 + threadIdx.x < a.T) {
+    const int64_t t = t0 + threadIdx.x;
+    int lo = 0, hi = a.n - 1;                    // the last sequence that starts at or before t
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (__ldg(a.starts + mid) <= t) lo = mid;
+      else hi = mid - 1;
+    }
+    const int first = __ldg(a.starts + lo), end = __ldg(a.starts + lo + 1), s = __ldg(a.which + lo);
+    int64_t at = -1;
+    int bad = 0;
+    if (t < first || t >= end || s < 0 || s >= a.slots) bad = KF_DEV_BAD_ROW;
+    else {
+      const int64_t pos = (int64_t)a.lens[s] - end + t;
+      if (pos < 0 || pos >= (int64_t)a.width * a.page) bad = KF_DEV_BAD_ROW;
+      else {
+        const int p = a.table[(int64_t)s * a.width + pos / a.page];
+        if (p < 0 || p >= a.n_pages) bad = KF_DEV_BAD_PAGE;
+        else at = ((int64_t)p * 2 * a.Hkv * a.page + pos % a.page) * a.chunks;
+      }
+    }
+    if (bad) atomicOr(err, bad);
+    row[threadIdx.x] = at;
+  }
+  __syncthreads();
+  const int per = 2 * a.Hkv * a.chunks, tokens = (int)min((int64_t)kTokens, a.T - t0);
+  const int total = tokens * per;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < total; i += kCopyThreads) {
+    const int j = i / per, e = i - j * per, h2 = e / a.chunks, ch = e - h2 * a.chunks;     // h2: K heads, then V heads
+    if (row[j] < 0) continue;
+    const bool v = h2 >= a.Hkv;
+    const uint8_t* from = v ? a.v + (t0 + j) * a.v_row + (h2 - a.Hkv) * a.v_head : a.k + (t0 + j) * a.k_row + h2 * a.k_head;
+    const int64_t to = row[j] + (int64_t)h2 * a.page * a.chunks + ch;
+    reinterpret_cast<uint4*>(a.pool)[to] = *reinterpret_cast<const uint4*>(from + ch * 16);
+  }
+}
+
+// ------------------------------------------------------------------ host
+Work layout(void* work, int n_pages, int slots, int n) {
+  int32_t* p = static_cast<int32_t*>(work);
+  Work w;
+  w.count = p;
+  w.mark = p + 64;
+  w.off = w.mark + slots;
+  w.src = w.off + n;
+  w.dst = w.src + n_pages;
+  w.to = w.dst + n_pages;
+  return w;
+}
+const char* book_fault(const Book& k, const void* work) {
+  if (k.n_pages < 1 || k.n_pages > (1 << 30) || k.slots < 1 || k.slots > (1 << 30) || k.width < 0 || k.width > (1 << 30)) return "pages, slots or width out of range";
+  if ((int64_t)k.slots * k.width > 0x7fffffffll) return "slots * width out of range";      // (sums of pages stay in 32 bits)
+  if (k.page < 1 || k.page > (1 << 20) || (int64_t)k.width * k.page > 0x7fffffffll) return "page, or width * page, out of range";
+  if (!k.ref || (k.width && !k.table) || !work) return "a null array";
+  if (!aligned(k.ref, 4) || !aligned(k.table, 4) || !aligned(k.lens, 4) || !aligned(work, 256)) return "an array is not aligned (work: 256 bytes)";
+  return nullptr;
+}
+const char* pool_fault(const void* pool, int layers, int64_t page_bytes) {
+  if (layers < 1 || layers > (1 << 20)) return "layers out of range";
+  if (page_bytes < 16 || page_bytes % 16 || page_bytes > (1 << 30)) return "page_bytes is a multiple of 16";
+  if (!pool || !aligned(pool, 16)) return "the pool is null or not 16-byte aligned";
+  return nullptr;
+}
+// A cluster's barriers cost a few microseconds that a small book does not repay: one CTA up
+// to 16 references and 16 table entries a thread
+bool small_book(int64_t pages, int64_t entries) { return pages <= 16 * kThreads && entries <= 16 * kThreads; }
+
+#define KF_TEAM(kernel, small, s, ...)                                                      \
+  do {                                                                                      \
+    if (small) launch_cluster(kernel<1>, dim3(1), dim3(kThreads), 0, 1, false, s, __VA_ARGS__); \
+    else launch_cluster(kernel<kTeam>, dim3(kTeam), dim3(kThreads), 0, kTeam, false, s, __VA_ARGS__); \
+  } while (0)
+
+void launch_move(uint8_t* pool, int layers, int n_pages, int64_t page_bytes, const int32_t* src, const int32_t* dst, int n,
+                 const int32_t* count, int* err, bool dependent, cudaStream_t s) {
+  const int64_t units = (int64_t)n * layers * ((page_bytes + kCopyUnit - 1) / kCopyUnit);
+  const int grid = (int)std::min<int64_t>(8ll * device_sms(), std::max<int64_t>(1, units));
+  launch_cluster(k_move, dim3(grid), dim3(kCopyThreads), 0, 1, dependent, s, pool, layers, n_pages, page_bytes, src, dst, n, count, err);
+}
+
+}  // namespace
+}  // namespace kf
+
+using namespace kf;
+
+extern "C" int64_t kf_op_pages_work(int32_t n_pages, int32_t slots, int32_t n) {
+  if (n_pages < 0 || slots < 0 || n < 0) return 0;
+  return 4 * (64 + (int64_t)slots + n + 3 * (int64_t)n_pages);
+}
+
+extern "C" int kf_op_pages_grow(int32_t n, const int32_t* which, const int32_t* new_lens, int32_t* ref, int32_t n_pages,
+                                int32_t* table, int32_t slots, int32_t width, int32_t* lens, int32_t page, void* work,
+                                void* stream) {
+  const char* what = "kf_op_pages_grow";
+  const Book k{ref, table, lens, n_pages, slots, width, page};
+  if (const char* f = book_fault(k, work)) return refuse(what, f);
+  if (n < 0 || n > slots) return refuse(what, "more slots listed than there are");
+  if (n == 0) return KF_OK;
+  if (!which || !new_lens || !lens || !aligned(which, 4) || !aligned(new_lens, 4)) return refuse(what, "a null or misaligned list");
+  int* err = serving_error_word();
+  if (!err) return refuse(what, "no error word", KF_E_CUDA);
+  KF_TEAM(k_grow, small_book(n_pages, n), (cudaStream_t)stream, k, n, which, new_lens, layout(work, n_pages, slots, n), err);
+  return launched(what);
+}
+
+extern "C" int kf_op_pages_free(int32_t n, const int32_t* which, int32_t* ref, int32_t n_pages, int32_t* table, int32_t slots,
+                                int32_t width, int32_t* lens, int32_t page, void* work, void* stream) {
+  const char* what = "kf_op_pages_free";
+  const Book k{ref, table, lens, n_pages, slots, width, page};
+  if (const char* f = book_fault(k, work)) return refuse(what, f);
+  if (n < 0 || n > slots) return refuse(what, "more slots listed than there are");
+  if (n == 0) return KF_OK;
+  if (!which || !lens || !aligned(which, 4)) return refuse(what, "a null or misaligned list");
+  int* err = serving_error_word();
+  if (!err) return refuse(what, "no error word", KF_E_CUDA);
+  KF_TEAM(k_free, small_book(0, (int64_t)n * width), (cudaStream_t)stream, k, n, which, layout(work, n_pages, slots, n), err);
+  return launched(what);
+}
+
+extern "C" int kf_op_pages_fork(int32_t n, const int32_t* src, const int32_t* dst, int32_t* ref, int32_t n_pages, int32_t* table,
+                                int32_t slots, int32_t width, int32_t* lens, int32_t page, void* pool, int32_t layers,
+                                int64_t page_bytes, void* work, void* stream) {
+  const char* what = "kf_op_pages_fork";
+  const Book k{ref, table, lens, n_pages, slots, width, page};
+  if (const char* f = book_fault(k, work)) return refuse(what, f);
+  if (const char* f = pool_fault(pool, layers, page_bytes)) return refuse(what, f);
+  if (n < 0 || n > slots) return refuse(what, "more slots listed than there are");
+  if (n == 0) return KF_OK;
+  if (!src || !dst || !lens || !aligned(src, 4) || !aligned(dst, 4)) return refuse(what, "a null or misaligned list");
+  int* err = serving_error_word();
+  if (!err) return refuse(what, "no error word", KF_E_CUDA);
+  const Work w = layout(work, n_pages, slots, n);
+  cudaStream_t s = (cudaStream_t)stream;
+  KF_TEAM(k_fork, small_book(n_pages, (int64_t)n * width), s, k, n, src, dst, w, err);
+  if (const int rc = launched(what)) return rc;
+  launch_move(static_cast<uint8_t*>(pool), layers, n_pages, page_bytes, w.src, w.dst, n, w.count, err, true, s);
+  return launched(what);
+}
+
+extern "C" int kf_op_pages_compact(int32_t* ref, int32_t n_pages, int32_t* table, int32_t slots, int32_t width, void* pool,
+                                   int32_t layers, int64_t page_bytes, int32_t* live, void* work, void* stream) {
+  const char* what = "kf_op_pages_compact";
+  const Book k{ref, table, nullptr, n_pages, slots, width, 1};
+  if (const char* f = book_fault(k, work)) return refuse(what, f);
+  if (const char* f = pool_fault(pool, layers, page_bytes)) return refuse(what, f);
+  if (!aligned(live, 4)) return refuse(what, "live is misaligned");
+  int* err = serving_error_word();
+  if (!err) return refuse(what, "no error word", KF_E_CUDA);
+  const Work w = layout(work, n_pages, slots, 0);
+  cudaStream_t s = (cudaStream_t)stream;
+  KF_TEAM(k_compact, small_book(n_pages, (int64_t)slots * width), s, k, w, live, err);
+  if (const int rc = launched(what)) return rc;
+  launch_move(static_cast<uint8_t*>(pool), layers, n_pages, page_bytes, w.src, w.dst, n_pages, w.count, err, true, s);
+  return launched(what);
+}
+
+extern "C" int kf_op_pages_copy(int32_t n, const int32_t* src, const int32_t* dst, void* pool, int32_t layers, int32_t n_pages,
+                                int64_t page_bytes, void* stream) {
+  const char* what = "kf_op_pages_copy";
+  if (const char* f = pool_fault(pool, layers, page_bytes)) return refuse(what, f);
+  if (n < 0 || n_pages < 1 || n > n_pages) return refuse(what, "more pages listed than there are");
+  if (n == 0) return KF_OK;
+  if (!src || !dst || !aligned(src, 4) || !aligned(dst, 4)) return refuse(what, "a null or misaligned list");
+  int* err = serving_error_word();
+  if (!err) return refuse(what, "no error word", KF_E_CUDA);
+  launch_move(static_cast<uint8_t*>(pool), layers, n_pages, page_bytes, src, dst, n, nullptr, err, false, (cudaStream_t)stream);
+  return launched(what);
+}
+
+extern "C" int kf_op_pages_append(int32_t n, const int32_t* which, const int32_t* starts, int64_t T, int32_t Hkv, int32_t hd,
+                                  const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
+                                  void* pool, int32_t n_pages, int32_t page, const int32_t* table, int32_t slots, int32_t width,
+                                  const int32_t* lens, void* stream) {
+  const char* what = "kf_op_pages_append";
+  if (n < 0 || T < 0 || T > 0x7fffffffll || n_pages < 1 || slots < 1 || width < 0) return refuse(what, "sequences, tokens, pages, slots or width out of range");
+  if (Hkv < 1 || Hkv > 4096 || hd < 8 || hd % 8 || hd > 4096) return refuse(what, "heads out of range, or hd no multiple of 8");
+  if (page < 1 || page > (1 << 20) || (int64_t)width * page > 0x7fffffffll) return refuse(what, "page, or width * page, out of range");
+  if (n == 0 || T == 0) return KF_OK;
+  if (!which || !starts || !k || !v || !pool || !lens || (width && !table)) return refuse(what, "a null array");
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(pool, 16) || !aligned(which, 4) || !aligned(starts, 4) || !aligned(table, 4) || !aligned(lens, 4))
+    return refuse(what, "k, v and the pool are 16-byte aligned");
+  if (k_row % 8 || k_head % 8 || v_row % 8 || v_head % 8) return refuse(what, "strides are multiples of 8 elements");
+  int* err = serving_error_word();
+  if (!err) return refuse(what, "no error word", KF_E_CUDA);
+  const Append a{which, starts, table, lens, static_cast<const uint8_t*>(k), static_cast<const uint8_t*>(v), static_cast<uint8_t*>(pool),
+                 T, k_row * 2, k_head * 2, v_row * 2, v_head * 2, n, Hkv, hd / 8, n_pages, page, slots, width};
+  launch_cluster(k_append, dim3((unsigned)((T + kTokens - 1) / kTokens)), dim3(kCopyThreads), 0, 1, false, (cudaStream_t)stream, a, err);
+  return launched(what);
+}

@@ -25,6 +25,14 @@ _SIGNATURES = {
     "kf_op_token_scores_grad": (ctypes.c_int, [_I32, _I64, _I32, _VP, _I64, _VP, _F32] + [_VP] * 6 + [_I64, _VP]),
     "kf_op_paged_attention_work": (_I64, [_I32]),
     "kf_op_paged_attention": (ctypes.c_int, [_I32] * 6 + [_VP] + [_I64] * 3 + [_VP, _I64, _I32, _VP, _I32, _VP, _F32] + [_VP] * 3),
+    "kf_op_pages_work": (_I64, [_I32] * 3),
+    "kf_op_pages_grow": (ctypes.c_int, [_I32, _VP, _VP, _VP, _I32, _VP, _I32, _I32, _VP, _I32, _VP, _VP]),
+    "kf_op_pages_free": (ctypes.c_int, [_I32, _VP, _VP, _I32, _VP, _I32, _I32, _VP, _I32, _VP, _VP]),
+    "kf_op_pages_fork": (ctypes.c_int, [_I32, _VP, _VP, _VP, _I32, _VP, _I32, _I32, _VP, _I32, _VP, _I32, _I64, _VP, _VP]),
+    "kf_op_pages_compact": (ctypes.c_int, [_VP, _I32, _VP, _I32, _I32, _VP, _I32, _I64, _VP, _VP, _VP]),
+    "kf_op_pages_copy": (ctypes.c_int, [_I32, _VP, _VP, _VP, _I32, _I32, _I64, _VP]),
+    "kf_op_pages_append": (ctypes.c_int, [_I32, _VP, _VP, _I64, _I32, _I32, _VP, _I64, _I64, _VP, _I64, _I64, _VP, _I32, _I32, _VP,
+                                          _I32, _I32, _VP, _VP]),
     "kf_op_status": (ctypes.c_int, [_VP]),
 }
 _lib = None
@@ -113,6 +121,96 @@ def paged_attention(q, pool, table, lens, scale=None, out=None):
          _on(table, dev, torch.int32, (B, width), "table"), width, _on(lens, dev, torch.int32, (B,), "lens"),
          1.0 / math.sqrt(hd) if scale is None else scale, _on(out, dev, q.dtype, q.shape, "out"), work.data_ptr(), _stream(q))
     return out
+
+
+# ------------------------------------------------------------------- pages
+#
+# The book of a cache: ``ref`` [pages] int32, ``table`` [slots, width] int32 (-1: no page) and ``lens``
+# [slots] int32, changed in place.  The pool is [layers, pages, 2, Hkv, page, hd].
+
+def new_book(n_pages, slots, width, device="cuda"):
+    """An empty book: (ref, table, lens)."""
+    return (torch.zeros(n_pages, dtype=torch.int32, device=device), torch.full((slots, width), -1, dtype=torch.int32, device=device),
+            torch.zeros(slots, dtype=torch.int32, device=device))
+
+
+def _book(ref, table, lens=None):
+    _need(ref.is_cuda and ref.dim() == 1 and table.dim() == 2, "ref: [pages], table: [slots, width], int32 on a GPU")
+    dev, (slots, width) = ref.device, table.shape
+    return (dev, ref.shape[0], slots, width, _on(ref, dev, torch.int32, ref.shape, "ref"), _on(table, dev, torch.int32, table.shape, "table"),
+            None if lens is None else _on(lens, dev, torch.int32, (slots,), "lens"))
+
+
+def _list(x, dev, n, what):
+    _need(x.dim() == 1, what + ": a list of int32 on the GPU")
+    return _on(x, dev, torch.int32, (n,), what)
+
+
+def _pool(pool, dev, n_pages):
+    """Address, layers and bytes of a page of one layer; pool [layers, pages, ...]."""
+    _need(pool.dim() >= 3 and pool.device == dev and pool.is_contiguous() and pool.shape[1] == n_pages,
+          "pool: a contiguous [layers, pages, ...] tensor on the book's device")
+    return pool.data_ptr(), pool.shape[0], pool.stride(1) * pool.element_size()
+
+
+def pages_grow(ref, table, lens, slots, new_lens, page=16):
+    """Slot slots[i] gets pages for new_lens[i] (>= its length) tokens, lowest free page first."""
+    dev, n_pages, n_slots, width, pr, pt, pl = _book(ref, table, lens)
+    n = slots.shape[0]
+    work = _scratch("kf_op_pages_work", dev, n_pages, n_slots, n)
+    _run("kf_op_pages_grow", dev, n, _list(slots, dev, n, "slots"), _list(new_lens, dev, n, "new_lens"), pr, n_pages, pt, n_slots, width,
+         pl, page, work.data_ptr(), _stream(ref))
+
+
+def pages_free(ref, table, lens, slots, page=16):
+    """The listed slots give up their pages and become empty."""
+    dev, n_pages, n_slots, width, pr, pt, pl = _book(ref, table, lens)
+    n = slots.shape[0]
+    work = _scratch("kf_op_pages_work", dev, n_pages, n_slots, n)
+    _run("kf_op_pages_free", dev, n, _list(slots, dev, n, "slots"), pr, n_pages, pt, n_slots, width, pl, page, work.data_ptr(), _stream(ref))
+
+
+def pages_fork(pool, ref, table, lens, src, dst):
+    """The sequence of slot src[i] continues in the empty slot dst[i] too: full pages are shared, a last page
+    that is not full is copied, in every layer of pool [layers, pages, 2, Hkv, page, hd]."""
+    dev, n_pages, n_slots, width, pr, pt, pl = _book(ref, table, lens)
+    _need(pool.dim() == 6, "pool: [layers, pages, 2, Hkv, page, hd]")
+    pp, layers, page_bytes = _pool(pool, dev, n_pages)
+    n = src.shape[0]
+    work = _scratch("kf_op_pages_work", dev, n_pages, n_slots, n)
+    _run("kf_op_pages_fork", dev, n, _list(src, dev, n, "src"), _list(dst, dev, n, "dst"), pr, n_pages, pt, n_slots, width, pl,
+         pool.shape[4], pp, layers, page_bytes, work.data_ptr(), _stream(ref))
+
+
+def pages_compact(pool, ref, table, live=None):
+    """The live pages move below their count (``live``, an int32 tensor of one, receives it); tables and references follow."""
+    dev, n_pages, n_slots, width, pr, pt, _ = _book(ref, table)
+    pp, layers, page_bytes = _pool(pool, dev, n_pages)
+    work = _scratch("kf_op_pages_work", dev, n_pages, n_slots, 0)
+    _run("kf_op_pages_compact", dev, pr, n_pages, pt, n_slots, width, pp, layers, page_bytes,
+         None if live is None else _on(live, dev, torch.int32, (1,), "live"), work.data_ptr(), _stream(ref))
+
+
+def pages_copy(pool, src, dst):
+    """Page src[i] to page dst[i] in every layer of pool [layers, pages, ...]."""
+    _need(pool.is_cuda, "pool: on a GPU")
+    dev, n = pool.device, src.shape[0]
+    pp, layers, page_bytes = _pool(pool, dev, pool.shape[1])
+    _run("kf_op_pages_copy", dev, n, _list(src, dev, n, "src"), _list(dst, dev, n, "dst"), pp, layers, pool.shape[1], page_bytes, _stream(pool))
+
+
+def pages_append(pool, k, v, starts, table, lens, slots):
+    """K and V rows of new tokens into their pages of one layer, pool [pages, 2, Hkv, page, hd]: rows
+    starts[i] .. starts[i + 1] - 1 of k and v [T, Hkv, hd] are the last tokens of slot slots[i]."""
+    _need(pool.is_cuda and pool.dim() == 5 and k.dim() == 3 and table.dim() == 2 and pool.element_size() == 2,
+          "pool: [pages, 2, Hkv, page, hd], k and v: [T, Hkv, hd], 16-bit elements on a GPU")
+    dev, (n_pages, two, Hkv, page, hd), (n_slots, width) = pool.device, pool.shape, table.shape
+    T, n = k.shape[0], slots.shape[0]
+    _need(two == 2 and pool.is_contiguous() and k.shape == v.shape == (T, Hkv, hd) and k.dtype == v.dtype == pool.dtype
+          and k.device == v.device == dev and k.stride(2) == v.stride(2) == 1, "k and v: rows of the pool's heads and type")
+    _run("kf_op_pages_append", dev, n, _list(slots, dev, n, "slots"), _list(starts, dev, n + 1, "starts"), T, Hkv, hd, k.data_ptr(),
+         k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), pool.data_ptr(), n_pages, page,
+         _on(table, dev, torch.int32, table.shape, "table"), n_slots, width, _on(lens, dev, torch.int32, (n_slots,), "lens"), _stream(pool))
 
 
 # ------------------------------------------------------------------ scores
