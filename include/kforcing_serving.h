@@ -1,7 +1,7 @@
 /*
  * kforcing_serving.h - serving operators of libkforcing.so for models with
- * grouped heads over a paged cache: attention of the newest rows, the
- * cache's pages (room, append, fork, free, compact, copy), and scores of tokens
+ * grouped heads over a paged cache: attention of whole prompts and of the
+ * newest rows, the cache's pages (room, append, fork, free, compact, copy), and scores of tokens
  * with their gradient.
  *
  * Device pointers only, caller-owned; work is enqueued on `stream`
@@ -38,6 +38,32 @@ extern "C" {
 #define KF_DEV_TIMEOUT 4       /* a bounded wait ran out                         */
 #define KF_DEV_BAD_ROW 8       /* a slot, length or start out of range           */
 #define KF_DEV_NO_PAGES 32     /* not enough free pages                          */
+
+/*
+ * Causal attention over n packed prompts: tokens starts[i] .. starts[i+1]-1 are
+ * sequence i, query row t of it sees its keys 0 .. t, and
+ *   out[t][h] = sum_j p_j v[j][h / (Hq / Hkv)],
+ *   p = softmax_j(scale q[t][h] . k[j][h / (Hq / Hkv)]).
+ * type: KF_TYPE_BF16 or KF_TYPE_FP16 (q, k, v and out alike); hd: 64 or 128;
+ * Hq a multiple of Hkv.  q [T][Hq][hd], k and v [T][Hkv][hd], out [T][Hq][hd]:
+ * elements of a head contiguous, *_row / *_head the strides of tokens and heads in elements
+ * (multiples of 8), so that q, k and v may be parts of one projection's output;
+ * out must not overlap them.  starts: int32 [n+1], on the device,
+ * starts[0] = 0, not falling, starts[n] = T; longest: at least the longest sequence's
+ * tokens (host; at most 524288).  scale: a finite number > 0, for instance 1/sqrt(hd).  A sequence of
+ * no tokens is allowed.  Scores, maxima, sums and the output's accumulation
+ * are fp32; the probabilities are rounded to `type` for the product with V.
+ * A NaN or infinity in a sequence's q, k or v stays in that sequence, and in a V
+ * row it reaches the rows of the 128-row tiles that hold or follow it.
+ * Starts that are not as said: KF_DEV_BAD_ROW, and out is left as it was.
+ * Errors: KF_E_ARG, KF_E_CUDA.
+ */
+int64_t kf_op_prompt_attention_work(int32_t n, int64_t T);
+int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_t longest, int32_t Hq, int32_t Hkv,
+                           int32_t hd, const void* q, int64_t q_row, int64_t q_head, const void* k,
+                           int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
+                           void* out, int64_t out_row, int64_t out_head, const int32_t* starts,
+                           float scale, void* work, void* stream);
 
 /*
  * Attention of the newest `rows` rows of each of B sequences over a paged

@@ -1,0 +1,566 @@
+// Causal attention over packed prompts (kf_op_prompt_attention): grouped heads,
+// head_dim 64 or 128, bf16 or fp16, on tcgen05.
+//
+// An item is two sub-tiles of 128 query rows that read the same K and V tiles: the same
+// rows under two heads of a group where groups are even (both sub-tiles then end at
+// the same key), else 256 consecutive rows of one head.  A CTA per SM of twelve warps:
+//   warp 0      takes items, and copies Q, K and V tiles (TMA, 128-byte swizzle);
+//   warp 1      issues S = Q K^T (128 x 128 x hd) and O += P V (128 x hd x 128), the two
+//               sub-tiles in turn, so that one's softmax runs under the other's products;
+//   warps 4-7, 8-11  the softmax of sub-tile 0 and 1, one thread per row (its TMEM
+//               lane): no exchange between threads.  P goes back to TMEM over the first
+//               half of its own S columns: the products of a thread's tcgen05.mma run in order,
+//               so the next S needs no other buffer.
+// Scores are taken against a reference per row that follows its maximum only past a factor of
+// 2^8, so O is rarely rescaled; sums are fp32, P is rounded to the inputs' type (the
+// tensor cores' operand).
+//
+// The items are sorted by their key tiles, longest first, by one block before
+// (k_plan), and handed out by a counter.  What bounds it: long prompts the tensor
+// cores (2,048 clocks a key tile of hd 128 and 256 rows), short ones the chain of an item.
+#include <algorithm>
+
+#include "kf_mma.cuh"
+#include "kf_serving.cuh"
+#include "kf_tc.cuh"
+
+namespace kf {
+namespace {
+
+constexpr int kRows = 128, kKeys = 128;
+constexpr int kThreads = 384;
+// registers a thread after the split of the launch's 384 x 168: 128 x 88 + 256 x 208
+constexpr int kRegsFew = 88, kRegsSoftmax = 208;
+constexpr uint32_t kAtom = kRows * 128;            // 128 rows of 64 elements: one swizzled box
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kColO = 256;
+constexpr float kRaise = 8.f;
+constexpr int kMaxTiles = 4096;                    // key tiles of a sequence: 524,288 tokens
+constexpr int kPlanThreads = 1024;
+
+template <int HD> constexpr int kStages = HD == 128 ? 5 : 8;
+template <int HD> constexpr uint32_t kTile = kAtom * (HD / 64);
+template <int HD> constexpr size_t kSmem = (2 + kStages<HD>) * (size_t)kTile<HD> + 512;
+
+struct PlanItem { int start, len, tile, pad; };     // a sequence's first token, its tokens, its tile of rows
+struct Plan {
+  int *count, *next;                                // items (without heads), the counter
+  PlanItem* item;
+};
+
+// one sub-tile pair, as the load warp hands it to the others
+struct Item {
+  int start, len;
+  int row[2], head[2], n[2];                        // first row, head, key tiles (0: no sub-tile)
+};
+
+struct Args {
+  void* out;
+  int64_t out_row, out_head;
+  Plan plan;
+  int* err;
+  int Hq, G, pairs;                                 // pairs: two heads per item (else two tiles of rows)
+  float scale2;
+};
+struct Maps { CUtensorMap q, k, v; };
+
+// ------------------------------------------------------------------ plan
+// Items of `rows` query rows, those with most keys first: with c tiles needed up to its
+// last row, an item of class c comes after all items of higher classes, and each
+// sequence of at least c tiles has one.  The order within a class is any.
+__global__ void __launch_bounds__(kPlanThreads) k_plan(int n, int T, int longest, int rows, int classes, const int32_t* starts,
+                                                        Plan plan, int grid, int* err) {
+  extern __shared__ __align__(1024) uint8_t sm[];
+  int* at_least = reinterpret_cast<int*>(sm);       // [classes + 2]: sequences of at least c tiles
+  int* first = at_least + classes + 2;                    // [classes + 2]: the first item of class c
+  __shared__ int warp_sum[32];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  for (int c = t; c < 2 * (classes + 2); c += kPlanThreads) at_least[c] = 0;
+  int bad = 0;
+  for (int s = t; s < n; s += kPlanThreads) {
+    const int a = starts[s], b = starts[s + 1];
+    bad |= a < 0 || b < a || b > T || b - a > longest || (s == 0 && a != 0) || (s == n - 1 && b != T);
+  }
+  bad = __syncthreads_or(bad);
+  if (bad) {
+    if (t == 0) {
+      atomicOr(err, KF_DEV_BAD_ROW);
+      *plan.count = 0;
+    }
+    return;
+  }
+  for (int s = t; s < n; s += kPlanThreads) atomicAdd(&at_least[(starts[s + 1] - starts[s] + rows - 1) / rows], 1);
+  __syncthreads();
+  // suffix sums of the counts, then of those (each thread a run of classes, from the top)
+  const int per = (classes + kPlanThreads - 1) / kPlanThreads;
+  for (int round = 0; round < 2; ++round) {
+    const int hi = classes - t * per, lo = max(0, hi - per);      // classes hi .. lo + 1
+    int mine = 0;
+    for (int c = hi; c > lo; --c) mine += at_least[c];
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(~0u, incl, o);
+      if (lane >= o) incl += v;
+    }
+    if (lane == 31) warp_sum[warp] = incl;
+    __syncthreads();
+    int run = __reduce_add_sync(~0u, lane < warp ? warp_sum[lane] : 0) + incl - mine;
+    for (int c = hi; c > lo; --c) {
+      if (round == 0) {
+        run += at_least[c];
+        at_least[c] = run;
+      } else {
+        first[c] = run;                             // the items of the classes above
+        run += at_least[c];
+      }
+    }
+    __syncthreads();
+  }
+  if (t == 0) {
+    *plan.count = classes > 0 ? first[1] + at_least[1] : 0;
+    *plan.next = grid;
+  }
+  // A sequence's place among all, those with more tiles first: class c has the places
+  // at_least[c + 1] .. at_least[c] - 1, taken from the end.  It holds in every class up to its own
+  for (int s0 = 0; s0 < n; s0 += 32) {              // warps take 32 sequences at a time
+    if ((s0 / 32) % 32 != warp) continue;
+    const int s = s0 + lane;
+    const int a = s < n ? starts[s] : 0, len = s < n ? starts[s + 1] - a : 0, c = (len + rows - 1) / rows;
+    const int place = c > 0 ? atomicSub(&at_least[c], 1) - 1 : 0;
+    for (int j = 0; j < 32; ++j) {
+      const int cj = __shfl_sync(~0u, c, j), aj = __shfl_sync(~0u, a, j), lj = __shfl_sync(~0u, len, j), pj = __shfl_sync(~0u, place, j);
+      for (int x = lane; x < cj; x += 32) plan.item[first[x + 1] + pj] = PlanItem{aj, lj, x, 0};
+    }
+  }
+}
+
+// ------------------------------------------------------------------ the products
+template <typename T> constexpr uint32_t idesc(int M, int N) {
+  // D fp32; A and B bf16 (1) or fp16 (0)
+  const uint32_t f = std::is_same<T, __half>::value ? 0u : 1u;
+  return (1u << 4) | (f << 7) | (f << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// MN-major operand of hd / 64 swizzled atoms: 64-wide atoms `kAtom` apart, 8-row K groups 1024 bytes apart
+__device__ __forceinline__ uint64_t sdesc_v(uint32_t addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr >> 4) & 0x3FFF);
+  d |= (uint64_t)(kAtom >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+__device__ __forceinline__ void mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  if constexpr (std::is_same<T, __half>::value) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  } else {
+    return mma::pack_bf16(lo, hi);
+  }
+}
+
+struct Bars {
+  uint64_t q_full, q_empty;
+  uint64_t item_full[2], item_empty[2];
+  uint64_t s_full[2], p_full[2], o_full[2], o_free[2];   // per sub-tile
+  uint64_t tail;                                         // a V tile whose last rows are to be cleared has landed
+  uint64_t kv_full[8], kv_empty[8];
+  Item item[2];
+  uint32_t tmem;
+};
+static_assert(sizeof(Bars) <= 512, "the barriers' part of the shared memory");
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ Maps maps, const Args a) {
+  extern __shared__ __align__(1024) uint8_t sm[];
+  constexpr int ST = kStages<HD>, AT = HD / 64;
+  constexpr uint32_t TILE = kTile<HD>;
+  Bars& b = *reinterpret_cast<Bars*>(sm + (2 + ST) * TILE);
+  const uint32_t sQ = smem_u32(sm), sKV = sQ + 2 * TILE;
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  if (sQ & 1023) {                              // (uniform) swizzle atoms need the alignment
+    if (t == 0) atomicOr(a.err, kErrInternal);
+    return;
+  }
+  if (t == 0) {
+    auto init = [](uint64_t* p, uint32_t n) { mbar_init(smem_u32(p), n); };
+    init(&b.q_full, 1);
+    init(&b.q_empty, 1);
+    for (int i = 0; i < 2; ++i) {
+      init(&b.item_full[i], 1);
+      init(&b.item_empty[i], 9);                // the MMA warp and eight softmax warps
+      init(&b.s_full[i], 1);
+      init(&b.p_full[i], 4);
+      init(&b.o_full[i], 1);
+      init(&b.o_free[i], 4);
+    }
+    init(&b.tail, 1);
+    for (int i = 0; i < ST; ++i) {
+      init(&b.kv_full[i], 1);
+      init(&b.kv_empty[i], 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&b.tmem)), "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = b.tmem;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+    if (warp == 0) {
+      // -------------------------------------------------------------- copies
+      const int heads = a.pairs ? a.Hq / 2 : a.Hq, per = a.pairs ? 1 : 2;
+      const int items = __ldcg(a.plan.count) * heads;
+      auto entry = [&](int w) -> int4 {
+        return w < items ? __ldcg(reinterpret_cast<const int4*>(a.plan.item) + w / heads) : make_int4(0, 0, 0, 0);
+      };
+      bool ok = true;
+      int w = blockIdx.x, w1 = 0, it = 0, q_issued = 0, g = 0, tails = 0;
+      int4 e = entry(w);
+      if (lane == 0) w1 = atomicAdd(a.plan.next, 1);
+      w1 = __shfl_sync(~0u, w1, 0);
+      auto wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, a.err)); };
+      for (;; ++it) {
+        Item im;
+        im.start = e.x;
+        im.len = e.y;
+        const int hu = w % heads;
+  #pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          im.head[i] = a.pairs ? 2 * hu + i : hu;
+          const int rt = e.z * per + (a.pairs ? 0 : i);
+          im.row[i] = rt * kRows;
+          im.n[i] = w < items && im.row[i] < im.len ? rt + 1 : 0;
+        }
+        const int slot = it & 1;
+        ok = wait(&b.item_empty[slot], ((it >> 1) & 1) ^ 1);
+        if (!ok) break;
+        if (lane == 0) {
+          b.item[slot] = im;
+          mbar_arrive(smem_u32(&b.item_full[slot]));
+        }
+        if (w >= items) break;                    // (an item without sub-tiles ends the others)
+        // the next item's entry and the counter for the one after it: used an item later
+        const int4 e1 = entry(w1);
+        int w2 = 0;
+        if (lane == 0) w2 = atomicAdd(a.plan.next, 1);
+        if (it > 0) ok = wait(&b.q_empty, (it - 1) & 1);
+        if (!ok) break;
+        if (lane == 0) {
+          mbar_expect_tx(smem_u32(&b.q_full), (im.n[1] > 0 ? 2 : 1) * TILE);
+          for (int i = 0; i < 2; ++i)
+            if (im.n[i] > 0)
+              for (int x = 0; x < AT; ++x)
+                tma_load_3d(sQ + i * TILE + x * kAtom, &maps.q, smem_u32(&b.q_full), 64 * x, im.head[i], im.start + im.row[i]);
+        }
+        q_issued = it + 1;
+        const int n = max(im.n[0], im.n[1]), hk = im.head[0] / a.G;
+        for (int j = 0; ok && j < n; ++j) {
+          for (int kv = 0; kv < 2; ++kv, ++g) {
+            const int st = g % ST;
+            ok = wait(&b.kv_empty[st], ((g / ST) & 1) ^ 1);
+            if (!ok) break;
+            const uint32_t dst = sKV + st * TILE;
+            // V rows past the sequence's end are another's, or nothing: their probabilities are 0,
+            // and 0 times them has to be 0
+            const int left = im.len - j * kKeys;
+            const bool tail = kv == 1 && left < kKeys;
+            uint64_t* bar = tail ? &b.tail : &b.kv_full[st];
+            if (lane == 0) {
+              mbar_expect_tx(smem_u32(bar), TILE);
+              for (int x = 0; x < AT; ++x)
+                tma_load_3d(dst + x * kAtom, kv ? &maps.v : &maps.k, smem_u32(bar), 64 * x, hk, im.start + j * kKeys);
+            }
+            __syncwarp();
+            if (tail) {
+              ok = wait(&b.tail, tails++ & 1);
+              if (!ok) break;
+              uint8_t* p = sm + (2 + st) * TILE;
+              for (int x = 0; x < AT; ++x)
+                for (int i = left * 128 + lane * 16; i < kKeys * 128; i += 32 * 16)
+                  *reinterpret_cast<uint4*>(p + x * kAtom + i) = make_uint4(0u, 0u, 0u, 0u);
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) mbar_arrive(smem_u32(&b.kv_full[st]));
+            }
+          }
+        }
+        if (!ok) break;
+        w = w1;
+        e = e1;
+        w1 = __shfl_sync(~0u, w2, 0);
+      }
+      if (!ok && lane == 0) {
+        // let the copies still in flight land before the CTA ends (bounded)
+        if (q_issued) mbar_wait(smem_u32(&b.q_full), (q_issued - 1) & 1, a.err);
+        for (int i = max(0, g - ST); i < g; ++i) mbar_wait(smem_u32(&b.kv_full[i % ST]), (i / ST) & 1, a.err);
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // ------------------------------------------------------------ products
+      if (lane == 0) {
+        constexpr uint32_t id_s = idesc<T>(kRows, kKeys), id_o = idesc<T>(kRows, HD) | (1u << 16);   // (V is MN-major)
+        int g = 0, tiles[2] = {0, 0}, subs[2] = {0, 0};
+        auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(smem_u32(bar), parity, a.err); };
+        auto full = [&](int r) { return wait(&b.kv_full[r % ST], (r / ST) & 1); };
+        auto s_product = [&](int i, int r) {
+          const uint32_t q = sQ + i * TILE, k = sKV + (r % ST) * TILE;
+  #pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            const uint32_t off = (kk / 4) * kAtom + (kk % 4) * 32;
+            mma_bf16(tmem + i * kKeys, sdesc(q + off), sdesc(k + off), id_s, kk > 0 ? 1u : 0u);
+          }
+          mma_commit(smem_u32(&b.s_full[i]));
+        };
+        bool ok = true;
+        for (int it = 0; ok; ++it) {
+          const int slot = it & 1;
+          if (!wait(&b.item_full[slot], (it >> 1) & 1)) break;
+          const int nn[2] = {b.item[slot].n[0], b.item[slot].n[1]}, n = max(nn[0], nn[1]);
+          mbar_arrive(smem_u32(&b.item_empty[slot]));
+          if (n == 0) break;
+          ok = wait(&b.q_full, it & 1) && full(g);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          for (int i = 0; i < 2; ++i)
+            if (nn[i] > 0) s_product(i, g);
+          mma_commit(smem_u32(&b.kv_empty[g % ST]));
+          if (n == 1) mma_commit(smem_u32(&b.q_empty));
+          for (int j = 0; ok && j < n; ++j, g += 2) {
+            ok = full(g + 1);
+            for (int i = 0; ok && i < 2; ++i) {
+              if (j < nn[i]) {
+                ok = wait(&b.p_full[i], tiles[i]++ & 1) && (j > 0 || subs[i] == 0 || wait(&b.o_free[i], (subs[i] - 1) & 1));
+                if (!ok) break;
+                if (j == 0) ++subs[i];
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t v = sKV + ((g + 1) % ST) * TILE;
+  #pragma unroll
+                for (int kk = 0; kk < kKeys / 16; ++kk)
+                  mma_ts(tmem + kColO + i * HD, tmem + i * kKeys + 8 * kk, sdesc_v(v + kk * 2048), id_o, (j > 0 || kk > 0) ? 1u : 0u);
+                mma_commit(smem_u32(&b.o_full[i]));
+              }
+              if (i == 1) mma_commit(smem_u32(&b.kv_empty[(g + 1) % ST]));
+              if (j + 1 < n) {
+                if (i == 0) ok = full(g + 2);
+                if (ok && j + 1 < nn[i]) s_product(i, g + 2);
+                if (i == 1) {
+                  mma_commit(smem_u32(&b.kv_empty[(g + 2) % ST]));
+                  if (j + 2 == n) mma_commit(smem_u32(&b.q_empty));
+                }
+              }
+            }
+          }
+        }
+      }
+      __syncwarp();
+    }
+  } else {
+    // ------------------------------------------------------------- softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    const int sub = warp >= 8, quarter = warp & 3, row = 32 * quarter + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(32 * quarter) << 16);
+    const uint32_t tS = lanes + sub * kKeys, tO = lanes + kColO + sub * HD;
+    const float sc = a.scale2;
+    auto wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, a.err)); };
+    auto arrive = [&](uint64_t* bar) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(bar));
+    };
+    int g = 0;                                  // this sub-tile's key tiles so far
+    bool ok = true;
+    for (int it = 0; ok; ++it) {
+      const int slot = it & 1;
+      if (!wait(&b.item_full[slot], (it >> 1) & 1)) break;
+      const Item im = b.item[slot];
+      arrive(&b.item_empty[slot]);
+      if (im.n[0] == 0 && im.n[1] == 0) break;
+      const int n = im.n[sub];
+      if (n == 0) continue;
+      float m = -INFINITY, l = 0.f;             // the reference (raw score), the sum
+      for (int j = 0; j < n; ++j, ++g) {
+        if (!wait(&b.s_full[sub], g & 1)) { ok = false; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        uint32_t s[128];
+        float mq[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        tmem_ld32_async(tS, s);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          tmem_wait32(s + 32 * c);
+          if (c < 3) tmem_ld32_async(tS + 32 * (c + 1), s + 32 * (c + 1));
+          if (j == n - 1 && c >= quarter) {     // the diagonal tile: keys 0 .. row
+            const int lim = c == quarter ? lane : -1;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) s[32 * c + e] = e <= lim ? s[32 * c + e] : 0xff800000u;
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 8)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              mq[x] = max3f(mq[x], __uint_as_float(s[32 * c + e + 2 * x]), __uint_as_float(s[32 * c + e + 2 * x + 1]));
+        }
+        const float mx = fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3]));
+        const bool raise = j == 0 || (mx - m) * sc > kRaise;
+        if (j > 0 && __any_sync(~0u, raise)) {
+          // O follows the new reference once the product before has been added
+          const float f = raise ? mma::ex2((m - mx) * sc) : 1.f;
+          if (!wait(&b.o_full[sub], (g - 1) & 1)) { ok = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+          for (int c = 0; c < HD / 32; ++c) {
+            float o[32];
+            tmem_ld32(tO + 32 * c, o);
+#pragma unroll
+            for (int d = 0; d < 32; ++d) o[d] *= f;
+            tmem_st32(tO + 32 * c, o);
+          }
+          l *= f;
+        }
+        if (raise) m = mx;
+        const float nm = m == -INFINITY ? 0.f : -m * sc;
+        uint64_t ps[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int u = 0; u < 16; ++u) {
+            const float x = mma::ex2(fmaf(__uint_as_float(s[32 * c + 2 * u]), sc, nm));
+            const float y = mma::ex2(fmaf(__uint_as_float(s[32 * c + 2 * u + 1]), sc, nm));
+            ps[u & 3] = add_f2(ps[u & 3], f2(x, y));
+            pk[u] = pack2<T>(x, y);
+          }
+          tmem_st16(tS + 16 * c, pk);
+        }
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        arrive(&b.p_full[sub]);
+        const float2 s2 = f2_split(add_f2(add_f2(ps[0], ps[1]), add_f2(ps[2], ps[3])));
+        l += s2.x + s2.y;
+      }
+      if (!ok) break;
+      if (!wait(&b.o_full[sub], (g - 1) & 1)) { ok = false; break; }
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const float inv = 1.f / l;
+      const bool mine = im.row[sub] + row < im.len;
+      uint4* dst = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + (int64_t)(im.start + im.row[sub] + row) * a.out_row +
+                                            im.head[sub] * a.out_head);
+#pragma unroll
+      for (int c = 0; c < HD / 32; ++c) {
+        float o[32];
+        tmem_ld32(tO + 32 * c, o);
+        if (c == HD / 32 - 1) {
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          arrive(&b.o_free[sub]);
+        }
+        if (mine)
+#pragma unroll
+          for (int d = 0; d < 32; d += 8)
+            dst[4 * c + d / 8] = make_uint4(pack2<T>(o[d] * inv, o[d + 1] * inv), pack2<T>(o[d + 2] * inv, o[d + 3] * inv),
+                                            pack2<T>(o[d + 4] * inv, o[d + 5] * inv), pack2<T>(o[d + 6] * inv, o[d + 7] * inv));
+      }
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+}
+
+// [T][heads][hd] as boxes of 128 tokens x 64 elements of one head
+bool head_map(CUtensorMap* m, const void* p, int64_t T, int heads, int hd, int64_t row, int64_t head) {
+  const uint64_t dims[3] = {(uint64_t)hd, (uint64_t)heads, (uint64_t)T};
+  const uint64_t strides[2] = {(uint64_t)head * 2, (uint64_t)row * 2};
+  const uint32_t box[3] = {64, 1, kRows};
+  return encode_map_bf16(m, p, 3, dims, strides, box);      // (fp16 is copied the same way)
+}
+
+template <typename T, int HD>
+int launch(const Maps& maps, const Args& a, int grid, cudaStream_t s) {
+  static PerDevice attr;
+  set_smem_attr(attr, k_prompt<T, HD>, kSmem<HD>);
+  launch_cluster(k_prompt<T, HD>, dim3(grid), dim3(kThreads), kSmem<HD>, 1, true, s, maps, a);
+  return launched("kf_op_prompt_attention");
+}
+int64_t plan_items(int n, int64_t T) { return T / kRows + n; }
+
+}  // namespace
+}  // namespace kf
+
+using namespace kf;
+
+extern "C" int64_t kf_op_prompt_attention_work(int32_t n, int64_t T) {
+  return n < 0 || T < 0 ? 0 : 256 + plan_items(n, T) * (int64_t)sizeof(PlanItem);
+}
+
+extern "C" int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_t longest, int32_t Hq, int32_t Hkv, int32_t hd,
+                                      const void* q, int64_t q_row, int64_t q_head, const void* k, int64_t k_row, int64_t k_head,
+                                      const void* v, int64_t v_row, int64_t v_head, void* out, int64_t out_row, int64_t out_head,
+                                      const int32_t* starts, float scale, void* work, void* stream) {
+  const char* what = "kf_op_prompt_attention";
+  if (type != KF_TYPE_BF16 && type != KF_TYPE_FP16) return refuse(what, "the type is bf16 or fp16");
+  if (hd != 64 && hd != 128) return refuse(what, "head_dim is 64 or 128");
+  if (n < 0 || T < 0 || T > (1 << 30) || longest < 0 || longest > kMaxTiles * kRows) return refuse(what, "sequences or tokens out of range (a sequence has at most 524288)");
+  if (Hkv < 1 || Hq < 1 || Hq % Hkv || Hq > 4096) return refuse(what, "heads out of range");
+  if (!(scale > 0.f) || std::isinf(scale)) return refuse(what, "scale is a positive number");
+  if (n == 0 || T == 0) return n == 0 && T > 0 ? refuse(what, "tokens of no sequence") : KF_OK;
+  if (!q || !k || !v || !out || !starts || !work) return refuse(what, "a null array");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(starts, 4) || !aligned(work, 256))
+    return refuse(what, "q, k, v and out are 16-byte aligned, work 256-byte");
+  for (const int64_t st : {q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head})
+    if (st % 8 || st < 0 || st > (1ll << 37)) return refuse(what, "strides are multiples of 8 elements");
+  const int64_t cap = plan_items(n, T);
+  if (cap * Hq > 0x7fffffff - 4096) return refuse(what, "too many rows and heads");
+  Maps maps;
+  if (!head_map(&maps.q, q, T, Hq, hd, q_row, q_head) || !head_map(&maps.k, k, T, Hkv, hd, k_row, k_head) ||
+      !head_map(&maps.v, v, T, Hkv, hd, v_row, v_head))
+    return refuse(what, "a tensor map is refused (strides)");
+  int* err = serving_error_word();
+  if (!err) return refuse(what, "no error word", KF_E_CUDA);
+  const int G = Hq / Hkv, pairs = G % 2 == 0, rows = pairs ? kRows : 2 * kRows;
+  const int classes = std::max(1, ceil_div(longest, rows));
+  int* head = static_cast<int*>(work);
+  const Plan plan{head, head + 1, reinterpret_cast<PlanItem*>(head + 64)};
+  const int grid = (int)std::min<int64_t>(device_sms(), cap * (pairs ? Hq / 2 : Hq));
+  cudaStream_t s = (cudaStream_t)stream;
+  launch_cluster(k_plan, dim3(1), dim3(kPlanThreads), 2 * (classes + 2) * sizeof(int), 1, false, s, n, (int)T, longest, rows, classes,
+                 starts, plan, grid, err);
+  if (const int rc = launched(what)) return rc;
+  const Args a{out, out_row, out_head, plan, err, Hq, G, pairs, scale * 1.4426950408889634f};
+  if (type == KF_TYPE_BF16) return hd == 64 ? launch<__nv_bfloat16, 64>(maps, a, grid, s) : launch<__nv_bfloat16, 128>(maps, a, grid, s);
+  return hd == 64 ? launch<__half, 64>(maps, a, grid, s) : launch<__half, 128>(maps, a, grid, s);
+}

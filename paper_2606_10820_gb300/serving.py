@@ -23,6 +23,8 @@ _I32, _I64, _F32, _VP = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c
 _SIGNATURES = {
     "kf_op_token_scores": (ctypes.c_int, [_I32, _I64, _I32, _VP, _I64, _VP, _F32, _I32] + [_VP] * 6),
     "kf_op_token_scores_grad": (ctypes.c_int, [_I32, _I64, _I32, _VP, _I64, _VP, _F32] + [_VP] * 6 + [_I64, _VP]),
+    "kf_op_prompt_attention_work": (_I64, [_I32, _I64]),
+    "kf_op_prompt_attention": (ctypes.c_int, [_I32, _I32, _I64] + [_I32] * 4 + [_VP, _I64, _I64] * 4 + [_VP, _F32, _VP, _VP]),
     "kf_op_paged_attention_work": (_I64, [_I32]),
     "kf_op_paged_attention": (ctypes.c_int, [_I32] * 6 + [_VP] + [_I64] * 3 + [_VP, _I64, _I32, _VP, _I32, _VP, _F32] + [_VP] * 3),
     "kf_op_pages_work": (_I64, [_I32] * 3),
@@ -98,6 +100,26 @@ def _scratch(name, device, *args):
         with torch.cuda.device(device):
             n = _work_bytes[key] = max(16, getattr(_lib or _library(), name)(*args))
     return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def prompt_attention(q, k, v, starts, longest, scale=None, out=None):
+    """Causal attention over packed prompts: q [T, Hq, hd], k and v [T, Hkv, hd] (bf16 or fp16; any strides but the
+    last, so they may be parts of one projection's output), starts [n + 1] int32 on the GPU, the first tokens of the
+    sequences and T; longest: at least the longest one's tokens.  scale: 1 / sqrt(hd)."""
+    _need(q.is_cuda and q.dim() == k.dim() == v.dim() == 3 and q.dtype in _HALF, "q: [T, Hq, hd], k and v: [T, Hkv, hd], bf16 or fp16 on a GPU")
+    T, Hq, hd = q.shape
+    Hkv, dev, n = k.shape[1], q.device, starts.shape[0] - 1
+    _need(k.shape == v.shape == (T, Hkv, hd) and k.dtype == v.dtype == q.dtype and k.device == v.device == dev
+          and q.stride(2) == k.stride(2) == v.stride(2) == 1, "k and v: like q, heads of contiguous elements")
+    if out is None:
+        out = torch.empty((T, Hq, hd), dtype=q.dtype, device=dev)
+    else:
+        _need(out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.stride(2) == 1, "out: a tensor like q")
+    work = _scratch("kf_op_prompt_attention_work", dev, n, T)
+    _run("kf_op_prompt_attention", dev, _HALF[q.dtype], n, T, longest, Hq, Hkv, hd, q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(),
+         k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), out.data_ptr(), out.stride(0), out.stride(1),
+         _on(starts, dev, torch.int32, (n + 1,), "starts"), 1.0 / math.sqrt(hd) if scale is None else scale, work.data_ptr(), _stream(q))
+    return out
 
 
 def paged_attention(q, pool, table, lens, scale=None, out=None):
