@@ -7,34 +7,38 @@
 // (the sums against the maximum: no term cancels against another of its size).
 // A thread keeps (m, S, T) of the 16-byte vectors it reads; two such triples
 // join as S = S1 f1 + S2 f2, T = f1 (T1 + d1 S1) + f2 (T2 + d2 S2) with d = m_i - m
-// and f = exp(d).  All of it is fp32.
+// and f = exp(d).  All of it is fp32, in base-2 units: 2^d with d = x log2(e) - m log2(e).
 //
-// Top alternatives: the 512 threads of a row's CTA (CTAs) form 64 groups, and the
+// Top alternatives: the 256 threads of a row's CTA (CTAs) form 64 groups, and the
 // n-th largest of the 64 groups' maxima is at or below the n-th largest logit (n
-// groups have an element at or above it).  So only the threads whose own maximum
-// reaches that bound read their vectors again (from L2) and list the elements at or
-// above it, a few dozen of a vocabulary; each one's rank among them is its place.
-// Rows where that list would not fit (ties in the hundreds) choose round by round.
+// groups have an element at or above it).  So only the vectors of threads whose own
+// maximum reaches that bound are read again (from L2, a warp per such thread), and their
+// elements at or above it listed, a few dozen of a vocabulary; each one's rank among
+// them is its place.  Rows where that list would not fit (ties in the hundreds) choose round by round.
 //
 // What bounds it: the logits' bytes, read once (scores) or read and written once (gradient:
-// the second reading comes from L2).
+// the second reading comes from L2), and close behind them the instructions: five an
+// element and pass, most of them on pairs (fma.rn.f32x2).
 #include <algorithm>
 #include <cooperative_groups.h>
 
 #include "kf_serving.cuh"
+#include "kf_tc.cuh"
 
 namespace cg = cooperative_groups;
 
 namespace kf {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kGroups = 64;        // groups whose maxima bound the n-th largest logit
 constexpr int kMaxTop = kGroups;
+constexpr int kLanes = kThreads / kGroups;   // lanes of a group (times the CTAs of the row)
 constexpr int kList = 1024;        // listed candidates of a row
 constexpr int kRanked = 256;       // up to so many are ranked against each other, more are chosen in rounds
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLeast = -200.f;   // exp of it is 0 in fp32: stands for -inf where it multiplies that 0
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLeast = -300.f;   // 2^-300 is 0 in fp32: stands for -inf where it multiplies that 0
+constexpr float kBig = 1e38f;      // references past it would overflow in base-2 units
 
 struct Args {
   const void* logits;
@@ -46,74 +50,111 @@ struct Args {
   void* grad;
   int64_t grad_stride;
   int V, top;
-  float inv_tau;
+  float inv_tau, c2;               // 1 / tau, log2(e) / tau
   int* err;
 };
 
+// 2^x on the special-function unit: relative error about 2^-22
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// exp with 2^x of the special-function unit: relative error about 2^-22 plus the
-// rounding of the argument
-__device__ __forceinline__ float exp_fast(float x) { return ex2(x * kLog2e); }
 __device__ __forceinline__ uint4 ld_stream(const void* p) {
   uint4 u;
   asm("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
   return u;
 }
 
-// (m, S, T) of some elements; m = -inf: none of them is open (S and T are 0, or NaN)
-struct Sums {
-  float m, s, t;
+// What scores are taken against: the largest logit `raw` of some elements.  A
+// reference past kBig (a row at the type's lowest value) keeps its differences in
+// natural units until they are formed
+struct Ref {
+  float raw, nm;                   // nm: minus the reference, base-2 units (natural where big)
+  bool big;
+  __device__ __forceinline__ void set(const Args& a, float r) {
+    const float m = r * a.inv_tau;
+    raw = r;
+    big = fabsf(m) > kBig && fabsf(m) < INFINITY;
+    nm = m == -INFINITY ? 0.f : big ? -m : -__fmul_rn(r, a.c2);
+  }
+  __device__ __forceinline__ bool open(const Args& a) const { return raw * a.inv_tau != -INFINITY; }
+  // log2 of exp(x - m)
+  __device__ __forceinline__ float less(const Args& a, float v) const {
+    return big ? fmaf(v, a.inv_tau, nm) * kLog2e : fmaf(v, a.c2, nm);
+  }
 };
-__device__ __forceinline__ Sums join(Sums a, Sums b) {
-  const float m = fmaxf(a.m, b.m);
-  Sums r{m, 0.f, 0.f};
+
+// S and T (base-2 units) of some elements against their Ref; without an open element they are 0 (or NaN)
+struct Sums {
+  float raw, s, t;
+};
+__device__ __forceinline__ Sums join(const Args& a, Sums x, Sums y) {
+  Ref r;
+  r.set(a, fmaxf(x.raw, y.raw));
+  Sums o{r.raw, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const Sums c = i ? b : a;
-    const float d = c.m == -INFINITY ? 0.f : fmaxf(c.m - m, kLeast), f = exp_fast(d);
-    r.s += f * c.s;
-    r.t += f * fmaf(d, c.s, c.t);
+    const Sums c = i ? y : x;
+    // (the difference of the two references as they were rounded: no fused multiply-add)
+    const float by = r.big ? r.less(a, c.raw) : __fadd_rn(__fmul_rn(c.raw, a.c2), r.nm);
+    const float d = c.raw * a.inv_tau == -INFINITY ? 0.f : fmaxf(by, kLeast), f = ex2(d);
+    o.s += f * c.s;
+    o.t += f * fmaf(d, c.s, c.t);
   }
-  return r;
+  return o;
 }
 
 // one thread's pass over its elements
 struct Pass {
-  float raw = -INFINITY;   // the largest logit so far
-  float nm = 0.f;          // minus the reference: -raw / tau (0 while that is infinite)
-  float s = 0.f, t = 0.f;
-  __device__ __forceinline__ float m(float inv_tau) const { return raw * inv_tau; }
-  __device__ __forceinline__ void raise(float to, float inv_tau) {
-    const float was = raw * inv_tau, m = to * inv_tau;
-    if (was != -INFINITY) {
-      const float d = fmaxf(was - m, kLeast), f = exp_fast(d);
-      t = f * fmaf(d, s, t);
-      s *= f;
+  Ref r;
+  uint64_t s = 0ull, t = 0ull;     // S and T, each in two lanes
+  __device__ __forceinline__ Pass() : r{-INFINITY, 0.f, false} {}
+  __device__ __forceinline__ void raise(const Args& a, float to) {
+    const Ref was = r;
+    r.set(a, to);
+    if (was.open(a)) {
+      const float by = r.big ? r.less(a, was.raw) : was.big ? -INFINITY : __fsub_rn(r.nm, was.nm);
+      const float d = fmaxf(by, kLeast), f = ex2(d);
+      t = mul_f2(f2(f, f), fma_f2(f2(d, d), s, t));
+      s = mul_f2(f2(f, f), s);
     }
-    raw = to;
-    nm = m == -INFINITY ? 0.f : -m;
+  }
+  __device__ __forceinline__ void pair(float dx, float dy) {
+    const uint64_t e = f2(ex2(dx), ex2(dy));
+    s = add_f2(s, e);
+    t = fma_f2(e, f2(fmaxf(dx, kLeast), fmaxf(dy, kLeast)), t);
   }
   template <int N>
-  __device__ __forceinline__ void add(const float* v, float inv_tau) {
-    float top = v[0];
+  __device__ __forceinline__ void add(const Args& a, const float* v) {
+    float top = fmaxf(v[0], v[1]);
 #pragma unroll
-    for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
-    if (top > raw) raise(top, inv_tau);
+    for (int i = 2; i < N; i += 2) top = max3f(top, v[i], v[i + 1]);
+    if (top > r.raw) raise(a, top);
+    if (!r.big) {
+      const uint64_t c = f2(a.c2, a.c2), nm = f2(r.nm, r.nm);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float d = fmaf(v[i], inv_tau, nm), e = exp_fast(d);
-      s += e;
-      t = fmaf(e, fmaxf(d, kLeast), t);
+      for (int i = 0; i < N; i += 2) {
+        const float2 d = f2_split(fma_f2(f2(v[i], v[i + 1]), c, nm));
+        pair(d.x, d.y);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; i += 2) pair(r.less(a, v[i]), r.less(a, v[i + 1]));
     }
+  }
+  __device__ __forceinline__ void add_one(const Args& a, float v) {
+    if (v > r.raw) raise(a, v);
+    pair(r.less(a, v), -INFINITY);
+  }
+  __device__ __forceinline__ Sums sums() const {
+    const float2 a = f2_split(s), b = f2_split(t);
+    return Sums{r.raw, a.x + a.y, b.x + b.y};
   }
 };
 
 // A row's elements in 16-byte vectors: `head` elements lie before the first
-// aligned one, then nvec vectors, then `tail` elements
+// aligned one, then nvec vectors, then the rest
 template <typename T>
 struct Row {
   const T* p;
@@ -127,20 +168,14 @@ struct Row {
   __device__ __forceinline__ int edge_id(int j) const { return j < head ? j : j + nvec * Vec16<T>::N; }
 };
 
-// f(id, x) for each element of thread `me` of `all` threads
+// f(id, logit) for the elements of vector i
 template <typename T, typename F>
-__device__ __forceinline__ void each_element(const Row<T>& row, int me, int all, F f) {
-  for (int j = me; j < row.edge(); j += all) {
-    const int id = row.edge_id(j);
-    f(id, to_f(row.p[id]));
-  }
-  for (int i = me; i < row.nvec; i += all) {
-    float v[Vec16<T>::N];
-    Vec16<T>::unpack(*reinterpret_cast<const uint4*>(row.vec(i)), v);
-    const int id0 = row.head + i * Vec16<T>::N;
+__device__ __forceinline__ void each_of_vector(const Row<T>& row, int i, F f) {
+  float v[Vec16<T>::N];
+  Vec16<T>::unpack(*reinterpret_cast<const uint4*>(row.vec(i)), v);
+  const int id0 = row.head + i * Vec16<T>::N;
 #pragma unroll
-    for (int e = 0; e < Vec16<T>::N; ++e) f(id0 + e, v[e]);
-  }
+  for (int e = 0; e < Vec16<T>::N; ++e) f(id0 + e, v[e]);
 }
 
 struct Cand {
@@ -169,7 +204,8 @@ struct Shared {
   Sums cta;
   float group[kGroups];
   float bound;
-  int count;
+  int count, again;
+  int thread[kThreads];            // threads whose vectors are read again
   Cand first[kWarps];
   Cand list[kList];
 };
@@ -177,7 +213,7 @@ struct Shared {
 // Clusters of CS CTAs share a row (CS = 1: no cluster).  GRAD: the gradient's
 // second pass instead of the alternatives.
 template <typename T, int CS, bool GRAD>
-__global__ void __launch_bounds__(kThreads, 2) k_scores(const Args a) {
+__global__ void __launch_bounds__(kThreads, 4) k_scores(const Args a) {
   __shared__ Shared sh;
   constexpr int N = Vec16<T>::N;
   constexpr int kAll = CS * kThreads;
@@ -200,49 +236,45 @@ __global__ void __launch_bounds__(kThreads, 2) k_scores(const Args a) {
       for (int j = 0; j < 4; ++j) {
         float v[N];
         Vec16<T>::unpack(u[j], v);
-        ps.add<N>(v, a.inv_tau);
+        ps.add<N>(a, v);
       }
     }
     for (; i < row.nvec; i += kAll) {
       float v[N];
       Vec16<T>::unpack(ld_stream(row.vec(i)), v);
-      ps.add<N>(v, a.inv_tau);
-    }
-    for (int j = me; j < row.edge(); j += kAll) {
-      const float v = to_f(row.p[row.edge_id(j)]);
-      ps.add<1>(&v, a.inv_tau);
+      ps.add<N>(a, v);
     }
   }
+  const float vec_max = ps.r.raw;
+  if (me < row.edge()) ps.add_one(a, to_f(row.p[row.edge_id(me)]));      // (fewer than 256 of them)
   // the row's sums, in one fixed order
-  Sums su{ps.m(a.inv_tau), ps.s, ps.t};
+  Sums su = ps.sums();
+  auto join_lanes = [&](int o) {
+    const Sums other{__shfl_xor_sync(~0u, su.raw, o), __shfl_xor_sync(~0u, su.s, o), __shfl_xor_sync(~0u, su.t, o)};
+    su = (lane & o) ? join(a, other, su) : join(a, su, other);
+  };
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const Sums other{__shfl_xor_sync(~0u, su.m, o), __shfl_xor_sync(~0u, su.s, o), __shfl_xor_sync(~0u, su.t, o)};
-    su = (lane & o) ? join(other, su) : join(su, other);
-  }
+  for (int o = 16; o; o >>= 1) join_lanes(o);
   if (lane == 0) sh.warp[warp] = su;
   if (!GRAD && a.top) {
-    // the groups' maxima: 8 CS lanes each
-    float gm = ps.raw;
+    // the groups' maxima
+    float gm = ps.r.raw;
 #pragma unroll
-    for (int o = 1; o < 8 * CS; o <<= 1) gm = fmaxf(gm, __shfl_xor_sync(~0u, gm, o));
-    if (t % (8 * CS) == 0) sh.group[t / (8 * CS)] = gm;
-    if (t == 0) sh.count = 0;
+    for (int o = 1; o < kLanes * CS; o <<= 1) gm = fmaxf(gm, __shfl_xor_sync(~0u, gm, o));
+    if (t % (kLanes * CS) == 0) sh.group[t / (kLanes * CS)] = gm;
+    if (t == 0) sh.count = sh.again = 0;
   }
   __syncthreads();
   su = sh.warp[lane % kWarps];
 #pragma unroll
-  for (int o = kWarps / 2; o; o >>= 1) {
-    const Sums other{__shfl_xor_sync(~0u, su.m, o), __shfl_xor_sync(~0u, su.s, o), __shfl_xor_sync(~0u, su.t, o)};
-    su = (lane & o) ? join(other, su) : join(su, other);
-  }
+  for (int o = kWarps / 2; o; o >>= 1) join_lanes(o);
   Shared* lead = &sh;
   if constexpr (CS > 1) {
     cg::cluster_group cl = cg::this_cluster();
     if (t == 0) sh.cta = su;
     cl.sync();
     su = cl.map_shared_rank(&sh, 0)->cta;
-    for (int c = 1; c < CS; ++c) su = join(su, cl.map_shared_rank(&sh, c)->cta);
+    for (int c = 1; c < CS; ++c) su = join(a, su, cl.map_shared_rank(&sh, c)->cta);
     lead = cl.map_shared_rank(&sh, 0);
     // every CTA has all groups' maxima
     const bool take = !GRAD && a.top && t < kGroups;
@@ -252,44 +284,63 @@ __global__ void __launch_bounds__(kThreads, 2) k_scores(const Args a) {
     if (take) sh.group[t] = g;
     __syncthreads();
   }
-  const bool none = su.m == -INFINITY && su.s == 0.f;     // every token closed
+  Ref ref;
+  ref.set(a, su.raw);
+  const bool none = !ref.open(a) && su.s == 0.f;          // every token closed
   const bool bad = !(su.s > 0.f) && !none;                // NaN or +inf in the row
-  const float logs = logf(su.s);
-  const float lse = none ? -INFINITY : bad ? NAN : su.m + logs;
-  const float H = none ? 0.f : bad ? NAN : logs - su.t / su.s;
+  const float logs = log2f(su.s);                         // (base-2 units)
+  const float lse = none ? -INFINITY : bad ? NAN : su.raw * a.inv_tau + logs * kLn2;
+  const float H = none ? 0.f : bad ? NAN : (logs - su.t / su.s) * kLn2;
+  // log p of a logit: from the difference to the reference, not from lse, which loses log S where the
+  // reference is the type's lowest value (and in natural units where base-2 ones overflow)
+  auto lp_of = [&](float v) {
+    const float x = v * a.inv_tau;
+    return fabsf(x) > kBig ? (x - ref.raw * a.inv_tau) - logs * kLn2 : (ref.less(a, v) - logs) * kLn2;
+  };
   if (rank == 0 && t == 0) {
     if (a.lse) a.lse[r] = lse;
     if (a.entropy) a.entropy[r] = H;
     if (token >= a.V) atomicOr(a.err, KF_DEV_BAD_TOKEN);
-    if (a.logp)
-      a.logp[r] = token < 0 ? 0.f : token >= a.V || bad ? NAN : none ? -INFINITY : (at_logit * a.inv_tau - su.m) - logs;
+    if (a.logp) a.logp[r] = token < 0 ? 0.f : token >= a.V || bad ? NAN : none ? -INFINITY : lp_of(at_logit);
   }
 
   if constexpr (GRAD) {
     const bool has = token >= 0 && token < a.V;
     const float gl = has && a.g_logp ? a.g_logp[r] : 0.f, gh = a.g_entropy ? a.g_entropy[r] : 0.f;
-    // grad = p (A + B lp) + (v == token) gl, over tau
-    const float A = (-gl - gh * H) * a.inv_tau, B = -gh * a.inv_tau;
-    const float at_token = gl * a.inv_tau;
+    // grad = p (A + B log2 p) + (v == token) gl / tau.  A row with a NaN has A = NaN; one
+    // without open tokens p = 0
+    const float A = (-gl - gh * H) * a.inv_tau, B = -gh * a.inv_tau * kLn2;
+    const float at_token = none ? 0.f : gl * a.inv_tau;
     T* out = static_cast<T*>(a.grad) + r * a.grad_stride;
-    auto one = [&](int id, float v) {
-      const float lp = fmaxf(fmaf(v, a.inv_tau, -su.m) - logs, kLeast);
-      float g = exp_fast(lp) * fmaf(B, lp, A);
-      if (id == token) g += at_token;
-      return none ? 0.f : bad ? NAN : g;
+    const uint64_t c2 = f2(a.c2, a.c2), nm = f2(ref.nm, ref.nm), nlogs = f2(-logs, -logs), A2 = f2(A, A), B2 = f2(B, B);
+    auto pair = [&](float& x, float& y) {
+      float2 d;
+      if (!ref.big) d = f2_split(add_f2(fma_f2(f2(x, y), c2, nm), nlogs));      // (one constant for both would lose log S)
+      else d = make_float2(ref.less(a, x) - logs, ref.less(a, y) - logs);
+      d.x = fmaxf(d.x, kLeast);
+      d.y = fmaxf(d.y, kLeast);
+      const float2 g = f2_split(mul_f2(f2(ex2(d.x), ex2(d.y)), fma_f2(B2, f2(d.x, d.y), A2)));
+      x = g.x;
+      y = g.y;
     };
     const bool same = (reinterpret_cast<uintptr_t>(out) & 15) == (reinterpret_cast<uintptr_t>(row.p) & 15);
-    for (int j = me; j < row.edge(); j += kAll) {
-      const int id = row.edge_id(j);
-      out[id] = from_f<T>(one(id, to_f(row.p[id])));
+    if (me < row.edge()) {
+      const int id = row.edge_id(me);
+      float x = to_f(row.p[id]), y = -INFINITY;
+      pair(x, y);
+      out[id] = from_f<T>(id == token ? x + at_token : x);
     }
-    int i = me;
     auto store = [&](int i, uint4 u) {
       float v[N];
       Vec16<T>::unpack(u, v);
       const int id0 = row.head + i * N;
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = one(id0 + e, v[e]);
+      for (int e = 0; e < N; e += 2) pair(v[e], v[e + 1]);
+      if (token >= id0 && token < id0 + N) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (id0 + e == token) v[e] += at_token;
+      }
       if (same) {
         *reinterpret_cast<uint4*>(out + id0) = Vec16<T>::pack(v);
       } else {
@@ -297,6 +348,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scores(const Args a) {
         for (int e = 0; e < N; ++e) out[id0 + e] = from_f<T>(v[e]);
       }
     };
+    int i = me;
     for (; i + 3 * kAll < row.nvec; i += 4 * kAll) {
       uint4 u[4];
 #pragma unroll
@@ -322,6 +374,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scores(const Args a) {
   if (t < kGroups) {
     const float g = sh.group[t];
     int rk = 0;
+#pragma unroll 16
     for (int j = 0; j < kGroups; ++j) rk += sh.group[j] > g || (sh.group[j] == g && j < t);
     if (rk == a.top - 1) sh.bound = g * a.inv_tau;
   }
@@ -329,21 +382,25 @@ __global__ void __launch_bounds__(kThreads, 2) k_scores(const Args a) {
   const float bound = sh.bound;
   // (a bound of -inf: the open tokens are listed, the closed ones follow by id)
   auto listed = [&](float x) { return x >= bound && x > -INFINITY; };
-  if (listed(ps.raw * a.inv_tau))
-    each_element(row, me, kAll, [&](int id, float v) {
-      const float x = v * a.inv_tau;
-      if (listed(x)) {
-        const int at = atomicAdd(&lead->count, 1);
-        if (at < kList) lead->list[at] = Cand{x, id};
-      }
-    });
+  auto list = [&](int id, float v) {
+    const float x = v * a.inv_tau;
+    if (listed(x)) {
+      const int at = atomicAdd(&lead->count, 1);
+      if (at < kList) lead->list[at] = Cand{x, id};
+    }
+  };
+  if (listed(vec_max * a.inv_tau)) sh.thread[atomicAdd(&sh.again, 1)] = t;
+  if (me < row.edge()) list(row.edge_id(me), to_f(row.p[row.edge_id(me)]));
+  __syncthreads();
+  for (int k = warp; k < sh.again; k += kWarps)
+    for (int i = rank * kThreads + sh.thread[k] + lane * kAll; i < row.nvec; i += 32 * kAll) each_of_vector(row, i, list);
   if constexpr (CS > 1) cg::this_cluster().sync();
   else __syncthreads();
   if (rank != 0) return;
   const int n = sh.count;
   auto put = [&](int place, Cand c) {
     ids[place] = c.id;
-    lps[place] = (c.x - su.m) - logs;      // (lse itself loses log S where m is the type's lowest value)
+    lps[place] = lp_of(to_f(row.p[c.id]));
   };
   if (n <= kRanked) {
     if (t < n) {
@@ -361,13 +418,16 @@ __global__ void __launch_bounds__(kThreads, 2) k_scores(const Args a) {
       auto look = [&](Cand d) {
         if (before(last, d) && before(d, c)) c = d;
       };
-      if (n <= kList)
+      auto look_at = [&](int id, float v) {
+        const float x = v * a.inv_tau;
+        if (listed(x)) look(Cand{x, id});
+      };
+      if (n <= kList) {
         for (int j = t; j < n; j += kThreads) look(sh.list[j]);
-      else
-        each_element(row, t, kThreads, [&](int id, float v) {
-          const float x = v * a.inv_tau;
-          if (listed(x)) look(Cand{x, id});
-        });
+      } else {
+        if (t < row.edge()) look_at(row.edge_id(t), to_f(row.p[row.edge_id(t)]));
+        for (int i = t; i < row.nvec; i += kThreads) each_of_vector(row, i, look_at);
+      }
       last = block_first(c, sh.first);
       if (t == 0) put(k, last);
     }
@@ -388,9 +448,11 @@ int launch(const Args& a, int64_t R, cudaStream_t s) {
   // Few rows: a row is split over a cluster while the CTAs fit the SMs, and each
   // thread keeps two vectors
   const int64_t sms = device_sms(), vecs = a.V / Vec16<T>::N;
-  const int cs = R * 4 <= sms && vecs >= 4 * 2 * kThreads ? 4 : R * 2 <= sms && vecs >= 2 * 2 * kThreads ? 2 : 1;
+  const int cs = R * 8 <= sms && vecs >= 8 * 2 * kThreads ? 8 : R * 4 <= 2 * sms && vecs >= 4 * 2 * kThreads ? 4
+                 : R * 2 <= 3 * sms && vecs >= 2 * 2 * kThreads ? 2 : 1;
   const dim3 grid((unsigned)(R * cs));
-  if (cs == 4) launch_cluster(k_scores<T, 4, GRAD>, grid, dim3(kThreads), 0, 4, false, s, a);
+  if (cs == 8) launch_cluster(k_scores<T, 8, GRAD>, grid, dim3(kThreads), 0, 8, false, s, a);
+  else if (cs == 4) launch_cluster(k_scores<T, 4, GRAD>, grid, dim3(kThreads), 0, 4, false, s, a);
   else if (cs == 2) launch_cluster(k_scores<T, 2, GRAD>, grid, dim3(kThreads), 0, 2, false, s, a);
   else launch_cluster(k_scores<T, 1, GRAD>, grid, dim3(kThreads), 0, 1, false, s, a);
   return launched(GRAD ? "kf_op_token_scores_grad" : "kf_op_token_scores");
@@ -411,6 +473,7 @@ int scores(const char* what, int32_t type, int64_t R, Args a, float tau, cudaStr
   if (GRAD && (!a.grad || !aligned(a.grad, size) || a.grad_stride < a.V)) return refuse(what, "grad: null, misaligned or rows too near");
   if (GRAD && a.grad == a.logits && a.grad_stride != a.stride) return refuse(what, "grad over the logits has their row stride");
   a.inv_tau = 1.f / tau;
+  a.c2 = a.inv_tau * kLog2e;
   if (!(a.err = serving_error_word())) return refuse(what, "no error word", KF_E_CUDA);
   if (type == KF_TYPE_FP32) return launch<float, GRAD>(a, R, s);
   if (type == KF_TYPE_BF16) return launch<__nv_bfloat16, GRAD>(a, R, s);
@@ -425,7 +488,7 @@ using namespace kf;
 extern "C" int kf_op_token_scores(int32_t type, int64_t R, int32_t V, const void* logits, int64_t stride,
                                   const int64_t* tokens, float tau, int32_t top, float* logp, float* entropy,
                                   float* lse, int32_t* top_ids, float* top_logp, void* stream) {
-  Args a{logits, stride, tokens, nullptr, nullptr, logp, entropy, lse, top_logp, top_ids, nullptr, 0, V, top, 1.f, nullptr};
+  Args a{logits, stride, tokens, nullptr, nullptr, logp, entropy, lse, top_logp, top_ids, nullptr, 0, V, top, 1.f, 1.f, nullptr};
   return scores<false>("kf_op_token_scores", type, R, a, tau, (cudaStream_t)stream);
 }
 
@@ -433,6 +496,6 @@ extern "C" int kf_op_token_scores_grad(int32_t type, int64_t R, int32_t V, const
                                        const int64_t* tokens, float tau, const float* g_logp,
                                        const float* g_entropy, float* logp, float* entropy, float* lse,
                                        void* grad, int64_t grad_stride, void* stream) {
-  Args a{logits, stride, tokens, g_logp, g_entropy, logp, entropy, lse, nullptr, nullptr, grad, grad_stride, V, 0, 1.f, nullptr};
+  Args a{logits, stride, tokens, g_logp, g_entropy, logp, entropy, lse, nullptr, nullptr, grad, grad_stride, V, 0, 1.f, 1.f, nullptr};
   return scores<true>("kf_op_token_scores_grad", type, R, a, tau, (cudaStream_t)stream);
 }

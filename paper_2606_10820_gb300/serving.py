@@ -51,8 +51,8 @@ def _library():
     return _lib
 
 
-def _stream(t):
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+_stream = torch._C._cuda_getCurrentRawStream     # the current stream of a device, by its index
+_empty, _F, _I = torch.empty, torch.float32, torch.int32
 
 
 def _need(ok, what):
@@ -99,7 +99,7 @@ def _scratch(name, device, *args):
     if n is None:
         with torch.cuda.device(device):
             n = _work_bytes[key] = max(16, getattr(_lib or _library(), name)(*args))
-    return torch.empty(n, dtype=torch.uint8, device=device)
+    return _empty(n, dtype=torch.uint8, device=device)
 
 
 def prompt_attention(q, k, v, starts, longest, scale=None, out=None):
@@ -112,13 +112,13 @@ def prompt_attention(q, k, v, starts, longest, scale=None, out=None):
     _need(k.shape == v.shape == (T, Hkv, hd) and k.dtype == v.dtype == q.dtype and k.device == v.device == dev
           and q.stride(2) == k.stride(2) == v.stride(2) == 1, "k and v: like q, heads of contiguous elements")
     if out is None:
-        out = torch.empty((T, Hq, hd), dtype=q.dtype, device=dev)
+        out = _empty((T, Hq, hd), dtype=q.dtype, device=dev)
     else:
         _need(out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.stride(2) == 1, "out: a tensor like q")
     work = _scratch("kf_op_prompt_attention_work", dev, n, T)
     _run("kf_op_prompt_attention", dev, _HALF[q.dtype], n, T, longest, Hq, Hkv, hd, q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(),
          k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), out.data_ptr(), out.stride(0), out.stride(1),
-         _on(starts, dev, torch.int32, (n + 1,), "starts"), 1.0 / math.sqrt(hd) if scale is None else scale, work.data_ptr(), _stream(q))
+         _on(starts, dev, _I, (n + 1,), "starts"), 1.0 / math.sqrt(hd) if scale is None else scale, work.data_ptr(), _stream(dev.index))
     return out
 
 
@@ -135,13 +135,13 @@ def paged_attention(q, pool, table, lens, scale=None, out=None):
     dev = q.device
     _need(two == 2 and q.stride(3) == 1, "pool: K and V of each page; q: heads of contiguous elements")
     if out is None:
-        out = torch.empty((B, rows, Hq, hd), dtype=q.dtype, device=dev)
+        out = _empty((B, rows, Hq, hd), dtype=q.dtype, device=dev)
     work = _scratch("kf_op_paged_attention_work", dev, hd)
     width = table.shape[1]
     _run("kf_op_paged_attention", dev, _HALF[q.dtype], B, rows, Hq, Hkv, hd, q.data_ptr(), q.stride(0), q.stride(1), q.stride(2),
          _on(pool, dev, q.dtype, (n_pages, 2, Hkv, page, hd), "pool"), n_pages, page,
-         _on(table, dev, torch.int32, (B, width), "table"), width, _on(lens, dev, torch.int32, (B,), "lens"),
-         1.0 / math.sqrt(hd) if scale is None else scale, _on(out, dev, q.dtype, q.shape, "out"), work.data_ptr(), _stream(q))
+         _on(table, dev, _I, (B, width), "table"), width, _on(lens, dev, _I, (B,), "lens"),
+         1.0 / math.sqrt(hd) if scale is None else scale, _on(out, dev, q.dtype, q.shape, "out"), work.data_ptr(), _stream(dev.index))
     return out
 
 
@@ -152,20 +152,20 @@ def paged_attention(q, pool, table, lens, scale=None, out=None):
 
 def new_book(n_pages, slots, width, device="cuda"):
     """An empty book: (ref, table, lens)."""
-    return (torch.zeros(n_pages, dtype=torch.int32, device=device), torch.full((slots, width), -1, dtype=torch.int32, device=device),
-            torch.zeros(slots, dtype=torch.int32, device=device))
+    return (torch.zeros(n_pages, dtype=_I, device=device), torch.full((slots, width), -1, dtype=_I, device=device),
+            torch.zeros(slots, dtype=_I, device=device))
 
 
 def _book(ref, table, lens=None):
     _need(ref.is_cuda and ref.dim() == 1 and table.dim() == 2, "ref: [pages], table: [slots, width], int32 on a GPU")
     dev, (slots, width) = ref.device, table.shape
-    return (dev, ref.shape[0], slots, width, _on(ref, dev, torch.int32, ref.shape, "ref"), _on(table, dev, torch.int32, table.shape, "table"),
-            None if lens is None else _on(lens, dev, torch.int32, (slots,), "lens"))
+    return (dev, ref.shape[0], slots, width, _on(ref, dev, _I, ref.shape, "ref"), _on(table, dev, _I, table.shape, "table"),
+            None if lens is None else _on(lens, dev, _I, (slots,), "lens"))
 
 
 def _list(x, dev, n, what):
     _need(x.dim() == 1, what + ": a list of int32 on the GPU")
-    return _on(x, dev, torch.int32, (n,), what)
+    return _on(x, dev, _I, (n,), what)
 
 
 def _pool(pool, dev, n_pages):
@@ -181,7 +181,7 @@ def pages_grow(ref, table, lens, slots, new_lens, page=16):
     n = slots.shape[0]
     work = _scratch("kf_op_pages_work", dev, n_pages, n_slots, n)
     _run("kf_op_pages_grow", dev, n, _list(slots, dev, n, "slots"), _list(new_lens, dev, n, "new_lens"), pr, n_pages, pt, n_slots, width,
-         pl, page, work.data_ptr(), _stream(ref))
+         pl, page, work.data_ptr(), _stream(dev.index))
 
 
 def pages_free(ref, table, lens, slots, page=16):
@@ -189,7 +189,7 @@ def pages_free(ref, table, lens, slots, page=16):
     dev, n_pages, n_slots, width, pr, pt, pl = _book(ref, table, lens)
     n = slots.shape[0]
     work = _scratch("kf_op_pages_work", dev, n_pages, n_slots, n)
-    _run("kf_op_pages_free", dev, n, _list(slots, dev, n, "slots"), pr, n_pages, pt, n_slots, width, pl, page, work.data_ptr(), _stream(ref))
+    _run("kf_op_pages_free", dev, n, _list(slots, dev, n, "slots"), pr, n_pages, pt, n_slots, width, pl, page, work.data_ptr(), _stream(dev.index))
 
 
 def pages_fork(pool, ref, table, lens, src, dst):
@@ -201,7 +201,7 @@ def pages_fork(pool, ref, table, lens, src, dst):
     n = src.shape[0]
     work = _scratch("kf_op_pages_work", dev, n_pages, n_slots, n)
     _run("kf_op_pages_fork", dev, n, _list(src, dev, n, "src"), _list(dst, dev, n, "dst"), pr, n_pages, pt, n_slots, width, pl,
-         pool.shape[4], pp, layers, page_bytes, work.data_ptr(), _stream(ref))
+         pool.shape[4], pp, layers, page_bytes, work.data_ptr(), _stream(dev.index))
 
 
 def pages_compact(pool, ref, table, live=None):
@@ -210,7 +210,7 @@ def pages_compact(pool, ref, table, live=None):
     pp, layers, page_bytes = _pool(pool, dev, n_pages)
     work = _scratch("kf_op_pages_work", dev, n_pages, n_slots, 0)
     _run("kf_op_pages_compact", dev, pr, n_pages, pt, n_slots, width, pp, layers, page_bytes,
-         None if live is None else _on(live, dev, torch.int32, (1,), "live"), work.data_ptr(), _stream(ref))
+         None if live is None else _on(live, dev, _I, (1,), "live"), work.data_ptr(), _stream(dev.index))
 
 
 def pages_copy(pool, src, dst):
@@ -218,7 +218,7 @@ def pages_copy(pool, src, dst):
     _need(pool.is_cuda, "pool: on a GPU")
     dev, n = pool.device, src.shape[0]
     pp, layers, page_bytes = _pool(pool, dev, pool.shape[1])
-    _run("kf_op_pages_copy", dev, n, _list(src, dev, n, "src"), _list(dst, dev, n, "dst"), pp, layers, pool.shape[1], page_bytes, _stream(pool))
+    _run("kf_op_pages_copy", dev, n, _list(src, dev, n, "src"), _list(dst, dev, n, "dst"), pp, layers, pool.shape[1], page_bytes, _stream(dev.index))
 
 
 def pages_append(pool, k, v, starts, table, lens, slots):
@@ -232,7 +232,7 @@ def pages_append(pool, k, v, starts, table, lens, slots):
           and k.device == v.device == dev and k.stride(2) == v.stride(2) == 1, "k and v: rows of the pool's heads and type")
     _run("kf_op_pages_append", dev, n, _list(slots, dev, n, "slots"), _list(starts, dev, n + 1, "starts"), T, Hkv, hd, k.data_ptr(),
          k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), pool.data_ptr(), n_pages, page,
-         _on(table, dev, torch.int32, table.shape, "table"), n_slots, width, _on(lens, dev, torch.int32, (n_slots,), "lens"), _stream(pool))
+         _on(table, dev, _I, table.shape, "table"), n_slots, width, _on(lens, dev, _I, (n_slots,), "lens"), _stream(dev.index))
 
 
 # ------------------------------------------------------------------ scores
@@ -253,16 +253,16 @@ def token_scores(logits, tokens, top=0, tau=1.0):
     R, V, stride, tok = _score_args(logits, tokens, tau)
     _need(0 <= top <= min(64, V), "top: 0 to 64, and at most the vocabulary")
     dev = logits.device
-    nums = torch.empty((3, R), dtype=torch.float32, device=dev)
-    out = {"logp": nums[0], "entropy": nums[1], "lse": nums[2]}
-    p = nums.data_ptr()
+    # (an allocation each: parts of one tensor whose whole is dropped cost more)
+    logp, entropy, lse = _empty((R,), dtype=_F, device=dev), _empty((R,), dtype=_F, device=dev), _empty((R,), dtype=_F, device=dev)
+    out = {"logp": logp, "entropy": entropy, "lse": lse}
     ids = lps = None
     if top:
-        out["top_ids"] = ids = torch.empty((R, top), dtype=torch.int32, device=dev)
-        out["top_logp"] = lps = torch.empty((R, top), dtype=torch.float32, device=dev)
+        out["top_ids"] = ids = _empty((R, top), dtype=_I, device=dev)
+        out["top_logp"] = lps = _empty((R, top), dtype=_F, device=dev)
         ids, lps = ids.data_ptr(), lps.data_ptr()
-    _run("kf_op_token_scores", dev, _TYPES[logits.dtype], R, V, logits.data_ptr(), stride, tok, tau, top, p, p + 4 * R,
-         p + 8 * R, ids, lps, _stream(logits))
+    _run("kf_op_token_scores", dev, _TYPES[logits.dtype], R, V, logits.data_ptr(), stride, tok, tau, top, logp.data_ptr(),
+         entropy.data_ptr(), lse.data_ptr(), ids, lps, _stream(dev.index))
     return out
 
 
@@ -273,12 +273,11 @@ def token_scores_grad(logits, tokens, g_logp=None, g_entropy=None, tau=1.0, out=
     R, V, stride, tok = _score_args(logits, tokens, tau)
     dev = logits.device
     gl, gh = (None if g is None else _on(g, dev, torch.float32, (R,), n) for g, n in ((g_logp, "g_logp"), (g_entropy, "g_entropy")))
-    grad = torch.empty((R, V), dtype=logits.dtype, device=dev) if out is None else out
+    grad = _empty((R, V), dtype=logits.dtype, device=dev) if out is None else out
     if out is not None:
         _need(out.dtype == logits.dtype and out.device == dev and out.shape == logits.shape and (out.stride(1) == 1 or V == 1),
               "out: a tensor like the logits")
-    nums = torch.empty((3, R), dtype=torch.float32, device=dev)
-    p = nums.data_ptr()
-    _run("kf_op_token_scores_grad", dev, _TYPES[logits.dtype], R, V, logits.data_ptr(), stride, tok, tau, gl, gh, p, p + 4 * R,
-         p + 8 * R, grad.data_ptr(), grad.stride(0) if R > 1 else V, _stream(logits))
-    return {"logp": nums[0], "entropy": nums[1], "lse": nums[2], "grad": grad}
+    logp, entropy, lse = _empty((R,), dtype=_F, device=dev), _empty((R,), dtype=_F, device=dev), _empty((R,), dtype=_F, device=dev)
+    _run("kf_op_token_scores_grad", dev, _TYPES[logits.dtype], R, V, logits.data_ptr(), stride, tok, tau, gl, gh, logp.data_ptr(),
+         entropy.data_ptr(), lse.data_ptr(), grad.data_ptr(), grad.stride(0) if R > 1 else V, _stream(dev.index))
+    return {"logp": logp, "entropy": entropy, "lse": lse, "grad": grad}
