@@ -1,10 +1,10 @@
 // Scores of tokens under rows of logits (kf_op_token_scores) and their
 // gradient (kf_op_token_scores_grad).
 //
-// With x = logits / tau and m = max x, one pass over a row gives
+// With x = logits / tau and a reference m near max x, one pass over a row gives
 //   S = sum exp(x - m),  T = sum (x - m) exp(x - m),
 //   lse = m + log S,     entropy = log S - T / S
-// (the sums against the maximum: no term cancels against another of its size).
+// (against a near reference no term cancels against a much larger one).
 // A thread keeps (m, S, T) of the 16-byte vectors it reads; two such triples
 // join as S = S1 f1 + S2 f2, T = f1 (T1 + d1 S1) + f2 (T2 + d2 S2) with d = m_i - m
 // and f = exp(d).  All of it is fp32, in base-2 units: 2^d with d = x log2(e) - m log2(e).
@@ -38,6 +38,7 @@ constexpr int kList = 1024;        // listed candidates of a row
 constexpr int kRanked = 256;       // up to so many are ranked against each other, more are chosen in rounds
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -300.f;   // 2^-300 is 0 in fp32: stands for -inf where it multiplies that 0
+constexpr float kRaise = 8.f;
 constexpr float kBig = 1e38f;      // references past it would overflow in base-2 units
 
 struct Args {
@@ -50,7 +51,7 @@ struct Args {
   void* grad;
   int64_t grad_stride;
   int V, top;
-  float inv_tau, c2;               // 1 / tau, log2(e) / tau
+  float inv_tau, c2, margin;       // 1 / tau, log2(e) / tau, kRaise / c2
   int* err;
 };
 
@@ -66,15 +67,19 @@ __device__ __forceinline__ uint4 ld_stream(const void* p) {
   return u;
 }
 
-// What scores are taken against: the largest logit `raw` of some elements.  A
-// reference past kBig (a row at the type's lowest value) keeps its differences in
-// natural units until they are formed
+// What scores are taken against: a logit `raw` that no element exceeds by more than
+// 2^kRaise.  (The maximum itself would change for some lane of a warp at almost every
+// vector: with a kRaise of 0 the changes were half of all instructions, 123 against
+// 81 us at 4096 x 50257.)  A reference past kBig (a row at the type's lowest value) keeps its
+// differences in natural units until they are formed
 struct Ref {
   float raw, nm;                   // nm: minus the reference, base-2 units (natural where big)
+  float limit;                     // a logit past this raises the reference
   bool big;
   __device__ __forceinline__ void set(const Args& a, float r) {
     const float m = r * a.inv_tau;
     raw = r;
+    limit = r == -INFINITY ? r : r + a.margin;
     big = fabsf(m) > kBig && fabsf(m) < INFINITY;
     nm = m == -INFINITY ? 0.f : big ? -m : -__fmul_rn(r, a.c2);
   }
@@ -108,8 +113,9 @@ __device__ __forceinline__ Sums join(const Args& a, Sums x, Sums y) {
 // one thread's pass over its elements
 struct Pass {
   Ref r;
+  float most = -INFINITY;          // the largest logit
   uint64_t s = 0ull, t = 0ull;     // S and T, each in two lanes
-  __device__ __forceinline__ Pass() : r{-INFINITY, 0.f, false} {}
+  __device__ __forceinline__ Pass() : r{-INFINITY, 0.f, -INFINITY, false} {}
   __device__ __forceinline__ void raise(const Args& a, float to) {
     const Ref was = r;
     r.set(a, to);
@@ -130,7 +136,8 @@ struct Pass {
     float top = fmaxf(v[0], v[1]);
 #pragma unroll
     for (int i = 2; i < N; i += 2) top = max3f(top, v[i], v[i + 1]);
-    if (top > r.raw) raise(a, top);
+    most = fmaxf(most, top);
+    if (top > r.limit) raise(a, top);
     if (!r.big) {
       const uint64_t c = f2(a.c2, a.c2), nm = f2(r.nm, r.nm);
 #pragma unroll
@@ -144,7 +151,8 @@ struct Pass {
     }
   }
   __device__ __forceinline__ void add_one(const Args& a, float v) {
-    if (v > r.raw) raise(a, v);
+    most = fmaxf(most, v);
+    if (v > r.limit) raise(a, v);
     pair(r.less(a, v), -INFINITY);
   }
   __device__ __forceinline__ Sums sums() const {
@@ -245,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_scores(const Args a) {
       ps.add<N>(a, v);
     }
   }
-  const float vec_max = ps.r.raw;
+  const float vec_max = ps.most;
   if (me < row.edge()) ps.add_one(a, to_f(row.p[row.edge_id(me)]));      // (fewer than 256 of them)
   // the row's sums, in one fixed order
   Sums su = ps.sums();
@@ -258,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_scores(const Args a) {
   if (lane == 0) sh.warp[warp] = su;
   if (!GRAD && a.top) {
     // the groups' maxima
-    float gm = ps.r.raw;
+    float gm = ps.most;
 #pragma unroll
     for (int o = 1; o < kLanes * CS; o <<= 1) gm = fmaxf(gm, __shfl_xor_sync(~0u, gm, o));
     if (t % (kLanes * CS) == 0) sh.group[t / (kLanes * CS)] = gm;
@@ -474,6 +482,7 @@ int scores(const char* what, int32_t type, int64_t R, Args a, float tau, cudaStr
   if (GRAD && a.grad == a.logits && a.grad_stride != a.stride) return refuse(what, "grad over the logits has their row stride");
   a.inv_tau = 1.f / tau;
   a.c2 = a.inv_tau * kLog2e;
+  a.margin = kRaise / a.c2;
   if (!(a.err = serving_error_word())) return refuse(what, "no error word", KF_E_CUDA);
   if (type == KF_TYPE_FP32) return launch<float, GRAD>(a, R, s);
   if (type == KF_TYPE_BF16) return launch<__nv_bfloat16, GRAD>(a, R, s);
@@ -488,7 +497,7 @@ using namespace kf;
 extern "C" int kf_op_token_scores(int32_t type, int64_t R, int32_t V, const void* logits, int64_t stride,
                                   const int64_t* tokens, float tau, int32_t top, float* logp, float* entropy,
                                   float* lse, int32_t* top_ids, float* top_logp, void* stream) {
-  Args a{logits, stride, tokens, nullptr, nullptr, logp, entropy, lse, top_logp, top_ids, nullptr, 0, V, top, 1.f, 1.f, nullptr};
+  Args a{logits, stride, tokens, nullptr, nullptr, logp, entropy, lse, top_logp, top_ids, nullptr, 0, V, top, 1.f, 1.f, 1.f, nullptr};
   return scores<false>("kf_op_token_scores", type, R, a, tau, (cudaStream_t)stream);
 }
 
@@ -496,6 +505,6 @@ extern "C" int kf_op_token_scores_grad(int32_t type, int64_t R, int32_t V, const
                                        const int64_t* tokens, float tau, const float* g_logp,
                                        const float* g_entropy, float* logp, float* entropy, float* lse,
                                        void* grad, int64_t grad_stride, void* stream) {
-  Args a{logits, stride, tokens, g_logp, g_entropy, logp, entropy, lse, nullptr, nullptr, grad, grad_stride, V, 0, 1.f, 1.f, nullptr};
+  Args a{logits, stride, tokens, g_logp, g_entropy, logp, entropy, lse, nullptr, nullptr, grad, grad_stride, V, 0, 1.f, 1.f, 1.f, nullptr};
   return scores<true>("kf_op_token_scores_grad", type, R, a, tau, (cudaStream_t)stream);
 }
