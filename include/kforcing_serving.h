@@ -150,7 +150,7 @@ int kf_op_pages_append(int32_t n, const int32_t* which, const int32_t* starts, i
 
 /*
  * Scores of R rows of logits [R][V] (type fp32, bf16 or fp16; rows `stride`
- * elements apart).  With x = logits * (1 / tau) in fp32, lse = log sum_v exp(x_v) and lp_v = x_v - lse:
+ * elements apart, at most 1 MiB each).  With x = logits * (1 / tau) in fp32, lse = log sum_v exp(x_v) and lp_v = x_v - lse:
  *   logp[r] = lp_token, entropy[r] = -sum_v exp(lp_v) lp_v, lse[r], and the top
  *   alternatives: the `top` (0 .. 64, <= V) ids of the largest x, largest first, ties to the
  *   lowest id, in top_ids [R][top], their lp in top_logp [R][top].

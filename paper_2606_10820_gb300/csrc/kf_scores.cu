@@ -5,23 +5,31 @@
 //   S = sum exp(x - m),  T = sum (x - m) exp(x - m),
 //   lse = m + log S,     entropy = log S - T / S
 // (against a near reference no term cancels against a much larger one).
-// A thread keeps (m, S, T) of the 16-byte vectors it reads; two such triples
-// join as S = S1 f1 + S2 f2, T = f1 (T1 + d1 S1) + f2 (T2 + d2 S2) with d = m_i - m
-// and f = exp(d).  All of it is fp32, in base-2 units: 2^d with d = x log2(e) - m log2(e).
+// A thread keeps (m, S, T) of the 16-byte vectors it reads; they move to another
+// reference as S' = f S, T' = f (T + d S) with d = m - m' and f = exp(d).  All of it is
+// fp32, in base-2 units: 2^d with d = x log2(e) - m log2(e).
 //
-// Top alternatives: the 256 threads of a row's CTA (CTAs) form 64 groups, and the
+// What bounds it: the logits' bytes, read once (scores) or read and written once
+// (gradient), and close behind them the instructions, about seven an element and pass, most of
+// the arithmetic on pairs (fma.rn.f32x2).  CTAs walk over the rows, and each thread streams its
+// vectors through slots of shared memory that are its own (cp.async, batches of four; no thread
+// waits for another's), the next row's while this one is reduced.
+//   Scores: a ring of three batches a thread, four CTAs of 256 threads a SM.
+//   Gradient: the row stays in the slots for the second pass, two CTAs of 512 threads a SM (a
+//   second pass from L2 found only half of the lines there: 369 MB read instead of 206 at
+//   2048 x 50257); a row wider than that is split over a cluster.
+//
+// Top alternatives: the threads of a row form 64 groups, and the
 // n-th largest of the 64 groups' maxima is at or below the n-th largest logit (n
 // groups have an element at or above it).  So only the vectors of threads whose own
-// maximum reaches that bound are read again (from L2, a warp per such thread), and their
+// maximum reaches that bound are looked at again (from L2, a warp per such thread), and their
 // elements at or above it listed, a few dozen of a vocabulary; each one's rank among
-// them is its place.  Rows where that list would not fit (ties in the hundreds) choose round by round.
-//
-// What bounds it: the logits' bytes, read once (scores) or read and written once (gradient:
-// the second reading comes from L2), and close behind them the instructions: five an
-// element and pass, most of them on pairs (fma.rn.f32x2).
+// them is its place.  Where masks close too many groups, the threads' own maxima give the
+// bound; rows where the list would not fit all the same (ties in the hundreds) choose round by round.
 #include <algorithm>
 #include <cooperative_groups.h>
 
+#include "kf_mma.cuh"
 #include "kf_serving.cuh"
 #include "kf_tc.cuh"
 
@@ -30,15 +38,18 @@ namespace cg = cooperative_groups;
 namespace kf {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kBatch = 4;          // vectors of a batch
+constexpr int kRing = 3;           // scores: batches under way or in use
+constexpr int kResident = 4;       // gradient: batches of a row, at most
+constexpr int kPairBytes = 13 * 512 * 16;    // gradient: slots of a CTA that leave room for a second one on the SM
 constexpr int kGroups = 64;        // groups whose maxima bound the n-th largest logit
 constexpr int kMaxTop = kGroups;
-constexpr int kLanes = kThreads / kGroups;   // lanes of a group (times the CTAs of the row)
-constexpr int kList = 1024;        // listed candidates of a row
+constexpr int kList = 768;         // listed candidates of a row
 constexpr int kRanked = 256;       // up to so many are ranked against each other, more are chosen in rounds
+constexpr int kMostRow = 8 * kResident * kBatch * 512 * 16;      // bytes of a row: the gradient's slots in eight CTAs
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -300.f;   // 2^-300 is 0 in fp32: stands for -inf where it multiplies that 0
-constexpr float kRaise = 8.f;
+constexpr float kRaise = 20.f;
 constexpr float kBig = 1e38f;      // references past it would overflow in base-2 units
 
 struct Args {
@@ -49,7 +60,7 @@ struct Args {
   float *logp, *entropy, *lse, *top_logp;
   int32_t* top_ids;
   void* grad;
-  int64_t grad_stride;
+  int64_t grad_stride, R;
   int V, top;
   float inv_tau, c2, margin;       // 1 / tau, log2(e) / tau, kRaise / c2
   int* err;
@@ -61,16 +72,10 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ uint4 ld_stream(const void* p) {
-  uint4 u;
-  asm("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
-  return u;
-}
 
 // What scores are taken against: a logit `raw` that no element exceeds by more than
-// 2^kRaise.  (The maximum itself would change for some lane of a warp at almost every
-// vector: with a kRaise of 0 the changes were half of all instructions, 123 against
-// 81 us at 4096 x 50257.)  A reference past kBig (a row at the type's lowest value) keeps its
+// 2^kRaise.  (The maximum itself changes for some lane of a warp at almost every
+// vector; the entropy's cancellation, 2^-24 of kRaise, stays below 2e-6.)  A reference past kBig (a row at the type's lowest value) keeps its
 // differences in natural units until they are formed
 struct Ref {
   float raw, nm;                   // nm: minus the reference, base-2 units (natural where big)
@@ -90,31 +95,26 @@ struct Ref {
   }
 };
 
-// S and T (base-2 units) of some elements against their Ref; without an open element they are 0 (or NaN)
+// S and T (base-2 units) of some elements against the reference `raw`; without an open element
+// they are 0 (or NaN)
 struct Sums {
   float raw, s, t;
-};
-__device__ __forceinline__ Sums join(const Args& a, Sums x, Sums y) {
-  Ref r;
-  r.set(a, fmaxf(x.raw, y.raw));
-  Sums o{r.raw, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const Sums c = i ? y : x;
+  // against the reference r (at or above this one)
+  __device__ __forceinline__ void move_to(const Args& a, const Ref& r) {
     // (the difference of the two references as they were rounded: no fused multiply-add)
-    const float by = r.big ? r.less(a, c.raw) : __fadd_rn(__fmul_rn(c.raw, a.c2), r.nm);
-    const float d = c.raw * a.inv_tau == -INFINITY ? 0.f : fmaxf(by, kLeast), f = ex2(d);
-    o.s += f * c.s;
-    o.t += f * fmaf(d, c.s, c.t);
+    const float by = r.big ? r.less(a, raw) : __fadd_rn(__fmul_rn(raw, a.c2), r.nm);
+    const float d = raw * a.inv_tau == -INFINITY ? 0.f : fmaxf(by, kLeast), f = ex2(d);
+    t = f * fmaf(d, s, t);
+    s *= f;
+    raw = r.raw;
   }
-  return o;
-}
+};
 
 // one thread's pass over its elements
 struct Pass {
   Ref r;
   float most = -INFINITY;          // the largest logit
-  uint64_t s = 0ull, t = 0ull;     // S and T, each in two lanes
+  uint64_t s = 0ull, t = 0ull;     // S and T, in two lanes each
   __device__ __forceinline__ Pass() : r{-INFINITY, 0.f, -INFINITY, false} {}
   __device__ __forceinline__ void raise(const Args& a, float to) {
     const Ref was = r;
@@ -126,10 +126,10 @@ struct Pass {
       s = mul_f2(f2(f, f), s);
     }
   }
-  __device__ __forceinline__ void pair(float dx, float dy) {
-    const uint64_t e = f2(ex2(dx), ex2(dy));
+  __device__ __forceinline__ void pair(float2 d) {
+    const uint64_t e = f2(ex2(d.x), ex2(d.y));
     s = add_f2(s, e);
-    t = fma_f2(e, f2(fmaxf(dx, kLeast), fmaxf(dy, kLeast)), t);
+    t = fma_f2(e, f2(fmaxf(d.x, kLeast), fmaxf(d.y, kLeast)), t);
   }
   template <int N>
   __device__ __forceinline__ void add(const Args& a, const float* v) {
@@ -141,28 +141,25 @@ struct Pass {
     if (!r.big) {
       const uint64_t c = f2(a.c2, a.c2), nm = f2(r.nm, r.nm);
 #pragma unroll
-      for (int i = 0; i < N; i += 2) {
-        const float2 d = f2_split(fma_f2(f2(v[i], v[i + 1]), c, nm));
-        pair(d.x, d.y);
-      }
+      for (int i = 0; i < N; i += 2) pair(f2_split(fma_f2(f2(v[i], v[i + 1]), c, nm)));
     } else {
 #pragma unroll
-      for (int i = 0; i < N; i += 2) pair(r.less(a, v[i]), r.less(a, v[i + 1]));
+      for (int i = 0; i < N; i += 2) pair(make_float2(r.less(a, v[i]), r.less(a, v[i + 1])));
     }
   }
   __device__ __forceinline__ void add_one(const Args& a, float v) {
     most = fmaxf(most, v);
     if (v > r.limit) raise(a, v);
-    pair(r.less(a, v), -INFINITY);
+    pair(make_float2(r.less(a, v), -INFINITY));
   }
   __device__ __forceinline__ Sums sums() const {
-    const float2 a = f2_split(s), b = f2_split(t);
-    return Sums{r.raw, a.x + a.y, b.x + b.y};
+    const float2 x = f2_split(s), y = f2_split(t);
+    return Sums{r.raw, x.x + x.y, y.x + y.y};
   }
 };
 
 // A row's elements in 16-byte vectors: `head` elements lie before the first
-// aligned one, then nvec vectors, then the rest
+// aligned one, then nvec vectors, then the rest.
 template <typename T>
 struct Row {
   const T* p;
@@ -176,22 +173,13 @@ struct Row {
   __device__ __forceinline__ int edge_id(int j) const { return j < head ? j : j + nvec * Vec16<T>::N; }
 };
 
-// f(id, logit) for the elements of vector i
-template <typename T, typename F>
-__device__ __forceinline__ void each_of_vector(const Row<T>& row, int i, F f) {
-  float v[Vec16<T>::N];
-  Vec16<T>::unpack(*reinterpret_cast<const uint4*>(row.vec(i)), v);
-  const int id0 = row.head + i * Vec16<T>::N;
-#pragma unroll
-  for (int e = 0; e < Vec16<T>::N; ++e) f(id0 + e, v[e]);
-}
-
 struct Cand {
   float x;
   int id;
 };
 __device__ __forceinline__ bool before(Cand a, Cand b) { return a.x > b.x || (a.x == b.x && a.id < b.id); }
 // the first of the block's candidates in that order (every thread gets it)
+template <int WARPS>
 __device__ __forceinline__ Cand block_first(Cand c, Cand* buf) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
@@ -202,129 +190,396 @@ __device__ __forceinline__ Cand block_first(Cand c, Cand* buf) {
   if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = c;
   __syncthreads();
   c = buf[0];
-  for (int i = 1; i < kWarps; ++i)
+  for (int i = 1; i < WARPS; ++i)
     if (before(buf[i], c)) c = buf[i];
   return c;
 }
 
+template <int THREADS>
 struct Shared {
-  Sums warp[kWarps];
-  Sums cta;
+  float ref[THREADS / 32], cta_ref;
+  float2 warp[THREADS / 32], cta;
   float group[kGroups];
   float bound;
   int count, again;
-  int thread[kThreads];            // threads whose vectors are read again
-  Cand first[kWarps];
+  uint16_t thread[THREADS];        // threads whose vectors are looked at again
+  Cand first[THREADS / 32];
   Cand list[kList];
 };
 
-// Clusters of CS CTAs share a row (CS = 1: no cluster).  GRAD: the gradient's
-// second pass instead of the alternatives.
-template <typename T, int CS, bool GRAD>
-__global__ void __launch_bounds__(kThreads, 4) k_scores(const Args a) {
-  __shared__ Shared sh;
-  constexpr int N = Vec16<T>::N;
-  constexpr int kAll = CS * kThreads;
-  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-  const int64_t r = blockIdx.x / CS;
-  const int rank = blockIdx.x % CS, me = rank * kThreads + t;
-  const Row<T> row(static_cast<const T*>(a.logits) + r * a.stride, a.V);
-  // (read before the barriers: the gradient may overwrite the logits)
-  const int64_t token = a.tokens[r];
-  const float at_logit = t == 0 && token >= 0 && token < a.V ? to_f(row.p[token]) : 0.f;
-
-  Pass ps;
-  {
-    int i = me;
-    for (; i + 3 * kAll < row.nvec; i += 4 * kAll) {
-      uint4 u[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) u[j] = ld_stream(row.vec(i + j * kAll));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float v[N];
-        Vec16<T>::unpack(u[j], v);
-        ps.add<N>(a, v);
-      }
-    }
-    for (; i < row.nvec; i += kAll) {
-      float v[N];
-      Vec16<T>::unpack(ld_stream(row.vec(i)), v);
-      ps.add<N>(a, v);
-    }
+// A row's numbers, the same in all of its threads
+struct Scores {
+  Ref ref;
+  float logs, lse, H;              // log2 S; H: the entropy
+  bool none, bad;                  // every token closed; a NaN or +inf in the row
+  // log p of a logit: from the difference to the reference, not from lse, which loses log S where the
+  // reference is the type's lowest value (and in natural units where base-2 ones overflow)
+  __device__ __forceinline__ float lp(const Args& a, float v) const {
+    const float x = v * a.inv_tau;
+    return fabsf(x) > kBig ? (x - ref.raw * a.inv_tau) - logs * kLn2 : (ref.less(a, v) - logs) * kLn2;
   }
-  const float vec_max = ps.most;
-  if (me < row.edge()) ps.add_one(a, to_f(row.p[row.edge_id(me)]));      // (fewer than 256 of them)
-  // the row's sums, in one fixed order
+};
+// The row's sums against its largest reference, added in one fixed order; with `groups` the
+// groups' maxima in sh.group (of every CTA)
+template <int THREADS, int CS, bool GROUPS>
+__device__ __forceinline__ Scores reduce_row(const Args& a, Shared<THREADS>& sh, const Pass& ps) {
+  constexpr int WARPS = THREADS / 32, LANES = THREADS * CS / kGroups;      // LANES: threads of a group
+  static_assert(!GROUPS || (LANES >= 1 && LANES <= 32), "a group lies in a warp");
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   Sums su = ps.sums();
-  auto join_lanes = [&](int o) {
-    const Sums other{__shfl_xor_sync(~0u, su.raw, o), __shfl_xor_sync(~0u, su.s, o), __shfl_xor_sync(~0u, su.t, o)};
-    su = (lane & o) ? join(a, other, su) : join(a, su, other);
-  };
+  Scores o;
+  float m = su.raw;
 #pragma unroll
-  for (int o = 16; o; o >>= 1) join_lanes(o);
-  if (lane == 0) sh.warp[warp] = su;
-  if (!GRAD && a.top) {
-    // the groups' maxima
+  for (int i = 16; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, i));
+  if (lane == 0) sh.ref[warp] = m;
+  if constexpr (GROUPS) {
     float gm = ps.most;
 #pragma unroll
-    for (int o = 1; o < kLanes * CS; o <<= 1) gm = fmaxf(gm, __shfl_xor_sync(~0u, gm, o));
-    if (t % (kLanes * CS) == 0) sh.group[t / (kLanes * CS)] = gm;
-    if (t == 0) sh.count = sh.again = 0;
+    for (int i = 1; i < LANES; i <<= 1) gm = fmaxf(gm, __shfl_xor_sync(~0u, gm, i));
+    if (t % LANES == 0) sh.group[t / LANES] = gm;
   }
-  __syncthreads();
-  su = sh.warp[lane % kWarps];
+  __syncthreads();                        // (all threads are done with the row before)
+  if (t == 0) sh.count = sh.again = 0;
+  m = sh.ref[lane % WARPS];
 #pragma unroll
-  for (int o = kWarps / 2; o; o >>= 1) join_lanes(o);
-  Shared* lead = &sh;
+  for (int i = WARPS / 2; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, i));
   if constexpr (CS > 1) {
     cg::cluster_group cl = cg::this_cluster();
-    if (t == 0) sh.cta = su;
+    if (t == 0) sh.cta_ref = m;
     cl.sync();
-    su = cl.map_shared_rank(&sh, 0)->cta;
-    for (int c = 1; c < CS; ++c) su = join(a, su, cl.map_shared_rank(&sh, c)->cta);
-    lead = cl.map_shared_rank(&sh, 0);
-    // every CTA has all groups' maxima
-    const bool take = !GRAD && a.top && t < kGroups;
+    for (int c = 0; c < CS; ++c) m = fmaxf(m, cl.map_shared_rank(&sh, c)->cta_ref);
+  }
+  o.ref.set(a, m);
+  su.move_to(a, o.ref);
+#pragma unroll
+  for (int i = 16; i; i >>= 1) {
+    su.s += __shfl_xor_sync(~0u, su.s, i);
+    su.t += __shfl_xor_sync(~0u, su.t, i);
+  }
+  if (lane == 0) sh.warp[warp] = make_float2(su.s, su.t);
+  __syncthreads();
+  float2 x = sh.warp[lane % WARPS];
+#pragma unroll
+  for (int i = WARPS / 2; i; i >>= 1) {
+    x.x += __shfl_xor_sync(~0u, x.x, i);
+    x.y += __shfl_xor_sync(~0u, x.y, i);
+  }
+  if constexpr (CS > 1) {
+    cg::cluster_group cl = cg::this_cluster();
+    if (t == 0) sh.cta = x;
+    cl.sync();
+    x = make_float2(0.f, 0.f);
+    for (int c = 0; c < CS; ++c) {
+      const float2 y = cl.map_shared_rank(&sh, c)->cta;
+      x.x += y.x;
+      x.y += y.y;
+    }
     float g = 0.f;
+    const bool take = GROUPS && t < kGroups;
     if (take) g = cl.map_shared_rank(&sh, t / (kGroups / CS))->group[t % (kGroups / CS)];
-    cl.sync();          // the other CTAs have read this one's part
+    cl.sync();                            // the other CTAs have read this one's part
     if (take) sh.group[t] = g;
     __syncthreads();
   }
-  Ref ref;
-  ref.set(a, su.raw);
-  const bool none = !ref.open(a) && su.s == 0.f;          // every token closed
-  const bool bad = !(su.s > 0.f) && !none;                // NaN or +inf in the row
-  const float logs = log2f(su.s);                         // (base-2 units)
-  const float lse = none ? -INFINITY : bad ? NAN : su.raw * a.inv_tau + logs * kLn2;
-  const float H = none ? 0.f : bad ? NAN : (logs - su.t / su.s) * kLn2;
-  // log p of a logit: from the difference to the reference, not from lse, which loses log S where the
-  // reference is the type's lowest value (and in natural units where base-2 ones overflow)
-  auto lp_of = [&](float v) {
-    const float x = v * a.inv_tau;
-    return fabsf(x) > kBig ? (x - ref.raw * a.inv_tau) - logs * kLn2 : (ref.less(a, v) - logs) * kLn2;
-  };
-  if (rank == 0 && t == 0) {
-    if (a.lse) a.lse[r] = lse;
-    if (a.entropy) a.entropy[r] = H;
-    if (token >= a.V) atomicOr(a.err, KF_DEV_BAD_TOKEN);
-    if (a.logp) a.logp[r] = token < 0 ? 0.f : token >= a.V || bad ? NAN : none ? -INFINITY : lp_of(at_logit);
+  o.none = !o.ref.open(a) && x.x == 0.f;
+  o.bad = !(x.x > 0.f) && !o.none;
+  o.logs = log2f(x.x);
+  o.lse = o.none ? -INFINITY : o.bad ? NAN : o.ref.raw * a.inv_tau + o.logs * kLn2;
+  o.H = o.none ? 0.f : o.bad ? NAN : (o.logs - x.y / x.x) * kLn2;
+  return o;
+}
+__device__ __forceinline__ void write_numbers(const Args& a, int64_t r, const Scores& o, int64_t token, float at_logit) {
+  if (a.lse) a.lse[r] = o.lse;
+  if (a.entropy) a.entropy[r] = o.H;
+  if (token >= a.V) atomicOr(a.err, KF_DEV_BAD_TOKEN);
+  if (a.logp) a.logp[r] = token < 0 ? 0.f : token >= a.V || o.bad ? NAN : o.none ? -INFINITY : o.lp(a, at_logit);
+}
+// what a row's threads hold beside their vectors: elements outside of them (fewer than 16), the
+// token and its logit (read before the barriers: the gradient may overwrite the logits)
+template <typename T>
+struct Extra {
+  int64_t token;
+  float at_logit, edge_logit;
+  int edge_id;
+  bool edge;
+  __device__ __forceinline__ Extra(const Args& a, const Row<T>& row, int64_t r, bool first_cta) {
+    const int t = threadIdx.x;
+    token = a.tokens[r];
+    at_logit = t == 0 && token >= 0 && token < a.V ? to_f(row.p[token]) : 0.f;
+    edge = first_cta && t < row.edge();
+    edge_id = edge ? row.edge_id(t) : 0;
+    edge_logit = edge ? to_f(row.p[edge_id]) : -INFINITY;
   }
+};
+template <typename T>
+__device__ __forceinline__ Row<T> row_at(const Args& a, int64_t r) {
+  return Row<T>(static_cast<const T*>(a.logits) + r * a.stride, a.V);
+}
+// The row's CTAs take consecutive stretches of per_cta * THREADS vectors: vector k of a thread is
+// first + k * THREADS, if it has k < have(row)
+template <int THREADS>
+struct Mine {
+  int per_cta, first;
+  __device__ __forceinline__ Mine(int vectors, int cs, int rank) {
+    per_cta = (vectors + cs * THREADS - 1) / (cs * THREADS);
+    first = rank * per_cta * THREADS + threadIdx.x;
+  }
+  template <typename T> __device__ __forceinline__ int have(const Row<T>& w) const {
+    return min(per_cta, (w.nvec - first + THREADS - 1) / THREADS);
+  }
+};
 
-  if constexpr (GRAD) {
-    const bool has = token >= 0 && token < a.V;
+// ------------------------------------------------------------------ scores
+template <typename T, int THREADS, int CS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a) {
+  extern __shared__ __align__(16) uint4 slots[];         // [batch of the ring][vector][thread]
+  __shared__ Shared<THREADS> sh;
+  constexpr int N = Vec16<T>::N, WARPS = THREADS / 32;
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5, rank = blockIdx.x % CS;
+  const Mine<THREADS> mine(a.V / N, CS, rank);
+  const int batches = (mine.per_cta + kBatch - 1) / kBatch;      // of a row
+  const int64_t step = gridDim.x / CS;
+  const uint32_t slot0 = mma::smem_addr(slots + t);
+
+  // the copies run kRing - 1 batches ahead, into the rows that follow
+  int64_t fr = blockIdx.x / CS;
+  int fb = 0, fslot = 0, fn = 0;
+  const T* fp = nullptr;
+  auto look = [&] {
+    if (fr >= a.R) return;
+    const Row<T> w = row_at<T>(a, fr);
+    fn = mine.have(w);
+    fp = w.vec(mine.first);
+  };
+  auto fill = [&] {                       // one group of copies, empty past the last row
+    if (fr < a.R) {
+      const T* p = fp + (size_t)fb * kBatch * THREADS * N;
+      const uint32_t d = slot0 + fslot * kBatch * THREADS * 16;
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (fb * kBatch + j < fn) mma::cp_async16(d + j * THREADS * 16, p + j * THREADS * N, 16);
+      if (++fb == batches) {
+        fb = 0;
+        fr += step;
+        look();
+      }
+      fslot = fslot + 1 == kRing ? 0 : fslot + 1;
+    }
+    mma::cp_commit();
+  };
+  look();
+#pragma unroll
+  for (int i = 0; i < kRing - 1; ++i) fill();
+  int slot = 0;
+#pragma unroll 1
+  for (int64_t r = blockIdx.x / CS; r < a.R; r += step) {
+    const Row<T> row = row_at<T>(a, r);
+    const Extra<T> ex(a, row, r, rank == 0);
+    const int n = mine.have(row);
+    Pass ps;
+#pragma unroll 1
+    for (int b = 0; b < batches; ++b) {
+      mma::cp_wait<kRing - 2>();          // this batch has landed
+      fill();                             // into the slots of the batch before
+      const uint4* s = slots + slot * kBatch * THREADS + t;
+      if ((b + 1) * kBatch <= n) {
+        float v[kBatch * N];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) Vec16<T>::unpack(s[j * THREADS], v + j * N);
+        ps.add<kBatch * N>(a, v);
+      } else {
+        for (int j = 0; b * kBatch + j < n; ++j) {
+          float v[N];
+          Vec16<T>::unpack(s[j * THREADS], v);
+          ps.add<N>(a, v);
+        }
+      }
+      slot = slot + 1 == kRing ? 0 : slot + 1;
+    }
+    const float vec_max = ps.most;
+    if (ex.edge) ps.add_one(a, ex.edge_logit);
+    const Scores o = reduce_row<THREADS, CS, true>(a, sh, ps);
+    if (rank == 0 && t == 0) write_numbers(a, r, o, ex.token, ex.at_logit);
+
+    if (a.top == 0) continue;             // (uniform)
+    int32_t* ids = a.top_ids + r * a.top;
+    float* lps = a.top_logp + r * a.top;
+    if (o.bad) {                          // (uniform over the row's CTAs)
+      if (rank == 0)
+        for (int i = t; i < a.top; i += THREADS) {
+          ids[i] = -1;
+          lps[i] = NAN;
+        }
+      continue;
+    }
+    // the bound: the top-th largest of the groups' maxima
+    if (t < kGroups) {
+      const float g = sh.group[t];
+      int rk = 0;
+#pragma unroll 16
+      for (int j = 0; j < kGroups; ++j) rk += sh.group[j] > g || (sh.group[j] == g && j < t);
+      if (rk == a.top - 1) sh.bound = g * a.inv_tau;
+    }
+    __syncthreads();
+    float bound = sh.bound;
+    if (bound == -INFINITY) {             // (uniform over the row's CTAs) a mask: this CTA's threads' own maxima
+      float* own = reinterpret_cast<float*>(sh.list);
+      own[t] = vec_max;
+      __syncthreads();
+      int rk = 0;
+      for (int j = 0; j < THREADS; ++j) rk += own[j] > vec_max || (own[j] == vec_max && j < t);
+      if (rk == min(a.top, THREADS) - 1) sh.bound = a.top <= THREADS ? vec_max * a.inv_tau : -INFINITY;
+      __syncthreads();
+      bound = sh.bound;
+      if constexpr (CS > 1) {
+        // the best of the CTAs' bounds: top elements of that one are at or above it
+        cg::cluster_group cl = cg::this_cluster();
+        cl.sync();
+        for (int c = 0; c < CS; ++c) bound = fmaxf(bound, cl.map_shared_rank(&sh, c)->bound);
+        cl.sync();
+      }
+    }
+    Shared<THREADS>* lead = &sh;
+    if constexpr (CS > 1) lead = cg::this_cluster().map_shared_rank(&sh, 0);
+    // (a bound of -inf: the open tokens are listed, the closed ones follow by id)
+    auto listed = [&](float x) { return x >= bound && x > -INFINITY; };
+    auto list = [&](int id, float v) {
+      const float x = v * a.inv_tau;
+      if (listed(x)) {
+        const int at = atomicAdd(&lead->count, 1);
+        if (at < kList) lead->list[at] = Cand{x, id};
+      }
+    };
+    if (listed(vec_max * a.inv_tau)) sh.thread[atomicAdd(&sh.again, 1)] = (uint16_t)t;
+    if (ex.edge) list(ex.edge_id, ex.edge_logit);
+    __syncthreads();
+    for (int j = warp; j < sh.again; j += WARPS)
+      for (int k = lane; k < mine.per_cta; k += 32) {
+        const int i = mine.first - t + sh.thread[j] + k * THREADS;
+        if (i >= row.nvec) break;
+        float v[N];
+        Vec16<T>::unpack(*reinterpret_cast<const uint4*>(row.vec(i)), v);
+        const int id0 = row.head + i * N;
+#pragma unroll
+        for (int e = 0; e < N; ++e) list(id0 + e, v[e]);
+      }
+    if constexpr (CS > 1) cg::this_cluster().sync();
+    else __syncthreads();
+    if (rank != 0) continue;
+    const int found = sh.count;
+    auto put = [&](int place, Cand c) {
+      ids[place] = c.id;
+      lps[place] = o.lp(a, to_f(row.p[c.id]));
+    };
+    if (found <= kRanked) {
+      for (int i = t; i < found; i += THREADS) {
+        const Cand c = sh.list[i];
+        int rk = 0;
+        for (int j = 0; j < found; ++j) rk += before(sh.list[j], c);
+        if (rk < a.top) put(rk, c);
+      }
+    } else {
+      // round by round: the first candidate after the last one chosen, of the list or
+      // (where that overflowed) of the row
+      Cand last{INFINITY, -1};
+      for (int k = 0; k < min(found, a.top); ++k) {
+        Cand c{-INFINITY, 0x7fffffff};
+        auto look_at = [&](Cand d) {
+          if (before(last, d) && before(d, c)) c = d;
+        };
+        if (found <= kList) {
+          for (int j = t; j < found; j += THREADS) look_at(sh.list[j]);
+        } else {
+          for (int id = t; id < a.V; id += THREADS) {
+            const float x = to_f(row.p[id]) * a.inv_tau;
+            if (listed(x)) look_at(Cand{x, id});
+          }
+        }
+        last = block_first<WARPS>(c, sh.first);
+        if (t == 0) put(k, last);
+      }
+    }
+    // fewer open tokens than asked for: closed ones by id
+    if (found < a.top && t == 0) {
+      int k = found;
+      for (int id = 0; k < a.top && id < a.V; ++id) {
+        if (to_f(row.p[id]) * a.inv_tau > -INFINITY) continue;
+        ids[k] = id;
+        lps[k++] = -INFINITY;
+      }
+    }
+  }
+  mma::cp_wait<0>();
+}
+
+// ---------------------------------------------------------------- gradient
+static_assert(2 * (kPairBytes + sizeof(Shared<512>) + 1024) <= 233472, "two CTAs on an SM");
+template <typename T, int THREADS, int CS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const Args a) {
+  extern __shared__ __align__(16) uint4 slots[];         // [vector][thread]
+  __shared__ Shared<THREADS> sh;
+  constexpr int N = Vec16<T>::N;
+  const int t = threadIdx.x, rank = blockIdx.x % CS;
+  const Mine<THREADS> mine(a.V / N, CS, rank);
+  const int64_t step = gridDim.x / CS;
+  const uint32_t slot0 = mma::smem_addr(slots + t);
+  auto fill = [&](const Row<T>& w, int n, int g) {       // batch g of a row: one group of copies, always
+    const T* p = w.vec(mine.first);
+#pragma unroll
+    for (int j = g * kBatch; j < (g + 1) * kBatch; ++j)
+      if (j < n) mma::cp_async16(slot0 + j * THREADS * 16, p + (size_t)j * THREADS * N, 16);
+    mma::cp_commit();
+  };
+  {
+    const Row<T> w = row_at<T>(a, blockIdx.x / CS);
+#pragma unroll
+    for (int g = 0; g < kResident; ++g) fill(w, mine.have(w), g);
+  }
+#pragma unroll 1
+  for (int64_t r = blockIdx.x / CS; r < a.R; r += step) {
+    const Row<T> row = row_at<T>(a, r);
+    const bool more = r + step < a.R;
+    const Row<T> next = row_at<T>(a, more ? r + step : r);
+    const Extra<T> ex(a, row, r, rank == 0);
+    const int n = mine.have(row), n_next = mine.have(next);
+    Pass ps;
+#pragma unroll
+    for (int g = 0; g < kResident; ++g) {
+      // this batch's copies are done, later ones may not be
+      if (g == 0) mma::cp_wait<kResident - 1>();
+      else if (g == 1) mma::cp_wait<kResident - 2>();
+      else if (g == 2) mma::cp_wait<kResident - 3>();
+      else mma::cp_wait<0>();
+      const uint4* s = slots + g * kBatch * THREADS + t;
+      if ((g + 1) * kBatch <= n) {
+        float v[kBatch * N];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) Vec16<T>::unpack(s[j * THREADS], v + j * N);
+        ps.add<kBatch * N>(a, v);
+      } else {
+        for (int j = 0; g * kBatch + j < n; ++j) {
+          float v[N];
+          Vec16<T>::unpack(s[j * THREADS], v);
+          ps.add<N>(a, v);
+        }
+      }
+    }
+    if (ex.edge) ps.add_one(a, ex.edge_logit);
+    const Scores o = reduce_row<THREADS, CS, false>(a, sh, ps);
+    if (rank == 0 && t == 0) write_numbers(a, r, o, ex.token, ex.at_logit);
+
+    const bool has = ex.token >= 0 && ex.token < a.V;
     const float gl = has && a.g_logp ? a.g_logp[r] : 0.f, gh = a.g_entropy ? a.g_entropy[r] : 0.f;
     // grad = p (A + B log2 p) + (v == token) gl / tau.  A row with a NaN has A = NaN; one
     // without open tokens p = 0
-    const float A = (-gl - gh * H) * a.inv_tau, B = -gh * a.inv_tau * kLn2;
-    const float at_token = none ? 0.f : gl * a.inv_tau;
+    const float A = (-gl - gh * o.H) * a.inv_tau, B = -gh * a.inv_tau * kLn2;
+    const float at_token = o.none ? 0.f : gl * a.inv_tau;
     T* out = static_cast<T*>(a.grad) + r * a.grad_stride;
-    const uint64_t c2 = f2(a.c2, a.c2), nm = f2(ref.nm, ref.nm), nlogs = f2(-logs, -logs), A2 = f2(A, A), B2 = f2(B, B);
+    const uint64_t c2 = f2(a.c2, a.c2), nm = f2(o.ref.nm, o.ref.nm), nlogs = f2(-o.logs, -o.logs), A2 = f2(A, A), B2 = f2(B, B);
     auto pair = [&](float& x, float& y) {
       float2 d;
-      if (!ref.big) d = f2_split(add_f2(fma_f2(f2(x, y), c2, nm), nlogs));      // (one constant for both would lose log S)
-      else d = make_float2(ref.less(a, x) - logs, ref.less(a, y) - logs);
+      if (!o.ref.big) d = f2_split(add_f2(fma_f2(f2(x, y), c2, nm), nlogs));      // (one constant for both would lose log S)
+      else d = make_float2(o.ref.less(a, x) - o.logs, o.ref.less(a, y) - o.logs);
       d.x = fmaxf(d.x, kLeast);
       d.y = fmaxf(d.y, kLeast);
       const float2 g = f2_split(mul_f2(f2(ex2(d.x), ex2(d.y)), fma_f2(B2, f2(d.x, d.y), A2)));
@@ -332,137 +587,80 @@ __global__ void __launch_bounds__(kThreads, 4) k_scores(const Args a) {
       y = g.y;
     };
     const bool same = (reinterpret_cast<uintptr_t>(out) & 15) == (reinterpret_cast<uintptr_t>(row.p) & 15);
-    if (me < row.edge()) {
-      const int id = row.edge_id(me);
-      float x = to_f(row.p[id]), y = -INFINITY;
+    if (ex.edge) {
+      float x = ex.edge_logit, y = -INFINITY;
       pair(x, y);
-      out[id] = from_f<T>(id == token ? x + at_token : x);
+      out[ex.edge_id] = from_f<T>(ex.edge_id == ex.token ? x + at_token : x);
     }
-    auto store = [&](int i, uint4 u) {
-      float v[N];
-      Vec16<T>::unpack(u, v);
-      const int id0 = row.head + i * N;
 #pragma unroll
-      for (int e = 0; e < N; e += 2) pair(v[e], v[e + 1]);
-      if (token >= id0 && token < id0 + N) {
+    for (int g = 0; g < kResident; ++g) {
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (id0 + e == token) v[e] += at_token;
+      for (int j = g * kBatch; j < (g + 1) * kBatch; ++j) {
+        if (j >= n) break;
+        float v[N];
+        Vec16<T>::unpack(slots[j * THREADS + t], v);
+        const int id0 = row.head + (mine.first + j * THREADS) * N;
+#pragma unroll
+        for (int e = 0; e < N; e += 2) pair(v[e], v[e + 1]);
+        if (ex.token >= id0 && ex.token < id0 + N) {
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (id0 + e == ex.token) v[e] += at_token;
+        }
+        if (same) {
+          *reinterpret_cast<uint4*>(out + id0) = Vec16<T>::pack(v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; ++e) out[id0 + e] = from_f<T>(v[e]);
+        }
       }
-      if (same) {
-        *reinterpret_cast<uint4*>(out + id0) = Vec16<T>::pack(v);
-      } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) out[id0 + e] = from_f<T>(v[e]);
-      }
-    };
-    int i = me;
-    for (; i + 3 * kAll < row.nvec; i += 4 * kAll) {
-      uint4 u[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) u[j] = *reinterpret_cast<const uint4*>(row.vec(i + j * kAll));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) store(i + j * kAll, u[j]);
-    }
-    for (; i < row.nvec; i += kAll) store(i, *reinterpret_cast<const uint4*>(row.vec(i)));
-    return;
-  }
-
-  if (a.top == 0) return;                 // (uniform)
-  int32_t* ids = a.top_ids + r * a.top;
-  float* lps = a.top_logp + r * a.top;
-  if (bad) {                              // (uniform over the row's CTAs)
-    if (rank == 0 && t < a.top) {
-      ids[t] = -1;
-      lps[t] = NAN;
-    }
-    return;
-  }
-  // the bound: the top-th largest of the groups' maxima
-  if (t < kGroups) {
-    const float g = sh.group[t];
-    int rk = 0;
-#pragma unroll 16
-    for (int j = 0; j < kGroups; ++j) rk += sh.group[j] > g || (sh.group[j] == g && j < t);
-    if (rk == a.top - 1) sh.bound = g * a.inv_tau;
-  }
-  __syncthreads();
-  const float bound = sh.bound;
-  // (a bound of -inf: the open tokens are listed, the closed ones follow by id)
-  auto listed = [&](float x) { return x >= bound && x > -INFINITY; };
-  auto list = [&](int id, float v) {
-    const float x = v * a.inv_tau;
-    if (listed(x)) {
-      const int at = atomicAdd(&lead->count, 1);
-      if (at < kList) lead->list[at] = Cand{x, id};
-    }
-  };
-  if (listed(vec_max * a.inv_tau)) sh.thread[atomicAdd(&sh.again, 1)] = t;
-  if (me < row.edge()) list(row.edge_id(me), to_f(row.p[row.edge_id(me)]));
-  __syncthreads();
-  for (int k = warp; k < sh.again; k += kWarps)
-    for (int i = rank * kThreads + sh.thread[k] + lane * kAll; i < row.nvec; i += 32 * kAll) each_of_vector(row, i, list);
-  if constexpr (CS > 1) cg::this_cluster().sync();
-  else __syncthreads();
-  if (rank != 0) return;
-  const int n = sh.count;
-  auto put = [&](int place, Cand c) {
-    ids[place] = c.id;
-    lps[place] = lp_of(to_f(row.p[c.id]));
-  };
-  if (n <= kRanked) {
-    if (t < n) {
-      const Cand c = sh.list[t];
-      int rk = 0;
-      for (int j = 0; j < n; ++j) rk += before(sh.list[j], c);
-      if (rk < a.top) put(rk, c);
-    }
-  } else {
-    // round by round: the first candidate after the last one chosen, of the list or
-    // (where that overflowed) of the row
-    Cand last{INFINITY, -1};
-    for (int k = 0; k < min(n, a.top); ++k) {
-      Cand c{-INFINITY, 0x7fffffff};
-      auto look = [&](Cand d) {
-        if (before(last, d) && before(d, c)) c = d;
-      };
-      auto look_at = [&](int id, float v) {
-        const float x = v * a.inv_tau;
-        if (listed(x)) look(Cand{x, id});
-      };
-      if (n <= kList) {
-        for (int j = t; j < n; j += kThreads) look(sh.list[j]);
-      } else {
-        if (t < row.edge()) look_at(row.edge_id(t), to_f(row.p[row.edge_id(t)]));
-        for (int i = t; i < row.nvec; i += kThreads) each_of_vector(row, i, look_at);
-      }
-      last = block_first(c, sh.first);
-      if (t == 0) put(k, last);
-    }
-  }
-  // fewer open tokens than asked for: closed ones by id
-  if (n < a.top && t == 0) {
-    int k = n;
-    for (int id = 0; k < a.top; ++id) {
-      if (to_f(row.p[id]) * a.inv_tau > -INFINITY) continue;
-      ids[k] = id;
-      lps[k++] = -INFINITY;
+      if (more) fill(next, n_next, g);
     }
   }
 }
 
+// ------------------------------------------------------------------ host
+// a grid of as many clusters as fit the SMs at once, for the rows that there are
+template <int THREADS, int CS, typename K>
+void launch_rows(K* kernel, PerDevice& attr, const Args& a, size_t bytes, cudaStream_t s) {
+  set_smem_attr(attr, kernel, bytes);
+  const int64_t per_sm = std::max<int64_t>(1, std::min<int64_t>(1024 / THREADS, 233472 / (bytes + sizeof(Shared<THREADS>) + 1024)));
+  const int64_t rows = std::min<int64_t>(a.R, std::max<int64_t>(1, per_sm * device_sms() / CS));
+  launch_cluster(kernel, dim3((unsigned)(rows * CS)), dim3(THREADS), bytes, CS, false, s, a);
+}
+template <typename T, int THREADS, int CS>
+void launch_scores(const Args& a, cudaStream_t s) {
+  static PerDevice attr;
+  launch_rows<THREADS, CS>(k_scores<T, THREADS, CS>, attr, a, (size_t)kRing * kBatch * THREADS * 16, s);
+}
+template <typename T, int THREADS, int CS>
+void launch_grad(const Args& a, cudaStream_t s) {
+  static PerDevice attr;
+  const int k = (a.V / Vec16<T>::N + CS * THREADS - 1) / (CS * THREADS);
+  launch_rows<THREADS, CS>(k_scores_grad<T, THREADS, CS>, attr, a, (size_t)k * THREADS * 16, s);
+}
 template <typename T, bool GRAD>
-int launch(const Args& a, int64_t R, cudaStream_t s) {
-  // Few rows: a row is split over a cluster while the CTAs fit the SMs, and each
-  // thread keeps two vectors
-  const int64_t sms = device_sms(), vecs = a.V / Vec16<T>::N;
-  const int cs = R * 8 <= sms && vecs >= 8 * 2 * kThreads ? 8 : R * 4 <= 2 * sms && vecs >= 4 * 2 * kThreads ? 4
-                 : R * 2 <= 3 * sms && vecs >= 2 * 2 * kThreads ? 2 : 1;
-  const dim3 grid((unsigned)(R * cs));
-  if (cs == 8) launch_cluster(k_scores<T, 8, GRAD>, grid, dim3(kThreads), 0, 8, false, s, a);
-  else if (cs == 4) launch_cluster(k_scores<T, 4, GRAD>, grid, dim3(kThreads), 0, 4, false, s, a);
-  else if (cs == 2) launch_cluster(k_scores<T, 2, GRAD>, grid, dim3(kThreads), 0, 2, false, s, a);
-  else launch_cluster(k_scores<T, 1, GRAD>, grid, dim3(kThreads), 0, 1, false, s, a);
+int launch(const Args& a, cudaStream_t s) {
+  // A row of up to 12 KB: two warps, so that an SM has ten such rows and more.  A wider one is split over a
+  // cluster while few rows leave SMs idle and each thread keeps two vectors; the gradient's also
+  // until it fits the slots
+  const int64_t bytes = (int64_t)a.V * sizeof(T), sms = device_sms();
+  int cs = 1;
+  if constexpr (GRAD) {
+    while (cs < 8 && (bytes > (int64_t)cs * kPairBytes || (a.R * cs * 2 <= sms && bytes >= cs * 2 * 2 * 512 * 16))) cs *= 2;
+    if (bytes <= 12288) launch_grad<T, 64, 1>(a, s);
+    else if (cs == 1) launch_grad<T, 512, 1>(a, s);
+    else if (cs == 2) launch_grad<T, 512, 2>(a, s);
+    else if (cs == 4) launch_grad<T, 512, 4>(a, s);
+    else launch_grad<T, 512, 8>(a, s);
+  } else {
+    while (cs < 8 && a.R * cs * 2 <= 2 * sms && bytes >= cs * 2 * 2 * 256 * 16) cs *= 2;
+    if (bytes <= 12288) launch_scores<T, 64, 1>(a, s);
+    else if (cs == 1) launch_scores<T, 256, 1>(a, s);
+    else if (cs == 2) launch_scores<T, 256, 2>(a, s);
+    else if (cs == 4) launch_scores<T, 256, 4>(a, s);
+    else launch_scores<T, 256, 8>(a, s);
+  }
   return launched(GRAD ? "kf_op_token_scores_grad" : "kf_op_token_scores");
 }
 
@@ -472,7 +670,7 @@ int scores(const char* what, int32_t type, int64_t R, Args a, float tau, cudaStr
   if (type != KF_TYPE_FP32 && type != KF_TYPE_BF16 && type != KF_TYPE_FP16)
     return refuse(what, "the logits' type is fp32, bf16 or fp16");
   if (R < 0 || R > (1 << 28)) return refuse(what, "rows out of range");
-  if (a.V < 1 || a.V > (1 << 30) || a.stride < a.V) return refuse(what, "vocabulary or row stride out of range");
+  if (a.V < 1 || a.V > kMostRow / size || a.stride < a.V) return refuse(what, "vocabulary (a row is at most 1 MiB) or row stride out of range");
   if (!(tau > 0.f) || !(1.f / tau > 0.f) || std::isinf(1.f / tau)) return refuse(what, "tau is a positive number");
   if (a.top < 0 || a.top > kMaxTop || a.top > a.V) return refuse(what, "top is 0 to 64 and at most the vocabulary");
   if (R == 0) return KF_OK;
@@ -484,9 +682,9 @@ int scores(const char* what, int32_t type, int64_t R, Args a, float tau, cudaStr
   a.c2 = a.inv_tau * kLog2e;
   a.margin = kRaise / a.c2;
   if (!(a.err = serving_error_word())) return refuse(what, "no error word", KF_E_CUDA);
-  if (type == KF_TYPE_FP32) return launch<float, GRAD>(a, R, s);
-  if (type == KF_TYPE_BF16) return launch<__nv_bfloat16, GRAD>(a, R, s);
-  return launch<__half, GRAD>(a, R, s);
+  if (type == KF_TYPE_FP32) return launch<float, GRAD>(a, s);
+  if (type == KF_TYPE_BF16) return launch<__nv_bfloat16, GRAD>(a, s);
+  return launch<__half, GRAD>(a, s);
 }
 
 }  // namespace
@@ -497,7 +695,7 @@ using namespace kf;
 extern "C" int kf_op_token_scores(int32_t type, int64_t R, int32_t V, const void* logits, int64_t stride,
                                   const int64_t* tokens, float tau, int32_t top, float* logp, float* entropy,
                                   float* lse, int32_t* top_ids, float* top_logp, void* stream) {
-  Args a{logits, stride, tokens, nullptr, nullptr, logp, entropy, lse, top_logp, top_ids, nullptr, 0, V, top, 1.f, 1.f, 1.f, nullptr};
+  Args a{logits, stride, tokens, nullptr, nullptr, logp, entropy, lse, top_logp, top_ids, nullptr, 0, R, V, top, 1.f, 1.f, 1.f, nullptr};
   return scores<false>("kf_op_token_scores", type, R, a, tau, (cudaStream_t)stream);
 }
 
@@ -505,6 +703,6 @@ extern "C" int kf_op_token_scores_grad(int32_t type, int64_t R, int32_t V, const
                                        const int64_t* tokens, float tau, const float* g_logp,
                                        const float* g_entropy, float* logp, float* entropy, float* lse,
                                        void* grad, int64_t grad_stride, void* stream) {
-  Args a{logits, stride, tokens, g_logp, g_entropy, logp, entropy, lse, nullptr, nullptr, grad, grad_stride, V, 0, 1.f, 1.f, 1.f, nullptr};
+  Args a{logits, stride, tokens, g_logp, g_entropy, logp, entropy, lse, nullptr, nullptr, grad, grad_stride, R, V, 0, 1.f, 1.f, 1.f, nullptr};
   return scores<true>("kf_op_token_scores_grad", type, R, a, tau, (cudaStream_t)stream);
 }
