@@ -152,12 +152,38 @@ __device__ __forceinline__ uint64_t sdesc_v(uint32_t addr) {
   d |= (uint64_t)2 << 61;
   return d;
 }
-__device__ __forceinline__ void mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// The product warp runs its loop as a whole and only the instructions themselves are one lane's
+// (`leader`): with a lane's branch around the loop every descriptor went from that
+// lane's registers to the uniform ones, about 80 clocks an instruction (3,390 clocks a key tile).
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(tmem_d),
-      "r"(tmem_a), "l"(b), "r"(idesc), "r"(accumulate)
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader)
+      : "memory");
+}
+// A (M = 128 rows, pairs of 16-bit values) in TMEM
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t tmem_d, uint32_t tmem_a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t leader, uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)), "r"(leader)
       : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
@@ -333,59 +359,76 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
       __syncwarp();
     } else if (warp == 1) {
       // ------------------------------------------------------------ products
-      if (lane == 0) {
-        constexpr uint32_t id_s = idesc<T>(kRows, kKeys), id_o = idesc<T>(kRows, HD) | (1u << 16);   // (V is MN-major)
-        int g = 0, tiles[2] = {0, 0}, subs[2] = {0, 0};
-        auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(smem_u32(bar), parity, a.err); };
-        auto full = [&](int r) { return wait(&b.kv_full[r % ST], (r / ST) & 1); };
-        auto s_product = [&](int i, int r) {
-          const uint32_t q = sQ + i * TILE, k = sKV + (r % ST) * TILE;
-  #pragma unroll
-          for (int kk = 0; kk < HD / 16; ++kk) {
-            const uint32_t off = (kk / 4) * kAtom + (kk % 4) * 32;
-            mma_bf16(tmem + i * kKeys, sdesc(q + off), sdesc(k + off), id_s, kk > 0 ? 1u : 0u);
-          }
-          mma_commit(smem_u32(&b.s_full[i]));
-        };
-        bool ok = true;
-        for (int it = 0; ok; ++it) {
-          const int slot = it & 1;
-          if (!wait(&b.item_full[slot], (it >> 1) & 1)) break;
-          const int nn[2] = {b.item[slot].n[0], b.item[slot].n[1]}, n = max(nn[0], nn[1]);
-          mbar_arrive(smem_u32(&b.item_empty[slot]));
-          if (n == 0) break;
-          ok = wait(&b.q_full, it & 1) && full(g);
+      constexpr uint32_t id_s = idesc<T>(kRows, kKeys), id_o = idesc<T>(kRows, HD) | (1u << 16);   // (V is MN-major)
+      const uint32_t leader = elect_one();
+      const uint32_t tm = __shfl_sync(~0u, tmem, 0);
+      const uint64_t q0 = sdesc(sQ), k0 = sdesc(sKV), v0 = sdesc_v(sKV);      // (bytes / 16 are added to their low bits)
+      // (uniform over the warp; the ring's position as a stage and a phase)
+      int st = 0, ph = 0, parity_p[2] = {0, 0}, parity_o[2] = {1, 1};
+      auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, a.err)); };
+      auto stage = [&](int ahead) { return st + ahead >= ST ? st + ahead - ST : st + ahead; };
+      auto full = [&](int ahead) { return wait(&b.kv_full[stage(ahead)], st + ahead >= ST ? ph ^ 1 : ph); };
+      auto s_product = [&](int i, int ahead) {
+        const uint64_t q = q0 + (i * TILE >> 4), k = k0 + (uint32_t)(stage(ahead) * (TILE >> 4));
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+          const uint32_t off = ((kk / 4) * kAtom + (kk % 4) * 32) >> 4;
+          mma_ss(leader, tm + i * kKeys, q + off, k + off, id_s, kk > 0 ? 1u : 0u);
+        }
+        commit(leader, &b.s_full[i]);
+      };
+      bool ok = true;
+      for (int it = 0; ok; ++it) {
+        const int slot = it & 1;
+        if (!wait(&b.item_full[slot], (it >> 1) & 1)) break;
+        const int nn[2] = {__shfl_sync(~0u, b.item[slot].n[0], 0), __shfl_sync(~0u, b.item[slot].n[1], 0)};
+        const int n = max(nn[0], nn[1]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&b.item_empty[slot]));
+        if (n == 0) break;
+        ok = wait(&b.q_full, it & 1) && full(0);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (nn[i] > 0) s_product(i, 0);
+        commit(leader, &b.kv_empty[st]);
+        if (n == 1) commit(leader, &b.q_empty);
+        for (int j = 0; j < n; ++j) {
+          ok = full(1);
           if (!ok) break;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          for (int i = 0; i < 2; ++i)
-            if (nn[i] > 0) s_product(i, g);
-          mma_commit(smem_u32(&b.kv_empty[g % ST]));
-          if (n == 1) mma_commit(smem_u32(&b.q_empty));
-          for (int j = 0; ok && j < n; ++j, g += 2) {
-            ok = full(g + 1);
-            for (int i = 0; ok && i < 2; ++i) {
-              if (j < nn[i]) {
-                ok = wait(&b.p_full[i], tiles[i]++ & 1) && (j > 0 || subs[i] == 0 || wait(&b.o_free[i], (subs[i] - 1) & 1));
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (j < nn[i]) {
+              ok = wait(&b.p_full[i], parity_p[i]);
+              parity_p[i] ^= 1;
+              if (!ok) break;
+              if (j == 0) {                     // (the item before has left O)
+                ok = wait(&b.o_free[i], parity_o[i]);
+                parity_o[i] ^= 1;
                 if (!ok) break;
-                if (j == 0) ++subs[i];
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t v = sKV + ((g + 1) % ST) * TILE;
-  #pragma unroll
-                for (int kk = 0; kk < kKeys / 16; ++kk)
-                  mma_ts(tmem + kColO + i * HD, tmem + i * kKeys + 8 * kk, sdesc_v(v + kk * 2048), id_o, (j > 0 || kk > 0) ? 1u : 0u);
-                mma_commit(smem_u32(&b.o_full[i]));
               }
-              if (i == 1) mma_commit(smem_u32(&b.kv_empty[(g + 1) % ST]));
-              if (j + 1 < n) {
-                if (i == 0) ok = full(g + 2);
-                if (ok && j + 1 < nn[i]) s_product(i, g + 2);
-                if (i == 1) {
-                  mma_commit(smem_u32(&b.kv_empty[(g + 2) % ST]));
-                  if (j + 2 == n) mma_commit(smem_u32(&b.q_empty));
-                }
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              const uint64_t v = v0 + (uint32_t)(stage(1) * (TILE >> 4));
+#pragma unroll
+              for (int kk = 0; kk < kKeys / 16; ++kk)
+                mma_ts(leader, tm + kColO + i * HD, tm + i * kKeys + 8 * kk, v + kk * (2048 >> 4), id_o, (j > 0 || kk > 0) ? 1u : 0u);
+              commit(leader, &b.o_full[i]);
+            }
+            if (i == 1) commit(leader, &b.kv_empty[stage(1)]);
+            if (j + 1 < n) {
+              if (i == 0) ok = full(2);
+              if (!ok) break;
+              if (j + 1 < nn[i]) s_product(i, 2);
+              if (i == 1) {
+                commit(leader, &b.kv_empty[stage(2)]);
+                if (j + 2 == n) commit(leader, &b.q_empty);
               }
             }
           }
+          if (!ok) break;
+          if (st + 2 >= ST) ph ^= 1;
+          st = stage(2);
         }
       }
       __syncwarp();
