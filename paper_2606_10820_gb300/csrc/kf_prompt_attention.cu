@@ -15,8 +15,10 @@
 // 2^8, so O is rarely rescaled; sums are fp32, P is rounded to the inputs' type (the
 // tensor cores' operand).
 //
-// The items are sorted by their key tiles, longest first, by one block before
-// (k_plan), and handed out by a counter.  What bounds it: long prompts the tensor
+// The items come sorted by their key tiles, longest first.  Up to 128 sequences each CTA's load
+// warp holds the lengths in registers and finds its items itself, dealt forwards and backwards
+// in turn; for more a block before (k_plan) writes the list, and a counter hands it out (a launch and
+// about 5 us that a short call does not repay).  What bounds it: long prompts the tensor
 // cores (2,048 clocks a key tile of hd 128 and 256 rows), short ones the chain of an item.
 #include <algorithm>
 
@@ -37,6 +39,7 @@ constexpr uint32_t kColO = 256;
 constexpr float kRaise = 8.f;
 constexpr int kMaxTiles = 4096;                    // key tiles of a sequence: 524,288 tokens
 constexpr int kPlanThreads = 1024;
+constexpr int kDirect = 4;                          // sequences that a lane of the load warp holds: up to 128 without a plan
 
 template <int HD> constexpr int kStages = HD == 128 ? 5 : 8;
 template <int HD> constexpr uint32_t kTile = kAtom * (HD / 64);
@@ -60,6 +63,8 @@ struct Args {
   Plan plan;
   int* err;
   int Hq, G, pairs;                                 // pairs: two heads per item (else two tiles of rows)
+  int direct, n, T, longest;                        // direct: the items are found from starts, without a plan
+  const int32_t* starts;
   float scale2;
 };
 struct Maps { CUtensorMap q, k, v; };
@@ -204,6 +209,12 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// 32 bytes of one row (a 32-byte aligned address): half as many lines touched as two 16-byte stores
+__device__ __forceinline__ void st_32(void* p, const uint32_t* r) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
 template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   if constexpr (std::is_same<T, __half>::value) {
     const __half2 h = __floats2half2_rn(lo, hi);
@@ -271,15 +282,80 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
     if (warp == 0) {
       // -------------------------------------------------------------- copies
       const int heads = a.pairs ? a.Hq / 2 : a.Hq, per = a.pairs ? 1 : 2;
-      const int items = __ldcg(a.plan.count) * heads;
+      int first[kDirect], len[kDirect], tiles[kDirect], total = 0, most = 0;
+      if (a.direct) {
+        bool bad = false;
+#pragma unroll
+        for (int x = 0; x < kDirect; ++x) {
+          const int s = lane + 32 * x;
+          const int p = s < a.n ? __ldg(a.starts + s) : a.T, e = s < a.n ? __ldg(a.starts + s + 1) : a.T;
+          bad |= p < 0 || e < p || e > a.T || e - p > a.longest || (s == 0 && p != 0) || (s == a.n - 1 && e != a.T);
+          first[x] = p;
+          len[x] = e - p;
+          tiles[x] = (len[x] + per * kRows - 1) / (per * kRows);
+        }
+        bad = __any_sync(~0u, bad);
+        if (bad && lane == 0 && blockIdx.x == 0) atomicOr(a.err, KF_DEV_BAD_ROW);
+#pragma unroll
+        for (int x = 0; x < kDirect; ++x) {
+          if (bad) tiles[x] = 0;
+          total += tiles[x];
+          most = max(most, tiles[x]);
+        }
+        total = __reduce_add_sync(~0u, total);
+        most = __reduce_max_sync(~0u, most);
+      } else {
+        total = __ldcg(a.plan.count);
+      }
+      const int items = total * heads;
+      // the w-th item's {first token, tokens, tile of rows}, those of most key tiles first
       auto entry = [&](int w) -> int4 {
-        return w < items ? __ldcg(reinterpret_cast<const int4*>(a.plan.item) + w / heads) : make_int4(0, 0, 0, 0);
+        if (w >= items) return make_int4(0, 0, 0, 0);
+        const int u = w / heads;
+        if (!a.direct) return __ldcg(reinterpret_cast<const int4*>(a.plan.item) + u);
+        // tile c - 1 of the sequences of c tiles and more: after the items of higher tiles,
+        // of which there are above(c); c is the least with above(c) <= u
+        auto above = [&](int c) {
+          int v = 0;
+#pragma unroll
+          for (int x = 0; x < kDirect; ++x) v += max(0, tiles[x] - c);
+          return __reduce_add_sync(~0u, v);
+        };
+        int lo = 1, hi = most;
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (above(mid) <= u) hi = mid;
+          else lo = mid + 1;
+        }
+        int rank = u - above(lo);
+        int4 e = make_int4(0, 0, lo - 1, 0);
+        bool found = false;
+#pragma unroll
+        for (int x = 0; x < kDirect; ++x) {
+          const bool has = tiles[x] >= lo;
+          const uint32_t m = __ballot_sync(~0u, has);
+          const uint32_t at = __ballot_sync(~0u, !found && has && __popc(m & ((1u << lane) - 1)) == rank);
+          if (at) {
+            e.x = __shfl_sync(~0u, first[x], __ffs(at) - 1);
+            e.y = __shfl_sync(~0u, len[x], __ffs(at) - 1);
+            found = true;
+          }
+          rank -= __popc(m);
+        }
+        return e;
+      };
+      // the CTA's i-th item: dealt forwards and backwards in turn, or drawn
+      auto drawn = [&](int i) -> int {
+        if (a.direct) return i * gridDim.x + ((i & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+        if (i == 0) return blockIdx.x;
+        int v = 0;
+        if (lane == 0) v = atomicAdd(a.plan.next, 1);
+        return v;                               // (lane 0's; shared where it is used)
       };
       bool ok = true;
-      int w = blockIdx.x, w1 = 0, it = 0, q_issued = 0, g = 0, tails = 0;
+      int w = drawn(0), it = 0, q_issued = 0, g = 0, tails = 0;
       int4 e = entry(w);
-      if (lane == 0) w1 = atomicAdd(a.plan.next, 1);
-      w1 = __shfl_sync(~0u, w1, 0);
+      int w1 = __shfl_sync(~0u, drawn(1), 0);
       auto wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, a.err)); };
       for (;; ++it) {
         Item im;
@@ -303,8 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
         if (w >= items) break;                    // (an item without sub-tiles ends the others)
         // the next item's entry and the counter for the one after it: used an item later
         const int4 e1 = entry(w1);
-        int w2 = 0;
-        if (lane == 0) w2 = atomicAdd(a.plan.next, 1);
+        const int w2 = drawn(it + 2);
         if (it > 0) ok = wait(&b.q_empty, (it - 1) & 1);
         if (!ok) break;
         if (lane == 0) {
@@ -520,8 +595,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const float inv = 1.f / l;
       const bool mine = im.row[sub] + row < im.len;
-      uint4* dst = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + (int64_t)(im.start + im.row[sub] + row) * a.out_row +
-                                            im.head[sub] * a.out_head);
+      T* dst = static_cast<T*>(a.out) + (int64_t)(im.start + im.row[sub] + row) * a.out_row + im.head[sub] * a.out_head;
+      const bool wide = (reinterpret_cast<uintptr_t>(dst) & 31) == 0;
 #pragma unroll
       for (int c = 0; c < HD / 32; ++c) {
         float o[32];
@@ -530,11 +605,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           arrive(&b.o_free[sub]);
         }
-        if (mine)
+        if (mine) {
+          uint32_t pk[16];
 #pragma unroll
-          for (int d = 0; d < 32; d += 8)
-            dst[4 * c + d / 8] = make_uint4(pack2<T>(o[d] * inv, o[d + 1] * inv), pack2<T>(o[d + 2] * inv, o[d + 3] * inv),
-                                            pack2<T>(o[d + 4] * inv, o[d + 5] * inv), pack2<T>(o[d + 6] * inv, o[d + 7] * inv));
+          for (int d = 0; d < 16; ++d) pk[d] = pack2<T>(o[2 * d] * inv, o[2 * d + 1] * inv);
+          if (wide) {
+            st_32(dst + 32 * c, pk);
+            st_32(dst + 32 * c + 16, pk + 8);
+          } else {
+#pragma unroll
+            for (int d = 0; d < 16; d += 4)
+              *reinterpret_cast<uint4*>(dst + 32 * c + 2 * d) = make_uint4(pk[d], pk[d + 1], pk[d + 2], pk[d + 3]);
+          }
+        }
       }
     }
   }
@@ -556,7 +639,7 @@ template <typename T, int HD>
 int launch(const Maps& maps, const Args& a, int grid, cudaStream_t s) {
   static PerDevice attr;
   set_smem_attr(attr, k_prompt<T, HD>, kSmem<HD>);
-  launch_cluster(k_prompt<T, HD>, dim3(grid), dim3(kThreads), kSmem<HD>, 1, true, s, maps, a);
+  launch_cluster(k_prompt<T, HD>, dim3(grid), dim3(kThreads), kSmem<HD>, 1, !a.direct, s, maps, a);
   return launched("kf_op_prompt_attention");
 }
 int64_t plan_items(int n, int64_t T) { return T / kRows + n; }
@@ -596,14 +679,15 @@ extern "C" int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_
   if (!err) return refuse(what, "no error word", KF_E_CUDA);
   const int G = Hq / Hkv, pairs = G % 2 == 0, rows = pairs ? kRows : 2 * kRows;
   const int classes = std::max(1, ceil_div(longest, rows));
+  const int direct = n <= 32 * kDirect;
   int* head = static_cast<int*>(work);
   const Plan plan{head, head + 1, reinterpret_cast<PlanItem*>(head + 64)};
   const int grid = (int)std::min<int64_t>(device_sms(), cap * (pairs ? Hq / 2 : Hq));
   cudaStream_t s = (cudaStream_t)stream;
-  launch_cluster(k_plan, dim3(1), dim3(kPlanThreads), 2 * (classes + 2) * sizeof(int), 1, false, s, n, (int)T, longest, rows, classes,
+  if (!direct) launch_cluster(k_plan, dim3(1), dim3(kPlanThreads), 2 * (classes + 2) * sizeof(int), 1, false, s, n, (int)T, longest, rows, classes,
                  starts, plan, grid, err);
   if (const int rc = launched(what)) return rc;
-  const Args a{out, out_row, out_head, plan, err, Hq, G, pairs, scale * 1.4426950408889634f};
+  const Args a{out, out_row, out_head, plan, err, Hq, G, pairs, direct, n, (int)T, longest, starts, scale * 1.4426950408889634f};
   if (type == KF_TYPE_BF16) return hd == 64 ? launch<__nv_bfloat16, 64>(maps, a, grid, s) : launch<__nv_bfloat16, 128>(maps, a, grid, s);
   return hd == 64 ? launch<__half, 64>(maps, a, grid, s) : launch<__half, 128>(maps, a, grid, s);
 }
