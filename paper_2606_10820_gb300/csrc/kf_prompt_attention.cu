@@ -8,9 +8,10 @@
 //   warp 1      issues S = Q K^T (128 x 128 x hd) and O += P V (128 x hd x 128), the two
 //               sub-tiles in turn, so that one's softmax runs under the other's products;
 //   warps 4-7, 8-11  the softmax of sub-tile 0 and 1, one thread per row (its TMEM
-//               lane): no exchange between threads.  P goes back to TMEM over the first
-//               half of its own S columns: the products of a thread's tcgen05.mma run in order,
-//               so the next S needs no other buffer.
+//               lane): no exchange between threads.  P goes back to TMEM in two halves, so
+//               that its product begins under the second half's exponentials: to columns of
+//               its own at head_dim 64, over the first half of its own S columns at 128 (the
+//               products run in the order of their instructions, so the next S needs no other buffer).
 // Scores are taken against a reference per row that follows its maximum only past a factor of
 // 2^8, so O is rarely rescaled; sums are fp32, P is rounded to the inputs' type (the
 // tensor cores' operand).
@@ -36,6 +37,10 @@ constexpr int kRegsFew = 88, kRegsSoftmax = 208;
 constexpr uint32_t kAtom = kRows * 128;            // 128 rows of 64 elements: one swizzled box
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColO = 256;
+// head_dim 64 leaves TMEM columns for a P of its own: the next S then runs under this one's exponentials
+template <int HD> constexpr bool kOwnP = HD == 64;
+template <int HD> constexpr uint32_t kColP = kOwnP<HD> ? kColO + 2 * HD : 0;
+template <int HD> constexpr uint32_t kPitchP = kOwnP<HD> ? 64 : 128;      // columns from sub-tile 0's P to 1's
 constexpr float kRaise = 8.f;
 constexpr int kMaxTiles = 4096;                    // key tiles of a sequence: 524,288 tokens
 constexpr int kPlanThreads = 1024;
@@ -227,7 +232,7 @@ template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float 
 struct Bars {
   uint64_t q_full, q_empty;
   uint64_t item_full[2], item_empty[2];
-  uint64_t s_full[2], p_full[2], o_full[2], o_free[2];   // per sub-tile
+  uint64_t s_full[2], s_free[2], p_full[2][2], o_full[2], o_free[2];   // per sub-tile (and half of P)
   uint64_t tail;                                         // a V tile whose last rows are to be cleared has landed
   uint64_t kv_full[8], kv_empty[8];
   Item item[2];
@@ -255,7 +260,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
       init(&b.item_full[i], 1);
       init(&b.item_empty[i], 9);                // the MMA warp and eight softmax warps
       init(&b.s_full[i], 1);
-      init(&b.p_full[i], 4);
+      init(&b.s_free[i], 4);
+      init(&b.p_full[i][0], 4);
+      init(&b.p_full[i][1], 4);
       init(&b.o_full[i], 1);
       init(&b.o_free[i], 4);
     }
@@ -439,11 +446,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
       const uint32_t tm = __shfl_sync(~0u, tmem, 0);
       const uint64_t q0 = sdesc(sQ), k0 = sdesc(sKV), v0 = sdesc_v(sKV);      // (bytes / 16 are added to their low bits)
       // (uniform over the warp; the ring's position as a stage and a phase)
-      int st = 0, ph = 0, parity_p[2] = {0, 0}, parity_o[2] = {1, 1};
+      int st = 0, ph = 0, parity_s[2] = {1, 1}, parity_p[2] = {0, 0}, parity_o[2] = {1, 1};
       auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, a.err)); };
       auto stage = [&](int ahead) { return st + ahead >= ST ? st + ahead - ST : st + ahead; };
       auto full = [&](int ahead) { return wait(&b.kv_full[stage(ahead)], st + ahead >= ST ? ph ^ 1 : ph); };
-      auto s_product = [&](int i, int ahead) {
+      // S of sub-tile i against the K tile `ahead`, once the softmax has read the S before (where P
+      // lies over S, its product has waited for that)
+      auto s_product = [&](int i, int ahead) -> bool {
+        if (kOwnP<HD>) {
+          if (!wait(&b.s_free[i], parity_s[i])) return false;
+          parity_s[i] ^= 1;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        }
         const uint64_t q = q0 + (i * TILE >> 4), k = k0 + (uint32_t)(stage(ahead) * (TILE >> 4));
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) {
@@ -451,6 +465,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
           mma_ss(leader, tm + i * kKeys, q + off, k + off, id_s, kk > 0 ? 1u : 0u);
         }
         commit(leader, &b.s_full[i]);
+        return true;
+      };
+      // the next K tile's S products of the sub-tiles that have one
+      auto next_s = [&](int i, int j, const int* nn, int n) -> bool {
+        if (j + 1 >= n) return true;
+        if (i == 0 && !full(2)) return false;
+        if (j + 1 < nn[i] && !s_product(i, 2)) return false;
+        if (i == 1) {
+          commit(leader, &b.kv_empty[stage(2)]);
+          if (j + 2 == n) commit(leader, &b.q_empty);
+        }
+        return true;
       };
       bool ok = true;
       for (int it = 0; ok; ++it) {
@@ -466,39 +492,44 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          if (nn[i] > 0) s_product(i, 0);
+          if (ok && nn[i] > 0) ok = s_product(i, 0);
+        if (!ok) break;
         commit(leader, &b.kv_empty[st]);
         if (n == 1) commit(leader, &b.q_empty);
         for (int j = 0; j < n; ++j) {
+          if (kOwnP<HD>) {
+            ok = next_s(0, j, nn, n) && next_s(1, j, nn, n);
+            if (!ok) break;
+          }
           ok = full(1);
           if (!ok) break;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             if (j < nn[i]) {
-              ok = wait(&b.p_full[i], parity_p[i]);
-              parity_p[i] ^= 1;
-              if (!ok) break;
               if (j == 0) {                     // (the item before has left O)
                 ok = wait(&b.o_free[i], parity_o[i]);
                 parity_o[i] ^= 1;
                 if (!ok) break;
               }
-              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
               const uint64_t v = v0 + (uint32_t)(stage(1) * (TILE >> 4));
 #pragma unroll
-              for (int kk = 0; kk < kKeys / 16; ++kk)
-                mma_ts(leader, tm + kColO + i * HD, tm + i * kKeys + 8 * kk, v + kk * (2048 >> 4), id_o, (j > 0 || kk > 0) ? 1u : 0u);
+              for (int h = 0; h < 2; ++h) {     // P's halves
+                ok = wait(&b.p_full[i][h], parity_p[i]);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                for (int kk = 4 * h; kk < 4 * h + 4; ++kk)
+                  mma_ts(leader, tm + kColO + i * HD, tm + kColP<HD> + i * kPitchP<HD> + 8 * kk, v + kk * (2048 >> 4), id_o,
+                         (j > 0 || kk > 0) ? 1u : 0u);
+              }
+              if (!ok) break;
+              parity_p[i] ^= 1;
               commit(leader, &b.o_full[i]);
             }
             if (i == 1) commit(leader, &b.kv_empty[stage(1)]);
-            if (j + 1 < n) {
-              if (i == 0) ok = full(2);
+            if (!kOwnP<HD>) {
+              ok = next_s(i, j, nn, n);
               if (!ok) break;
-              if (j + 1 < nn[i]) s_product(i, 2);
-              if (i == 1) {
-                commit(leader, &b.kv_empty[stage(2)]);
-                if (j + 2 == n) commit(leader, &b.q_empty);
-              }
             }
           }
           if (!ok) break;
@@ -513,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     const int sub = warp >= 8, quarter = warp & 3, row = 32 * quarter + lane;
     const uint32_t lanes = tmem + ((uint32_t)(32 * quarter) << 16);
-    const uint32_t tS = lanes + sub * kKeys, tO = lanes + kColO + sub * HD;
+    const uint32_t tS = lanes + sub * kKeys, tO = lanes + kColO + sub * HD, tP = lanes + kColP<HD> + sub * kPitchP<HD>;
     const float sc = a.scale2;
     auto wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, a.err)); };
     auto arrive = [&](uint64_t* bar) {
@@ -552,6 +583,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
             for (int x = 0; x < 4; ++x)
               mq[x] = max3f(mq[x], __uint_as_float(s[32 * c + e + 2 * x]), __uint_as_float(s[32 * c + e + 2 * x + 1]));
         }
+        if (kOwnP<HD>) {
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          arrive(&b.s_free[sub]);
+        }
         const float mx = fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3]));
         const bool raise = j == 0 || (mx - m) * sc > kRaise;
         if (j > 0 && __any_sync(~0u, raise)) {
@@ -572,6 +607,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
         if (raise) m = mx;
         const float nm = m == -INFINITY ? 0.f : -m * sc;
         uint64_t ps[4] = {0ull, 0ull, 0ull, 0ull};
+        if (kOwnP<HD> && g > 0) {               // the product before has read P
+          if (!wait(&b.o_full[sub], (g - 1) & 1)) { ok = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        }
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           uint32_t pk[16];
@@ -582,11 +621,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
             ps[u & 3] = add_f2(ps[u & 3], f2(x, y));
             pk[u] = pack2<T>(x, y);
           }
-          tmem_st16(tS + 16 * c, pk);
+          tmem_st16(tP + 16 * c, pk);
+          if (c & 1) {
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            arrive(&b.p_full[sub][c >> 1]);
+          }
         }
-        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        arrive(&b.p_full[sub]);
         const float2 s2 = f2_split(add_f2(add_f2(ps[0], ps[1]), add_f2(ps[2], ps[3])));
         l += s2.x + s2.y;
       }
