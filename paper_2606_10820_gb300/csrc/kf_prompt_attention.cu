@@ -606,6 +606,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
         }
         if (raise) m = mx;
         const float nm = m == -INFINITY ? 0.f : -m * sc;
+        const uint64_t sc2 = f2(sc, sc), nm2 = f2(nm, nm);
         uint64_t ps[4] = {0ull, 0ull, 0ull, 0ull};
         if (kOwnP<HD> && g > 0) {               // the product before has read P
           if (!wait(&b.o_full[sub], (g - 1) & 1)) { ok = false; break; }
@@ -616,8 +617,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
           uint32_t pk[16];
 #pragma unroll
           for (int u = 0; u < 16; ++u) {
-            const float x = mma::ex2(fmaf(__uint_as_float(s[32 * c + 2 * u]), sc, nm));
-            const float y = mma::ex2(fmaf(__uint_as_float(s[32 * c + 2 * u + 1]), sc, nm));
+            const float2 d = f2_split(fma_f2(f2(__uint_as_float(s[32 * c + 2 * u]), __uint_as_float(s[32 * c + 2 * u + 1])), sc2, nm2));
+            const float x = mma::ex2(d.x), y = mma::ex2(d.y);
             ps[u & 3] = add_f2(ps[u & 3], f2(x, y));
             pk[u] = pack2<T>(x, y);
           }
