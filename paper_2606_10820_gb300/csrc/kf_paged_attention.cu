@@ -3,18 +3,20 @@
 //
 // The query rows of one (sequence, KV head) are its rows x group heads; tiles of
 // 16 of them run on warp-level MMA (m16n8k16, fp32 accumulation) with the
-// softmax in registers, so K and V are read once for all heads of a group.
+// softmax in registers, so K and V are read once for all heads of a group (and at
+// head_dim 64 for 32 rows at a time, which the registers hold there).
 // What bounds it is those bytes, so the layout serves the loads:
 //   - The keys of all (sequence, KV head, tile) segments, in units of 8 KB of K
 //     and V (16 keys of 128, 32 of 64), form one list that the CTAs share
-//     evenly: a ragged batch and a single long sequence fill the SMs alike.  A segment that
+//     evenly: a ragged batch and a single long sequence fill the SMs alike.  A segment counts
+//     kExtra units more than it has, for its start and end.  One that
 //     ends in another CTA than it began in leaves fp32 partials, which k_join
 //     adds in list order (so the same lengths give the same bits).
 //   - In a CTA unit x belongs to warp x mod 4, which copies it into
-//     a ring of its own (cp.async, two units ahead, across segment ends)
+//     a ring of its own (cp.async, ahead of the products and across segment ends)
 //     and waits for nobody; the warps of a segment meet once, to merge.
-//   - Two CTAs per SM: 8 warps with two units in flight are 128 KB a SM, about
-//     three times what DRAM latency asks for at 45 GB/s a SM.
+//   - Two CTAs per SM with two units a warp under way, or (head_dim 64, one tile) three
+//     with one: 128 or 96 KB a SM, twice and more what DRAM latency asks for at 45 GB/s a SM.
 #include <algorithm>
 
 #include "kf_mma.cuh"
@@ -24,11 +26,17 @@ namespace kf {
 namespace {
 
 constexpr int NW = 4, kThreads = 32 * NW;     // warps of a CTA
-constexpr int kStages = 3;
-constexpr int kCtasPerSm = 2;
 constexpr int kUnitBytes = 8192;              // K and V of a unit
-constexpr int kTile = 16;                     // query rows of a segment
 constexpr int kMinUnits = 4;                  // units of a CTA where the work allows it: one per warp
+constexpr int kExtra = 6;                     // a segment's start and end, in units
+// what a (head_dim, tiles of 16 rows per segment) pair of kernels uses
+template <int HD, int TILES> constexpr bool kThree = HD == 64 && TILES == 1;
+template <int HD, int TILES> constexpr int kStages = kThree<HD, TILES> ? 2 : 3;
+template <int HD, int TILES> constexpr int kCtasPerSm = kThree<HD, TILES> ? 3 : 2;
+constexpr int kMostCtasPerSm = 3, kMostRows = 32, kMostValues = 2048;      // of a segment: rows, rows x hd
+
+// a segment that CTA c began and others went on with
+struct Split { int b, s, pieces, pad; };
 
 struct Args {
   const void* q;
@@ -36,12 +44,14 @@ struct Args {
   const void* pool;
   const int32_t *table, *lens;
   void* out;
-  float* part_o;        // [2 CTAs][16][hd]
-  float2* part_ml;      // [2 CTAs][16]
+  float* part_o;        // [2 CTAs][rows of a segment][hd]
+  float2* part_ml;      // [2 CTAs][kMostRows]
+  Split* split;         // [CTAs]
   int* err;
   int64_t n_pages;
-  int B, rows, Hq, Hkv, G, MT, page, width;
+  int B, rows, Hq, Hkv, G, MT, page, page_shift, width;    // page_shift: -1 where page is no power of two
   float scale2;         // scale log2(e): scores in base-2 units
+  __device__ __forceinline__ int page_of(int key) const { return page_shift >= 0 ? key >> page_shift : key / page; }
 };
 
 template <int HD> constexpr int kUnit = kUnitBytes / (4 * HD);      // keys
@@ -73,25 +83,22 @@ template <int HD> __device__ __forceinline__ int units_of(const Args& a, int b) 
   return max(1, (seq_len(a, b) + kUnit<HD> - 1) / kUnit<HD>);
 }
 
-// The list: sequence by sequence, each one's Hkv * MT segments, each one's units.
-// Part c of `parts` even ones is [x0, x1); b and base: the sequence that x0 lies
-// in, and its first unit.  Called by the whole block.
+// The list: sequence by sequence, each one's Hkv * MT segments, each one's units and kExtra
+// places more.  Part c of `parts` even ones is [x0, x1); b and base: the sequence that x0 lies
+// in, and its first place.  Called by the whole block.
 struct Part {
   long long total, x0, x1, base;
   int b, parts;
 };
+__device__ __forceinline__ long long part_begin(long long total, int parts, int c) { return total * c / parts; }
 template <int HD>
-__device__ __forceinline__ long long part_begin(long long total, int parts, int c) {
-  return total * c / parts;
-}
-template <int HD, int THREADS>
 __device__ Part find_part(const Args& a, int c, int ctas) {
-  __shared__ long long warp_sum[THREADS / 32];
+  __shared__ long long warp_sum[NW];
   __shared__ Part found;
-  const int t = threadIdx.x, per = (a.B + THREADS - 1) / THREADS, sb = a.Hkv * a.MT;
+  const int t = threadIdx.x, per = (a.B + kThreads - 1) / kThreads, sb = a.Hkv * a.MT;
   const int first = min(a.B, t * per), last = min(a.B, first + per);
   long long mine = 0;
-  for (int b = first; b < last; ++b) mine += units_of<HD>(a, b);
+  for (int b = first; b < last; ++b) mine += units_of<HD>(a, b) + kExtra;
   mine *= sb;
   long long incl = mine;
 #pragma unroll
@@ -102,51 +109,55 @@ __device__ Part find_part(const Args& a, int c, int ctas) {
   if ((t & 31) == 31) warp_sum[t >> 5] = incl;
   __syncthreads();
   long long before = 0, total = 0;
-  for (int w = 0; w < THREADS / 32; ++w) {
+  for (int w = 0; w < NW; ++w) {
     if (w < (t >> 5)) before += warp_sum[w];
     total += warp_sum[w];
   }
   const int parts = (int)min((long long)ctas, max(1ll, total / kMinUnits));
-  const long long x0 = part_begin<HD>(total, parts, c), lo = before + incl - mine;
+  const long long x0 = part_begin(total, parts, c), lo = before + incl - mine;
   if (c < parts && x0 >= lo && x0 < lo + mine) {
     long long base = lo;
     int b = first;
-    for (long long n = (long long)units_of<HD>(a, b) * sb; x0 >= base + n; n = (long long)units_of<HD>(a, b) * sb) {
+    for (long long n = (long long)(units_of<HD>(a, b) + kExtra) * sb; x0 >= base + n; n = (long long)(units_of<HD>(a, b) + kExtra) * sb) {
       base += n;
       ++b;
     }
-    found = Part{total, x0, part_begin<HD>(total, parts, c + 1), base, b, parts};
+    found = Part{total, x0, part_begin(total, parts, c + 1), base, b, parts};
   }
   if (t == 0 && c >= parts) found = Part{total, total, total, 0, a.B, parts};
   __syncthreads();
   return found;
 }
 
-// one segment's units within a CTA's part
+// one segment's places within a CTA's part
 template <int HD>
 struct Piece {
-  long long xs, xa, xb;    // the segment's first unit, the piece's units
-  int b, s, n, len;        // sequence, segment of it, units of the segment, tokens
+  long long xs, xa, xb, xe;    // the segment's first unit; the piece's units [xa, xb) (or none) and its end
+  int b, s, n, len;            // sequence, segment of it, units of the segment, tokens
+  __device__ __forceinline__ void cut(const Part& p) {
+    xa = max(xs, p.x0);
+    xb = min(xs + n, p.x1);
+    xe = min(xs + n + kExtra, p.x1);
+  }
   __device__ __forceinline__ void at(const Args& a, const Part& p) {
     b = p.b;
     n = units_of<HD>(a, b);
     len = seq_len(a, b);
-    s = (int)((p.x0 - p.base) / n);
-    xs = p.base + (long long)s * n;
-    xa = p.x0;
-    xb = min(xs + n, p.x1);
+    s = (int)((p.x0 - p.base) / (n + kExtra));
+    xs = p.base + (long long)s * (n + kExtra);
+    cut(p);
   }
   // the next piece; false past the part's end
   __device__ __forceinline__ bool next(const Args& a, const Part& p) {
-    if (xb >= p.x1) return false;
+    if (xe >= p.x1) return false;
     if (++s == a.Hkv * a.MT) {
       s = 0;
       ++b;
       n = units_of<HD>(a, b);
       len = seq_len(a, b);
     }
-    xs = xa = xb;
-    xb = min(xs + n, p.x1);
+    xs = xe;
+    cut(p);
     return true;
   }
 };
@@ -163,11 +174,14 @@ struct Feed {
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
       const int key = (int)(x - pc.xs) * U + 16 * h;
-      page[h] = key < pc.len ? __ldg(a.table + (size_t)pc.b * a.width + key / a.page) : -1;
+      page[h] = key < pc.len ? __ldg(a.table + (size_t)pc.b * a.width + a.page_of(key)) : -1;
     }
   }
   __device__ __forceinline__ void skip(const Args& a, const Part& p) {
-    while (more && x >= pc.xb) more = pc.next(a, p);
+    while (more && x >= pc.xb) {
+      more = pc.next(a, p);
+      if (x < pc.xa) x += (pc.xa - x + NW - 1) / NW * NW;
+    }
     if (more) look(a);
   }
   __device__ __forceinline__ void start(const Args& a, const Part& p, int warp) {
@@ -190,7 +204,7 @@ struct Feed {
         if (in) ok |= 1u << h;
         else if (left > 0 && lane == 0) atomicOr(a.err, KF_DEV_BAD_PAGE);
         const T* kb = static_cast<const T*>(a.pool) +
-                      (((in ? (int64_t)page[h] : 0) * 2 * a.Hkv + hk) * a.page + key0 % a.page) * HD + c * 8;
+                      (((in ? (int64_t)page[h] : 0) * 2 * a.Hkv + hk) * a.page + key0 - a.page_of(key0) * a.page) * HD + c * 8;
         const T* vb = kb + (int64_t)a.Hkv * a.page * HD;
 #pragma unroll
         for (int i = 0; i < 16 / RP; ++i) {
@@ -209,66 +223,81 @@ struct Feed {
   }
 };
 
-template <int HD> constexpr int kMergeFloats = kTile * (HD + 2);    // one warp's O, m and l
-// (two CTAs of 114,992 bytes, their static arrays and 1 KB each fit the SM's 228 KB)
-template <int HD> constexpr size_t kSmem = NW * kStages * kUnitBytes + (NW / 2) * kMergeFloats<HD> * 4 + NW * kStages * 4;
+template <int HD, int TILES> constexpr int kMergeFloats = 16 * TILES * (HD + 2);    // one warp's O, m and l
+// (two CTAs of 114,992 bytes, their static arrays and 1 KB each fit the SM's 228 KB; three of 74,096)
+template <int HD, int TILES>
+constexpr size_t kSmem = NW * kStages<HD, TILES> * kUnitBytes + (NW / 2) * kMergeFloats<HD, TILES> * 4 + NW * kStages<HD, TILES> * 4;
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_paged(const Args a) {
+template <typename T, int HD, int TILES>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const Args a) {
   extern __shared__ __align__(128) uint8_t sm[];
+  constexpr int ST = kStages<HD, TILES>, ROWS = 16 * TILES;
   constexpr int U = kUnit<HD>, NT = U / 8, KS = HD / 16, DT = HD / 8;   // key tiles, dim steps of S, dim tiles of O
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31, g = lane >> 2, c = lane & 3;
-  float* merge = reinterpret_cast<float*>(sm + NW * kStages * kUnitBytes);
-  uint32_t* open_all = reinterpret_cast<uint32_t*>(merge + (NW / 2) * kMergeFloats<HD>);
-  uint32_t* open = open_all + warp * kStages;
-  const uint32_t ring = mma::smem_addr(sm) + warp * kStages * kUnitBytes;
+  float* merge = reinterpret_cast<float*>(sm + NW * ST * kUnitBytes);
+  uint32_t* open = reinterpret_cast<uint32_t*>(merge + (NW / 2) * kMergeFloats<HD, TILES>) + warp * ST;
+  const uint32_t ring = mma::smem_addr(sm) + warp * ST * kUnitBytes;
 
   if (blockIdx.x == 0)
     for (int b = t; b < a.B; b += kThreads) {
       const int n = a.lens[b];
       if (n < 0 || n > a.width * a.page) atomicOr(a.err, KF_DEV_BAD_ROW);
     }
-  const Part part = find_part<HD, kThreads>(a, blockIdx.x, gridDim.x);
+  if (t == 0) a.split[blockIdx.x].pieces = 0;
+  const Part part = find_part<HD>(a, blockIdx.x, gridDim.x);
   if (part.x0 < part.x1) {
     Feed<T, HD> feed;
     feed.start(a, part, warp);
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) feed.copy(a, part, ring + i * kUnitBytes, open + i, lane);
+    for (int i = 0; i < ST - 1; ++i) feed.copy(a, part, ring + i * kUnitBytes, open + i, lane);
     int st = 0;
 
     Piece<HD> pc;
     pc.at(a, part);
     do {
-      const int hk = pc.s / a.MT, r0 = (pc.s % a.MT) * kTile, R = a.rows * a.G;
+      if (pc.xa >= pc.xb) continue;                // (uniform) only places without units
+      const int hk = pc.s / a.MT, r0 = (pc.s % a.MT) * ROWS, R = a.rows * a.G;
       const int f = (int)(pc.xa % NW), nw = (int)min((long long)NW, pc.xb - pc.xa);
       const int j = (warp - f + NW) % NW;          // this warp's place among the piece's
-      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[DT][4];
+      // this lane's rows of tile i: r0 + 16 i + g and 8 more.  m: raw scores' maximum
+      float m[TILES][2], l[TILES][2], o[TILES][DT][4];
 #pragma unroll
-      for (int d = 0; d < DT; ++d) o[d][0] = o[d][1] = o[d][2] = o[d][3] = 0.f;
+      for (int i = 0; i < TILES; ++i) {
+        m[i][0] = m[i][1] = -INFINITY;
+        l[i][0] = l[i][1] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[i][d][0] = o[i][d][1] = o[i][d][2] = o[i][d][3] = 0.f;
+      }
       if (j < nw) {
-        // this lane's two rows: r0 + g and r0 + g + 8
-        uint32_t q[KS][4];
-        int last[2];                                // the last key each sees
+        uint32_t q[TILES][KS][4];
+        int last[TILES][2];                         // the last key each row sees
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = r0 + g + 8 * h, i = r / a.G;
-          last[h] = r < R ? pc.len - a.rows + i : -1;
-          const T* qp = static_cast<const T*>(a.q) + pc.b * a.q_seq + i * a.q_row + (int64_t)(hk * a.G + r - i * a.G) * a.q_head;
+        for (int i = 0; i < TILES; ++i)
 #pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            q[k][h] = r < R ? __ldg(reinterpret_cast<const uint32_t*>(qp + 16 * k + 2 * c)) : 0u;
-            q[k][h + 2] = r < R ? __ldg(reinterpret_cast<const uint32_t*>(qp + 16 * k + 8 + 2 * c)) : 0u;
+          for (int h = 0; h < 2; ++h) {
+            const int r = r0 + 16 * i + g + 8 * h, tok = r / a.G;
+            last[i][h] = r < R ? pc.len - a.rows + tok : -1;
+            const T* qp = static_cast<const T*>(a.q) + pc.b * a.q_seq + tok * a.q_row + (int64_t)(hk * a.G + r - tok * a.G) * a.q_head;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              q[i][k][h] = r < R ? __ldg(reinterpret_cast<const uint32_t*>(qp + 16 * k + 2 * c)) : 0u;
+              q[i][k][h + 2] = r < R ? __ldg(reinterpret_cast<const uint32_t*>(qp + 16 * k + 8 + 2 * c)) : 0u;
+            }
           }
-        }
         const int free_to = pc.len - a.rows;        // keys up to here are seen by every row
         for (long long x = pc.xa + j; x < pc.xb; x += NW) {
-          mma::cp_wait<kStages - 2>();
-          __syncwarp();
-          const uint32_t kst = ring + st * kUnitBytes, vst = kst + kUnitBytes / 2;
+          mma::cp_wait<ST - 2>();
+          __syncwarp();                             // all lanes' copies; and the stage before this one is free
           const uint32_t ok = open[st];
-          float s[NT][4];
+          const uint32_t kst = ring + st * kUnitBytes, vst = kst + kUnitBytes / 2;
+          const int fr = st == 0 ? ST - 1 : st - 1;
+          feed.copy(a, part, ring + fr * kUnitBytes, open + fr, lane);
+          st = st + 1 == ST ? 0 : st + 1;
+          float s[TILES][NT][4];
 #pragma unroll
-          for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+          for (int i = 0; i < TILES; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) s[i][n][0] = s[i][n][1] = s[i][n][2] = s[i][n][3] = 0.f;
           // S: 16 keys x 16 dims per ldmatrix
 #pragma unroll
           for (int k = 0; k < KS; ++k)
@@ -277,130 +306,159 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_paged(const Args a) {
               const int row = 8 * n + (lane & 7) + ((lane >> 4) << 3), ch = 2 * k + ((lane >> 3) & 1);
               uint32_t kb[4];
               mma::ldsm_x4(kst + row * (HD * 2) + ((ch ^ (row & 7)) << 4), kb);
-              mma16816<T>(s[n], q[k], kb[0], kb[1]);
-              mma16816<T>(s[n + 1], q[k], kb[2], kb[3]);
+#pragma unroll
+              for (int i = 0; i < TILES; ++i) {
+                mma16816<T>(s[i][n], q[i][k], kb[0], kb[1]);
+                mma16816<T>(s[i][n + 1], q[i][k], kb[2], kb[3]);
+              }
             }
           const int key0 = (int)(x - pc.xs) * U;
-          const bool masked = key0 + U - 1 > free_to || ok != (1u << (U / 16)) - 1;
-          float mx[2] = {-INFINITY, -INFINITY};
+          if (key0 + U - 1 > free_to || ok != (1u << (U / 16)) - 1) {       // (uniform)
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+            for (int i = 0; i < TILES; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float v = s[n][e] * a.scale2;
-              if (masked && (key0 + 8 * n + 2 * c + (e & 1) > last[e >> 1] || !((ok >> (n >> 1)) & 1u))) v = -INFINITY;
-              s[n][e] = v;
-              mx[e >> 1] = fmaxf(mx[e >> 1], v);
-            }
-          float ref[2], fac[2];
+              for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            mx[h] = fmaxf(mx[h], __shfl_xor_sync(~0u, mx[h], 1));
-            mx[h] = fmaxf(mx[h], __shfl_xor_sync(~0u, mx[h], 2));
-            mx[h] = fmaxf(mx[h], m[h]);
-            fac[h] = m[h] == -INFINITY ? 1.f : mma::ex2(m[h] - mx[h]);    // (nothing to scale yet)
-            ref[h] = mx[h] == -INFINITY ? 0.f : mx[h];
-            m[h] = mx[h];
-          }
-          if (__any_sync(~0u, fac[0] != 1.f || fac[1] != 1.f)) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) l[h] *= fac[h];
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-              o[d][0] *= fac[0];
-              o[d][1] *= fac[0];
-              o[d][2] *= fac[1];
-              o[d][3] *= fac[1];
-            }
+                for (int e = 0; e < 4; ++e)
+                  if (key0 + 8 * n + 2 * c + (e & 1) > last[i][e >> 1] || !((ok >> (n >> 1)) & 1u)) s[i][n][e] = -INFINITY;
           }
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+          for (int i = 0; i < TILES; ++i) {
+            float nm[2], fac[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              s[n][e] = mma::ex2(s[n][e] - ref[e >> 1]);
-              l[e >> 1] += s[n][e];
+            for (int h = 0; h < 2; ++h) {
+              float mx = fmaxf(s[i][0][2 * h], s[i][0][2 * h + 1]);
+#pragma unroll
+              for (int n = 1; n < NT; ++n) mx = fmaxf(mx, fmaxf(s[i][n][2 * h], s[i][n][2 * h + 1]));
+              mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 1));
+              mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, 2));
+              mx = fmaxf(mx, m[i][h]);
+              fac[h] = m[i][h] == -INFINITY ? 1.f : mma::ex2((m[i][h] - mx) * a.scale2);     // (nothing to scale yet)
+              nm[h] = mx == -INFINITY ? 0.f : -mx * a.scale2;
+              m[i][h] = mx;
             }
+            if (__any_sync(~0u, fac[0] != 1.f || fac[1] != 1.f)) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) l[i][h] *= fac[h];
+#pragma unroll
+              for (int d = 0; d < DT; ++d) {
+                o[i][d][0] *= fac[0];
+                o[i][d][1] *= fac[0];
+                o[i][d][2] *= fac[1];
+                o[i][d][3] *= fac[1];
+              }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                s[i][n][e] = mma::ex2(fmaf(s[i][n][e], a.scale2, nm[e >> 1]));
+                l[i][e >> 1] += s[i][n][e];
+              }
+          }
           // O: 16 keys x 16 dims of V per ldmatrix; the probabilities are rounded to the
           // cache's type, the tensor cores' operand (the sum l is not)
 #pragma unroll
           for (int n = 0; n < NT; n += 2) {
-            const uint32_t p[4] = {pack2<T>(s[n][0], s[n][1]), pack2<T>(s[n][2], s[n][3]), pack2<T>(s[n + 1][0], s[n + 1][1]),
-                                   pack2<T>(s[n + 1][2], s[n + 1][3])};
+            uint32_t p[TILES][4];
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) {
+              p[i][0] = pack2<T>(s[i][n][0], s[i][n][1]);
+              p[i][1] = pack2<T>(s[i][n][2], s[i][n][3]);
+              p[i][2] = pack2<T>(s[i][n + 1][0], s[i][n + 1][1]);
+              p[i][3] = pack2<T>(s[i][n + 1][2], s[i][n + 1][3]);
+            }
 #pragma unroll
             for (int d = 0; d < DT; d += 2) {
               const int row = 8 * n + (lane & 15), ch = d + (lane >> 4);
               uint32_t vb[4];
               mma::ldsm_x4_t(vst + row * (HD * 2) + ((ch ^ (row & 7)) << 4), vb);
-              mma16816<T>(o[d], p, vb[0], vb[1]);
-              mma16816<T>(o[d + 1], p, vb[2], vb[3]);
+#pragma unroll
+              for (int i = 0; i < TILES; ++i) {
+                mma16816<T>(o[i][d], p[i], vb[0], vb[1]);
+                mma16816<T>(o[i][d + 1], p[i], vb[2], vb[3]);
+              }
             }
           }
-          __syncwarp();                             // the stage before this one is free for all lanes
-          feed.copy(a, part, ring + (st + kStages - 1) % kStages * kUnitBytes, open + (st + kStages - 1) % kStages, lane);
-          st = (st + 1) % kStages;
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          l[h] += __shfl_xor_sync(~0u, l[h], 1);
-          l[h] += __shfl_xor_sync(~0u, l[h], 2);
-        }
+        for (int i = 0; i < TILES; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            l[i][h] += __shfl_xor_sync(~0u, l[i][h], 1);
+            l[i][h] += __shfl_xor_sync(~0u, l[i][h], 2);
+          }
       }
       // the piece's warps merge in pairs: j + w into j
 #pragma unroll
       for (int w = NW / 2; w; w >>= 1) {
         if (nw <= w) continue;                      // (uniform)
         if (j >= w && j < min(2 * w, nw)) {
-          float* d = merge + (j - w) * kMergeFloats<HD>;
+          float* d = merge + (j - w) * kMergeFloats<HD, TILES>;
 #pragma unroll
-          for (int i = 0; i < DT; ++i) *reinterpret_cast<float4*>(d + (i * 32 + lane) * 4) = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
-          if (c == 0)
+          for (int i = 0; i < TILES; ++i) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) *reinterpret_cast<float2*>(d + kTile * HD + 2 * (g + 8 * h)) = make_float2(m[h], l[h]);
+            for (int x = 0; x < DT; ++x)
+              *reinterpret_cast<float4*>(d + ((i * DT + x) * 32 + lane) * 4) = make_float4(o[i][x][0], o[i][x][1], o[i][x][2], o[i][x][3]);
+            if (c == 0)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                *reinterpret_cast<float2*>(d + ROWS * HD + 2 * (16 * i + g + 8 * h)) = make_float2(m[i][h], l[i][h]);
+          }
         }
         __syncthreads();
         if (j < w && j + w < nw) {
-          const float* d = merge + j * kMergeFloats<HD>;
-          float fa[2], fb[2];
+          const float* d = merge + j * kMergeFloats<HD, TILES>;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float2 ml = *reinterpret_cast<const float2*>(d + kTile * HD + 2 * (g + 8 * h));
-            const float mm = fmaxf(m[h], ml.x);
-            fa[h] = m[h] == -INFINITY ? 0.f : mma::ex2(m[h] - mm);
-            fb[h] = ml.x == -INFINITY ? 0.f : mma::ex2(ml.x - mm);
-            l[h] = l[h] * fa[h] + ml.y * fb[h];
-            m[h] = mm;
-          }
+          for (int i = 0; i < TILES; ++i) {
+            float fa[2], fb[2];
 #pragma unroll
-          for (int i = 0; i < DT; ++i) {
-            const float4 v = *reinterpret_cast<const float4*>(d + (i * 32 + lane) * 4);
-            o[i][0] = o[i][0] * fa[0] + v.x * fb[0];
-            o[i][1] = o[i][1] * fa[0] + v.y * fb[0];
-            o[i][2] = o[i][2] * fa[1] + v.z * fb[1];
-            o[i][3] = o[i][3] * fa[1] + v.w * fb[1];
+            for (int h = 0; h < 2; ++h) {
+              const float2 ml = *reinterpret_cast<const float2*>(d + ROWS * HD + 2 * (16 * i + g + 8 * h));
+              const float mm = fmaxf(m[i][h], ml.x);
+              fa[h] = m[i][h] == -INFINITY ? 0.f : mma::ex2((m[i][h] - mm) * a.scale2);
+              fb[h] = ml.x == -INFINITY ? 0.f : mma::ex2((ml.x - mm) * a.scale2);
+              l[i][h] = l[i][h] * fa[h] + ml.y * fb[h];
+              m[i][h] = mm;
+            }
+#pragma unroll
+            for (int x = 0; x < DT; ++x) {
+              const float4 v = *reinterpret_cast<const float4*>(d + ((i * DT + x) * 32 + lane) * 4);
+              o[i][x][0] = o[i][x][0] * fa[0] + v.x * fb[0];
+              o[i][x][1] = o[i][x][1] * fa[0] + v.y * fb[0];
+              o[i][x][2] = o[i][x][2] * fa[1] + v.z * fb[1];
+              o[i][x][3] = o[i][x][3] * fa[1] + v.w * fb[1];
+            }
           }
         }
         __syncthreads();
       }
       if (j == 0) {
-        const bool whole = pc.xa == pc.xs && pc.xb == pc.xs + pc.n;
+        const long long end = pc.xs + pc.n;
+        const bool whole = pc.xa == pc.xs && pc.xb == end;
         const int slot = 2 * blockIdx.x + (pc.xa == pc.xs);       // 0: a segment begun elsewhere, 1: one that goes on elsewhere
+        // (parts up to the last that begins before the segment's end: total p / parts < end)
+        if (!whole && pc.xa == pc.xs && lane == 0)
+          a.split[blockIdx.x] = Split{pc.b, pc.s, (int)((end * part.parts + part.total - 1) / part.total) - (int)blockIdx.x, 0};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = r0 + g + 8 * h, i = r / a.G;
-          if (r >= R) continue;
-          if (whole) {
-            const float inv = l[h] == 0.f ? 0.f : 1.f / l[h];     // (no key seen: zeros)
-            T* op = static_cast<T*>(a.out) + (((int64_t)pc.b * a.rows + i) * a.Hq + hk * a.G + r - i * a.G) * HD;
+        for (int i = 0; i < TILES; ++i)
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
-              *reinterpret_cast<uint32_t*>(op + 8 * d + 2 * c) = pack2<T>(o[d][2 * h] * inv, o[d][2 * h + 1] * inv);
-          } else {
-            float* op = a.part_o + ((int64_t)slot * kTile + g + 8 * h) * HD;
+          for (int h = 0; h < 2; ++h) {
+            const int rr = 16 * i + g + 8 * h, r = r0 + rr, tok = r / a.G;
+            if (r >= R) continue;
+            if (whole) {
+              const float inv = l[i][h] == 0.f ? 0.f : 1.f / l[i][h];     // (no key seen: zeros)
+              T* op = static_cast<T*>(a.out) + (((int64_t)pc.b * a.rows + tok) * a.Hq + hk * a.G + r - tok * a.G) * HD;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) *reinterpret_cast<float2*>(op + 8 * d + 2 * c) = make_float2(o[d][2 * h], o[d][2 * h + 1]);
-            if (c == 0) a.part_ml[slot * kTile + g + 8 * h] = make_float2(m[h], l[h]);
+              for (int d = 0; d < DT; ++d)
+                *reinterpret_cast<uint32_t*>(op + 8 * d + 2 * c) = pack2<T>(o[i][d][2 * h] * inv, o[i][d][2 * h + 1] * inv);
+            } else {
+              float* op = a.part_o + ((int64_t)slot * ROWS + rr) * HD;
+#pragma unroll
+              for (int d = 0; d < DT; ++d) *reinterpret_cast<float2*>(op + 8 * d + 2 * c) = make_float2(o[i][d][2 * h], o[i][d][2 * h + 1]);
+              if (c == 0) a.part_ml[slot * kMostRows + rr] = make_float2(m[i][h], l[i][h]);
+            }
           }
-        }
       }
     } while (pc.next(a, part));
     mma::cp_wait<0>();
@@ -408,78 +466,72 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_paged(const Args a) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// Block (c, row): the segment that goes on from part c - 1 into part c, if it began
-// in part c - 1: its pieces (slot 1 of c - 1, slot 0 of c, c + 1, ...) added in order
-template <typename T, int HD>
-__global__ void __launch_bounds__(256) k_join(const Args a, int ctas) {
-  constexpr int V4 = HD / 4, GR = 256 / V4;          // float4s of a row; groups that share the pieces
+// Block (c, y): rows y, y + gridDim.y, ... of the segment that CTA c began and others went on
+// with: its pieces (slot 1 of c, slot 0 of c + 1, c + 2, ...) added in order
+constexpr int kJoinThreads = 256;
+template <typename T, int HD, int TILES>
+__global__ void __launch_bounds__(kJoinThreads) k_join(const Args a) {
+  constexpr int ROWS = 16 * TILES, V4 = HD / 4, GR = kJoinThreads / V4;      // float4s of a row; groups that share the pieces
   __shared__ float4 so[GR][V4];
   __shared__ float2 sml[GR];
-  const int t = threadIdx.x, c = blockIdx.x + 1, v = t % V4, gr = t / V4;
-  const Part part = find_part<HD, 256>(a, c, ctas);
+  const int t = threadIdx.x, c = blockIdx.x, v = t % V4, gr = t / V4;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (c >= part.parts || part.x0 >= part.x1) return;
-  Piece<HD> pc;
-  pc.at(a, part);
-  if (pc.xs >= part.x0 || pc.xs < part_begin<HD>(part.total, part.parts, c - 1)) return;
-  const int r0 = (pc.s % a.MT) * kTile, hk = pc.s / a.MT, r = r0 + blockIdx.y;
-  if (r >= a.rows * a.G) return;
-  // parts c .. e - 1 begin inside the segment
-  const long long end = pc.xs + pc.n;
-  int e = c + 1;
-  {
-    int lo = c + 1, hi = part.parts;                 // the first part that begins at or past the end
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (part_begin<HD>(part.total, part.parts, mid) < end) lo = mid + 1;
-      else hi = mid;
-    }
-    e = lo;
-  }
-  const int n = e - c + 1;
-  auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * (c - 1) + 1 : 2 * (c + i - 1)) * kTile + blockIdx.y; };
-  float m = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [&](float m2, float l2, float4 x) {
-    const float mm = fmaxf(m, m2), fa = m == -INFINITY ? 0.f : mma::ex2(m - mm), fb = m2 == -INFINITY ? 0.f : mma::ex2(m2 - mm);
-    m = mm;
-    l = l * fa + l2 * fb;
-    o = make_float4(o.x * fa + x.x * fb, o.y * fa + x.y * fb, o.z * fa + x.z * fb, o.w * fa + x.w * fb);
-  };
   // (written by the kernel before this one: not through the read-only path)
+  const int4 sp = __ldcg(reinterpret_cast<const int4*>(a.split + c));
+  const int n = sp.z, r0 = (sp.y % a.MT) * ROWS, hk = sp.y / a.MT;
+  if (n == 0) return;
+  for (int rr = blockIdx.y; rr < min(ROWS, a.rows * a.G - r0); rr += gridDim.y) {
+    auto slot = [&](int i) { return (int64_t)(i == 0 ? 2 * c + 1 : 2 * (c + i)); };
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float m2, float l2, float4 x) {
+      const float mm = fmaxf(m, m2);
+      const float fa = m == -INFINITY ? 0.f : mma::ex2((m - mm) * a.scale2), fb = m2 == -INFINITY ? 0.f : mma::ex2((m2 - mm) * a.scale2);
+      m = mm;
+      l = l * fa + l2 * fb;
+      o = make_float4(o.x * fa + x.x * fb, o.y * fa + x.y * fb, o.z * fa + x.z * fb, o.w * fa + x.w * fb);
+    };
 #pragma unroll 4
-  for (int i = gr; i < n; i += GR) {
-    const float2 ml = __ldcg(a.part_ml + slot(i));
-    add(ml.x, ml.y, __ldcg(reinterpret_cast<const float4*>(a.part_o + slot(i) * HD) + v));
-  }
-  so[gr][v] = o;
-  if (v == 0) sml[gr] = make_float2(m, l);
-  __syncthreads();
-  if (gr == 0) {
-    for (int i = 1; i < min(GR, n); ++i) add(sml[i].x, sml[i].y, so[i][v]);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int i = r / a.G;
-    T* op = static_cast<T*>(a.out) + (((int64_t)pc.b * a.rows + i) * a.Hq + hk * a.G + r - i * a.G) * HD;
-    reinterpret_cast<uint2*>(op)[v] = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
+    for (int i = gr; i < n; i += GR) {
+      const float2 ml = __ldcg(a.part_ml + slot(i) * kMostRows + rr);
+      add(ml.x, ml.y, __ldcg(reinterpret_cast<const float4*>(a.part_o + (slot(i) * ROWS + rr) * HD) + v));
+    }
+    so[gr][v] = o;
+    if (v == 0) sml[gr] = make_float2(m, l);
+    __syncthreads();
+    if (gr == 0) {
+      for (int i = 1; i < min(GR, n); ++i) add(sml[i].x, sml[i].y, so[i][v]);
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int r = r0 + rr, tok = r / a.G;
+      T* op = static_cast<T*>(a.out) + (((int64_t)sp.x * a.rows + tok) * a.Hq + hk * a.G + r - tok * a.G) * HD;
+      reinterpret_cast<uint2*>(op)[v] = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
+    }
+    __syncthreads();
   }
 }
 
-int paged_ctas() { return kCtasPerSm * device_sms(); }
+int paged_ctas() { return kMostCtasPerSm * device_sms(); }
 
-template <typename T, int HD>
+template <typename T, int HD, int TILES>
 int launch(Args a, void* work, cudaStream_t s) {
-  const int ctas = paged_ctas();
-  a.part_ml = static_cast<float2*>(work);
-  a.part_o = reinterpret_cast<float*>(a.part_ml + 2 * (size_t)ctas * kTile);
-  // no more CTAs than the longest lists the table could hold fill
-  const long long units = (long long)a.B * a.Hkv * a.MT * std::max(1, ceil_div(a.width * a.page, kUnit<HD>));
+  const int most = paged_ctas(), ctas = kCtasPerSm<HD, TILES> * device_sms();
+  a.MT = ceil_div(a.rows * a.G, 16 * TILES);
+  a.split = static_cast<Split*>(work);
+  a.part_ml = reinterpret_cast<float2*>(a.split + most);
+  a.part_o = reinterpret_cast<float*>(a.part_ml + 2 * (size_t)most * kMostRows);
+  // no more CTAs than the longest list that the table could hold fills
+  const long long units = (long long)a.B * a.Hkv * a.MT * (std::max(1, ceil_div(a.width * a.page, kUnit<HD>)) + kExtra);
   const int grid = (int)std::min<long long>(ctas, std::max(1ll, units / kMinUnits));
   static PerDevice attr;
-  set_smem_attr(attr, k_paged<T, HD>, kSmem<HD>);
-  launch_cluster(k_paged<T, HD>, dim3(grid), dim3(kThreads), kSmem<HD>, 1, false, s, a);
-  if (grid > 1)
-    launch_cluster(k_join<T, HD>, dim3(grid - 1, std::min(kTile, a.rows * a.G)), dim3(256), 0, 1, true, s, a, grid);
+  set_smem_attr(attr, k_paged<T, HD, TILES>, kSmem<HD, TILES>);
+  launch_cluster(k_paged<T, HD, TILES>, dim3(grid), dim3(kThreads), kSmem<HD, TILES>, 1, false, s, a);
+  if (grid > 1) launch_cluster(k_join<T, HD, TILES>, dim3(grid, std::min(4, a.rows * a.G)), dim3(kJoinThreads), 0, 1, true, s, a);
   return launched("kf_op_paged_attention");
+}
+template <typename T>
+int launch_any(int hd, const Args& a, void* work, cudaStream_t s) {
+  if (hd == 128) return launch<T, 128, 1>(a, work, s);
+  return a.rows * a.G > 16 ? launch<T, 64, 2>(a, work, s) : launch<T, 64, 1>(a, work, s);
 }
 
 }  // namespace
@@ -488,7 +540,7 @@ int launch(Args a, void* work, cudaStream_t s) {
 using namespace kf;
 
 extern "C" int64_t kf_op_paged_attention_work(int32_t hd) {
-  return 2ll * paged_ctas() * kTile * (8 + 4ll * hd);
+  return hd == 64 || hd == 128 ? paged_ctas() * (int64_t)(sizeof(Split) + 2 * (kMostRows * sizeof(float2) + kMostValues * sizeof(float))) : 0;
 }
 
 extern "C" int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd,
@@ -507,12 +559,14 @@ extern "C" int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int3
   if (!aligned(q, 16) || !aligned(pool, 16) || !aligned(out, 16) || !aligned(work, 256) || !aligned(table, 4) || !aligned(lens, 4))
     return refuse(what, "q, pool and out are 16-byte aligned, work 256-byte");
   if (q_seq % 8 || q_row % 8 || q_head % 8) return refuse(what, "q's strides are multiples of 8 elements");
-  const int G = Hq / Hkv, MT = ceil_div(rows * G, kTile);
-  if ((long long)B * Hkv * MT * (std::max(1, ceil_div(width * page, 16))) > (1ll << 40)) return refuse(what, "too many keys");
-  Args a{q, q_seq, q_row, q_head, pool, table, lens, out, nullptr, nullptr, serving_error_word(), n_pages,
-         B, rows, Hq, Hkv, G, MT, page, width, scale * 1.4426950408889634f};
+  const int G = Hq / Hkv;
+  if ((long long)B * Hkv * ceil_div(rows * G, 16) * (width * (long long)page / 16 + kExtra + 1) > (1ll << 40)) return refuse(what, "too many keys");
+  int shift = -1;
+  if ((page & (page - 1)) == 0)
+    for (shift = 0; (1 << shift) < page;) ++shift;
+  const Args a{q, q_seq, q_row, q_head, pool, table, lens, out, nullptr, nullptr, nullptr, serving_error_word(), n_pages,
+               B, rows, Hq, Hkv, G, 0, page, shift, width, scale * 1.4426950408889634f};
   if (!a.err) return refuse(what, "no error word", KF_E_CUDA);
   cudaStream_t s = (cudaStream_t)stream;
-  if (type == KF_TYPE_BF16) return hd == 64 ? launch<__nv_bfloat16, 64>(a, work, s) : launch<__nv_bfloat16, 128>(a, work, s);
-  return hd == 64 ? launch<__half, 64>(a, work, s) : launch<__half, 128>(a, work, s);
+  return type == KF_TYPE_BF16 ? launch_any<__nv_bfloat16>(hd, a, work, s) : launch_any<__half>(hd, a, work, s);
 }
