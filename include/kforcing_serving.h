@@ -7,7 +7,7 @@
  * Device pointers only, caller-owned; work is enqueued on `stream`
  * (cudaStream_t, NULL = legacy default) and nothing is allocated or
  * synchronised, so every call may be captured in a CUDA graph.  A call that
- * needs scratch takes `work`, at least kf_op_*_work(...) bytes, 256-byte
+ * needs scratch takes `work`, at least kf_op_*_work(...) bytes (0: it may be NULL), 256-byte
  * aligned, with any contents; it is free again when the call's work is done,
  * and calls that may overlap on the GPU take different ones.
  *
@@ -83,7 +83,7 @@ int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_t longest, 
  * The same lengths give the same bits, whatever the pages' order.
  * Errors: KF_E_ARG, KF_E_CUDA.
  */
-int64_t kf_op_paged_attention_work(int32_t hd);
+int64_t kf_op_paged_attention_work(int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, int32_t page, int32_t width);
 int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd,
                           const void* q, int64_t q_seq, int64_t q_row, int64_t q_head, const void* pool,
                           int64_t n_pages, int32_t page, const int32_t* table, int32_t width,

@@ -519,32 +519,54 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(const Args a) {
   }
 }
 
-int paged_ctas() { return kMostCtasPerSm * device_sms(); }
+int64_t most_ctas() { return (int64_t)kMostCtasPerSm * device_sms(); }
+
+// Segments of at most kDirect units by the table's width, no more of them than CTAs fit at once: one CTA each, no
+// search, no scratch and no join (3 sequences of 150 tokens, 64 heads over 8 of 64, 8 rows: 14.6 -> 7.5 us)
+struct Shape {
+  int tiles, MT, longest;      // tiles of 16 rows per segment, segments of a (sequence, KV head), units of the widest sequence
+  long long segments;
+  bool direct;
+};
+Shape shape_of(int B, int rows, int G, int Hkv, int hd, int page, int width) {
+  Shape s;
+  s.tiles = hd == 64 && rows * G > 16 ? 2 : 1;
+  s.MT = ceil_div(rows * G, 16 * s.tiles);
+  s.longest = std::max(1, ceil_div(width * page, kUnitBytes / (4 * hd)));
+  s.segments = (long long)B * Hkv * s.MT;
+  s.direct = s.longest <= kDirect && s.segments <= (hd == 64 && s.tiles == 1 ? kCtasPerSm<64, 1> : 2) * device_sms();
+  return s;
+}
 
 template <typename T, int HD, int TILES>
-int launch(Args a, void* work, cudaStream_t s) {
-  const int most = paged_ctas(), ctas = kCtasPerSm<HD, TILES> * device_sms();
-  a.MT = ceil_div(a.rows * a.G, 16 * TILES);
+int launch(Args a, const Shape& sh, void* work, cudaStream_t s) {
+  const int64_t most = most_ctas();
+  a.MT = sh.MT;
+  a.direct = sh.direct;
   a.split = static_cast<Split*>(work);
   a.part_ml = reinterpret_cast<float2*>(a.split + most);
-  a.part_o = reinterpret_cast<float*>(a.part_ml + 2 * (size_t)most * kMostRows);
-  // Segments of at most kDirect units by the table's width, no more of them than CTAs fit at once: one CTA each, no
-  // search and no join (3 sequences of 150 tokens, 64 heads over 8 of 64, 8 rows: 14.6 -> 7.5 us).  Else no more CTAs than
-  // the longest list that the table could hold fills
-  const int longest = std::max(1, ceil_div(a.width * a.page, kUnit<HD>));
-  const long long segments = (long long)a.B * a.Hkv * a.MT;
-  a.direct = longest <= kDirect && segments <= ctas;
-  const int grid = (int)(a.direct ? segments : std::min<long long>(ctas, std::max(1ll, segments * (longest + kExtra) / kMinUnits)));
+  a.part_o = reinterpret_cast<float*>(a.part_ml + 2 * most * kMostRows);
+  // no more CTAs than the longest list that the table could hold fills
+  const int grid = (int)(sh.direct ? sh.segments : std::min<long long>(kCtasPerSm<HD, TILES> * device_sms(),
+                                                                       std::max(1ll, sh.segments * (sh.longest + kExtra) / kMinUnits)));
   static PerDevice attr;
   set_smem_attr(attr, k_paged<T, HD, TILES>, kSmem<HD, TILES>);
   launch_cluster(k_paged<T, HD, TILES>, dim3(grid), dim3(kThreads), kSmem<HD, TILES>, 1, false, s, a);
-  if (!a.direct && grid > 1) launch_cluster(k_join<T, HD, TILES>, dim3(grid, std::min(4, a.rows * a.G)), dim3(kJoinThreads), 0, 1, true, s, a);
+  if (!sh.direct && grid > 1) launch_cluster(k_join<T, HD, TILES>, dim3(grid, std::min(4, a.rows * a.G)), dim3(kJoinThreads), 0, 1, true, s, a);
   return launched("kf_op_paged_attention");
 }
 template <typename T>
-int launch_any(int hd, const Args& a, void* work, cudaStream_t s) {
-  if (hd == 128) return launch<T, 128, 1>(a, work, s);
-  return a.rows * a.G > 16 ? launch<T, 64, 2>(a, work, s) : launch<T, 64, 1>(a, work, s);
+int launch_any(int hd, const Args& a, const Shape& sh, void* work, cudaStream_t s) {
+  if (hd == 128) return launch<T, 128, 1>(a, sh, work, s);
+  return sh.tiles == 2 ? launch<T, 64, 2>(a, sh, work, s) : launch<T, 64, 1>(a, sh, work, s);
+}
+// the arguments' sizes; nullptr if they are fine
+const char* sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int width) {
+  if (hd != 64 && hd != 128) return "head_dim is 64 or 128";
+  if (B < 0 || rows < 1 || Hkv < 1 || Hq < 1 || Hq % Hkv || Hq > 4096 || rows > 4096) return "sequences, rows or heads out of range";
+  if (page < 16 || page % 16 || page > 4096 || width < 0 || (int64_t)width * page > (1 << 30)) return "page is a multiple of 16, width * page at most 2^30";
+  if ((long long)B * Hkv * ceil_div(rows * (Hq / Hkv), 16) * (width * (long long)page / 16 + kExtra + 1) > (1ll << 40)) return "too many keys";
+  return nullptr;
 }
 
 }  // namespace
@@ -552,8 +574,10 @@ int launch_any(int hd, const Args& a, void* work, cudaStream_t s) {
 
 using namespace kf;
 
-extern "C" int64_t kf_op_paged_attention_work(int32_t hd) {
-  return hd == 64 || hd == 128 ? paged_ctas() * (int64_t)(sizeof(Split) + 2 * (kMostRows * sizeof(float2) + kMostValues * sizeof(float))) : 0;
+extern "C" int64_t kf_op_paged_attention_work(int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, int32_t page, int32_t width) {
+  if (B <= 0 || sizes_fault(B, rows, Hq, Hkv, hd, page, width)) return 0;
+  if (shape_of(B, rows, Hq / Hkv, Hkv, hd, page, width).direct) return 0;
+  return most_ctas() * (int64_t)(sizeof(Split) + 2 * (kMostRows * sizeof(float2) + kMostValues * sizeof(float)));
 }
 
 extern "C" int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd,
@@ -562,18 +586,16 @@ extern "C" int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int3
                                      const int32_t* lens, float scale, void* out, void* work, void* stream) {
   const char* what = "kf_op_paged_attention";
   if (type != KF_TYPE_BF16 && type != KF_TYPE_FP16) return refuse(what, "the type is bf16 or fp16");
-  if (hd != 64 && hd != 128) return refuse(what, "head_dim is 64 or 128");
-  if (B < 0 || rows < 1 || Hkv < 1 || Hq < 1 || Hq % Hkv || Hq > 4096 || rows > 4096) return refuse(what, "sequences, rows or heads out of range");
-  if (page < 16 || page % 16 || page > 4096 || width < 0 || (int64_t)width * page > (1 << 30)) return refuse(what, "page is a multiple of 16, width * page at most 2^30");
+  if (const char* f = sizes_fault(B, rows, Hq, Hkv, hd, page, width)) return refuse(what, f);
   if (n_pages < 0 || n_pages > 0x7fffffffll) return refuse(what, "pages out of range");
   if (!(scale > 0.f) || std::isinf(scale)) return refuse(what, "scale is a positive number");
   if (B == 0) return KF_OK;
-  if (!q || !out || !lens || !work || (width && !table) || (n_pages && !pool)) return refuse(what, "a null array");
+  const int G = Hq / Hkv;
+  const Shape sh = shape_of(B, rows, G, Hkv, hd, page, width);
+  if (!q || !out || !lens || (!work && !sh.direct) || (width && !table) || (n_pages && !pool)) return refuse(what, "a null array");
   if (!aligned(q, 16) || !aligned(pool, 16) || !aligned(out, 16) || !aligned(work, 256) || !aligned(table, 4) || !aligned(lens, 4))
     return refuse(what, "q, pool and out are 16-byte aligned, work 256-byte");
   if (q_seq % 8 || q_row % 8 || q_head % 8) return refuse(what, "q's strides are multiples of 8 elements");
-  const int G = Hq / Hkv;
-  if ((long long)B * Hkv * ceil_div(rows * G, 16) * (width * (long long)page / 16 + kExtra + 1) > (1ll << 40)) return refuse(what, "too many keys");
   int shift = -1;
   if ((page & (page - 1)) == 0)
     for (shift = 0; (1 << shift) < page;) ++shift;
@@ -581,5 +603,5 @@ extern "C" int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int3
                B, rows, Hq, Hkv, G, 0, page, shift, width, 0, scale * 1.4426950408889634f};
   if (!a.err) return refuse(what, "no error word", KF_E_CUDA);
   cudaStream_t s = (cudaStream_t)stream;
-  return type == KF_TYPE_BF16 ? launch_any<__nv_bfloat16>(hd, a, work, s) : launch_any<__half>(hd, a, work, s);
+  return type == KF_TYPE_BF16 ? launch_any<__nv_bfloat16>(hd, a, sh, work, s) : launch_any<__half>(hd, a, sh, work, s);
 }

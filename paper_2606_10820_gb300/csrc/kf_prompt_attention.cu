@@ -685,6 +685,7 @@ int launch(const Maps& maps, const Args& a, int grid, cudaStream_t s) {
   return launched("kf_op_prompt_attention");
 }
 int64_t plan_items(int n, int64_t T) { return T / kRows + n; }
+bool without_plan(int n) { return n <= 32 * kDirect; }
 
 }  // namespace
 }  // namespace kf
@@ -692,7 +693,7 @@ int64_t plan_items(int n, int64_t T) { return T / kRows + n; }
 using namespace kf;
 
 extern "C" int64_t kf_op_prompt_attention_work(int32_t n, int64_t T) {
-  return n < 0 || T < 0 ? 0 : 256 + plan_items(n, T) * (int64_t)sizeof(PlanItem);
+  return n < 0 || T < 0 || without_plan(n) ? 0 : 256 + plan_items(n, T) * (int64_t)sizeof(PlanItem);
 }
 
 extern "C" int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_t longest, int32_t Hq, int32_t Hkv, int32_t hd,
@@ -706,7 +707,7 @@ extern "C" int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_
   if (Hkv < 1 || Hq < 1 || Hq % Hkv || Hq > 4096) return refuse(what, "heads out of range");
   if (!(scale > 0.f) || std::isinf(scale)) return refuse(what, "scale is a positive number");
   if (n == 0 || T == 0) return n == 0 && T > 0 ? refuse(what, "tokens of no sequence") : KF_OK;
-  if (!q || !k || !v || !out || !starts || !work) return refuse(what, "a null array");
+  if (!q || !k || !v || !out || !starts || (!work && !without_plan(n))) return refuse(what, "a null array");
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(starts, 4) || !aligned(work, 256))
     return refuse(what, "q, k, v and out are 16-byte aligned, work 256-byte");
   for (const int64_t st : {q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head})
@@ -721,7 +722,7 @@ extern "C" int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_
   if (!err) return refuse(what, "no error word", KF_E_CUDA);
   const int G = Hq / Hkv, pairs = G % 2 == 0, rows = pairs ? kRows : 2 * kRows;
   const int classes = std::max(1, ceil_div(longest, rows));
-  const int direct = n <= 32 * kDirect;
+  const int direct = without_plan(n);
   int* head = static_cast<int*>(work);
   const Plan plan{head, head + 1, reinterpret_cast<PlanItem*>(head + 64)};
   const int grid = (int)std::min<int64_t>(device_sms(), cap * (pairs ? Hq / 2 : Hq));
