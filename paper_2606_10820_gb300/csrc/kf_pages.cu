@@ -5,9 +5,10 @@
 // that a scheduler's calls need no readback and can be captured.  One team of 1024 threads,
 // or of a cluster of 8 x 1024 where the book is large, does a call's whole bookkeeping in one
 // launch: it checks everything first and writes only when all of it can be
-// done.  Free pages are found by counting: each warp counts its stretch of the
-// references by ballots, the counts before it give the rank of its first one, so
-// the i-th lowest free page goes to the i-th request whatever the team's size.
+// done.  Free pages are found by counting: each warp holds its stretch of the
+// references as ballots, the counts before it give the rank of its first one, so
+// the i-th lowest free page goes to the i-th request whatever the team's size.  What
+// bounds a call is its barriers and the loads between them (two or three of each).
 // Page contents are moved by a second, dependent launch over all SMs that
 // reads the list of moves (its bound: HBM, each moved byte read and written once).
 #include <algorithm>
@@ -34,173 +35,205 @@ struct Work {
   int32_t *count, *mark, *off, *src, *dst, *to;
 };
 
+constexpr int kCached = 8;                // ballots of 32 pages that a warp keeps
+
+// What the team's warps tell each other at a barrier; two of them in turn, so that one
+// is not written before everybody has read it
+struct Exchange {
+  int flag[kWarps], a[kWarps], b[kWarps];
+};
 struct Shared {
-  int flag;
-  int warp[2][kWarps];
-  int scan[kWarps];
+  Exchange x[2];
+  int scan[kWarps], total;
 };
 
 template <int C>
 struct Team {
   Shared& sh;
-  int t, lane, warp, rank, id;
+  int t, lane, warp, rank, id, turn;
+  uint32_t live[kCached], none[kCached];   // this warp's pages with references, and without
+  int lo, hi;                              // its stretch
+  bool cached;
   __device__ __forceinline__ explicit Team(Shared& s) : sh(s) {
     t = threadIdx.x;
     lane = t & 31;
     warp = t >> 5;
     rank = C > 1 ? blockIdx.x : 0;
     id = rank * kThreads + t;
-    if (t == 0) sh.flag = 0;
-    sync();
+    turn = 0;
   }
   static constexpr int size = C * kThreads;
   __device__ __forceinline__ void sync() const {
     if constexpr (C > 1) cg::this_cluster().sync();
     else __syncthreads();
   }
+  // before a CTA leaves: the others may still read its shared memory
+  __device__ __forceinline__ void leave() const {
+    if constexpr (C > 1) cg::this_cluster().sync();
+  }
   __device__ __forceinline__ const Shared* of(int c) const {
     if constexpr (C > 1) return cg::this_cluster().map_shared_rank(&sh, c);
     else return &sh;
   }
-  // all threads' bits so far (also orders their memory accesses)
-  __device__ __forceinline__ int any(int bits) const {
-    if (bits) atomicOr(&sh.flag, bits);
-    sync();
-    int all = 0;
-    for (int c = 0; c < C; ++c) all |= of(c)->flag;
-    sync();
-    return all;
+  // the pages' references as ballots (a negative one is in neither)
+  __device__ __forceinline__ void look(const Book& k) {
+    const int per = round_up(ceil_div(k.n_pages, C * kWarps), 32);
+    lo = (int)min((int64_t)k.n_pages, (int64_t)(rank * kWarps + warp) * per);
+    hi = min(k.n_pages, lo + per);
+    cached = per <= 32 * kCached;
+    if (!cached) return;
+    int r[kCached];
+#pragma unroll
+    for (int j = 0; j < kCached; ++j) r[j] = lo + 32 * j + lane < hi ? __ldcg(k.ref + lo + 32 * j + lane) : -1;
+#pragma unroll
+    for (int j = 0; j < kCached; ++j) {
+      live[j] = __ballot_sync(~0u, r[j] > 0);
+      none[j] = __ballot_sync(~0u, r[j] == 0);
+    }
   }
-  // this warp's stretch of the pages
-  __device__ __forceinline__ int per_warp(int n_pages) const { return round_up(ceil_div(n_pages, C * kWarps), 32); }
-  __device__ __forceinline__ int begin(int n_pages) const { return min(n_pages, (rank * kWarps + warp) * per_warp(n_pages)); }
-  // f(id, ballots of a and b) over 32 pages at a time; A and B: predicates of (id, references)
-  template <typename A, typename B, typename F>
-  __device__ __forceinline__ void walk(const Book& k, A a, B b, F f) const {
-    const int lo = begin(k.n_pages), hi = min(k.n_pages, lo + per_warp(k.n_pages));
+  // f(first page, ballot of live ones, of free ones) over the stretch
+  template <typename F>
+  __device__ __forceinline__ void each(const Book& k, F f) const {
+    if (cached) {
+#pragma unroll
+      for (int j = 0; j < kCached; ++j)
+        if (lo + 32 * j < hi) f(lo + 32 * j, live[j], none[j]);
+    } else {
 #pragma unroll 4
-    for (int p = lo; p < hi; p += 32) {
-      const int i = p + lane;
-      const bool in = i < hi;
-      const int r = in ? __ldcg(k.ref + i) : -1;
-      f(i, __ballot_sync(~0u, in && a(i, r)), __ballot_sync(~0u, in && b(i, r)));
-    }
-  }
-  // the counts of a and b before this warp's stretch, and all of them
-  template <typename A, typename B>
-  __device__ __forceinline__ void count(const Book& k, A a, B b, int2* before, int2* all) const {
-    int na = 0, nb = 0;
-    walk(k, a, b, [&](int, uint32_t x, uint32_t y) {
-      na += __popc(x);
-      nb += __popc(y);
-    });
-    if (lane == 0) {
-      sh.warp[0][warp] = na;
-      sh.warp[1][warp] = nb;
-    }
-    sync();
-    int2 pre = make_int2(0, 0), tot = make_int2(0, 0);
-    for (int c = 0; c < C; ++c) {
-      const Shared* s = of(c);
-      const int x = s->warp[0][lane], y = s->warp[1][lane];
-      tot.x += x;
-      tot.y += y;
-      if (c < rank || (c == rank && lane < warp)) {
-        pre.x += x;
-        pre.y += y;
+      for (int p = lo; p < hi; p += 32) {
+        const int r = p + lane < hi ? __ldcg(k.ref + p + lane) : -1;
+        f(p, __ballot_sync(~0u, r > 0), __ballot_sync(~0u, r == 0));
       }
     }
+  }
+  // A barrier of the team that also orders its memory accesses: all threads' bits; of the warps'
+  // counts a and b those before this warp and all of them
+  __device__ __forceinline__ int exchange(int bits, int a, int b, int2* before, int2* all) {
+    Exchange& x = sh.x[turn];
+    bits = __reduce_or_sync(~0u, bits);
+    if (lane == 0) {
+      x.flag[warp] = bits;
+      x.a[warp] = a;
+      x.b[warp] = b;
+    }
+    sync();
+    int flag = 0;
+    int2 pre = make_int2(0, 0), tot = make_int2(0, 0);
+    for (int c = 0; c < C; ++c) {
+      const Exchange& y = of(c)->x[turn];
+      const int ya = y.a[lane], yb = y.b[lane];
+      flag |= y.flag[lane];
+      tot.x += ya;
+      tot.y += yb;
+      if (c < rank || (c == rank && lane < warp)) {
+        pre.x += ya;
+        pre.y += yb;
+      }
+    }
+    turn ^= 1;
     before->x = __reduce_add_sync(~0u, pre.x);
     before->y = __reduce_add_sync(~0u, pre.y);
     all->x = __reduce_add_sync(~0u, tot.x);
     all->y = __reduce_add_sync(~0u, tot.y);
-    sync();
+    return __reduce_or_sync(~0u, flag);
   }
-  // the n lowest free pages to list; false if there are fewer
-  __device__ bool free_pages(const Book& k, int n, int32_t* list) const {
-    auto is_free = [](int, int r) { return r == 0; };
-    auto no = [](int, int) { return false; };
-    int2 at, all;
-    count(k, is_free, no, &at, &all);
-    if (all.x < n) return false;
-    int base = at.x;
-    walk(k, is_free, no, [&](int i, uint32_t x, uint32_t) {
-      const int rk = base + __popc(x & ((1u << lane) - 1));
-      if (((x >> lane) & 1u) && rk < n) list[rk] = i;
-      base += __popc(x);
+  __device__ __forceinline__ int exchange(int bits) {
+    int2 x, y;
+    return exchange(bits, 0, 0, &x, &y);
+  }
+  __device__ __forceinline__ int count_free(const Book& k) const {
+    int n = 0;
+    each(k, [&](int, uint32_t, uint32_t z) { n += __popc(z); });
+    return n;
+  }
+  // the n lowest free pages to list (there are as many); base: the free ones before this warp's
+  __device__ __forceinline__ void list_free(const Book& k, int n, int base, int32_t* list) const {
+    each(k, [&](int p, uint32_t, uint32_t z) {
+      const int rk = base + __popc(z & ((1u << lane) - 1));
+      if (((z >> lane) & 1u) && rk < n) list[rk] = p + lane;
+      base += __popc(z);
     });
-    return true;
   }
-  // off[i] = sum of f(0 .. i-1) for i < n, by the first CTA; the sum (to every thread)
+  // off[i] = sum of f(0 .. i-1) for i < n and sh.total all of them, by the first CTA (ordered by the next exchange)
   template <typename F>
-  __device__ int offsets(int n, int32_t* off, int32_t* total, F f) const {
-    if (rank == 0) {
-      int run = 0;
-      for (int i0 = 0; i0 < n; i0 += kThreads) {
-        const int i = i0 + t, v = i < n ? f(i) : 0;
-        int incl = v;
+  __device__ __forceinline__ void offsets(int n, int32_t* off, F f) const {
+    if (rank != 0) return;
+    int run = 0;
+    for (int i0 = 0; i0 < n; i0 += kThreads) {
+      const int i = i0 + t, v = i < n ? f(i) : 0;
+      int incl = v;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int u = __shfl_up_sync(~0u, incl, o);
-          if (lane >= o) incl += u;
-        }
-        if (lane == 31) sh.scan[warp] = incl;
-        __syncthreads();
-        const int w = sh.scan[lane];
-        const int before = __reduce_add_sync(~0u, lane < warp ? w : 0), all = __reduce_add_sync(~0u, w);
-        if (i < n) off[i] = run + before + incl - v;
-        run += all;
-        __syncthreads();
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(~0u, incl, o);
+        if (lane >= o) incl += u;
       }
-      if (t == 0) *total = run;
+      if (lane == 31) sh.scan[warp] = incl;
+      __syncthreads();
+      const int w = sh.scan[lane];
+      const int before = __reduce_add_sync(~0u, lane < warp ? w : 0), all = __reduce_add_sync(~0u, w);
+      if (i < n) off[i] = run + before + incl - v;
+      run += all;
+      __syncthreads();
     }
-    sync();
-    return __ldcg(total);
+    if (t == 0) sh.total = run;
   }
 };
 
 __device__ __forceinline__ int pages_of(int len, int page) { return (len + page - 1) / page; }
-
-// which[i] in range and listed once (mark needs no clearing: a slot listed twice holds
-// the stamp of one of the two)
+// Slot which[i] in range, and stamped with i.  (A slot listed twice holds the stamp of one of the two, so
+// after a barrier the other's check fails; the stamps need no clearing)
 template <int C>
-__device__ int check_slots(const Team<C>& team, const Book& k, const int32_t* which, int n, int32_t* mark) {
+__device__ __forceinline__ int stamp(const Team<C>& team, const Book& k, const int32_t* which, int n, int32_t* mark) {
   int bad = 0;
   for (int i = team.id; i < n; i += team.size) {
     const int s = which[i];
-    if (s < 0 || s >= k.slots) bad |= KF_DEV_BAD_ROW;
+    if (s < 0 || s >= k.slots) bad = KF_DEV_BAD_ROW;
     else mark[s] = i;
   }
-  bad = team.any(bad);
-  if (bad) return bad;
+  return bad;
+}
+template <int C>
+__device__ __forceinline__ int twice(const Team<C>& team, const int32_t* which, int n, const int32_t* mark) {
+  int bad = 0;
   for (int i = team.id; i < n; i += team.size)
-    if (__ldcg(mark + which[i]) != i) bad |= KF_DEV_BAD_ROW;
-  return team.any(bad);
+    if (__ldcg(mark + which[i]) != i) bad = KF_DEV_BAD_ROW;
+  return bad;
 }
 template <int C>
 __device__ __forceinline__ bool refused(const Team<C>& team, int bad, int* err) {
-  if (bad && team.id == 0) atomicOr(err, bad);
-  return bad != 0;
+  if (!bad) return false;
+  if (bad & KF_DEV_BAD_ROW) bad = KF_DEV_BAD_ROW;      // (what a bad list makes of the pages is no fault of theirs)
+  if (team.id == 0) atomicOr(err, bad);
+  team.leave();
+  return true;
 }
 
 template <int C>
-__global__ void __launch_bounds__(kThreads) k_grow(const Book k, int n, const int32_t* which, const int32_t* new_lens, const Work w, int* err) {
+__global__ void __launch_bounds__(kThreads, 1) k_grow(const Book k, int n, const int32_t* which, const int32_t* new_lens, const Work w, int* err) {
   __shared__ Shared sh;
-  const Team<C> team(sh);
-  int bad = check_slots(team, k, which, n, w.mark);
+  Team<C> team(sh);
+  team.look(k);
+  int bad = stamp(team, k, which, n, w.mark);
+  // new pages of request i (0 for a bad one)
+  auto more = [&](int i) {
+    const int s = which[i], now = new_lens[i];
+    if (s < 0 || s >= k.slots) return 0;
+    const int was = k.lens[s];
+    if (was < 0 || now < was || now > (int64_t)k.width * k.page) {
+      bad |= KF_DEV_BAD_ROW;
+      return 0;
+    }
+    return pages_of(now, k.page) - pages_of(was, k.page);
+  };
+  team.offsets(n, w.off, more);
+  int2 before, all;
+  bad = team.exchange(bad, team.count_free(k), 0, &before, &all);
+  const int total = team.of(0)->total;
+  if (!bad && total > all.x) bad = KF_DEV_NO_PAGES;
   if (refused(team, bad, err)) return;
-  for (int i = team.id; i < n; i += team.size) {
-    const int was = k.lens[which[i]], now = new_lens[i];
-    if (was < 0 || now < was || now > (int64_t)k.width * k.page) bad |= KF_DEV_BAD_ROW;
-  }
-  bad = team.any(bad);
+  team.list_free(k, total, before.x, w.src);
+  bad = team.exchange(twice(team, which, n, w.mark));
   if (refused(team, bad, err)) return;
-  const int total = team.offsets(n, w.off, w.count, [&](int i) { return pages_of(new_lens[i], k.page) - pages_of(k.lens[which[i]], k.page); });
-  if (!team.free_pages(k, total, w.src)) {
-    refused(team, KF_DEV_NO_PAGES, err);
-    return;
-  }
-  team.sync();
   // a warp per request
   for (int i = team.id >> 5; i < n; i += team.size >> 5) {
     const int s = which[i], have = pages_of(k.lens[s], k.page), need = pages_of(new_lens[i], k.page), off = __ldcg(w.off + i);
@@ -212,49 +245,57 @@ __global__ void __launch_bounds__(kThreads) k_grow(const Book k, int n, const in
     }
     if (team.lane == 0) k.lens[s] = new_lens[i];
   }
+  team.leave();
 }
 
 template <int C>
-__global__ void __launch_bounds__(kThreads) k_free(const Book k, int n, const int32_t* which, const Work w, int* err) {
+__global__ void __launch_bounds__(kThreads, 1) k_free(const Book k, int n, const int32_t* which, const Work w, int* err) {
   __shared__ Shared sh;
-  const Team<C> team(sh);
-  int bad = check_slots(team, k, which, n, w.mark);
+  Team<C> team(sh);
+  int bad = team.exchange(stamp(team, k, which, n, w.mark));
   if (refused(team, bad, err)) return;
   const uint32_t all = (uint32_t)n * k.width, width = k.width;
+  bad = twice(team, which, n, w.mark);
   for (uint32_t e = team.id; e < all; e += team.size) {
     const int p = k.table[(int64_t)which[e / width] * k.width + e % width];
     if (p == -1) continue;
     if (p < 0 || p >= k.n_pages || atomicSub(k.ref + p, 1) <= 0) bad |= KF_DEV_BAD_PAGE;
   }
-  bad = team.any(bad);
-  for (uint32_t e = team.id; e < all; e += team.size) {
-    int32_t* at = k.table + (int64_t)which[e / width] * k.width + e % width;
-    const int p = *at;
-    if (!bad) *at = -1;
-    else if (p >= 0 && p < k.n_pages) atomicAdd(k.ref + p, 1);      // as it was
-  }
+  bad = team.exchange(bad);
+  if (bad)
+    // the references as they were
+    for (uint32_t e = team.id; e < all; e += team.size) {
+      const int p = k.table[(int64_t)which[e / width] * k.width + e % width];
+      if (p >= 0 && p < k.n_pages) atomicAdd(k.ref + p, 1);
+    }
   if (refused(team, bad, err)) return;
+  for (uint32_t e = team.id; e < all; e += team.size) k.table[(int64_t)which[e / width] * k.width + e % width] = -1;
   for (int i = team.id; i < n; i += team.size) k.lens[which[i]] = 0;
+  team.leave();
 }
 
 template <int C>
-__global__ void __launch_bounds__(kThreads) k_fork(const Book k, int n, const int32_t* src, const int32_t* dst, const Work w, int* err) {
+__global__ void __launch_bounds__(kThreads, 1) k_fork(const Book k, int n, const int32_t* src, const int32_t* dst, const Work w, int* err) {
   __shared__ Shared sh;
-  const Team<C> team(sh);
+  Team<C> team(sh);
   if (team.id == 0) *w.count = 0;            // (a refused call copies nothing)
-  int bad = check_slots(team, k, dst, n, w.mark);
-  if (refused(team, bad, err)) return;
+  team.look(k);
+  int bad = stamp(team, k, dst, n, w.mark);
   for (int i = team.id; i < n; i += team.size) {
-    const int s = src[i];
-    if (s < 0 || s >= k.slots) {
-      bad |= KF_DEV_BAD_ROW;
-      continue;
-    }
-    const int m = __ldcg(w.mark + s), len = k.lens[s];
-    if ((m >= 0 && m < n && dst[m] == s) || len < 0 || len > (int64_t)k.width * k.page || k.lens[dst[i]] != 0) bad |= KF_DEV_BAD_ROW;
+    const int s = src[i], d = dst[i];
+    if (s < 0 || s >= k.slots || k.lens[s] < 0 || k.lens[s] > (int64_t)k.width * k.page) bad |= KF_DEV_BAD_ROW;
+    if (d >= 0 && d < k.slots && k.lens[d] != 0) bad |= KF_DEV_BAD_ROW;
   }
-  bad = team.any(bad);
+  team.offsets(n, w.off, [&](int i) { return src[i] >= 0 && src[i] < k.slots && k.lens[src[i]] % k.page != 0 ? 1 : 0; });
+  int2 before, free;
+  bad = team.exchange(bad, team.count_free(k), 0, &before, &free);
   if (refused(team, bad, err)) return;
+  const int total = team.of(0)->total;
+  bad = twice(team, dst, n, w.mark);
+  for (int i = team.id; i < n; i += team.size) {
+    const int s = src[i], m = __ldcg(w.mark + s);
+    if (m >= 0 && m < n && dst[m] == s) bad |= KF_DEV_BAD_ROW;      // a source that is a destination
+  }
   const uint32_t all = (uint32_t)n * k.width, width = k.width;
   for (uint32_t e = team.id; e < all; e += team.size) {
     const int i = (int)(e / width), c = (int)(e % width);
@@ -263,14 +304,10 @@ __global__ void __launch_bounds__(kThreads) k_fork(const Book k, int n, const in
     const int p = k.table[(int64_t)src[i] * k.width + c];
     if (p < 0 || p >= k.n_pages || __ldcg(k.ref + p) <= 0) bad |= KF_DEV_BAD_PAGE;
   }
-  bad = team.any(bad);
+  team.list_free(k, min(total, free.x), before.x, w.dst);
+  bad = team.exchange(bad);
+  if (!bad && total > free.x) bad = KF_DEV_NO_PAGES;
   if (refused(team, bad, err)) return;
-  const int total = team.offsets(n, w.off, w.to, [&](int i) { return k.lens[src[i]] % k.page != 0; });
-  if (!team.free_pages(k, total, w.dst)) {
-    refused(team, KF_DEV_NO_PAGES, err);
-    return;
-  }
-  team.sync();
   for (uint32_t e = team.id; e < all; e += team.size) {
     const int i = (int)(e / width), c = (int)(e % width), len = k.lens[src[i]], full = len / k.page;
     int p = -1;
@@ -283,54 +320,63 @@ __global__ void __launch_bounds__(kThreads) k_fork(const Book k, int n, const in
       p = __ldcg(w.dst + off);
       k.ref[p] = 1;
     }
-    k.table[(int64_t)dst[i] * k.width + c] = p;
+    if (p != -1) k.table[(int64_t)dst[i] * k.width + c] = p;
     if (c == 0) k.lens[dst[i]] = len;
   }
-  if (k.width == 0)
-    for (int i = team.id; i < n; i += team.size) k.lens[dst[i]] = 0;
   if (team.id == 0) *w.count = total;
+  team.leave();
 }
 
 template <int C>
-__global__ void __launch_bounds__(kThreads) k_compact(const Book k, const Work w, int32_t* live, int* err) {
+__global__ void __launch_bounds__(kThreads, 1) k_compact(const Book k, const Work w, int32_t* live, int* err) {
   __shared__ Shared sh;
-  const Team<C> team(sh);
+  Team<C> team(sh);
   if (team.id == 0) *w.count = 0;
-  auto is_live = [](int, int r) { return r > 0; };
-  auto is_bad = [](int, int r) { return r < 0; };
-  int2 at, all;
-  team.count(k, is_live, is_bad, &at, &all);
-  const int L = all.x;
-  int bad = all.y ? KF_DEV_BAD_PAGE : 0;
+  team.look(k);
+  int bad = 0, n = 0;
+  team.each(k, [&](int p, uint32_t x, uint32_t z) {
+    n += __popc(x);
+    const uint32_t in = p + 32 <= team.hi ? ~0u : (1u << (team.hi - p)) - 1;
+    if ((x | z) != in) bad |= KF_DEV_BAD_PAGE;             // a negative reference count
+  });
   const uint32_t entries = (uint32_t)k.slots * k.width;
   for (uint32_t e = team.id; e < entries; e += team.size) {
     const int p = k.table[e];
     if (p != -1 && (p < 0 || p >= k.n_pages || __ldcg(k.ref + p) <= 0)) bad |= KF_DEV_BAD_PAGE;
   }
-  bad = team.any(bad);
+  int2 before, all;
+  bad = team.exchange(bad, n, 0, &before, &all);
   if (refused(team, bad, err)) return;
-  auto high = [L](int i, int r) { return r > 0 && i >= L; };
-  auto hole = [L](int i, int r) { return r == 0 && i < L; };
-  team.count(k, high, hole, &at, &all);
-  team.walk(k, high, hole, [&](int i, uint32_t x, uint32_t y) {
-    const uint32_t below = (1u << team.lane) - 1;
-    if ((x >> team.lane) & 1u) w.src[at.x + __popc(x & below)] = i;
-    if ((y >> team.lane) & 1u) w.dst[at.y + __popc(y & below)] = i;
-    at.x += __popc(x);
-    at.y += __popc(y);
+  const int L = all.x;
+  // the live pages at or above L, and as many free ones below
+  auto high = [&](int p, uint32_t x) { return p >= L ? x : p + 32 <= L ? 0u : x & ~((1u << (L - p)) - 1); };
+  auto hole = [&](int p, uint32_t z) { return p >= L ? 0u : p + 32 <= L ? z : z & ((1u << (L - p)) - 1); };
+  int nh = 0, nz = 0;
+  team.each(k, [&](int p, uint32_t x, uint32_t z) {
+    nh += __popc(high(p, x));
+    nz += __popc(hole(p, z));
+  });
+  team.exchange(0, nh, nz, &before, &all);
+  team.each(k, [&](int p, uint32_t x, uint32_t z) {
+    const uint32_t h = high(p, x), o = hole(p, z), below = (1u << team.lane) - 1;
+    if ((h >> team.lane) & 1u) {
+      const int rk = before.x + __popc(h & below);
+      w.src[rk] = p + team.lane;
+      w.to[p + team.lane] = rk;
+    }
+    if ((o >> team.lane) & 1u) w.dst[before.y + __popc(o & below)] = p + team.lane;
+    before.x += __popc(h);
+    before.y += __popc(o);
   });
   team.sync();
-  // (as many live pages above as holes below)
   for (int i = team.id; i < all.x; i += team.size) {
     const int s = __ldcg(w.src + i), d = __ldcg(w.dst + i);
     k.ref[d] = __ldcg(k.ref + s);
     k.ref[s] = 0;
-    w.to[s] = d;
   }
-  team.sync();
   for (uint32_t e = team.id; e < entries; e += team.size) {
     const int p = k.table[e];
-    if (p >= L) k.table[e] = __ldcg(w.to + p);
+    if (p >= L) k.table[e] = __ldcg(w.dst + __ldcg(w.to + p));
   }
   if (team.id == 0) {
     *w.count = all.x;
