@@ -67,7 +67,7 @@ struct Args {
   int64_t out_row, out_head;
   Plan plan;
   int* err;
-  int Hq, G, pairs;                                 // pairs: two heads per item (else two tiles of rows)
+  int Hq, G, heads, tiles;                          // of an item: heads x tiles of 128 rows (2 x 1, 1 x 2 or 1 x 1)
   int direct, n, T, longest;                        // direct: the items are found from starts, without a plan
   const int32_t* starts;
   float scale2;
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
     if (warp == 0) {
       // -------------------------------------------------------------- copies
-      const int heads = a.pairs ? a.Hq / 2 : a.Hq, per = a.pairs ? 1 : 2;
+      const int heads = a.Hq / a.heads, per = a.tiles;
       int first[kDirect], len[kDirect], tiles[kDirect], total = 0, most = 0;
       if (a.direct) {
         bool bad = false;
@@ -371,10 +371,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
         const int hu = w % heads;
   #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          im.head[i] = a.pairs ? 2 * hu + i : hu;
-          const int rt = e.z * per + (a.pairs ? 0 : i);
+          im.head[i] = a.heads * hu + (a.heads == 2 ? i : 0);
+          const int rt = e.z * per + (a.heads == 2 ? 0 : i);
           im.row[i] = rt * kRows;
-          im.n[i] = w < items && im.row[i] < im.len ? rt + 1 : 0;
+          im.n[i] = w < items && i < a.heads * a.tiles && im.row[i] < im.len ? rt + 1 : 0;
         }
         const int slot = it & 1;
         ok = wait(&b.item_empty[slot], ((it >> 1) & 1) ^ 1);
@@ -720,17 +720,28 @@ extern "C" int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_
     return refuse(what, "a tensor map is refused (strides)");
   int* err = serving_error_word();
   if (!err) return refuse(what, "no error word", KF_E_CUDA);
-  const int G = Hq / Hkv, pairs = G % 2 == 0, rows = pairs ? kRows : 2 * kRows;
+  const int G = Hq / Hkv;
+  // One sub-tile an item where that ends sooner: a key tile then takes kAlone clocks, in pairs kPaired for both, and
+  // an item kItem more.  Where few long items leave SMs idle the longest item's chain is what a call takes (one of 4096, 8
+  // heads of 64: 41.4 us alone, 51.1 in pairs; one of 7074: 109.6 and 82.9).  (Lengths are on the device: the
+  // estimate takes equal ones, and `longest` for the chain.)
+  const double kAlone = hd == 64 ? 2050 : 2800, kPaired = hd == 64 ? 2600 : 2860, kItem = 2500;
+  const double tiles = std::max<double>(1, (double)T / n / kRows), chain = std::max<double>(1, (double)longest / kRows);
+  const double items = n * (double)Hq * tiles / device_sms();      // sub-tiles of an SM
+  const double alone_clocks = std::max(chain * kAlone, items * ((tiles + 1) / 2 * kAlone + kItem));
+  const double paired_clocks = std::max(chain * kPaired, items / 2 * ((tiles + 1) / 2 * kPaired + kItem));
+  const bool alone = alone_clocks < paired_clocks;
+  const int heads = !alone && G % 2 == 0 ? 2 : 1, rows = alone || heads == 2 ? kRows : 2 * kRows;
   const int classes = std::max(1, ceil_div(longest, rows));
   const int direct = without_plan(n);
   int* head = static_cast<int*>(work);
   const Plan plan{head, head + 1, reinterpret_cast<PlanItem*>(head + 64)};
-  const int grid = (int)std::min<int64_t>(device_sms(), cap * (pairs ? Hq / 2 : Hq));
+  const int grid = (int)std::min<int64_t>(device_sms(), cap * (Hq / heads));
   cudaStream_t s = (cudaStream_t)stream;
   if (!direct) launch_cluster(k_plan, dim3(1), dim3(kPlanThreads), 2 * (classes + 2) * sizeof(int), 1, false, s, n, (int)T, longest, rows, classes,
                  starts, plan, grid, err);
   if (const int rc = launched(what)) return rc;
-  const Args a{out, out_row, out_head, plan, err, Hq, G, pairs, direct, n, (int)T, longest, starts, scale * 1.4426950408889634f};
+  const Args a{out, out_row, out_head, plan, err, Hq, G, heads, rows / kRows, direct, n, (int)T, longest, starts, scale * 1.4426950408889634f};
   if (type == KF_TYPE_BF16) return hd == 64 ? launch<__nv_bfloat16, 64>(maps, a, grid, s) : launch<__nv_bfloat16, 128>(maps, a, grid, s);
   return hd == 64 ? launch<__half, 64>(maps, a, grid, s) : launch<__half, 128>(maps, a, grid, s);
 }
