@@ -39,13 +39,14 @@ namespace kf {
 namespace {
 
 constexpr int kBatch = 4;          // vectors of a batch
-constexpr int kRing = 3;           // scores: batches under way or in use
+// scores: batches under way or in use (two for the narrow rows' CTAs, so that sixteen of them fit an SM)
+template <int THREADS> constexpr int kRing = THREADS == 64 ? 2 : 3;
 constexpr int kResident = 4;       // gradient: batches of a row, at most
 constexpr int kPairBytes = 13 * 512 * 16;    // gradient: slots of a CTA that leave room for a second one on the SM
 constexpr int kGroups = 64;        // groups whose maxima bound the n-th largest logit
 constexpr int kMaxTop = kGroups;
-constexpr int kList = 768;         // listed candidates of a row
-constexpr int kRanked = 256;       // up to so many are ranked against each other, more are chosen in rounds
+template <int THREADS> constexpr int kList = THREADS == 64 ? 256 : 768;      // listed candidates of a row
+constexpr int kRanked = 192;       // up to so many are ranked against each other, more are chosen in rounds
 constexpr int kMostRow = 8 * kResident * kBatch * 512 * 16;      // bytes of a row: the gradient's slots in eight CTAs
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -300.f;   // 2^-300 is 0 in fp32: stands for -inf where it multiplies that 0
@@ -204,7 +205,7 @@ struct Shared {
   int count, again;
   uint16_t thread[THREADS];        // threads whose vectors are looked at again
   Cand first[THREADS / 32];
-  Cand list[kList];
+  Cand list[kList<THREADS>];
 };
 
 // A row's numbers, the same in all of its threads
@@ -341,7 +342,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
   const int64_t step = gridDim.x / CS;
   const uint32_t slot0 = mma::smem_addr(slots + t);
 
-  // the copies run kRing - 1 batches ahead, into the rows that follow
+  // the copies run kRing<THREADS> - 1 batches ahead, into the rows that follow
   int64_t fr = blockIdx.x / CS;
   int fb = 0, fslot = 0, fn = 0;
   const T* fp = nullptr;
@@ -363,13 +364,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
         fr += step;
         look();
       }
-      fslot = fslot + 1 == kRing ? 0 : fslot + 1;
+      fslot = fslot + 1 == kRing<THREADS> ? 0 : fslot + 1;
     }
     mma::cp_commit();
   };
   look();
 #pragma unroll
-  for (int i = 0; i < kRing - 1; ++i) fill();
+  for (int i = 0; i < kRing<THREADS> - 1; ++i) fill();
   int slot = 0;
 #pragma unroll 1
   for (int64_t r = blockIdx.x / CS; r < a.R; r += step) {
@@ -379,7 +380,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
     Pass ps;
 #pragma unroll 1
     for (int b = 0; b < batches; ++b) {
-      mma::cp_wait<kRing - 2>();          // this batch has landed
+      mma::cp_wait<kRing<THREADS> - 2>();          // this batch has landed
       fill();                             // into the slots of the batch before
       const uint4* s = slots + slot * kBatch * THREADS + t;
       if ((b + 1) * kBatch <= n) {
@@ -394,7 +395,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
           ps.add<N>(a, v);
         }
       }
-      slot = slot + 1 == kRing ? 0 : slot + 1;
+      slot = slot + 1 == kRing<THREADS> ? 0 : slot + 1;
     }
     const float vec_max = ps.most;
     if (ex.edge) ps.add_one(a, ex.edge_logit);
@@ -447,22 +448,32 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
       const float x = v * a.inv_tau;
       if (listed(x)) {
         const int at = atomicAdd(&lead->count, 1);
-        if (at < kList) lead->list[at] = Cand{x, id};
+        if (at < kList<THREADS>) lead->list[at] = Cand{x, id};
       }
     };
     if (listed(vec_max * a.inv_tau)) sh.thread[atomicAdd(&sh.again, 1)] = (uint16_t)t;
     if (ex.edge) list(ex.edge_id, ex.edge_logit);
     __syncthreads();
-    for (int j = warp; j < sh.again; j += WARPS)
-      for (int k = lane; k < mine.per_cta; k += 32) {
-        const int i = mine.first - t + sh.thread[j] + k * THREADS;
-        if (i >= row.nvec) break;
-        float v[N];
-        Vec16<T>::unpack(*reinterpret_cast<const uint4*>(row.vec(i)), v);
-        const int id0 = row.head + i * N;
+    auto list_vector = [&](int i) {
+      float v[N];
+      Vec16<T>::unpack(*reinterpret_cast<const uint4*>(row.vec(i)), v);
+      const int id0 = row.head + i * N;
 #pragma unroll
-        for (int e = 0; e < N; ++e) list(id0 + e, v[e]);
-      }
+      for (int e = 0; e < N; ++e) list(id0 + e, v[e]);
+    };
+    // a warp per such thread; each by itself where a narrow row has many of them for its two warps (4096 x
+    // 1770, 20 alternatives: 24.6 -> 20.9 us; with 8 warps and 50257 it loses, 115 -> 167)
+    if (THREADS > 64 || sh.again <= 4 * WARPS) {
+      for (int j = warp; j < sh.again; j += WARPS)
+        for (int k = lane; k < mine.per_cta; k += 32) {
+          const int i = mine.first - t + sh.thread[j] + k * THREADS;
+          if (i >= row.nvec) break;
+          list_vector(i);
+        }
+    } else if (listed(vec_max * a.inv_tau)) {
+#pragma unroll 4
+      for (int k = 0; k < n; ++k) list_vector(mine.first + k * THREADS);
+    }
     if constexpr (CS > 1) cg::this_cluster().sync();
     else __syncthreads();
     if (rank != 0) continue;
@@ -487,7 +498,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
         auto look_at = [&](Cand d) {
           if (before(last, d) && before(d, c)) c = d;
         };
-        if (found <= kList) {
+        if (found <= kList<THREADS>) {
           for (int j = t; j < found; j += THREADS) look_at(sh.list[j]);
         } else {
           for (int id = t; id < a.V; id += THREADS) {
@@ -631,7 +642,7 @@ void launch_rows(K* kernel, PerDevice& attr, const Args& a, size_t bytes, cudaSt
 template <typename T, int THREADS, int CS>
 void launch_scores(const Args& a, cudaStream_t s) {
   static PerDevice attr;
-  launch_rows<THREADS, CS>(k_scores<T, THREADS, CS>, attr, a, (size_t)kRing * kBatch * THREADS * 16, s);
+  launch_rows<THREADS, CS>(k_scores<T, THREADS, CS>, attr, a, (size_t)kRing<THREADS> * kBatch * THREADS * 16, s);
 }
 template <typename T, int THREADS, int CS>
 void launch_grad(const Args& a, cudaStream_t s) {
@@ -641,7 +652,7 @@ void launch_grad(const Args& a, cudaStream_t s) {
 }
 template <typename T, bool GRAD>
 int launch(const Args& a, cudaStream_t s) {
-  // A row of up to 12 KB: two warps, so that an SM has ten such rows and more.  A wider one is split over a
+  // A row of up to 12 KB: two warps, so that an SM has sixteen such rows (ten for the gradient).  A wider one is split over a
   // cluster while few rows leave SMs idle and each thread keeps two vectors; the gradient's also
   // until it fits the slots
   const int64_t bytes = (int64_t)a.V * sizeof(T), sms = device_sms();
