@@ -77,7 +77,8 @@ int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_t longest, 
  * pool: one layer's pages [n_pages][2: K, V][Hkv][page][hd], contiguous, page a
  * multiple of 16; table: int32 [B][width] page ids; lens: int32 [B], 0 ..
  * width * page.  Scores, maxima, sums and the accumulation are fp32.
- * KV beyond a sequence's length is never used, whatever it holds.
+ * KV beyond a sequence's length is never used, whatever it holds; a NaN or infinity in
+ * the V of the newest rows reaches all of that sequence's rows.
  * A page id outside the pool: KF_DEV_BAD_PAGE, its keys count as unseen.
  * A length outside 0 .. width * page: KF_DEV_BAD_ROW, clamped.
  * The same lengths give the same bits, whatever the pages' order.

@@ -599,6 +599,7 @@ extern "C" int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int3
   int shift = -1;
   if ((page & (page - 1)) == 0)
     for (shift = 0; (1 << shift) < page;) ++shift;
+  if (!n_pages) pool = q;      // (nothing of it is read)
   const Args a{q, q_seq, q_row, q_head, pool, table, lens, out, nullptr, nullptr, nullptr, serving_error_word(), n_pages,
                B, rows, Hq, Hkv, G, 0, page, shift, width, 0, scale * 1.4426950408889634f};
   if (!a.err) return refuse(what, "no error word", KF_E_CUDA);

@@ -203,6 +203,17 @@ def test_copy_past_32_bits(sv):
     assert (pool[0, 4] == 7).all() and (pool[1, 4] == 8).all() and (pool[:, 3] == 0).all() and (pool[:, 5] == 0).all()
 
 
+def test_append_past_32_bits(sv):
+    """Pages past 2^32 bytes of a layer."""
+    pool = torch.zeros(5000, 2, 8, 64, 1024, device="cuda", dtype=torch.float16)      # 10.5 GB
+    table = i32([[4999, 2], [4998, 7]])
+    k, v = (torch.randn(130, 8, 1024, device="cuda").half() for _ in range(2))
+    sv.pages_append(pool, k, v, i32([0, 70, 130]), table, i32([70, 60]), i32([0, 1]))
+    sv.status()
+    assert torch.equal(pool[4999, 0].transpose(0, 1), k[:64]) and torch.equal(pool[2, 1, :, :6].transpose(0, 1), v[64:70])
+    assert torch.equal(pool[4998, 1, :, :60].transpose(0, 1), v[70:]) and (pool[7] == 0).all() and (pool[2, :, :, 6:] == 0).all()
+
+
 def test_refused_calls_change_nothing(sv):
     """What the device finds wrong with a call leaves the book and the pool as they were."""
     n_pages, slots, width = 20, 6, 4

@@ -117,6 +117,19 @@ def test_strides(sv):
     assert torch.equal(wide[:, 2:6], want) and (wide[:, :2] == 3).all() and (wide[:, 6:] == 3).all()
 
 
+def test_far_rows(sv):
+    """Token strides that pass 2^31 elements within the call."""
+    T, stride = 2500, 1 << 20
+    buf = torch.zeros(T * stride, device="cuda", dtype=torch.bfloat16)           # 5.2 GB
+    wide = buf.view(T, stride // 64, 64)
+    q, k, v, starts = make([700, 1800], 4, 2, 64, seed=11)
+    parts = [wide[:, 0:4], wide[:, 4:6], wide[:, 6:8], wide[:, 100:104]]
+    for x, y in zip(parts, (q, k, v)):
+        x.copy_(y)
+    sv.prompt_attention(*parts[:3], starts, 1800, out=parts[3])
+    assert torch.equal(parts[3], sv.prompt_attention(q, k, v, starts, 1800))
+
+
 def test_what_is_not_a_number_stays_in_its_sequence(sv):
     """NaN and infinity in K, V and Q of a neighbour, and past the end of the tokens."""
     lens = [70, 130, 200, 129]
