@@ -17,11 +17,13 @@
 // tensor cores' operand).
 //
 // The items come sorted by their key tiles, longest first.  Up to 128 sequences each CTA's load
-// warp holds the lengths in registers and finds its items itself, dealt forwards and backwards
-// in turn; for more a block before (k_plan) writes the list, and a counter hands it out (a launch and
+// warp holds the lengths in registers and finds its items itself: the grid has a CTA per
+// item, and a CTA that is through takes over one that has not started; for more sequences a block
+// before (k_plan) writes the list, and a counter hands it out (a launch and
 // about 5 us that a short call does not repay).  What bounds it: long prompts the tensor
 // cores (2,048 clocks a key tile of hd 128 and 256 rows), short ones the chain of an item.
 #include <algorithm>
+#include <climits>
 
 #include "kf_mma.cuh"
 #include "kf_serving.cuh"
@@ -68,7 +70,8 @@ struct Args {
   Plan plan;
   int* err;
   int Hq, G, heads, tiles;                          // of an item: heads x tiles of 128 rows (2 x 1, 1 x 2 or 1 x 1)
-  int direct, n, T, longest;                        // direct: the items are found from starts, without a plan
+  int direct, steal, n, T, longest;                 // direct: the items are found from starts, without a plan; steal: a CTA per item, whose
+                                                    // CTAs take over those that have not started
   const int32_t* starts;
   float scale2;
 };
@@ -229,12 +232,38 @@ template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float 
   }
 }
 
+// Cluster launch control: a running CTA cancels one that has not started and does its work (the
+// hardware's queue instead of a counter in memory that a call would have to clear)
+__device__ __forceinline__ void ask_for_cta(uint64_t* answer, uint64_t* bar) {
+  mbar_expect_tx(smem_u32(bar), 16);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(answer)),
+               "r"(smem_u32(bar))
+               : "memory");
+}
+// its index, or -1: none is left
+__device__ __forceinline__ int cta_taken(const uint64_t* answer) {
+  uint64_t lo, hi;
+  asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(lo), "=l"(hi) : "r"(smem_u32(answer)) : "memory");
+  int x;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
+      "mov.b128 r, {%1, %2};\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+      "mov.s32 %0, -1;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, r;\n\t}"
+      : "=&r"(x)
+      : "l"(lo), "l"(hi));
+  return x;
+}
+
 struct Bars {
   uint64_t q_full, q_empty;
   uint64_t item_full[2], item_empty[2];
   uint64_t s_full[2], s_free[2], p_full[2][2], o_full[2], o_free[2];   // per sub-tile (and half of P)
   uint64_t tail;                                         // a V tile whose last rows are to be cleared has landed
   uint64_t kv_full[8], kv_empty[8];
+  uint64_t taken;                                        // a request to take over a CTA is answered
+  alignas(16) uint64_t answer[2];
   Item item[2];
   uint32_t tmem;
 };
@@ -267,6 +296,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
       init(&b.o_free[i], 4);
     }
     init(&b.tail, 1);
+    init(&b.taken, 1);
     for (int i = 0; i < ST; ++i) {
       init(&b.kv_full[i], 1);
       init(&b.kv_empty[i], 1);
@@ -351,19 +381,31 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
         }
         return e;
       };
-      // the CTA's i-th item: dealt forwards and backwards in turn, or drawn
+      // the CTA's i-th item: its own, then (without stealing) none where each item has a CTA, or one drawn
       auto drawn = [&](int i) -> int {
-        if (a.direct) return i * gridDim.x + ((i & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
         if (i == 0) return blockIdx.x;
+        if (a.direct) return INT_MAX;
         int v = 0;
         if (lane == 0) v = atomicAdd(a.plan.next, 1);
         return v;                               // (lane 0's; shared where it is used)
       };
       bool ok = true;
-      int w = drawn(0), it = 0, q_issued = 0, g = 0, tails = 0;
+      int w = drawn(0), it = 0, q_issued = 0, g = 0, tails = 0, asks = 0, takes = 0;
       int4 e = entry(w);
-      int w1 = __shfl_sync(~0u, drawn(1), 0);
+      int w1 = a.steal ? 0 : __shfl_sync(~0u, drawn(1), 0);
       auto wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, a.err)); };
+      auto ask = [&] {
+        __syncwarp();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (the answer before has been read)
+        if (lane == 0) ask_for_cta(b.answer, &b.taken);
+        ++asks;
+        __syncwarp();
+      };
+      auto take = [&](int* cta) -> bool {
+        if (!wait(&b.taken, takes++ & 1)) return false;
+        *cta = cta_taken(b.answer);
+        return true;
+      };
       for (;; ++it) {
         Item im;
         im.start = e.x;
@@ -383,10 +425,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
           b.item[slot] = im;
           mbar_arrive(smem_u32(&b.item_full[slot]));
         }
-        if (w >= items) break;                    // (an item without sub-tiles ends the others)
+        if (w >= items) {                         // (an item without sub-tiles ends the others)
+          // (the grid is for the most items that the lengths could have: what is left of it need not start)
+          for (int x = 0; a.steal && ok && w != INT_MAX && x >= 0;) {
+            ask();
+            ok = take(&x);
+          }
+          break;
+        }
         // the next item's entry and the counter for the one after it: used an item later
-        const int4 e1 = entry(w1);
-        const int w2 = drawn(it + 2);
+        int4 e1 = make_int4(0, 0, 0, 0);
+        int w2 = 0;
+        if (a.steal) {
+          ask();
+        } else {
+          e1 = entry(w1);
+          w2 = drawn(it + 2);
+        }
         if (it > 0) ok = wait(&b.q_empty, (it - 1) & 1);
         if (!ok) break;
         if (lane == 0) {
@@ -429,13 +484,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
           }
         }
         if (!ok) break;
-        w = w1;
-        e = e1;
-        w1 = __shfl_sync(~0u, w2, 0);
+        if (a.steal) {
+          ok = take(&w);
+          if (!ok) break;
+          if (w < 0) w = INT_MAX;
+          e = entry(w);
+        } else {
+          w = w1;
+          e = e1;
+          w1 = __shfl_sync(~0u, w2, 0);
+        }
       }
       if (!ok && lane == 0) {
         // let the copies still in flight land before the CTA ends (bounded)
         if (q_issued) mbar_wait(smem_u32(&b.q_full), (q_issued - 1) & 1, a.err);
+        if (asks > takes) mbar_wait(smem_u32(&b.taken), takes & 1, a.err);
         for (int i = max(0, g - ST); i < g; ++i) mbar_wait(smem_u32(&b.kv_full[i % ST]), (i / ST) & 1, a.err);
       }
       __syncwarp();
@@ -736,12 +799,14 @@ extern "C" int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_
   const int direct = without_plan(n);
   int* head = static_cast<int*>(work);
   const Plan plan{head, head + 1, reinterpret_cast<PlanItem*>(head + 64)};
-  const int grid = (int)std::min<int64_t>(device_sms(), cap * (Hq / heads));
+  const int64_t most = (T / rows + n) * (Hq / heads);      // items, by the lengths' sum
+  const int steal = direct && most > device_sms();
+  const int grid = (int)(steal ? most : std::min<int64_t>(device_sms(), most));
   cudaStream_t s = (cudaStream_t)stream;
   if (!direct) launch_cluster(k_plan, dim3(1), dim3(kPlanThreads), 2 * (classes + 2) * sizeof(int), 1, false, s, n, (int)T, longest, rows, classes,
                  starts, plan, grid, err);
   if (const int rc = launched(what)) return rc;
-  const Args a{out, out_row, out_head, plan, err, Hq, G, heads, rows / kRows, direct, n, (int)T, longest, starts, scale * 1.4426950408889634f};
+  const Args a{out, out_row, out_head, plan, err, Hq, G, heads, rows / kRows, direct, steal, n, (int)T, longest, starts, scale * 1.4426950408889634f};
   if (type == KF_TYPE_BF16) return hd == 64 ? launch<__nv_bfloat16, 64>(maps, a, grid, s) : launch<__nv_bfloat16, 128>(maps, a, grid, s);
   return hd == 64 ? launch<__half, 64>(maps, a, grid, s) : launch<__half, 128>(maps, a, grid, s);
 }
