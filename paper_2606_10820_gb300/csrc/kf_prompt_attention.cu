@@ -17,10 +17,10 @@
 // tensor cores' operand).
 //
 // The items come sorted by their key tiles, longest first.  Up to 128 sequences each CTA's load
-// warp holds the lengths in registers and finds its items itself: the grid has a CTA per
-// item, and a CTA that is through takes over one that has not started; for more sequences a block
-// before (k_plan) writes the list, and a counter hands it out (a launch and
-// about 5 us that a short call does not repay).  What bounds it: long prompts the tensor
+// warp holds the lengths in registers and finds its items itself; for more a block before
+// (k_plan) writes the list (a launch and about 5 us that a short call does not repay).  The grid has a
+// CTA per item, and a CTA that is through takes over one that has not started (dealt out beforehand
+// the items took 30.2 us against 26.6 at 16 prompts of 128 to 896, 12 heads over 4 of 64).  What bounds it: long prompts the tensor
 // cores (2,048 clocks a key tile of hd 128 and 256 rows), short ones the chain of an item.
 #include <algorithm>
 #include <climits>
@@ -54,7 +54,7 @@ template <int HD> constexpr size_t kSmem = (2 + kStages<HD>) * (size_t)kTile<HD>
 
 struct PlanItem { int start, len, tile, pad; };     // a sequence's first token, its tokens, its tile of rows
 struct Plan {
-  int *count, *next;                                // items (without heads), the counter
+  int* count;                                       // items (without heads)
   PlanItem* item;
 };
 
@@ -82,7 +82,7 @@ struct Maps { CUtensorMap q, k, v; };
 // last row, an item of class c comes after all items of higher classes, and each
 // sequence of at least c tiles has one.  The order within a class is any.
 __global__ void __launch_bounds__(kPlanThreads) k_plan(int n, int T, int longest, int rows, int classes, const int32_t* starts,
-                                                        Plan plan, int grid, int* err) {
+                                                        Plan plan, int* err) {
   extern __shared__ __align__(1024) uint8_t sm[];
   int* at_least = reinterpret_cast<int*>(sm);       // [classes + 2]: sequences of at least c tiles
   int* first = at_least + classes + 2;                    // [classes + 2]: the first item of class c
@@ -131,10 +131,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(int n, int T, int longest
     }
     __syncthreads();
   }
-  if (t == 0) {
-    *plan.count = classes > 0 ? first[1] + at_least[1] : 0;
-    *plan.next = grid;
-  }
+  if (t == 0) *plan.count = first[1] + at_least[1];
   // A sequence's place among all, those with more tiles first: class c has the places
   // at_least[c + 1] .. at_least[c] - 1, taken from the end.  It holds in every class up to its own
   for (int s0 = 0; s0 < n; s0 += 32) {              // warps take 32 sequences at a time
@@ -381,18 +378,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
         }
         return e;
       };
-      // the CTA's i-th item: its own, then (without stealing) none where each item has a CTA, or one drawn
-      auto drawn = [&](int i) -> int {
-        if (i == 0) return blockIdx.x;
-        if (a.direct) return INT_MAX;
-        int v = 0;
-        if (lane == 0) v = atomicAdd(a.plan.next, 1);
-        return v;                               // (lane 0's; shared where it is used)
-      };
       bool ok = true;
-      int w = drawn(0), it = 0, q_issued = 0, g = 0, tails = 0, asks = 0, takes = 0;
+      int w = blockIdx.x, it = 0, q_issued = 0, g = 0, tails = 0, asks = 0, takes = 0;
       int4 e = entry(w);
-      int w1 = a.steal ? 0 : __shfl_sync(~0u, drawn(1), 0);
       auto wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, a.err)); };
       auto ask = [&] {
         __syncwarp();
@@ -433,15 +421,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
           }
           break;
         }
-        // the next item's entry and the counter for the one after it: used an item later
-        int4 e1 = make_int4(0, 0, 0, 0);
-        int w2 = 0;
-        if (a.steal) {
-          ask();
-        } else {
-          e1 = entry(w1);
-          w2 = drawn(it + 2);
-        }
+        if (a.steal) ask();
         if (it > 0) ok = wait(&b.q_empty, (it - 1) & 1);
         if (!ok) break;
         if (lane == 0) {
@@ -484,16 +464,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_prompt(const __grid_constant__ 
           }
         }
         if (!ok) break;
-        if (a.steal) {
-          ok = take(&w);
-          if (!ok) break;
-          if (w < 0) w = INT_MAX;
-          e = entry(w);
-        } else {
-          w = w1;
-          e = e1;
-          w1 = __shfl_sync(~0u, w2, 0);
-        }
+        int next = -1;
+        if (a.steal) ok = take(&next);
+        if (!ok) break;
+        w = next < 0 ? INT_MAX : next;
+        e = entry(w);
       }
       if (!ok && lane == 0) {
         // let the copies still in flight land before the CTA ends (bounded)
@@ -798,13 +773,13 @@ extern "C" int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_
   const int classes = std::max(1, ceil_div(longest, rows));
   const int direct = without_plan(n);
   int* head = static_cast<int*>(work);
-  const Plan plan{head, head + 1, reinterpret_cast<PlanItem*>(head + 64)};
+  const Plan plan{head, reinterpret_cast<PlanItem*>(head + 64)};
   const int64_t most = (T / rows + n) * (Hq / heads);      // items, by the lengths' sum
-  const int steal = direct && most > device_sms();
+  const int steal = most > device_sms();
   const int grid = (int)(steal ? most : std::min<int64_t>(device_sms(), most));
   cudaStream_t s = (cudaStream_t)stream;
   if (!direct) launch_cluster(k_plan, dim3(1), dim3(kPlanThreads), 2 * (classes + 2) * sizeof(int), 1, false, s, n, (int)T, longest, rows, classes,
-                 starts, plan, grid, err);
+                 starts, plan, err);
   if (const int rc = launched(what)) return rc;
   const Args a{out, out_row, out_head, plan, err, Hq, G, heads, rows / kRows, direct, steal, n, (int)T, longest, starts, scale * 1.4426950408889634f};
   if (type == KF_TYPE_BF16) return hd == 64 ? launch<__nv_bfloat16, 64>(maps, a, grid, s) : launch<__nv_bfloat16, 128>(maps, a, grid, s);
