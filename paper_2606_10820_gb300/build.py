@@ -68,7 +68,7 @@ def _compile_binding(nvcc: str) -> tuple:
 def _link_binding(obj: str) -> None:
     lib = os.path.join(_torch()[1], "lib")
     tmp = BINDING + ".tmp"
-    cmd = ["g++", "-shared", "-o", tmp, obj, "-L", HERE, "-l:libkforcing.so", "-L", lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+    cmd = ["g++", "-shared", "-o", tmp, obj, "-L", HERE, "-l:libkforcing.so", "-L", lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python",
            "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib]
     p = subprocess.run(cmd, capture_output=True, text=True)
     if p.returncode != 0:

@@ -9,12 +9,13 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
-#include <ATen/ops/empty.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include <algorithm>
 #include <cmath>
+#include <optional>
 #include <string>
 
 #include "../../include/kforcing.h"
@@ -73,7 +74,7 @@ int32_t* ints(PyObject* o, c10::Device dev, at::IntArrayRef shape, const char* n
   return static_cast<int32_t*>(on(tensor(o, name), dev, at::kInt, shape, name));
 }
 at::Tensor make(at::IntArrayRef shape, at::ScalarType type, c10::Device dev) {
-  return at::empty(shape, at::TensorOptions().dtype(type).device(dev));
+  return at::Tensor(at::detail::empty_cuda(shape, type, dev, std::nullopt));      // (at::empty without the dispatcher)
 }
 // scratch of one call (calls on several streams may overlap): none where 0 bytes are enough
 struct Scratch {
