@@ -14,7 +14,8 @@
 // the arithmetic on pairs (fma.rn.f32x2).  CTAs walk over the rows, and each thread streams its
 // vectors through slots of shared memory that are its own (cp.async, batches of four; no thread
 // waits for another's), the next row's while this one is reduced.
-//   Scores: a ring of three batches a thread, four CTAs of 256 threads a SM.
+//   Scores: a ring of three batches a thread, four CTAs of 256 threads a SM (many rows that are
+//   not wide: sixteen of 64 with two batches).
 //   Gradient: the row stays in the slots for the second pass, two CTAs of 512 threads a SM (a
 //   second pass from L2 found only half of the lines there: 369 MB read instead of 206 at
 //   2048 x 50257); a row wider than that is split over a cluster.
@@ -25,7 +26,10 @@
 // maximum reaches that bound are looked at again (from L2, a warp per such thread), and their
 // elements at or above it listed, a few dozen of a vocabulary; each one's rank among
 // them is its place.  Where masks close too many groups, the threads' own maxima give the
-// bound; rows where the list would not fit all the same (ties in the hundreds) choose round by round.
+// bound; rows where the list would not fit all the same (ties in the hundreds) raise the bound.
+//
+// Measured: 4096 bf16 rows of 50257 in 100 us with eight alternatives (4.1 TB/s), 74 without (5.5); 8 fp32
+// rows 7.6; the gradient of 2048 bf16 rows 87 us (4.7 TB/s).
 #include <algorithm>
 #include <cooperative_groups.h>
 
@@ -39,14 +43,17 @@ namespace kf {
 namespace {
 
 constexpr int kBatch = 4;          // vectors of a batch
-// scores: batches under way or in use (two for the narrow rows' CTAs, so that sixteen of them fit an SM)
+// scores: batches under way or in use (two for CTAs of two warps, so that sixteen of them fit an SM)
 template <int THREADS> constexpr int kRing = THREADS == 64 ? 2 : 3;
 constexpr int kResident = 4;       // gradient: batches of a row, at most
 constexpr int kPairBytes = 13 * 512 * 16;    // gradient: slots of a CTA that leave room for a second one on the SM
 constexpr int kGroups = 64;        // groups whose maxima bound the n-th largest logit
 constexpr int kMaxTop = kGroups;
-template <int THREADS> constexpr int kList = THREADS == 64 ? 256 : 768;      // listed candidates of a row
-constexpr int kRanked = 192;       // up to so many are ranked against each other, more are chosen in rounds
+// Alternatives that the groups' maxima bound well; for more, CTAs of over 64 threads take their
+// threads' own (4096 bf16 rows, groups and threads, us: 56 of 18000  110  147, 64 of them 303  154;
+// 56 of 50257  199  197, 64 of them 396  205)
+constexpr int kFew = 56;
+template <int THREADS> constexpr int kList = THREADS == 64 ? 512 : 768;      // listed candidates of a row
 constexpr int kMostRow = 8 * kResident * kBatch * 512 * 16;      // bytes of a row: the gradient's slots in eight CTAs
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -300.f;   // 2^-300 is 0 in fp32: stands for -inf where it multiplies that 0
@@ -179,22 +186,6 @@ struct Cand {
   int id;
 };
 __device__ __forceinline__ bool before(Cand a, Cand b) { return a.x > b.x || (a.x == b.x && a.id < b.id); }
-// the first of the block's candidates in that order (every thread gets it)
-template <int WARPS>
-__device__ __forceinline__ Cand block_first(Cand c, Cand* buf) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const Cand d{__shfl_xor_sync(~0u, c.x, o), __shfl_xor_sync(~0u, c.id, o)};
-    if (before(d, c)) c = d;
-  }
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = c;
-  __syncthreads();
-  c = buf[0];
-  for (int i = 1; i < WARPS; ++i)
-    if (before(buf[i], c)) c = buf[i];
-  return c;
-}
 
 template <int THREADS>
 struct Shared {
@@ -204,7 +195,7 @@ struct Shared {
   float bound;
   int count, again;
   uint16_t thread[THREADS];        // threads whose vectors are looked at again
-  Cand first[THREADS / 32];
+  int tied[THREADS / 32];
   Cand list[kList<THREADS>];
 };
 
@@ -331,6 +322,67 @@ struct Mine {
 };
 
 // ------------------------------------------------------------------ scores
+// More candidates than the list holds (ties at the bound, as of a mask of the type's lowest value): those
+// above the bound, then above the top-th largest of the listed, until they fit (each pass after the
+// first drops all but top of the listed at least); ones at that bound follow by id.  Returns
+// how many are listed.  A call, so that the kernel's registers stay its own (inline: 106 us for 99 at
+// 4096 x 50257); 8 rows of 50257 with five open ones take 21 us
+template <typename T, int THREADS>
+__device__ __noinline__ int raise_bound(Shared<THREADS>& sh, const T* p, int V, int top, float inv_tau, float bound) {
+  constexpr int N = Vec16<T>::N, WARPS = THREADS / 32;
+  const Row<T> row(p, V);
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  int found = kList<THREADS> + 1;
+#pragma unroll 1
+  for (bool first = true; found > kList<THREADS>; first = false) {      // (uniform)
+    if (!first) {
+      for (int i = t; i < kList<THREADS>; i += THREADS) {
+        const Cand c = sh.list[i];
+        int rk = 0;
+        for (int j = 0; j < kList<THREADS>; ++j) rk += before(sh.list[j], c);
+        if (rk == top - 1) sh.bound = c.x;
+      }
+      __syncthreads();
+      bound = sh.bound;
+    }
+    __syncthreads();
+    if (t == 0) sh.count = 0;
+    __syncthreads();
+    auto above = [&](int id, float v) {
+      const float x = v * inv_tau;
+      if (x > bound) {
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < kList<THREADS>) sh.list[at] = Cand{x, id};
+      }
+    };
+    if (t < row.edge()) above(row.edge_id(t), to_f(p[row.edge_id(t)]));
+    for (int i = t; i < row.nvec; i += THREADS) {
+      float v[N];
+      Vec16<T>::unpack(*reinterpret_cast<const uint4*>(row.vec(i)), v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) above(row.head + i * N + e, v[e]);
+    }
+    __syncthreads();
+    found = sh.count;
+  }
+  if (found >= top) return found;
+  for (int id0 = 0; found < top && id0 < V; id0 += THREADS) {            // (uniform)
+    const int id = id0 + t;
+    const bool tie = id < V && to_f(p[id]) * inv_tau == bound;
+    const uint32_t same = __ballot_sync(~0u, tie);
+    if (lane == 0) sh.tied[warp] = __popc(same);
+    __syncthreads();
+    int at = found + __popc(same & ((1u << lane) - 1));
+    for (int w = 0; w < WARPS; ++w) {
+      found += sh.tied[w];
+      at += w < warp ? sh.tied[w] : 0;
+    }
+    if (tie && at < top) sh.list[at] = Cand{bound, id};
+    __syncthreads();
+  }
+  return min(found, top);
+}
+
 template <typename T, int THREADS, int CS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a) {
   extern __shared__ __align__(16) uint4 slots[];         // [batch of the ring][vector][thread]
@@ -339,21 +391,20 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, rank = blockIdx.x % CS;
   const Mine<THREADS> mine(a.V / N, CS, rank);
   const int batches = (mine.per_cta + kBatch - 1) / kBatch;      // of a row
-  const int64_t step = gridDim.x / CS;
+  const int step = gridDim.x / CS, R = (int)a.R;         // (up to 2^28 rows)
   const uint32_t slot0 = mma::smem_addr(slots + t);
 
   // the copies run kRing<THREADS> - 1 batches ahead, into the rows that follow
-  int64_t fr = blockIdx.x / CS;
-  int fb = 0, fslot = 0, fn = 0;
+  int fr = blockIdx.x / CS, fb = 0, fslot = 0, fn = 0;
   const T* fp = nullptr;
   auto look = [&] {
-    if (fr >= a.R) return;
+    if (fr >= R) return;
     const Row<T> w = row_at<T>(a, fr);
     fn = mine.have(w);
     fp = w.vec(mine.first);
   };
   auto fill = [&] {                       // one group of copies, empty past the last row
-    if (fr < a.R) {
+    if (fr < R) {
       const T* p = fp + (size_t)fb * kBatch * THREADS * N;
       const uint32_t d = slot0 + fslot * kBatch * THREADS * 16;
 #pragma unroll
@@ -373,7 +424,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
   for (int i = 0; i < kRing<THREADS> - 1; ++i) fill();
   int slot = 0;
 #pragma unroll 1
-  for (int64_t r = blockIdx.x / CS; r < a.R; r += step) {
+  for (int r = blockIdx.x / CS; r < R; r += step) {
     const Row<T> row = row_at<T>(a, r);
     const Extra<T> ex(a, row, r, rank == 0);
     const int n = mine.have(row);
@@ -403,8 +454,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
     if (rank == 0 && t == 0) write_numbers(a, r, o, ex.token, ex.at_logit);
 
     if (a.top == 0) continue;             // (uniform)
-    int32_t* ids = a.top_ids + r * a.top;
-    float* lps = a.top_logp + r * a.top;
+    int32_t* ids = a.top_ids + (int64_t)r * a.top;
+    float* lps = a.top_logp + (int64_t)r * a.top;
     if (o.bad) {                          // (uniform over the row's CTAs)
       if (rank == 0)
         for (int i = t; i < a.top; i += THREADS) {
@@ -423,7 +474,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
     }
     __syncthreads();
     float bound = sh.bound;
-    if (bound == -INFINITY) {             // (uniform over the row's CTAs) a mask: this CTA's threads' own maxima
+    // (uniform over the row's CTAs) masks, or many alternatives: this CTA's threads' own maxima
+    if (bound == -INFINITY || (CS == 1 && THREADS > kGroups && a.top > kFew)) {
       float* own = reinterpret_cast<float*>(sh.list);
       own[t] = vec_max;
       __syncthreads();
@@ -461,9 +513,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
 #pragma unroll
       for (int e = 0; e < N; ++e) list(id0 + e, v[e]);
     };
-    // a warp per such thread; each by itself where a narrow row has many of them for its two warps (4096 x
-    // 1770, 20 alternatives: 24.6 -> 20.9 us; with 8 warps and 50257 it loses, 115 -> 167)
-    if (THREADS > 64 || sh.again <= 4 * WARPS) {
+    // a warp per such thread, or each by itself, whichever has fewer vectors in turn
+    if (sh.again * ((mine.per_cta + 31) / 32) <= WARPS * mine.per_cta) {
       for (int j = warp; j < sh.again; j += WARPS)
         for (int k = lane; k < mine.per_cta; k += 32) {
           const int i = mine.first - t + sh.thread[j] + k * THREADS;
@@ -477,38 +528,17 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
     if constexpr (CS > 1) cg::this_cluster().sync();
     else __syncthreads();
     if (rank != 0) continue;
-    const int found = sh.count;
+    int found = sh.count;
+    if (found > kList<THREADS>) found = raise_bound(sh, row.p, a.V, a.top, a.inv_tau, bound);      // (uniform)
     auto put = [&](int place, Cand c) {
       ids[place] = c.id;
       lps[place] = o.lp(a, to_f(row.p[c.id]));
     };
-    if (found <= kRanked) {
-      for (int i = t; i < found; i += THREADS) {
-        const Cand c = sh.list[i];
-        int rk = 0;
-        for (int j = 0; j < found; ++j) rk += before(sh.list[j], c);
-        if (rk < a.top) put(rk, c);
-      }
-    } else {
-      // round by round: the first candidate after the last one chosen, of the list or
-      // (where that overflowed) of the row
-      Cand last{INFINITY, -1};
-      for (int k = 0; k < min(found, a.top); ++k) {
-        Cand c{-INFINITY, 0x7fffffff};
-        auto look_at = [&](Cand d) {
-          if (before(last, d) && before(d, c)) c = d;
-        };
-        if (found <= kList<THREADS>) {
-          for (int j = t; j < found; j += THREADS) look_at(sh.list[j]);
-        } else {
-          for (int id = t; id < a.V; id += THREADS) {
-            const float x = to_f(row.p[id]) * a.inv_tau;
-            if (listed(x)) look_at(Cand{x, id});
-          }
-        }
-        last = block_first<WARPS>(c, sh.first);
-        if (t == 0) put(k, last);
-      }
+    for (int i = t; i < found; i += THREADS) {
+      const Cand c = sh.list[i];
+      int rk = 0;
+      for (int j = 0; j < found; ++j) rk += before(sh.list[j], c);
+      if (rk < a.top) put(rk, c);
     }
     // fewer open tokens than asked for: closed ones by id
     if (found < a.top && t == 0) {
@@ -652,21 +682,28 @@ void launch_grad(const Args& a, cudaStream_t s) {
 }
 template <typename T, bool GRAD>
 int launch(const Args& a, cudaStream_t s) {
-  // A row of up to 12 KB: two warps, so that an SM has sixteen such rows (ten for the gradient).  A wider one is split over a
-  // cluster while few rows leave SMs idle and each thread keeps two vectors; the gradient's also
-  // until it fits the slots
+  // Many rows that are not wide take CTAs of two warps, sixteen a SM (the gradient's ten): less of
+  // a row's time goes to its joins (up to kFew alternatives, see there).  Measured on bf16 with two warps against wide CTAs, us:
+  //   scores, five alternatives   6000 of 304 rows  7.6  5.5, of 608  8.2  7.6, of 4096  23.8  38.6;
+  //                               18000 of 4096  44.5  54.9, 30000  69.0  69.7, 50257  104  96
+  //   without alternatives        50257 of 608  14.7  14.2, of 4096  72.7  81.4
+  //   gradient                    6000 of 304  7.6  5.6, of 608  7.8  9.5, of 4096  28.5  54.7
+  // Few rows are split over a cluster while half the SMs would idle and each thread keeps two
+  // vectors (50257, one CTA a row against the cluster: 8 rows 8.2  6.8, 32 rows 8.2  7.8, 64 rows 8.4
+  // 8.7, 128 rows 8.4  9.7; the gradient 8.8  6.2, 8.8  6.8, 8.9  8.2, 8.9  11.5); the gradient's
+  // also until they fit the slots
   const int64_t bytes = (int64_t)a.V * sizeof(T), sms = device_sms();
   int cs = 1;
   if constexpr (GRAD) {
     while (cs < 8 && (bytes > (int64_t)cs * kPairBytes || (a.R * cs * 2 <= sms && bytes >= cs * 2 * 2 * 512 * 16))) cs *= 2;
-    if (bytes <= 12288) launch_grad<T, 64, 1>(a, s);
+    if (bytes <= 12288 && a.R > 2 * sms) launch_grad<T, 64, 1>(a, s);
     else if (cs == 1) launch_grad<T, 512, 1>(a, s);
     else if (cs == 2) launch_grad<T, 512, 2>(a, s);
     else if (cs == 4) launch_grad<T, 512, 4>(a, s);
     else launch_grad<T, 512, 8>(a, s);
   } else {
-    while (cs < 8 && a.R * cs * 2 <= 2 * sms && bytes >= cs * 2 * 2 * 256 * 16) cs *= 2;
-    if (bytes <= 12288) launch_scores<T, 64, 1>(a, s);
+    while (cs < 8 && a.R * cs * 2 <= sms && bytes >= cs * 2 * 2 * 256 * 16) cs *= 2;
+    if (a.R > 4 * sms && a.top <= kFew && bytes <= (a.top ? 49152 : 114688)) launch_scores<T, 64, 1>(a, s);
     else if (cs == 1) launch_scores<T, 256, 1>(a, s);
     else if (cs == 2) launch_scores<T, 256, 2>(a, s);
     else if (cs == 4) launch_scores<T, 256, 4>(a, s);

@@ -190,6 +190,31 @@ def test_ties_and_orders(sv, R, dtype):
         check_top(got, formulas(x, tok, 1.0), top)
 
 
+@pytest.mark.parametrize("R,V", [(3, 9001), (3, 50257), (70, 50257), (640, 18003)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_masks_of_the_lowest_value(sv, R, V, dtype):
+    """A few open tokens, all others at the type's lowest value: thousands tie at the bound.  And a
+    staircase, where more than the list holds stand above any first bound."""
+    x, tok, _, _ = rows(R, V, dtype, 17)
+    low = torch.finfo(dtype).min
+    x[0, 11:] = low
+    x[1] = low
+    x[1, V - 2:] = 1.0
+    x[2] = low
+    x[2, ::64 * 8] = torch.arange(x[2, ::64 * 8].numel(), device="cuda").to(dtype)      # few threads hold what is open
+    if R > 3:
+        x[3:, 20:] = low
+        x[4] = -math.inf
+        x[4, :3000] = (torch.arange(3000, device="cuda") // 4).to(dtype)
+        x[5, 2000:] = -math.inf
+    ref = formulas(x, tok, 1.0)
+    for top in (1, 8, 48, 49, 64):
+        got = sv.token_scores(x, tok, top=top)
+        check_top(got, ref, top)
+        near(got["lse"], ref["lse"])
+    sv.status()
+
+
 @pytest.mark.parametrize("V", [50, 50257])
 def test_not_numbers(sv, V):
     x, tok, gl, gh = rows(5, V, torch.float32, 1)
@@ -207,6 +232,42 @@ def test_not_numbers(sv, V):
     ref = formulas(x[3:], tok[3:], 1.0)
     near(got["logp"][3:], ref["logp"])
     assert torch.isfinite(grad[3:]).all()
+
+
+@pytest.mark.parametrize("V", [1, 2, 33, 130, 1000, 4097, 6144, 8200, 16411, 24500, 50257])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_many_rows(sv, V, dtype):
+    """More rows than one wave of CTAs (which take other shapes then), ordinary ones between masked,
+    tied and broken ones; the odd widths start rows at every alignment."""
+    R = 700
+    x, tok, gl, gh = rows(R, V, dtype, V + 5)
+    x[::7, V // 3 + 1:] = -math.inf
+    x[1::7, V // 2 + 1:] = torch.finfo(dtype).min
+    x[2::7] = (torch.arange(V, device="cuda") % 3).to(dtype)
+    tok[::7] = 0
+    tok[3::7] = -1
+    dead, broken = list(range(4, R, 70)), list(range(5, R, 70))
+    x[dead] = -math.inf
+    x[broken, V - 1] = math.nan
+    fine = torch.ones(R, dtype=torch.bool, device="cuda")
+    fine[broken] = False
+    ref = formulas(x[fine], tok[fine], 1.0, gl[fine], gh[fine])
+    for top in sorted({0, 1, min(8, V), min(64, V)}):
+        got = sv.token_scores(x, tok, top=top)
+        assert torch.isnan(got["lse"][broken]).all() and torch.isnan(got["entropy"][broken]).all()
+        good = {k: v[fine] for k, v in got.items()}
+        for k in ("logp", "entropy", "lse"):
+            near(good[k], ref[k])
+        if top:
+            check_top(good, ref, top)
+            assert (got["top_ids"][broken] == -1).all()
+    got = sv.token_scores_grad(x, tok, gl, gh)
+    assert torch.isnan(got["grad"][broken]).all()
+    assert (got["grad"][dead] == 0).all()
+    none = torch.isneginf(ref["lse"])
+    ref["grad"][none] = 0.0       # rows without open tokens
+    grad_near(got["grad"][fine], ref, torch.where(tok >= 0, gl, 0.0)[fine], gh[fine], 1.0, dtype)
+    sv.status()
 
 
 def test_strides_streams_and_repeats(sv):

@@ -163,6 +163,8 @@ def test_score_kernels(lib):
         assert len(got) == 1
         return got[0].threads, got[0].cluster
 
-    assert shape(V=1000, stride=1000)[0] == 64 and shape(R=4096)[0] == 256
+    assert shape(R=4096, V=1000, stride=1000)[0] == 64 and shape(R=64, V=1000, stride=1000)[0] == 256 and shape(R=4096)[0] == 256
     assert shape(R=1)[1] > 1 and shape(R=4096)[1] <= 1
+    assert shape(True, R=4096, V=1000, stride=1000, grad_stride=1000)[0] == 64
+    assert shape(True, R=64, V=1000, stride=1000, grad_stride=1000)[0] == 512
     assert shape(True, R=4096)[0] == 512 and shape(True, R=4096, type=0)[1] == 2      # 201 KB a row: two CTAs
