@@ -11,6 +11,8 @@
 // bounds a call is its barriers and the loads between them (two or three of each).
 // Page contents are moved by a second, dependent launch over all SMs that
 // reads the list of moves (its bound: HBM, each moved byte read and written once).
+// Measured: k_move 1.05 GB (read and written) in 159 us (6.6 TB/s); the bookkeeping of a compact of 16,384
+// pages and 32,768 entries 16 us, of 1,024 pages 6; k_append 0.53 GB in 84 us (6.3 TB/s).
 #include <algorithm>
 #include <cooperative_groups.h>
 
@@ -489,8 +491,10 @@ const char* pool_fault(const void* pool, int layers, int64_t page_bytes) {
   return nullptr;
 }
 // A cluster's barriers cost a few microseconds that a small book does not repay: one CTA up
-// to 16 references and 16 table entries a thread
-bool small_book(int64_t pages, int64_t entries) { return pages <= 16 * kThreads && entries <= 16 * kThreads; }
+// to 8 references (what its warps keep as ballots) and 8 table entries a thread.  Measured on
+// compact's bookkeeping, one CTA and the cluster: 1,024 pages 6.3 and 13.7 us, 8,192 10.9 and
+// 14.2, 16,384 21.1 and 15.0, 131,072 144 and 31
+bool small_book(int64_t pages, int64_t entries) { return pages <= 8 * kThreads && entries <= 8 * kThreads; }
 
 #define KF_TEAM(kernel, small, s, ...)                                                      \
   do {                                                                                      \

@@ -22,6 +22,9 @@
 // CTA per item, and a CTA that is through takes over one that has not started (dealt out beforehand
 // the items took 30.2 us against 26.6 at 16 prompts of 128 to 896, 12 heads over 4 of 64).  What bounds it: long prompts the tensor
 // cores (2,048 clocks a key tile of hd 128 and 256 rows), short ones the chain of an item.
+//
+// Measured (bf16): prompts of 7,411 and 8,192, 16 heads over 4 of 128, in 317 us (1.57 PFLOP/s); 16
+// of 128 to 896, 12 over 4 of 64, in 26 us; five of 1 to 77, 7 over 1 of 128, fp16, in 6.7 us.
 #include <algorithm>
 #include <climits>
 
