@@ -4,7 +4,8 @@
 // The query rows of one (sequence, KV head) are its rows x group heads; tiles of
 // 16 of them run on warp-level MMA (m16n8k16, fp32 accumulation) with the
 // softmax in registers, so K and V are read once for all heads of a group (and at
-// head_dim 64 for 32 rows at a time, which the registers hold there).
+// head_dim 64 for 32 rows at a time, which the registers hold there; at 128 two tiles of a large
+// cache take turns on each unit, so that the second read comes from L2).
 // What bounds it is those bytes, so the layout serves the loads:
 //   - The keys of all (sequence, KV head, tile) segments, in units of 8 KB of K
 //     and V (16 keys of 128, 32 of 64), form one list that the CTAs share
@@ -32,12 +33,17 @@ constexpr int NW = 4, kThreads = 32 * NW;     // warps of a CTA
 constexpr int kUnitBytes = 8192;              // K and V of a unit
 constexpr int kMinUnits = 4;                  // units of a CTA where the work allows it: one per warp
 constexpr int kDirect = 16;                   // units of a segment that one CTA takes as a whole where the CTAs suffice
+constexpr int64_t kL2Bytes = 128 << 20;
 constexpr int kExtra = 6;                     // a segment's start and end, in units
 // what a (head_dim, tiles of 16 rows per segment) pair of kernels uses
+// head_dim 128 has registers for one tile a warp: of two tiles the warps take turns (units come twice, once for
+// each tile, to neighbouring warps), so that their keys come from DRAM once and the second time from L2
+template <int HD, int TILES> constexpr bool kTurns = HD == 128 && TILES == 2;
+template <int HD, int TILES> constexpr int kHeld = kTurns<HD, TILES> ? 1 : TILES;      // tiles of a warp
 template <int HD, int TILES> constexpr bool kThree = HD == 64 && TILES == 1;
 template <int HD, int TILES> constexpr int kStages = kThree<HD, TILES> ? 2 : 3;
 template <int HD, int TILES> constexpr int kCtasPerSm = kThree<HD, TILES> ? 3 : 2;
-constexpr int kMostCtasPerSm = 3, kMostRows = 32, kMostValues = 2048;      // of a segment: rows, rows x hd
+constexpr int kMostCtasPerSm = 3, kMostRows = 32, kMostValues = 4096;      // of a segment: rows, rows x hd
 
 // a segment that CTA c began and others went on with
 struct Split { int b, s, pieces, pad; };
@@ -95,15 +101,17 @@ struct Part {
   long long total, x0, x1, base;
   int b, parts;
 };
+template <int HD, int TILES>
+__device__ __forceinline__ int places_of(const Args& a, int b) { return units_of<HD>(a, b) * (kTurns<HD, TILES> ? 2 : 1); }
 __device__ __forceinline__ long long part_begin(long long total, int parts, int c) { return total * c / parts; }
-template <int HD>
+template <int HD, int TILES>
 __device__ Part find_part(const Args& a, int c, int ctas) {
   __shared__ long long warp_sum[NW];
   __shared__ Part found;
   const int t = threadIdx.x, per = (a.B + kThreads - 1) / kThreads, sb = a.Hkv * a.MT;
   const int first = min(a.B, t * per), last = min(a.B, first + per);
   long long mine = 0;
-  for (int b = first; b < last; ++b) mine += units_of<HD>(a, b) + kExtra;
+  for (int b = first; b < last; ++b) mine += places_of<HD, TILES>(a, b) + kExtra;
   mine *= sb;
   long long incl = mine;
 #pragma unroll
@@ -123,7 +131,7 @@ __device__ Part find_part(const Args& a, int c, int ctas) {
   if (c < parts && x0 >= lo && x0 < lo + mine) {
     long long base = lo;
     int b = first;
-    for (long long n = (long long)(units_of<HD>(a, b) + kExtra) * sb; x0 >= base + n; n = (long long)(units_of<HD>(a, b) + kExtra) * sb) {
+    for (long long n = (long long)(places_of<HD, TILES>(a, b) + kExtra) * sb; x0 >= base + n; n = (long long)(places_of<HD, TILES>(a, b) + kExtra) * sb) {
       base += n;
       ++b;
     }
@@ -135,10 +143,11 @@ __device__ Part find_part(const Args& a, int c, int ctas) {
 }
 
 // one segment's places within a CTA's part
-template <int HD>
+template <int HD, int TILES>
 struct Piece {
   long long xs, xa, xb, xe;    // the segment's first unit; the piece's units [xa, xb) (or none) and its end
   int b, s, n, len;            // sequence, segment of it, units of the segment, tokens
+  __device__ __forceinline__ int unit(long long x) const { return (int)(x - xs) >> (kTurns<HD, TILES> ? 1 : 0); }
   __device__ __forceinline__ void cut(const Part& p) {
     xa = max(xs, p.x0);
     xb = min(xs + n, p.x1);
@@ -146,7 +155,7 @@ struct Piece {
   }
   __device__ __forceinline__ void at(const Args& a, const Part& p) {
     b = p.b;
-    n = units_of<HD>(a, b);
+    n = places_of<HD, TILES>(a, b);
     len = seq_len(a, b);
     s = (int)((p.x0 - p.base) / (n + kExtra));
     xs = p.base + (long long)s * (n + kExtra);
@@ -158,7 +167,7 @@ struct Piece {
     if (++s == a.Hkv * a.MT) {
       s = 0;
       ++b;
-      n = units_of<HD>(a, b);
+      n = places_of<HD, TILES>(a, b);
       len = seq_len(a, b);
     }
     xs = xe;
@@ -168,17 +177,17 @@ struct Piece {
 };
 
 // a warp's copies: unit after unit of its own, ahead of the products
-template <typename T, int HD>
+template <typename T, int HD, int TILES>
 struct Feed {
   static constexpr int U = kUnit<HD>, kHalves = U / 16;
-  Piece<HD> pc;
+  Piece<HD, TILES> pc;
   long long x;
   int page[kHalves];       // pages of unit x
   bool more;
   __device__ __forceinline__ void look(const Args& a) {
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
-      const int key = (int)(x - pc.xs) * U + 16 * h;
+      const int key = pc.unit(x) * U + 16 * h;
       page[h] = key < pc.len ? __ldg(a.table + (size_t)pc.b * a.width + a.page_of(key)) : -1;
     }
   }
@@ -204,7 +213,7 @@ struct Feed {
       uint32_t ok = 0;
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
-        const int key0 = (int)(x - pc.xs) * U + 16 * h, left = pc.len - key0;
+        const int key0 = pc.unit(x) * U + 16 * h, left = pc.len - key0;
         const bool in = page[h] >= 0 && page[h] < a.n_pages;
         if (in) ok |= 1u << h;
         else if (left > 0 && lane == 0) atomicOr(a.err, KF_DEV_BAD_PAGE);
@@ -228,7 +237,7 @@ struct Feed {
   }
 };
 
-template <int HD, int TILES> constexpr int kMergeFloats = 16 * TILES * (HD + 2);    // one warp's O, m and l
+template <int HD, int TILES> constexpr int kMergeFloats = 16 * kHeld<HD, TILES> * (HD + 2);    // one warp's O, m and l
 // (two CTAs of 114,992 bytes, their static arrays and 1 KB each fit the SM's 228 KB; three of 74,096)
 template <int HD, int TILES>
 constexpr size_t kSmem = NW * kStages<HD, TILES> * kUnitBytes + (NW / 2) * kMergeFloats<HD, TILES> * 4 + NW * kStages<HD, TILES> * 4;
@@ -236,7 +245,8 @@ constexpr size_t kSmem = NW * kStages<HD, TILES> * kUnitBytes + (NW / 2) * kMerg
 template <typename T, int HD, int TILES>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const Args a) {
   extern __shared__ __align__(128) uint8_t sm[];
-  constexpr int ST = kStages<HD, TILES>, ROWS = 16 * TILES;
+  constexpr int ST = kStages<HD, TILES>, ROWS = 16 * TILES, HELD = kHeld<HD, TILES>;
+  constexpr int PARTS = kTurns<HD, TILES> ? 2 : 1;      // warps of a piece that hold its rows in the end
   constexpr int U = kUnit<HD>, NT = U / 8, KS = HD / 16, DT = HD / 8;   // key tiles, dim steps of S, dim tiles of O
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31, g = lane >> 2, c = lane & 3;
   float* merge = reinterpret_cast<float*>(sm + NW * ST * kUnitBytes);
@@ -251,40 +261,41 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
   Part part;
   if (a.direct) {
     // this segment's places are the whole list: [0, n + kExtra)
-    const int sb = a.Hkv * a.MT, b = blockIdx.x / sb, n = units_of<HD>(a, b) + kExtra;
+    const int sb = a.Hkv * a.MT, b = blockIdx.x / sb, n = places_of<HD, TILES>(a, b) + kExtra;
     part = Part{n, 0, n, -(long long)(blockIdx.x - b * sb) * n, b, 1};
   } else {
     if (t == 0) a.split[blockIdx.x].pieces = 0;
-    part = find_part<HD>(a, blockIdx.x, gridDim.x);
+    part = find_part<HD, TILES>(a, blockIdx.x, gridDim.x);
   }
   if (part.x0 < part.x1) {
-    Feed<T, HD> feed;
+    Feed<T, HD, TILES> feed;
     feed.start(a, part, warp);
 #pragma unroll
     for (int i = 0; i < ST - 1; ++i) feed.copy(a, part, ring + i * kUnitBytes, open + i, lane);
     int st = 0;
 
-    Piece<HD> pc;
+    Piece<HD, TILES> pc;
     pc.at(a, part);
     do {
       if (pc.xa >= pc.xb) continue;                // (uniform) only places without units
-      const int hk = pc.s / a.MT, r0 = (pc.s % a.MT) * ROWS, R = a.rows * a.G;
+      const int hk = pc.s / a.MT, seg0 = (pc.s % a.MT) * ROWS, R = a.rows * a.G;
       const int f = (int)(pc.xa % NW), nw = (int)min((long long)NW, pc.xb - pc.xa);
       const int j = (warp - f + NW) % NW;          // this warp's place among the piece's
+      const int tile = PARTS > 1 ? ((int)(pc.xa - pc.xs) + j) & 1 : 0, r0 = seg0 + 16 * tile;
       // this lane's rows of tile i: r0 + 16 i + g and 8 more.  m: raw scores' maximum
-      float m[TILES][2], l[TILES][2], o[TILES][DT][4];
+      float m[HELD][2], l[HELD][2], o[HELD][DT][4];
 #pragma unroll
-      for (int i = 0; i < TILES; ++i) {
+      for (int i = 0; i < HELD; ++i) {
         m[i][0] = m[i][1] = -INFINITY;
         l[i][0] = l[i][1] = 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[i][d][0] = o[i][d][1] = o[i][d][2] = o[i][d][3] = 0.f;
       }
       if (j < nw) {
-        uint32_t q[TILES][KS][4];
-        int last[TILES][2];                         // the last key each row sees
+        uint32_t q[HELD][KS][4];
+        int last[HELD][2];                         // the last key each row sees
 #pragma unroll
-        for (int i = 0; i < TILES; ++i)
+        for (int i = 0; i < HELD; ++i)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const int r = r0 + 16 * i + g + 8 * h, tok = r / a.G;
@@ -305,9 +316,9 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
           const int fr = st == 0 ? ST - 1 : st - 1;
           feed.copy(a, part, ring + fr * kUnitBytes, open + fr, lane);
           st = st + 1 == ST ? 0 : st + 1;
-          float s[TILES][NT][4];
+          float s[HELD][NT][4];
 #pragma unroll
-          for (int i = 0; i < TILES; ++i)
+          for (int i = 0; i < HELD; ++i)
 #pragma unroll
             for (int n = 0; n < NT; ++n) s[i][n][0] = s[i][n][1] = s[i][n][2] = s[i][n][3] = 0.f;
           // S: 16 keys x 16 dims per ldmatrix
@@ -319,15 +330,15 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
               uint32_t kb[4];
               mma::ldsm_x4(kst + row * (HD * 2) + ((ch ^ (row & 7)) << 4), kb);
 #pragma unroll
-              for (int i = 0; i < TILES; ++i) {
+              for (int i = 0; i < HELD; ++i) {
                 mma16816<T>(s[i][n], q[i][k], kb[0], kb[1]);
                 mma16816<T>(s[i][n + 1], q[i][k], kb[2], kb[3]);
               }
             }
-          const int key0 = (int)(x - pc.xs) * U;
+          const int key0 = pc.unit(x) * U;
           if (key0 + U - 1 > free_to || ok != (1u << (U / 16)) - 1) {       // (uniform)
 #pragma unroll
-            for (int i = 0; i < TILES; ++i)
+            for (int i = 0; i < HELD; ++i)
 #pragma unroll
               for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -335,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
                   if (key0 + 8 * n + 2 * c + (e & 1) > last[i][e >> 1] || !((ok >> (n >> 1)) & 1u)) s[i][n][e] = -INFINITY;
           }
 #pragma unroll
-          for (int i = 0; i < TILES; ++i) {
+          for (int i = 0; i < HELD; ++i) {
             float nm[2], fac[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -372,9 +383,9 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
           // cache's type, the tensor cores' operand (the sum l is not)
 #pragma unroll
           for (int n = 0; n < NT; n += 2) {
-            uint32_t p[TILES][4];
+            uint32_t p[HELD][4];
 #pragma unroll
-            for (int i = 0; i < TILES; ++i) {
+            for (int i = 0; i < HELD; ++i) {
               p[i][0] = pack2<T>(s[i][n][0], s[i][n][1]);
               p[i][1] = pack2<T>(s[i][n][2], s[i][n][3]);
               p[i][2] = pack2<T>(s[i][n + 1][0], s[i][n + 1][1]);
@@ -386,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
               uint32_t vb[4];
               mma::ldsm_x4_t(vst + row * (HD * 2) + ((ch ^ (row & 7)) << 4), vb);
 #pragma unroll
-              for (int i = 0; i < TILES; ++i) {
+              for (int i = 0; i < HELD; ++i) {
                 mma16816<T>(o[i][d], p[i], vb[0], vb[1]);
                 mma16816<T>(o[i][d + 1], p[i], vb[2], vb[3]);
               }
@@ -394,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
           }
         }
 #pragma unroll
-        for (int i = 0; i < TILES; ++i)
+        for (int i = 0; i < HELD; ++i)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             l[i][h] += __shfl_xor_sync(~0u, l[i][h], 1);
@@ -403,30 +414,30 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
       }
       // the piece's warps merge in pairs: j + w into j
 #pragma unroll
-      for (int w = NW / 2; w; w >>= 1) {
+      for (int w = NW / 2; w >= PARTS; w >>= 1) {
         if (nw <= w) continue;                      // (uniform)
         if (j >= w && j < min(2 * w, nw)) {
           float* d = merge + (j - w) * kMergeFloats<HD, TILES>;
 #pragma unroll
-          for (int i = 0; i < TILES; ++i) {
+          for (int i = 0; i < HELD; ++i) {
 #pragma unroll
             for (int x = 0; x < DT; ++x)
               *reinterpret_cast<float4*>(d + ((i * DT + x) * 32 + lane) * 4) = make_float4(o[i][x][0], o[i][x][1], o[i][x][2], o[i][x][3]);
             if (c == 0)
 #pragma unroll
               for (int h = 0; h < 2; ++h)
-                *reinterpret_cast<float2*>(d + ROWS * HD + 2 * (16 * i + g + 8 * h)) = make_float2(m[i][h], l[i][h]);
+                *reinterpret_cast<float2*>(d + 16 * HELD * HD + 2 * (16 * i + g + 8 * h)) = make_float2(m[i][h], l[i][h]);
           }
         }
         __syncthreads();
         if (j < w && j + w < nw) {
           const float* d = merge + j * kMergeFloats<HD, TILES>;
 #pragma unroll
-          for (int i = 0; i < TILES; ++i) {
+          for (int i = 0; i < HELD; ++i) {
             float fa[2], fb[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const float2 ml = *reinterpret_cast<const float2*>(d + ROWS * HD + 2 * (16 * i + g + 8 * h));
+              const float2 ml = *reinterpret_cast<const float2*>(d + 16 * HELD * HD + 2 * (16 * i + g + 8 * h));
               const float mm = fmaxf(m[i][h], ml.x);
               fa[h] = m[i][h] == -INFINITY ? 0.f : mma::ex2((m[i][h] - mm) * a.scale2);
               fb[h] = ml.x == -INFINITY ? 0.f : mma::ex2((ml.x - mm) * a.scale2);
@@ -445,18 +456,18 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
         }
         __syncthreads();
       }
-      if (j == 0) {
+      if (j < PARTS) {                             // (of a piece of one unit the second warp's rows are empty)
         const long long end = pc.xs + pc.n;
         const bool whole = pc.xa == pc.xs && pc.xb == end;
         const int slot = 2 * blockIdx.x + (pc.xa == pc.xs);       // 0: a segment begun elsewhere, 1: one that goes on elsewhere
         // (parts up to the last that begins before the segment's end: total p / parts < end)
-        if (!whole && pc.xa == pc.xs && lane == 0)
+        if (!whole && pc.xa == pc.xs && j == 0 && lane == 0)
           a.split[blockIdx.x] = Split{pc.b, pc.s, (int)((end * part.parts + part.total - 1) / part.total) - (int)blockIdx.x, 0};
 #pragma unroll
-        for (int i = 0; i < TILES; ++i)
+        for (int i = 0; i < HELD; ++i)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int rr = 16 * i + g + 8 * h, r = r0 + rr, tok = r / a.G;
+            const int rr = 16 * (tile + i) + g + 8 * h, r = seg0 + rr, tok = r / a.G;
             if (r >= R) continue;
             if (whole) {
               const float inv = l[i][h] == 0.f ? 0.f : 1.f / l[i][h];     // (no key seen: zeros)
@@ -531,13 +542,25 @@ struct Shape {
   long long segments;
   bool direct;
 };
-Shape shape_of(int B, int rows, int G, int Hkv, int hd, int page, int width) {
+// (tokens: at most so many in the sequences)
+Shape shape_of(int B, int rows, int G, int Hkv, int hd, int page, int width, int64_t tokens) {
   Shape s;
-  s.tiles = hd == 64 && rows * G > 16 ? 2 : 1;
-  s.MT = ceil_div(rows * G, 16 * s.tiles);
   s.longest = std::max(1, ceil_div(width * page, kUnitBytes / (4 * hd)));
-  s.segments = (long long)B * Hkv * s.MT;
+  auto split = [&](int tiles) {
+    s.tiles = tiles;
+    s.MT = ceil_div(rows * G, 16 * tiles);
+    s.segments = (long long)B * Hkv * s.MT;
+  };
+  split(hd == 64 && rows * G > 16 ? 2 : 1);
   s.direct = s.longest <= kDirect && s.segments <= (hd == 64 && s.tiles == 1 ? kCtasPerSm<64, 1> : 2) * device_sms();
+  // Tiles that take turns pay where the second read of the keys would be one from DRAM: a cache larger than the L2
+  // (8 rows, 32 heads over 8, one tile and turns, us: 128 sequences of 512 to 8,192  685  450, 64 of 128 to 1,024  60  53; 8
+  // heads over 2: 64 of 2,000, 131 MB  42.3  41.6, 16 of them  18.5  21.6); an odd tile would be read with nothing beside it
+  // (24 heads over 4, 32 of 1,000 to 4,000: 66  77)
+  if (hd == 128 && s.MT % 2 == 0 && !s.direct && tokens * Hkv * hd * 4 > kL2Bytes) {
+    split(2);
+    s.longest *= 2;
+  }
   return s;
 }
 
@@ -552,15 +575,18 @@ int launch(Args a, const Shape& sh, void* work, cudaStream_t s) {
   // no more CTAs than the longest list that the table could hold fills
   const int grid = (int)(sh.direct ? sh.segments : std::min<long long>(kCtasPerSm<HD, TILES> * device_sms(),
                                                                        std::max(1ll, sh.segments * (sh.longest + kExtra) / kMinUnits)));
+  // few segments in many pieces: a row of one for each of more blocks (2 sequences of 4000, 8 heads over 2, 8 rows, with 4, 8
+  // and 16 blocks: 20.2, 15.1, 13.1 us; 128 of 512 to 8192, 32 heads over 8: 685, 686, 691)
+  const int by = (int)std::min<long long>(16, std::max(4ll, 2 * grid / sh.segments));
   static PerDevice attr;
   set_smem_attr(attr, k_paged<T, HD, TILES>, kSmem<HD, TILES>);
   launch_cluster(k_paged<T, HD, TILES>, dim3(grid), dim3(kThreads), kSmem<HD, TILES>, 1, false, s, a);
-  if (!sh.direct && grid > 1) launch_cluster(k_join<T, HD, TILES>, dim3(grid, std::min(4, a.rows * a.G)), dim3(kJoinThreads), 0, 1, true, s, a);
+  if (!sh.direct && grid > 1) launch_cluster(k_join<T, HD, TILES>, dim3(grid, std::min(by, a.rows * a.G)), dim3(kJoinThreads), 0, 1, true, s, a);
   return launched("kf_op_paged_attention");
 }
 template <typename T>
 int launch_any(int hd, const Args& a, const Shape& sh, void* work, cudaStream_t s) {
-  if (hd == 128) return launch<T, 128, 1>(a, sh, work, s);
+  if (hd == 128) return sh.tiles == 2 ? launch<T, 128, 2>(a, sh, work, s) : launch<T, 128, 1>(a, sh, work, s);
   return sh.tiles == 2 ? launch<T, 64, 2>(a, sh, work, s) : launch<T, 64, 1>(a, sh, work, s);
 }
 // the arguments' sizes; nullptr if they are fine
@@ -579,7 +605,7 @@ using namespace kf;
 
 extern "C" int64_t kf_op_paged_attention_work(int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, int32_t page, int32_t width) {
   if (B <= 0 || sizes_fault(B, rows, Hq, Hkv, hd, page, width)) return 0;
-  if (shape_of(B, rows, Hq / Hkv, Hkv, hd, page, width).direct) return 0;
+  if (shape_of(B, rows, Hq / Hkv, Hkv, hd, page, width, 0).direct) return 0;
   return most_ctas() * (int64_t)(sizeof(Split) + 2 * (kMostRows * sizeof(float2) + kMostValues * sizeof(float)));
 }
 
@@ -594,7 +620,7 @@ extern "C" int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int3
   if (!(scale > 0.f) || std::isinf(scale)) return refuse(what, "scale is a positive number");
   if (B == 0) return KF_OK;
   const int G = Hq / Hkv;
-  const Shape sh = shape_of(B, rows, G, Hkv, hd, page, width);
+  const Shape sh = shape_of(B, rows, G, Hkv, hd, page, width, std::min((int64_t)B * width, n_pages) * page);
   if (!q || !out || !lens || (!work && !sh.direct) || (width && !table) || (n_pages && !pool)) return refuse(what, "a null array");
   if (!aligned(q, 16) || !aligned(pool, 16) || !aligned(out, 16) || !aligned(work, 256) || !aligned(table, 4) || !aligned(lens, 4))
     return refuse(what, "q, pool and out are 16-byte aligned, work 256-byte");

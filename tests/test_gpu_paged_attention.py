@@ -85,6 +85,19 @@ def test_matches_plain(sv, hd, dtype, lens, rows, Hq, Hkv):
     check(sv, *make(lens, rows, Hq, Hkv, hd, dtype, seed=len(lens) + rows))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("lens,rows,Hq,Hkv", [
+    ([20011, 5], 5, 32, 8), ([3000, 0, 1, 15, 16, 17, 4099], 8, 8, 2), ([700 + 37 * i for i in range(40)], 7, 8, 1),
+    (list(range(0, 2400, 7)), 3, 6, 1), ([9000, 4], 17, 1, 1), ([2500, 2, 33], 7, 16, 2), ([5001], 33, 2, 2), ([0, 0], 8, 8, 2),
+])
+@pytest.mark.parametrize("wide", [False, True])
+def test_many_rows_of_long_sequences(sv, dtype, lens, rows, Hq, Hkv, wide):
+    """Two and more tiles of 16 rows of a group, past what one CTA takes as a whole; tiles that are full, ragged
+    and without a partner.  wide: a cache past the L2's size, where two tiles share a segment."""
+    more = (140 << 20) // (16 * Hkv * 512) if wide else 0
+    check(sv, *make(lens, rows, Hq, Hkv, 128, dtype, seed=len(lens) + rows, spare=3 + more, extra_width=30 + -(-more // len(lens))))
+
+
 @pytest.mark.parametrize("page", [32, 48, 128])
 def test_page_sizes(sv, page):
     check(sv, *make([1, 47, 48, 49, 500, 1300], 2, 8, 2, 128, page=page, seed=page))

@@ -90,6 +90,10 @@ def test_paged_kernels(lib):
     # 32 query rows a pass at head_dim 64 only
     assert kernels(hd=64, rows=4, Hq=16)[0].endswith("64, 2>") and kernels(hd=64)[0].endswith("64, 1>")
     assert kernels(rows=8)[0].endswith("128, 1>")
+    # two tiles that take turns: an even number of them over a cache past the L2
+    large = dict(width=4096, n_pages=20000)
+    assert kernels(rows=8, **large)[0].endswith("128, 2>") and kernels(rows=16, **large)[0].endswith("128, 2>")
+    assert kernels(rows=4, **large)[0].endswith("128, 1>") and kernels(rows=12, **large)[0].endswith("128, 1>")
     assert paged(lib, B=0) == OK and not launches(lib)
 
 
