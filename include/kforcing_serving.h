@@ -151,7 +151,7 @@ int kf_op_pages_append(int32_t n, const int32_t* which, const int32_t* starts, i
 
 /*
  * Scores of R rows of logits [R][V] (type fp32, bf16 or fp16; rows `stride`
- * elements apart, at most 1 MiB each).  With x = logits * (1 / tau) in fp32, lse = log sum_v exp(x_v) and lp_v = x_v - lse:
+ * elements apart, at most 1 MiB each; log2(e) / tau a finite fp32 number).  With x = logits * (1 / tau) in fp32, lse = log sum_v exp(x_v) and lp_v = x_v - lse:
  *   logp[r] = lp_token, entropy[r] = -sum_v exp(lp_v) lp_v, lse[r], and the top
  *   alternatives: the `top` (0 .. 64, <= V) ids of the largest x, largest first, ties to the
  *   lowest id, in top_ids [R][top], their lp in top_logp [R][top].
@@ -164,7 +164,7 @@ int kf_op_pages_append(int32_t n, const int32_t* which, const int32_t* starts, i
  * (fp32 [R], NULL: zeros) the gradient of sum_r g_logp logp + g_entropy entropy:
  *   grad_v = (g_logp (1[v = token] - p_v) - g_entropy p_v (lp_v + entropy)) / tau, p = exp(lp),
  * in grad [R][V] (the logits' type, rows grad_stride apart; it may be the logits themselves).
- * Padding and bad tokens: g_logp counts as 0.  A row with every logit -inf: zeros;
+ * Padding and bad tokens: g_logp counts as 0; a p below 2^-126 is 0.  A row with every logit -inf: zeros;
  * with a NaN or +inf: NaN.
  * Errors: KF_E_ARG, KF_E_CUDA.
  */

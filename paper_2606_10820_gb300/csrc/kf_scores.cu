@@ -28,8 +28,8 @@
 // them is its place.  Where masks close too many groups, the threads' own maxima give the
 // bound; rows where the list would not fit all the same (ties in the hundreds) raise the bound.
 //
-// Measured: 4096 bf16 rows of 50257 in 100 us with eight alternatives (4.1 TB/s), 74 without (5.5); 8 fp32
-// rows 7.6; the gradient of 2048 bf16 rows 87 us (4.7 TB/s).
+// Measured: 4096 bf16 rows of 50257 in 96 us with eight alternatives (4.3 TB/s), 72 without (5.7); 8 fp32
+// rows 7.5; the gradient of 2048 bf16 rows 86 us (4.8 TB/s).
 #include <algorithm>
 #include <cooperative_groups.h>
 
@@ -58,7 +58,7 @@ constexpr int kMostRow = 8 * kResident * kBatch * 512 * 16;      // bytes of a r
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -300.f;   // 2^-300 is 0 in fp32: stands for -inf where it multiplies that 0
 constexpr float kRaise = 20.f;
-constexpr float kBig = 1e38f;      // references past it would overflow in base-2 units
+constexpr float kLarge = 16777216.f;      // 2^24: from there on the rounding of a reference in base-2 units passes 1
 
 struct Args {
   const void* logits;
@@ -83,23 +83,35 @@ __device__ __forceinline__ float ex2(float x) {
 
 // What scores are taken against: a logit `raw` that no element exceeds by more than
 // 2^kRaise.  (The maximum itself changes for some lane of a warp at almost every
-// vector; the entropy's cancellation, 2^-24 of kRaise, stays below 2e-6.)  A reference past kBig (a row at the type's lowest value) keeps its
-// differences in natural units until they are formed
+// vector; the entropy's cancellation, 2^-24 of kRaise, stays below 2e-6.)  In base-2 units one fused
+// multiply-add gives an element's difference, and what the reference lost in rounding is a factor of S and T alike that
+// cancels; past kLarge (rows at a mask's value, a small tau) that factor would leave fp32's range,
+// so there the logits' difference is formed first and scaled after
 struct Ref {
-  float raw, nm;                   // nm: minus the reference, base-2 units (natural where big)
+  float raw, nm;                   // nm: minus the reference, base-2 units (a logit where big)
   float limit;                     // a logit past this raises the reference
   bool big;
+  static __device__ __forceinline__ bool large(const Args& a, float r) {
+    const float m = fabsf(r * a.inv_tau);
+    return m >= kLarge && m < INFINITY;
+  }
   __device__ __forceinline__ void set(const Args& a, float r) {
     const float m = r * a.inv_tau;
     raw = r;
     limit = r == -INFINITY ? r : r + a.margin;
-    big = fabsf(m) > kBig && fabsf(m) < INFINITY;
-    nm = m == -INFINITY ? 0.f : big ? -m : -__fmul_rn(r, a.c2);
+    big = large(a, r);
+    nm = m == -INFINITY ? 0.f : big ? -r : -__fmul_rn(r, a.c2);
   }
   __device__ __forceinline__ bool open(const Args& a) const { return raw * a.inv_tau != -INFINITY; }
   // log2 of exp(x - m)
   __device__ __forceinline__ float less(const Args& a, float v) const {
-    return big ? fmaf(v, a.inv_tau, nm) * kLog2e : fmaf(v, a.c2, nm);
+    return big ? (v + nm) * a.c2 : fmaf(v, a.c2, nm);
+  }
+  // log2 of exp(m' - m) for an open reference m' of the logit `from`, both as they were rounded
+  __device__ __forceinline__ float less_ref(const Args& a, float from) const {
+    if (large(a, from)) return less(a, from);
+    const float was = __fmul_rn(from, a.c2);
+    return big ? fmaf(nm, a.c2, was) : __fadd_rn(was, nm);      // (no fused multiply-add)
   }
 };
 
@@ -109,9 +121,7 @@ struct Sums {
   float raw, s, t;
   // against the reference r (at or above this one)
   __device__ __forceinline__ void move_to(const Args& a, const Ref& r) {
-    // (the difference of the two references as they were rounded: no fused multiply-add)
-    const float by = r.big ? r.less(a, raw) : __fadd_rn(__fmul_rn(raw, a.c2), r.nm);
-    const float d = raw * a.inv_tau == -INFINITY ? 0.f : fmaxf(by, kLeast), f = ex2(d);
+    const float d = raw * a.inv_tau == -INFINITY ? 0.f : fmaxf(r.less_ref(a, raw), kLeast), f = ex2(d);
     t = f * fmaf(d, s, t);
     s *= f;
     raw = r.raw;
@@ -128,8 +138,7 @@ struct Pass {
     const Ref was = r;
     r.set(a, to);
     if (was.open(a)) {
-      const float by = r.big ? r.less(a, was.raw) : was.big ? -INFINITY : __fsub_rn(r.nm, was.nm);
-      const float d = fmaxf(by, kLeast), f = ex2(d);
+      const float d = fmaxf(r.less_ref(a, was.raw), kLeast), f = ex2(d);
       t = mul_f2(f2(f, f), fma_f2(f2(d, d), s, t));
       s = mul_f2(f2(f, f), s);
     }
@@ -146,13 +155,13 @@ struct Pass {
     for (int i = 2; i < N; i += 2) top = max3f(top, v[i], v[i + 1]);
     most = fmaxf(most, top);
     if (top > r.limit) raise(a, top);
+    const uint64_t c = f2(a.c2, a.c2), nm = f2(r.nm, r.nm);
     if (!r.big) {
-      const uint64_t c = f2(a.c2, a.c2), nm = f2(r.nm, r.nm);
 #pragma unroll
       for (int i = 0; i < N; i += 2) pair(f2_split(fma_f2(f2(v[i], v[i + 1]), c, nm)));
     } else {
 #pragma unroll
-      for (int i = 0; i < N; i += 2) pair(make_float2(r.less(a, v[i]), r.less(a, v[i + 1])));
+      for (int i = 0; i < N; i += 2) pair(f2_split(mul_f2(add_f2(f2(v[i], v[i + 1]), nm), c)));
     }
   }
   __device__ __forceinline__ void add_one(const Args& a, float v) {
@@ -205,10 +214,11 @@ struct Scores {
   float logs, lse, H;              // log2 S; H: the entropy
   bool none, bad;                  // every token closed; a NaN or +inf in the row
   // log p of a logit: from the difference to the reference, not from lse, which loses log S where the
-  // reference is the type's lowest value (and in natural units where base-2 ones overflow)
+  // reference is large (the last form where a difference leaves fp32's range before it is scaled)
   __device__ __forceinline__ float lp(const Args& a, float v) const {
-    const float x = v * a.inv_tau;
-    return fabsf(x) > kBig ? (x - ref.raw * a.inv_tau) - logs * kLn2 : (ref.less(a, v) - logs) * kLn2;
+    const float d = ref.big ? v + ref.nm : ref.less(a, v);
+    if (fabsf(d) < INFINITY) return ref.big ? d * a.inv_tau - logs * kLn2 : (d - logs) * kLn2;
+    return (v * a.inv_tau - ref.raw * a.inv_tau) - logs * kLn2;
   }
 };
 // The row's sums against its largest reference, added in one fixed order; with `groups` the
@@ -620,7 +630,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
     auto pair = [&](float& x, float& y) {
       float2 d;
       if (!o.ref.big) d = f2_split(add_f2(fma_f2(f2(x, y), c2, nm), nlogs));      // (one constant for both would lose log S)
-      else d = make_float2(o.ref.less(a, x) - o.logs, o.ref.less(a, y) - o.logs);
+      else d = f2_split(add_f2(mul_f2(add_f2(f2(x, y), nm), c2), nlogs));
       d.x = fmaxf(d.x, kLeast);
       d.y = fmaxf(d.y, kLeast);
       const float2 g = f2_split(mul_f2(f2(ex2(d.x), ex2(d.y)), fma_f2(B2, f2(d.x, d.y), A2)));
@@ -719,7 +729,7 @@ int scores(const char* what, int32_t type, int64_t R, Args a, float tau, cudaStr
     return refuse(what, "the logits' type is fp32, bf16 or fp16");
   if (R < 0 || R > (1 << 28)) return refuse(what, "rows out of range");
   if (a.V < 1 || a.V > kMostRow / size || a.stride < a.V) return refuse(what, "vocabulary (a row is at most 1 MiB) or row stride out of range");
-  if (!(tau > 0.f) || !(1.f / tau > 0.f) || std::isinf(1.f / tau)) return refuse(what, "tau is a positive number");
+  if (!(tau > 0.f) || !(1.f / tau > 0.f) || std::isinf(1.f / tau * kLog2e)) return refuse(what, "tau is a positive number, and log2(e) / tau one of fp32's");
   if (a.top < 0 || a.top > kMaxTop || a.top > a.V) return refuse(what, "top is 0 to 64 and at most the vocabulary");
   if (R == 0) return KF_OK;
   if (!a.logits || !a.tokens || (a.top && (!a.top_ids || !a.top_logp))) return refuse(what, "a null array");
