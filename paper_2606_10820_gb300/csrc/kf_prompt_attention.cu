@@ -132,9 +132,10 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(int n, int T, int longest
         run += at_least[c];
       }
     }
+    // (all items; before the barrier, behind which at_least counts down)
+    if (round == 1 && hi > 0 && lo == 0) *plan.count = run;
     __syncthreads();
   }
-  if (t == 0) *plan.count = first[1] + at_least[1];
   // A sequence's place among all, those with more tiles first: class c has the places
   // at_least[c + 1] .. at_least[c] - 1, taken from the end.  It holds in every class up to its own
   for (int s0 = 0; s0 < n; s0 += 32) {              // warps take 32 sequences at a time
