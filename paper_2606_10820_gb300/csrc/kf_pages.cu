@@ -181,7 +181,8 @@ struct Team {
   }
 };
 
-__device__ __forceinline__ int pages_of(int len, int page) { return (len + page - 1) / page; }
+// (len + page - 1 may pass 32 bits)
+__device__ __forceinline__ int pages_of(int len, int page) { return len / page + (len % page != 0); }
 // Slot which[i] in range, and stamped with i.  (A slot listed twice holds the stamp of one of the two, so
 // after a barrier the other's check fails; the stamps need no clearing)
 template <int C>
