@@ -99,8 +99,10 @@ int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int
  * the table's columns, so a book and a call give one result.
  * A call that cannot be done as a whole (a slot out of range or twice in a
  * list, a length past width * page, pages run out, a table that contradicts the
- * references) sets KF_DEV_BAD_ROW, KF_DEV_NO_PAGES or KF_DEV_BAD_PAGE and
- * leaves book and pool as they were.
+ * references where the call looks) sets KF_DEV_BAD_ROW, KF_DEV_NO_PAGES or KF_DEV_BAD_PAGE and
+ * leaves book and pool as they were.  Free and fork look at the listed slots' rows, compact at the whole
+ * table, grow at the columns that it fills, which have to be -1: a page without references that a
+ * table still lists elsewhere is handed out again.
  *
  * kf_op_pages_grow: slot slots[i] (i < n, all different) gets pages for
  *   new_lens[i] >= lens tokens, and that length.

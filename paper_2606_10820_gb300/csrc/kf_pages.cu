@@ -231,23 +231,43 @@ __global__ void __launch_bounds__(kThreads, 1) k_grow(const Book k, int n, const
   team.offsets(n, w.off, more);
   int2 before, all;
   bad = team.exchange(bad, team.count_free(k), 0, &before, &all);
-  const int total = team.of(0)->total;
+  if (refused(team, bad, err)) return;
+  const int total = team.of(0)->total, warps = team.size >> 5;
+  team.list_free(k, min(total, all.x), before.x, w.src);
+  bad = twice(team, which, n, w.mark);
+  // f(place in the table, rank among the new pages) of every new column, then done(request): a warp's lanes hold a request
+  // each and take its one column, or all of them the columns of one after the other
+  auto columns = [&](auto f, auto done) {
+    for (int i0 = team.id >> 5; i0 < n; i0 += 32 * warps) {
+      const int i = i0 + warps * team.lane;
+      int s = 0, have = 0, add = 0, off = 0;
+      if (i < n) {
+        s = which[i];
+        have = pages_of(k.lens[s], k.page);
+        add = pages_of(new_lens[i], k.page) - have;
+        off = __ldcg(w.off + i);
+      }
+      if (add == 1) f((int64_t)s * k.width + have, off);
+      for (uint32_t wide = __ballot_sync(~0u, add > 1); wide; wide &= wide - 1) {
+        const int j = __ffs(wide) - 1, nj = __shfl_sync(~0u, add, j), oj = __shfl_sync(~0u, off, j);
+        const int64_t at = (int64_t)__shfl_sync(~0u, s, j) * k.width + __shfl_sync(~0u, have, j);
+        for (int c = team.lane; c < nj; c += 32) f(at + c, oj + c);
+      }
+      if (i < n) done(i);
+    }
+  };
+  // (a page there, as after a length that was lowered by hand, would be lost)
+  columns([&](int64_t at, int) { bad |= k.table[at] != -1 ? KF_DEV_BAD_PAGE : 0; }, [](int) {});
+  bad = team.exchange(bad);
   if (!bad && total > all.x) bad = KF_DEV_NO_PAGES;
   if (refused(team, bad, err)) return;
-  team.list_free(k, total, before.x, w.src);
-  bad = team.exchange(twice(team, which, n, w.mark));
-  if (refused(team, bad, err)) return;
-  // a warp per request
-  for (int i = team.id >> 5; i < n; i += team.size >> 5) {
-    const int s = which[i], have = pages_of(k.lens[s], k.page), need = pages_of(new_lens[i], k.page), off = __ldcg(w.off + i);
-    __syncwarp();
-    for (int c = have + team.lane; c < need; c += 32) {
-      const int p = __ldcg(w.src + off + c - have);
-      k.table[(int64_t)s * k.width + c] = p;
-      k.ref[p] = 1;
-    }
-    if (team.lane == 0) k.lens[s] = new_lens[i];
-  }
+  columns(
+      [&](int64_t at, int rank) {
+        const int p = __ldcg(w.src + rank);
+        k.table[at] = p;
+        k.ref[p] = 1;
+      },
+      [&](int i) { k.lens[which[i]] = new_lens[i]; });
   team.leave();
 }
 

@@ -156,6 +156,7 @@ static inline int __reduce_or_sync(unsigned, int v) {
 }
 template <typename T> static inline T __ldcg(const T* p) { return *p; }
 template <typename T> static inline T __ldg(const T* p) { return *p; }
+static inline int __ffs(int x) { return __builtin_ffs(x); }
 static inline int __popc(unsigned x) { return __builtin_popcount(x); }
 template <typename T> static inline T atomicAdd(T* p, T v) { const T r = *p; *p += v; return r; }
 template <typename T> static inline T atomicSub(T* p, T v) { const T r = *p; *p -= v; return r; }

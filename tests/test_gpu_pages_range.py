@@ -1,4 +1,5 @@
-"""The cache's pages at the end of the lengths' range (needs a GB300)."""
+"""The cache's pages at the end of the lengths' range, and rows that hold pages past their length
+(needs a GB300)."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +44,21 @@ def test_lengths_within_a_page_of_2_31(sv):
     sv.pages_fork(pool, *book, i32([1]), i32([2]))
     sv.status()
     assert torch.equal(table[2], table[1]) and (ref[:width] == 2).all() and lens[2].item() == length
+
+
+@pytest.mark.parametrize("n_pages", [400, 20000])      # a CTA, and a cluster
+def test_grow_refuses_columns_that_hold_a_page(sv, n_pages):
+    ref, table, lens = book = sv.new_book(n_pages, 5, 120)
+    sv.pages_grow(*book, i32([0, 1, 3]), i32([100, 16, 1000]))
+    sv.status()
+    lens[0] = 70
+    for slots, new in (([2, 0, 1], [16, 81, 17]), ([2, 0], [16, 1900])):
+        keep = [x.clone() for x in book]
+        sv.pages_grow(*book, i32(slots), i32(new))
+        with pytest.raises(Exception, match="flags 2$"):
+            sv.status()
+        assert all(torch.equal(a, b) for a, b in zip(keep, book))
+    lens[0] = 100
+    sv.pages_grow(*book, i32([2, 0, 1]), i32([16, 113, 17]))
+    sv.status()
+    assert table[2, 0].item() == 71 and table[0, 7].item() == 72 and table[1, 1].item() == 73 and lens.tolist() == [113, 17, 16, 1000, 0]

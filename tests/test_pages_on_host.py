@@ -115,3 +115,39 @@ def test_lengths_at_the_end_of_their_range(lib, page, width):
     b.table[0] = b.table[1]
     assert b.call("fork_", [0], [2]) == 0
     assert (b.table[2] == b.table[1]).all() and b.lens[2] == length and (b.ref[1: width + 1] == 2).all()
+
+
+@pytest.mark.parametrize("order", range(3))
+def test_grow_refuses_columns_that_hold_a_page(lib, order):
+    """A length lowered by hand leaves pages in the row; filling their columns would lose them."""
+    b = Book(lib, 400, 5, 120, 16)
+    assert b.call("grow", [0, 1, 3], [100, 16, 1000], order=order) == 0
+    b.lens[0] = 70                                     # (of 7 pages: 5 are left in use)
+    b.refused(BAD_PAGE, "grow", [2, 0, 1], [16, 81, 17], order=order)
+    b.refused(BAD_PAGE, "grow", [2, 0], [16, 1900], order=order)
+    b.lens[0] = 100
+    b.table[1, 1] = 399                                # a page that nobody holds
+    b.refused(BAD_PAGE, "grow", [1], [17], order=order)
+    b.table[1, 1], b.table[1, 60] = -1, -5
+    b.refused(BAD_PAGE, "grow", [0, 1, 2], [101, 1600, 5], order=order)
+    assert b.call("grow", [0, 1, 2], [101, 900, 5], order=order) == 0
+    b.refused(NO_PAGES, "grow", [4, 2, 3], [1920] * 3, order=order)
+
+
+@pytest.mark.parametrize("n", [40, 1500])
+def test_grow_of_many_slots(lib, n):
+    """More requests than a warp holds at once, with and without new pages."""
+    rng = np.random.default_rng(n)
+    b = Book(lib, 12 * n, n, 9, 4)
+    want = np.full((n, 9), -1, np.int32)
+    lens, used = np.zeros(n, np.int32), 0
+    for step in range(3):
+        which = rng.permutation(n)[: n - step]
+        new = np.minimum(36, lens[which] + rng.integers(0, [2, 15, 5][step], len(which)))
+        for s, x in zip(which, new):
+            for c in range(-(-lens[s] // 4), -(-x // 4)):
+                want[s, c] = used
+                used += 1
+            lens[s] = x
+        assert b.call("grow", which.tolist(), new.tolist(), order=step) == 0
+        assert (b.table == want).all() and (b.lens == lens).all() and (b.ref[:used] == 1).all() and (b.ref[used:] == 0).all()
