@@ -231,7 +231,8 @@ struct Pool {
     p = addr(t);
     layers = narrow(t.size(0), "pool");
     n_pages = narrow(pages, "pool");
-    page_bytes = t.stride(1) * (int64_t)t.element_size();
+    // (not t.stride(1): a dimension of one page may have any)
+    page_bytes = layers && n_pages ? t.numel() / layers / n_pages * (int64_t)t.element_size() : 0;
   }
 };
 
