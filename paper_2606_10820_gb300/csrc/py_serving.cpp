@@ -73,6 +73,8 @@ void* on(const at::Tensor& t, c10::Device dev, at::ScalarType type, at::IntArray
 int32_t* ints(PyObject* o, c10::Device dev, at::IntArrayRef shape, const char* name) {
   return static_cast<int32_t*>(on(tensor(o, name), dev, at::kInt, shape, name));
 }
+// the stride of a dimension; of one of a single element any will do, whatever the tensor says
+int64_t step(const at::Tensor& t, int64_t d) { return t.size(d) == 1 ? t.size(-1) : t.stride(d); }
 at::Tensor make(at::IntArrayRef shape, at::ScalarType type, c10::Device dev) {
   return at::Tensor(at::detail::empty_cuda(shape, type, dev, std::nullopt));      // (at::empty without the dispatcher)
 }
@@ -165,9 +167,9 @@ KF_PY(prompt_attention, 7) {
          "out: a tensor like q");
   }
   const Scratch work(kf_op_prompt_attention_work(n, T), dev);
-  if (failed(kf_op_prompt_attention(type, n, T, longest, narrow(Hq, "q"), narrow(Hkv, "k"), narrow(hd, "q"), addr(q), q.stride(0),
-                                    q.stride(1), addr(k), k.stride(0), k.stride(1), addr(v), v.stride(0), v.stride(1), addr(out),
-                                    out.stride(0), out.stride(1), starts, scale, work.ptr(), at.stream)))
+  if (failed(kf_op_prompt_attention(type, n, T, longest, narrow(Hq, "q"), narrow(Hkv, "k"), narrow(hd, "q"), addr(q), step(q, 0), step(q, 1),
+                                    addr(k), step(k, 0), step(k, 1), addr(v), step(v, 0), step(v, 1), addr(out), step(out, 0),
+                                    step(out, 1), starts, scale, work.ptr(), at.stream)))
     return nullptr;
   return THPVariable_Wrap(out);
 }
@@ -192,7 +194,7 @@ KF_PY(paged_attention, 6) {
   const int32_t b = narrow(B, "q"), r = narrow(rows, "q"), hq = narrow(Hq, "q"), hk = narrow(Hkv, "pool"), d = narrow(hd, "q"),
                 pg = narrow(page, "pool"), w = narrow(width, "table");
   const Scratch work(kf_op_paged_attention_work(b, r, hq, hk, d, pg, w), dev);
-  if (failed(kf_op_paged_attention(type, b, r, hq, hk, d, addr(q), q.stride(0), q.stride(1), q.stride(2), pp, n_pages, pg, tp, w, lp, scale,
+  if (failed(kf_op_paged_attention(type, b, r, hq, hk, d, addr(q), step(q, 0), step(q, 1), step(q, 2), pp, n_pages, pg, tp, w, lp, scale,
                                    op, work.ptr(), at.stream)))
     return nullptr;
   return THPVariable_Wrap(out);
@@ -310,8 +312,8 @@ KF_PY(pages_append, 7) {
   const int32_t *which = ints(a[6], dev, {(int64_t)n}, "slots"), *starts = ints(a[3], dev, {(int64_t)n + 1}, "starts");
   const int32_t *tp = ints(a[4], dev, {(int64_t)slots, (int64_t)width}, "table"), *lens = ints(a[5], dev, {(int64_t)slots}, "lens");
   const On at(dev);
-  return failed(kf_op_pages_append(n, which, starts, T, narrow(Hkv, "pool"), narrow(hd, "pool"), addr(k), k.stride(0), k.stride(1), addr(v),
-                                   v.stride(0), v.stride(1), addr(pool), narrow(pool.size(0), "pool"), narrow(pool.size(3), "pool"), tp,
+  return failed(kf_op_pages_append(n, which, starts, T, narrow(Hkv, "pool"), narrow(hd, "pool"), addr(k), step(k, 0), step(k, 1), addr(v),
+                                   step(v, 0), step(v, 1), addr(pool), narrow(pool.size(0), "pool"), narrow(pool.size(3), "pool"), tp,
                                    slots, width, lens, at.stream))
              ? nullptr
              : done();
