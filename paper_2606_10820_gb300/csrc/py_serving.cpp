@@ -10,6 +10,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
@@ -64,6 +65,16 @@ int32_t type_of(const at::Tensor& t, bool fp32, const char* what) {
   throw Refused{what};
 }
 void* addr(const at::Tensor& t) { return t.data_ptr(); }
+// the operators have no backward pass: what would need one is refused, not dropped
+bool wants_gradient(const at::Tensor& t) { return t.requires_grad() && at::GradMode::is_enabled(); }
+void plain(const at::Tensor& t, const char* name) {
+  if (wants_gradient(t))
+    throw Refused{std::string(name) + ": requires a gradient, which this call does not pass on (detach it, or call under torch.no_grad())"};
+}
+// a call has written the tensor: autograd is to see it
+void changed(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 // a contiguous tensor of this type and shape on the device
 void* on(const at::Tensor& t, c10::Device dev, at::ScalarType type, at::IntArrayRef shape, const char* name) {
   if (t.device() != dev || t.scalar_type() != type || t.sizes() != shape || !t.is_contiguous())
@@ -152,6 +163,9 @@ KF_PY(prompt_attention, 7) {
            v.scalar_type() == q.scalar_type() && k.device() == dev && v.device() == dev,
        "k and v: [T, Hkv, hd] of q's type and device");
   need(q.stride(2) == 1 && k.stride(2) == 1 && v.stride(2) == 1, "q, k and v: heads of contiguous elements");
+  plain(q, "q");
+  plain(k, "k");
+  plain(v, "v");
   const at::Tensor& st = tensor(a[3], "starts");
   need(st.dim() == 1 && st.size(0) >= 1, "starts: [n + 1]");
   const int32_t n = narrow(st.size(0) - 1, "starts"), longest = int32(a[4], "longest");
@@ -165,12 +179,14 @@ KF_PY(prompt_attention, 7) {
     out = tensor(a[6], "out");
     need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type() && out.device() == dev && out.stride(2) == 1,
          "out: a tensor like q");
+    plain(out, "out");
   }
   const Scratch work(kf_op_prompt_attention_work(n, T), dev);
   if (failed(kf_op_prompt_attention(type, n, T, longest, narrow(Hq, "q"), narrow(Hkv, "k"), narrow(hd, "q"), addr(q), step(q, 0), step(q, 1),
                                     addr(k), step(k, 0), step(k, 1), addr(v), step(v, 0), step(v, 1), addr(out), step(out, 0),
                                     step(out, 1), starts, scale, work.ptr(), at.stream)))
     return nullptr;
+  if (!none(a[6])) changed(out);
   return THPVariable_Wrap(out);
 }
 
@@ -188,15 +204,19 @@ KF_PY(paged_attention, 6) {
   const int32_t* tp = ints(a[2], dev, {B, width}, "table");
   const int32_t* lp = ints(a[3], dev, {B}, "lens");
   const float scale = scale_of(a[4], hd);
+  plain(q, "q");
+  plain(pool, "pool");
   const On at(dev);
   at::Tensor out = none(a[5]) ? make({B, rows, Hq, hd}, q.scalar_type(), dev) : tensor(a[5], "out");
   void* op = on(out, dev, q.scalar_type(), q.sizes(), "out");
+  plain(out, "out");
   const int32_t b = narrow(B, "q"), r = narrow(rows, "q"), hq = narrow(Hq, "q"), hk = narrow(Hkv, "pool"), d = narrow(hd, "q"),
                 pg = narrow(page, "pool"), w = narrow(width, "table");
   const Scratch work(kf_op_paged_attention_work(b, r, hq, hk, d, pg, w), dev);
   if (failed(kf_op_paged_attention(type, b, r, hq, hk, d, addr(q), step(q, 0), step(q, 1), step(q, 2), pp, n_pages, pg, tp, w, lp, scale,
                                    op, work.ptr(), at.stream)))
     return nullptr;
+  if (!none(a[5])) changed(out);
   return THPVariable_Wrap(out);
 }
 
@@ -205,7 +225,8 @@ struct Book {
   c10::Device dev;
   int32_t n_pages, slots, width;
   int32_t *ref, *table, *lens;
-  Book(PyObject* r, PyObject* t, PyObject* l) : dev(c10::kCPU) {
+  PyObject* parts[3];
+  Book(PyObject* r, PyObject* t, PyObject* l) : dev(c10::kCPU), parts{r, t, l} {
     const at::Tensor &rt = tensor(r, "ref"), &tt = tensor(t, "table");
     need(rt.is_cuda() && rt.dim() == 1 && tt.dim() == 2, "ref: [pages], table: [slots, width], int32 on a GPU");
     dev = rt.device();
@@ -216,6 +237,10 @@ struct Book {
     table = ints(t, dev, {(int64_t)slots, (int64_t)width}, "table");
     lens = l ? ints(l, dev, {(int64_t)slots}, "lens") : nullptr;
   }
+  void written() const {
+    for (PyObject* o : parts)
+      if (o) changed(THPVariable_Unpack(o));
+  }
 };
 // a list of int32 on the device; its length
 int32_t length(PyObject* o, const char* name) {
@@ -224,12 +249,14 @@ int32_t length(PyObject* o, const char* name) {
   return narrow(t.size(0), name);
 }
 struct Pool {
+  const at::Tensor& t;
   void* p;
   int32_t layers, n_pages;
   int64_t page_bytes;
-  Pool(const at::Tensor& t, c10::Device dev, int64_t pages) {
+  Pool(const at::Tensor& t_, c10::Device dev, int64_t pages) : t(t_) {
     need(t.dim() >= 3 && t.device() == dev && t.is_contiguous() && t.size(1) == pages,
          "pool: a contiguous [layers, pages, ...] tensor on the book's device");
+    plain(t, "pool");
     p = addr(t);
     layers = narrow(t.size(0), "pool");
     n_pages = narrow(pages, "pool");
@@ -245,10 +272,11 @@ KF_PY(pages_grow, 6) {
   const int32_t *which = ints(a[3], b.dev, {(int64_t)n}, "slots"), *lens = ints(a[4], b.dev, {(int64_t)n}, "new_lens");
   const On at(b.dev);
   const Scratch work(kf_op_pages_work(b.n_pages, b.slots, n), b.dev);
-  return failed(kf_op_pages_grow(n, which, lens, b.ref, b.n_pages, b.table, b.slots, b.width, b.lens, int32(a[5], "page"), work.ptr(),
-                                 at.stream))
-             ? nullptr
-             : done();
+  if (failed(kf_op_pages_grow(n, which, lens, b.ref, b.n_pages, b.table, b.slots, b.width, b.lens, int32(a[5], "page"), work.ptr(),
+                                 at.stream)))
+    return nullptr;
+  b.written();
+  return done();
 }
 // ref, table, lens, slots, page
 KF_PY(pages_free, 5) {
@@ -257,9 +285,10 @@ KF_PY(pages_free, 5) {
   const int32_t* which = ints(a[3], b.dev, {(int64_t)n}, "slots");
   const On at(b.dev);
   const Scratch work(kf_op_pages_work(b.n_pages, b.slots, n), b.dev);
-  return failed(kf_op_pages_free(n, which, b.ref, b.n_pages, b.table, b.slots, b.width, b.lens, int32(a[4], "page"), work.ptr(), at.stream))
-             ? nullptr
-             : done();
+  if (failed(kf_op_pages_free(n, which, b.ref, b.n_pages, b.table, b.slots, b.width, b.lens, int32(a[4], "page"), work.ptr(), at.stream)))
+    return nullptr;
+  b.written();
+  return done();
 }
 // pool, ref, table, lens, src, dst
 KF_PY(pages_fork, 6) {
@@ -271,10 +300,12 @@ KF_PY(pages_fork, 6) {
   const int32_t *src = ints(a[4], b.dev, {(int64_t)n}, "src"), *dst = ints(a[5], b.dev, {(int64_t)n}, "dst");
   const On at(b.dev);
   const Scratch work(kf_op_pages_work(b.n_pages, b.slots, n), b.dev);
-  return failed(kf_op_pages_fork(n, src, dst, b.ref, b.n_pages, b.table, b.slots, b.width, b.lens, narrow(t.size(4), "pool"), p.p, p.layers,
-                                 p.page_bytes, work.ptr(), at.stream))
-             ? nullptr
-             : done();
+  if (failed(kf_op_pages_fork(n, src, dst, b.ref, b.n_pages, b.table, b.slots, b.width, b.lens, narrow(t.size(4), "pool"), p.p, p.layers,
+                                 p.page_bytes, work.ptr(), at.stream)))
+    return nullptr;
+  b.written();
+  changed(p.t);
+  return done();
 }
 // pool, ref, table, live | None
 KF_PY(pages_compact, 4) {
@@ -283,9 +314,12 @@ KF_PY(pages_compact, 4) {
   int32_t* live = none(a[3]) ? nullptr : ints(a[3], b.dev, {1}, "live");
   const On at(b.dev);
   const Scratch work(kf_op_pages_work(b.n_pages, b.slots, 0), b.dev);
-  return failed(kf_op_pages_compact(b.ref, b.n_pages, b.table, b.slots, b.width, p.p, p.layers, p.page_bytes, live, work.ptr(), at.stream))
-             ? nullptr
-             : done();
+  if (failed(kf_op_pages_compact(b.ref, b.n_pages, b.table, b.slots, b.width, p.p, p.layers, p.page_bytes, live, work.ptr(), at.stream)))
+    return nullptr;
+  b.written();
+  changed(p.t);
+  if (!none(a[3])) changed(THPVariable_Unpack(a[3]));
+  return done();
 }
 // pool, src, dst
 KF_PY(pages_copy, 3) {
@@ -295,7 +329,9 @@ KF_PY(pages_copy, 3) {
   const int32_t n = length(a[1], "src");
   const int32_t *src = ints(a[1], t.device(), {(int64_t)n}, "src"), *dst = ints(a[2], t.device(), {(int64_t)n}, "dst");
   const On at(t.device());
-  return failed(kf_op_pages_copy(n, src, dst, p.p, p.layers, p.n_pages, p.page_bytes, at.stream)) ? nullptr : done();
+  if (failed(kf_op_pages_copy(n, src, dst, p.p, p.layers, p.n_pages, p.page_bytes, at.stream))) return nullptr;
+  changed(t);
+  return done();
 }
 // pool, k, v, starts, table, lens, slots
 KF_PY(pages_append, 7) {
@@ -308,15 +344,19 @@ KF_PY(pages_append, 7) {
   need(k.size(1) == Hkv && k.size(2) == hd && v.sizes() == k.sizes() && k.scalar_type() == pool.scalar_type() &&
            v.scalar_type() == pool.scalar_type() && k.device() == dev && v.device() == dev && k.stride(2) == 1 && v.stride(2) == 1,
        "k and v: rows of the pool's heads, type and device");
+  plain(pool, "pool");
+  plain(k, "k");
+  plain(v, "v");
   const int32_t n = length(a[6], "slots"), slots = narrow(table.size(0), "table"), width = narrow(table.size(1), "table");
   const int32_t *which = ints(a[6], dev, {(int64_t)n}, "slots"), *starts = ints(a[3], dev, {(int64_t)n + 1}, "starts");
   const int32_t *tp = ints(a[4], dev, {(int64_t)slots, (int64_t)width}, "table"), *lens = ints(a[5], dev, {(int64_t)slots}, "lens");
   const On at(dev);
-  return failed(kf_op_pages_append(n, which, starts, T, narrow(Hkv, "pool"), narrow(hd, "pool"), addr(k), step(k, 0), step(k, 1), addr(v),
+  if (failed(kf_op_pages_append(n, which, starts, T, narrow(Hkv, "pool"), narrow(hd, "pool"), addr(k), step(k, 0), step(k, 1), addr(v),
                                    step(v, 0), step(v, 1), addr(pool), narrow(pool.size(0), "pool"), narrow(pool.size(3), "pool"), tp,
-                                   slots, width, lens, at.stream))
-             ? nullptr
-             : done();
+                                   slots, width, lens, at.stream)))
+    return nullptr;
+  changed(pool);
+  return done();
 }
 
 // ------------------------------------------------------------------ scores
@@ -355,6 +395,7 @@ struct Logits {
 // logits, tokens, top, tau
 KF_PY(token_scores, 4) {
   Logits x(a[0], a[1]);
+  plain(x.t, "logits");
   const int32_t top = (int32_t)integer(a[2], "top: 0 to 64, and at most the vocabulary", 0, std::min(64, x.V));
   const float tau = number(a[3], "tau");
   const On at(x.dev);
@@ -378,9 +419,11 @@ KF_PY(token_scores, 4) {
 KF_PY(token_scores_grad, 6) {
   Logits x(a[0], a[1]);
   const float* g[2];
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < 2; ++i) {
     g[i] = none(a[2 + i]) ? nullptr
                           : static_cast<const float*>(on(tensor(a[2 + i], "g_logp, g_entropy"), x.dev, at::kFloat, {x.R}, "g_logp, g_entropy"));
+    if (g[i]) plain(THPVariable_Unpack(a[2 + i]), "g_logp, g_entropy");
+  }
   const float tau = number(a[4], "tau");
   const On at(x.dev);
   at::Tensor grad;
@@ -390,11 +433,13 @@ KF_PY(token_scores_grad, 6) {
     grad = tensor(a[5], "out");
     need(grad.scalar_type() == x.t.scalar_type() && grad.device() == x.dev && grad.sizes() == x.t.sizes() && (grad.stride(1) == 1 || x.V == 1),
          "out: a tensor like the logits");
+    need(!wants_gradient(grad) || !grad.is_leaf(), "out: a leaf that requires a gradient cannot be written (detach it, or call under torch.no_grad())");
   }
   x.outputs();
   if (failed(kf_op_token_scores_grad(x.type, x.R, x.V, addr(x.t), x.stride, x.tokens, tau, g[0], g[1], x.p(x.logp), x.p(x.entropy),
                                      x.p(x.lse), addr(grad), x.R > 1 ? grad.stride(0) : x.V, at.stream)))
     return nullptr;
+  if (!none(a[5])) changed(grad);
   PyObject* d = x.dict();
   put(d, "grad", grad);
   return d;

@@ -7,6 +7,11 @@ types, devices); what only the device can see is reported by ``status()``.
 Outputs and scratch come from torch's allocator, so they belong to the current
 stream; tensors that are made on another stream need that stream's work
 to be waited for, as with any torch operator.
+
+The operators have no backward pass of their own: a tensor that requires a gradient raises ``ValueError``
+while torch records gradients, instead of losing it.  ``token_scores_grad`` gives the logits' gradient
+explicitly, so its logits may require one (``logits.backward(out["grad"])``).  What a call changes in
+place counts up its version, so autograd notices a saved tensor that was written.
 """
 from __future__ import annotations
 
