@@ -3,8 +3,10 @@ _serving.so, the serving operators' Python binding, from csrc/py_serving.cpp
 against the installed torch.
 
 Objects go to ``_build/`` next to this file and the shared libraries
-beside it.  Translation units compile in parallel; the
-build is skipped when the sources, flags, compiler and torch are unchanged.
+beside it.  Translation units compile in parallel; each of the two is skipped when its
+sources, flags and compiler (the binding's torch and Python) are unchanged.  The library needs
+nvcc alone; where the binding's tools are missing the build says so and leaves it out, and
+``serving`` then raises when it is used.
 """
 from __future__ import annotations
 
@@ -44,14 +46,28 @@ def _sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
-def _torch() -> tuple:
-    """The installed torch's version and folder (found without importing it)."""
+def _torch():
+    """The installed torch's version and folder (found without importing it), or None."""
     import importlib.metadata
     import importlib.util
     spec = importlib.util.find_spec("torch")
     if spec is None or not spec.origin:
-        raise RuntimeError("torch is required to build the serving operators' binding")
+        return None
     return importlib.metadata.version("torch"), os.path.dirname(spec.origin)
+
+
+def binding_lacks():
+    """What the binding cannot be built without and is not here, or None."""
+    found = _torch()
+    if found is None:
+        return "torch"
+    if not os.path.exists(os.path.join(found[1], "lib", "libtorch_cuda.so")):
+        return "a torch with CUDA"
+    if not shutil.which("g++"):
+        return "g++"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python's headers"
+    return None
 
 
 def _compile_binding(nvcc: str) -> tuple:
@@ -77,19 +93,23 @@ def _link_binding(obj: str) -> None:
     os.replace(tmp, BINDING)
 
 
-def _digest(nvcc: str) -> str:
+def _digest(names, files) -> str:
     h = hashlib.sha256()
-    h.update(" ".join(ARCH + FLAGS).encode())
-    h.update(nvcc.encode())
-    h.update(os.uname().machine.encode())
-    h.update((_torch()[0] + sys.version).encode())
-    for f in _sources() + [BINDING_SRC] + sorted(glob.glob(os.path.join(CSRC, "*.cuh"))) + \
-            sorted(glob.glob(os.path.join(ROOT, "include", "*.h"))):
+    for x in names:
+        h.update(x.encode())
+    for f in files + sorted(glob.glob(os.path.join(CSRC, "*.cuh"))) + sorted(glob.glob(os.path.join(ROOT, "include", "*.h"))):
         if os.path.exists(f):
             h.update(f.encode())
             with open(f, "rb") as fh:
                 h.update(fh.read())
     return h.hexdigest()
+
+
+def _stamped(lib, stamp, digest) -> bool:
+    if not os.path.exists(lib) or not os.path.exists(stamp):
+        return False
+    with open(stamp) as f:
+        return f.read().strip() == digest
 
 
 def _compile(nvcc: str, src: str) -> tuple:
@@ -102,16 +122,18 @@ def _compile(nvcc: str, src: str) -> tuple:
 def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = nvcc_path()
     os.makedirs(BUILD, exist_ok=True)
-    stamp = os.path.join(BUILD, "stamp")
-    dig = _digest(nvcc)
-    if not force and os.path.exists(LIB) and os.path.exists(BINDING) and os.path.exists(stamp):
-        with open(stamp) as f:
-            if f.read().strip() == dig:
-                return LIB
-    srcs = _sources()
+    lacks = binding_lacks()
+    stamp, dig = os.path.join(BUILD, "stamp"), _digest(ARCH + FLAGS + [nvcc, os.uname().machine], _sources())
+    with_lib = force or not _stamped(LIB, stamp, dig)
+    if not lacks:
+        binding_stamp, binding_dig = os.path.join(BUILD, "stamp_serving"), _digest([*_torch(), sys.version, os.uname().machine], [BINDING_SRC])
+    with_binding = not lacks and (force or not _stamped(BINDING, binding_stamp, binding_dig))
+    if lacks:
+        sys.stderr.write(f"the serving operators' Python binding (_serving.so) is left out: {lacks} is missing\n")
+    srcs = _sources() if with_lib else []
     objs = []
     with cf.ThreadPoolExecutor(max_workers=min(len(srcs) + 1, os.cpu_count() or 4)) as ex:
-        binding = ex.submit(_compile_binding, nvcc)
+        binding = ex.submit(_compile_binding, nvcc) if with_binding else None
         for obj, rc, log, cmd in ex.map(lambda s: _compile(nvcc, s), srcs):
             with open(obj + ".log", "w") as f:
                 f.write(" ".join(cmd) + "\n" + log)
@@ -121,20 +143,25 @@ def build(force: bool = False, verbose: bool = False) -> str:
             if verbose:
                 sys.stderr.write(log)
             objs.append(obj)
-        binding_obj, rc, log, cmd = binding.result()
-        if rc != 0:
-            sys.stderr.write(log)
-            raise RuntimeError("g++ failed: " + " ".join(cmd))
-    tmp = LIB + ".tmp"
-    cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *objs, "-cudart", "static"]
-    p = subprocess.run(cmd, capture_output=True, text=True)
-    if p.returncode != 0:
-        sys.stderr.write(p.stdout + p.stderr)
-        raise RuntimeError("link failed: " + " ".join(cmd))
-    os.replace(tmp, LIB)
-    _link_binding(binding_obj)
-    with open(stamp, "w") as f:
-        f.write(dig)
+        if with_binding:
+            binding_obj, rc, log, cmd = binding.result()
+            if rc != 0:
+                sys.stderr.write(log)
+                raise RuntimeError("g++ failed: " + " ".join(cmd))
+    if with_lib:
+        tmp = LIB + ".tmp"
+        cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *objs, "-cudart", "static"]
+        p = subprocess.run(cmd, capture_output=True, text=True)
+        if p.returncode != 0:
+            sys.stderr.write(p.stdout + p.stderr)
+            raise RuntimeError("link failed: " + " ".join(cmd))
+        os.replace(tmp, LIB)
+        with open(stamp, "w") as f:
+            f.write(dig)
+    if with_binding:
+        _link_binding(binding_obj)
+        with open(binding_stamp, "w") as f:
+            f.write(binding_dig)
     return LIB
 
 

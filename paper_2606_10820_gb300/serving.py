@@ -32,7 +32,7 @@ def _load():
     lib = kf.load_library()
     lib.kf_op_status.argtypes, lib.kf_op_status.restype = [ctypes.c_void_p], ctypes.c_int
     if not os.path.exists(os.path.join(os.path.dirname(os.path.abspath(__file__)), "_serving.so")):
-        raise RuntimeError("_serving.so is missing: build it with __graft_entry__.build()")
+        raise RuntimeError("_serving.so is missing: build it with __graft_entry__.build() (with torch for CUDA, g++ and Python's headers)")
     from . import _serving
     _serving.set_check(kf._check)
     _m = _serving
