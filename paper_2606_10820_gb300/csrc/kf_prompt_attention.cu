@@ -766,13 +766,17 @@ extern "C" int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_
   // One sub-tile an item where that ends sooner: a key tile then takes kAlone clocks, in pairs kPaired for both, and
   // an item kItem more.  Where few long items leave SMs idle the longest item's chain is what a call takes (one of 4096, 8
   // heads of 64: 41.4 us alone, 51.1 in pairs; one of 7074: 109.6 and 82.9).  (Lengths are on the device: the
-  // estimate takes equal ones, and `longest` for the chain.)
+  // estimate takes equal ones, and `longest` for the chain.  That is only a bound, so what the longer chain would
+  // gain alone is set against what is lost if all sequences have the mean length: 64 of 512, 32 heads over 8 of 128, at
+  // a bound of 131,072: 283 us alone, 184 in pairs; 1,606 and 3,063, 8 heads of 128: 52.1 and 42.9.)
   const double kAlone = hd == 64 ? 2050 : 2800, kPaired = hd == 64 ? 2600 : 2860, kItem = 2500;
-  const double tiles = std::max<double>(1, (double)T / n / kRows), chain = std::max<double>(1, (double)longest / kRows);
+  const double tiles = std::max<double>(1, (double)T / n / kRows);
   const double items = n * (double)Hq * tiles / device_sms();      // sub-tiles of an SM
-  const double alone_clocks = std::max(chain * kAlone, items * ((tiles + 1) / 2 * kAlone + kItem));
-  const double paired_clocks = std::max(chain * kPaired, items / 2 * ((tiles + 1) / 2 * kPaired + kItem));
-  const bool alone = alone_clocks < paired_clocks;
+  auto alone_by = [&](double chain) {                              // the time in pairs over that alone
+    return std::max(chain * kPaired, items / 2 * ((tiles + 1) / 2 * kPaired + kItem)) / std::max(chain * kAlone, items * ((tiles + 1) / 2 * kAlone + kItem));
+  };
+  const double by_bound = alone_by(std::max<double>(1, (double)std::min<int64_t>(longest, T) / kRows)), by_mean = alone_by(tiles);
+  const bool alone = by_bound > 1 && by_bound * by_mean >= 1;
   const int heads = !alone && G % 2 == 0 ? 2 : 1, rows = alone || heads == 2 ? kRows : 2 * kRows;
   const int classes = std::max(1, ceil_div(longest, rows));
   const int direct = without_plan(n);
