@@ -81,7 +81,8 @@ int kf_op_prompt_attention(int32_t type, int32_t n, int64_t T, int32_t longest, 
  * the V of the newest rows reaches all of that sequence's rows.
  * A page id outside the pool: KF_DEV_BAD_PAGE, its keys count as unseen.
  * A length outside 0 .. width * page: KF_DEV_BAD_ROW, clamped.
- * The same lengths give the same bits, whatever the pages' order.
+ * The same lengths in a table of the same width and a pool of the same size give the same bits on one
+ * device, whatever the pages' order (a call's kernels and their split go by these).
  * Errors: KF_E_ARG, KF_E_CUDA.
  */
 int64_t kf_op_paged_attention_work(int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, int32_t page, int32_t width);
