@@ -238,9 +238,12 @@ struct Feed {
 };
 
 template <int HD, int TILES> constexpr int kMergeFloats = 16 * kHeld<HD, TILES> * (HD + 2);    // one warp's O, m and l
-// (two CTAs of 114,992 bytes, their static arrays and 1 KB each fit the SM's 228 KB; three of 74,096)
 template <int HD, int TILES>
 constexpr size_t kSmem = NW * kStages<HD, TILES> * kUnitBytes + (NW / 2) * kMergeFloats<HD, TILES> * 4 + NW * kStages<HD, TILES> * 4;
+// an SM's 228 KB hold the CTAs, their static arrays (find_part's, at most 128 bytes) and 1 KB for each
+template <int HD, int TILES> constexpr bool kFits = kCtasPerSm<HD, TILES> * (kSmem<HD, TILES> + 128 + 1024) <= 233472;
+static_assert(sizeof(Part) + NW * sizeof(long long) <= 128, "the static arrays");
+static_assert(kFits<64, 1> && kFits<64, 2> && kFits<128, 1> && kFits<128, 2>, "the CTAs of an SM");
 
 template <typename T, int HD, int TILES>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const Args a) {
