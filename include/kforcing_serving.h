@@ -105,6 +105,11 @@ int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int
  * table, grow at the columns that it fills, which have to be -1: a page without references that a
  * table still lists elsewhere is handed out again.
  *
+ * No call shortens a sequence.  Rows that are not all kept (a joint step's) take room ahead: grow to the
+ * kept tokens and those rows, and give append and paged attention lengths of the step's own, which may be
+ * below the book's; the next step's rows then overwrite what was not kept.  Fork shares every page that the
+ * book's length fills, so it wants a book whose length counts kept tokens only (before the first such step).
+ *
  * kf_op_pages_grow: slot slots[i] (i < n, all different) gets pages for
  *   new_lens[i] >= lens tokens, and that length.
  * kf_op_pages_free: the listed slots (all different) give up their pages:
