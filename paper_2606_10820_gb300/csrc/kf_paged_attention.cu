@@ -12,7 +12,7 @@
 //     evenly: a ragged batch and a single long sequence fill the SMs alike.  A segment counts
 //     kExtra units more than it has, for its start and end.  One that
 //     ends in another CTA than it began in leaves fp32 partials, which k_join
-//     adds in list order (so the same lengths give the same bits).
+//     adds in list order (so the same list gives the same bits).
 //   - In a CTA unit x belongs to warp x mod 4, which copies it into
 //     a ring of its own (cp.async, ahead of the products and across segment ends)
 //     and waits for nobody; the warps of a segment meet once, to merge.

@@ -10,8 +10,8 @@
 // fp32, in base-2 units: 2^d with d = x log2(e) - m log2(e).
 //
 // What bounds it: the logits' bytes, read once (scores) or read and written once
-// (gradient), and close behind them the instructions, about seven an element and pass, most of
-// the arithmetic on pairs (fma.rn.f32x2).  CTAs walk over the rows, and each thread streams its
+// (gradient), and close behind them the instructions: 8.3 an element without alternatives, 11.6 with
+// eight, ten a pass of the gradient, most of the arithmetic on pairs (fma.rn.f32x2).  CTAs walk over the rows, and each thread streams its
 // vectors through slots of shared memory that are its own (cp.async, batches of four; no thread
 // waits for another's), the next row's while this one is reduced.
 //   Scores: a ring of three batches a thread, four CTAs of 256 threads a SM (many rows that are
@@ -50,8 +50,8 @@ constexpr int kPairBytes = 13 * 512 * 16;    // gradient: slots of a CTA that le
 constexpr int kGroups = 64;        // groups whose maxima bound the n-th largest logit
 constexpr int kMaxTop = kGroups;
 // Alternatives that the groups' maxima bound well; for more, CTAs of over 64 threads take their
-// threads' own (4096 bf16 rows, groups and threads, us: 56 of 18000  110  147, 64 of them 303  154;
-// 56 of 50257  199  197, 64 of them 396  205)
+// threads' own (4096 bf16 rows, groups and threads, us: 56 of 18000  116  144, 64 of them 260  152;
+// 56 of 50257  190  191, 64 of them 380  198)
 constexpr int kFew = 56;
 template <int THREADS> constexpr int kList = THREADS == 64 ? 512 : 768;      // listed candidates of a row
 constexpr int kMostRow = 8 * kResident * kBatch * 512 * 16;      // bytes of a row: the gradient's slots in eight CTAs
@@ -694,13 +694,13 @@ template <typename T, bool GRAD>
 int launch(const Args& a, cudaStream_t s) {
   // Many rows that are not wide take CTAs of two warps, sixteen a SM (the gradient's ten): less of
   // a row's time goes to its joins (up to kFew alternatives, see there).  Measured on bf16 with two warps against wide CTAs, us:
-  //   scores, five alternatives   6000 of 304 rows  7.6  5.5, of 608  8.2  7.6, of 4096  23.8  38.6;
-  //                               18000 of 4096  44.5  54.9, 30000  69.0  69.7, 50257  104  96
-  //   without alternatives        50257 of 608  14.7  14.2, of 4096  72.7  81.4
-  //   gradient                    6000 of 304  7.6  5.6, of 608  7.8  9.5, of 4096  28.5  54.7
+  //   scores, five alternatives   6000 of 304 rows  7.2  5.3, of 608  7.8  7.2, of 4096  23.2  37.7;
+  //                               18000 of 4096  43.6  52.9, 30000  67.2  67.0, 50257  113  92
+  //   without alternatives        50257 of 608  14.4  13.5, of 4096  71.5  76.0
+  //   gradient                    6000 of 304  7.2  5.5, of 608  7.4  9.4, of 4096  29.7  54.1
   // Few rows are split over a cluster while half the SMs would idle and each thread keeps two
-  // vectors (50257, one CTA a row against the cluster: 8 rows 8.2  6.8, 32 rows 8.2  7.8, 64 rows 8.4
-  // 8.7, 128 rows 8.4  9.7; the gradient 8.8  6.2, 8.8  6.8, 8.9  8.2, 8.9  11.5); the gradient's
+  // vectors (50257, one CTA a row against the cluster: 8 rows 8.1  7.0, 32 rows 8.0  7.6, 64 rows 8.2
+  // 8.8, 128 rows 8.2  9.6; the gradient 8.4  6.1, 8.6  6.5, 8.5  8.1, 8.7  11.1); the gradient's
   // also until they fit the slots
   const int64_t bytes = (int64_t)a.V * sizeof(T), sms = device_sms();
   int cs = 1;
