@@ -1,8 +1,8 @@
 /*
  * kforcing_serving.h - serving operators of libkforcing.so for models with
- * grouped heads over a paged cache: attention of whole prompts and of the
- * newest rows, the cache's pages (room, append, fork, free, compact, copy), and scores of tokens
- * with their gradient.
+ * grouped heads over a paged cache: norms and rotary positions of heads, attention of whole prompts and of the
+ * newest rows (also of sequences that begin with the same tokens), the cache's pages (room, append, fork, free, compact, copy),
+ * scores of tokens with their gradient, and a policy loss with its own.
  *
  * Device pointers only, caller-owned; work is enqueued on `stream`
  * (cudaStream_t, NULL = legacy default) and nothing is allocated or
@@ -38,6 +38,47 @@ extern "C" {
 #define KF_DEV_TIMEOUT 4       /* a bounded wait ran out                         */
 #define KF_DEV_BAD_ROW 8       /* a slot, length or start out of range           */
 #define KF_DEV_NO_PAGES 32     /* not enough free pages                          */
+
+/*
+ * Norms and rotary positions of the query and key heads of T tokens.  A head x of hd (64 or 128) elements, bf16 or fp16:
+ *   y = x (mean(x^2) + eps)^-1/2 weight      (eps < 0: no norm, y = x; a NULL weight: ones),
+ * then its pairs (y_i, y_i+n), or with neighbours (y_2i, y_2i+1), i < n, turned by the angle pos freq[i]:
+ *   (a, b) -> (a cos - b sin, b cos + a sin);  elements 2 n .. hd - 1 stay as they are.
+ * n: n_freq, a multiple of 8, at most hd / 2 (0: norms alone).  freq: fp64 [n], on the device, finite and below 2^32
+ * in magnitude (NaN heads otherwise); pos: int32 [T], any values.  Angles are exact to 2^-24 of a
+ * turn's radius at every position; norms and products are fp32, rounded once to the type.  A sum of squares past fp32's range
+ * makes zeros.  Weights: [hd] of the heads' type, 16-byte aligned.
+ * q [T][Hq][hd] and k [T][Hkv][hd]: elements of a head contiguous, *_row / *_head the strides of tokens and heads in
+ * elements (multiples of 8); q_out and k_out likewise.  An output may be its input itself (same strides), and
+ * overlaps nothing else.
+ * kf_op_rotate_append: the same for new tokens of a paged cache, in one pass: rows starts[i] .. starts[i+1]-1 are the
+ * last tokens of slot which[i], as in kf_op_pages_append (below), at positions lens[slot] - count .. lens[slot] - 1, which
+ * are also the angles' positions.  q goes to q_out [T][Hq][hd], contiguous; k, rotated, and v, as it is,
+ * to the pool.  A token whose slot or position is out of range: KF_DEV_BAD_ROW, its q row is zeros and nothing goes to the pool; one
+ * whose page is: KF_DEV_BAD_PAGE, and only the pool is not written.
+ * kf_op_rotate_heads_grad: from dq and dk, the gradients of kf_op_rotate_heads' outputs, those of q and k (q_grad [T][Hq][hd],
+ * k_grad [T][Hkv][hd], contiguous) and of the weights (fp32 [hd], summed over tokens and heads in a
+ * fixed order; NULL: not wanted).  Without norms q and k are not read.
+ * Errors: KF_E_ARG, KF_E_CUDA.
+ */
+int kf_op_rotate_heads(int32_t type, int64_t T, int32_t Hq, int32_t Hkv, int32_t hd, const void* q, int64_t q_row,
+                       int64_t q_head, const void* k, int64_t k_row, int64_t k_head, const int32_t* pos,
+                       const double* freq, int32_t n_freq, int32_t neighbours, float eps, const void* q_weight,
+                       const void* k_weight, void* q_out, int64_t q_out_row, int64_t q_out_head, void* k_out,
+                       int64_t k_out_row, int64_t k_out_head, void* stream);
+int kf_op_rotate_append(int32_t type, int32_t n, const int32_t* which, const int32_t* starts, int64_t T, int32_t Hq,
+                        int32_t Hkv, int32_t hd, const void* q, int64_t q_row, int64_t q_head, const void* k,
+                        int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
+                        const double* freq, int32_t n_freq, int32_t neighbours, float eps, const void* q_weight,
+                        const void* k_weight, void* q_out, void* pool, int32_t n_pages, int32_t page,
+                        const int32_t* table, int32_t slots, int32_t width, const int32_t* lens, void* stream);
+int64_t kf_op_rotate_heads_grad_work(int64_t T, int32_t Hq, int32_t Hkv, int32_t hd);
+int kf_op_rotate_heads_grad(int32_t type, int64_t T, int32_t Hq, int32_t Hkv, int32_t hd, const void* dq, int64_t dq_row,
+                            int64_t dq_head, const void* dk, int64_t dk_row, int64_t dk_head, const void* q,
+                            int64_t q_row, int64_t q_head, const void* k, int64_t k_row, int64_t k_head,
+                            const int32_t* pos, const double* freq, int32_t n_freq, int32_t neighbours, float eps,
+                            const void* q_weight, const void* k_weight, void* q_grad, void* k_grad,
+                            float* q_weight_grad, float* k_weight_grad, void* work, void* stream);
 
 /*
  * Causal attention over n packed prompts: tokens starts[i] .. starts[i+1]-1 are
@@ -183,6 +224,29 @@ int kf_op_token_scores_grad(int32_t type, int64_t R, int32_t V, const void* logi
                             const int64_t* tokens, float tau, const float* g_logp, const float* g_entropy,
                             float* logp, float* entropy, float* lse, void* grad, int64_t grad_stride,
                             void* stream);
+
+/*
+ * The clipped policy loss of R rows and the gradient of its sum, in one pass over the logits (types, rows, strides, tau
+ * and refusals as above; tau is taken in 64 bits).  With lp = log p of the row's token, H the row's
+ * entropy, A its advantage, w its weight (NULL: 1), ratio = exp(lp - old_logp), u = ref_logp - lp and kl = e^u - 1 - u
+ * (an unbiased estimate of KL(p || ref) under tokens of p, never negative):
+ *   loss = w (kl_weight kl - min(ratio A, clip(ratio, 1 - clip_low, 1 + clip_high) A) - entropy_weight H),
+ *   grad = d loss / d logits  (where the clip decides, ratio A has no part in it; at its ends it has).
+ * old_logp, advantage, ref_logp, weight: fp32 [R]; ref_logp may be NULL where kl_weight is 0, and then no kl is
+ * written.  clip_low: 0 .. 1; clip_high: 0 or more, also infinity.  loss, logp, entropy, ratio, kl: fp32 [R]; grad
+ * as in kf_op_token_scores_grad (it may be the logits themselves).
+ * Rows that the loss leaves out have loss 0 and a gradient of zeros, whatever else they hold: a weight of 0, and padding
+ * (a negative token), whose logp and kl are 0 and whose ratio is 1.  A weight of a term that is 0
+ * leaves that term out.  A row with every logit -inf: a gradient of zeros.  A row with a NaN or +inf: NaN.  A token closed by
+ * -inf: ratio 0 and an infinite kl, which a kl_weight passes on to the loss (and NaN to the gradient).
+ * A token >= V: KF_DEV_BAD_TOKEN, NaN numbers, a gradient of zeros.
+ * Errors: KF_E_ARG, KF_E_CUDA.
+ */
+int kf_op_policy_loss(int32_t type, int64_t R, int32_t V, const void* logits, int64_t stride, const int64_t* tokens,
+                      double tau, const float* old_logp, const float* advantage, const float* ref_logp,
+                      const float* weight, float clip_low, float clip_high, float kl_weight, float entropy_weight,
+                      float* loss, float* logp, float* entropy, float* ratio, float* kl, void* grad,
+                      int64_t grad_stride, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,605 @@
+// Norms of query and key heads and their rotary positions (kf_op_rotate_heads), the same
+// with K and V rows to the pages of a cache (kf_op_rotate_append), and the
+// gradients (kf_op_rotate_heads_grad).
+//
+// A head x of hd elements: r = (mean x^2 + eps)^-1/2, y = x r w, and the pairs (y_i, y_i+n) (or
+// (y_2i, y_2i+1)), i < n, turned by t = pos freq_i: (a cos t - b sin t, b cos t + a sin t).  Back: g = R^T dy,
+//   dw = sum g xh,  dx = r (g w - xh mean(g w xh)),  xh = x r.
+//
+// Angles: freq_i / 2 pi turns as a fraction of 64 bits; times the position (mod 2^64) it leaves the
+// fraction of a turn with an error below pos 2^-64, where a product in fp32 would have lost the angle
+// from positions of a few thousand on.  The nearest quarter turn comes off in whole numbers, so the
+// sine and cosine are taken of |t| <= pi / 4.
+//
+// What bounds it: the heads, read and written once.  A warp takes a token: hd / 16 lanes a head (two 16-byte
+// vectors a lane, both elements of a pair in one lane), 4 or 8 heads a pass, the
+// next pass' loads ahead of this one's arithmetic; the token's angles are computed once by the
+// warp's lanes and passed on through shared memory.
+#include <algorithm>
+
+#include "kf_mma.cuh"
+#include "kf_serving.cuh"
+
+namespace kf {
+namespace {
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps;      // of a CTA
+constexpr int kAhead = 4;                   // passes whose loads are under way
+constexpr int kJoinThreads = 256;
+
+struct Rows {
+  const void* p;
+  int64_t row, head;
+};
+struct Out {
+  void* p;
+  int64_t row, head;
+};
+struct Book {
+  const int32_t *which, *starts, *table, *lens;
+  void* pool;
+  int64_t n_pages;
+  int n, page, slots, width;
+};
+struct Args {
+  Rows q, k, v, dq, dk;          // v: append; dq, dk: gradient
+  Out oq, ok;
+  const void *wq, *wk;
+  const int32_t* pos;
+  const double* freq;
+  float* part;                   // [CTAs][2][hd]: the weights' gradients
+  Book book;
+  int* err;
+  int64_t T;
+  int Hq, Hkv, n, split;         // n: pairs; split: warps of a token
+  float eps, sign;               // eps < 0: no norms; sign: -1 turns back
+};
+
+// freq / 2 pi mod 1 as a fraction of 64 bits: the mantissa times 2^66 / 2 pi (2^63 <= it < 2^64), shifted.  NaN,
+// infinities and |freq| >= 2^32: *bad
+__device__ __forceinline__ uint64_t turns_of(double freq, bool* bad) {
+  constexpr uint64_t k = 11743562013128004906ull;      // round(2^66 / 2 pi)
+  const uint64_t u = (uint64_t)__double_as_longlong(freq);
+  const int e = (int)(u >> 52) & 0x7ff;
+  const uint64_t m = (u & 0xfffffffffffffull) | (e ? 1ull << 52 : 0ull);
+  *bad = e >= 1023 + 32;
+  // m 2^(e - 1075) / 2 pi 2^64 = (m k) 2^(e - 1077): to the right by 22 and more
+  const uint64_t hi = __umul64hi(m, k), lo = m * k;
+  const int s = *bad ? 127 : 1077 - max(e, 1);
+  uint64_t t;
+  if (s < 64) t = (hi << (64 - s)) | (lo >> s);
+  else t = s < 128 ? hi >> (s - 64) : 0ull;
+  return (u >> 63) ? 0ull - t : t;
+}
+// (cos, sin) of pos times these turns
+__device__ __forceinline__ float2 turn(int pos, uint64_t turns, bool bad) {
+  const uint64_t a = (uint64_t)(int64_t)pos * turns;
+  const int q = (int)(((a >> 61) + 1) >> 1);                     // the nearest quarter turn (0 .. 4)
+  const int64_t rest = (int64_t)(a - ((uint64_t)q << 62));       // at most 2^61 away
+  float s, c;
+  sincospif((float)rest * 0x1p-63f, &s, &c);
+  if (q & 1) {
+    const float x = c;
+    c = -s;
+    s = x;
+  }
+  if (q & 2) {
+    c = -c;
+    s = -s;
+  }
+  return bad ? make_float2(NAN, NAN) : make_float2(c, s);
+}
+
+// Where a lane's two vectors lie in a head, and the first of its angles
+template <int HD, bool NB>
+struct Place {
+  static constexpr int LANES = HD / 16, PER = 32 / LANES;
+  int c0, c1, a0;                // vectors; angle (NB: of the first vector, the second's are HD / 4 on); < 0: none
+  __device__ __forceinline__ Place(int lane, int n) {
+    const int l = lane % LANES, n8 = n / 8;
+    if (NB) {
+      c0 = l;
+      c1 = l + LANES;
+      a0 = 4 * l;
+    } else if (l < n8) {
+      c0 = l;
+      c1 = l + n8;
+      a0 = 8 * l;
+    } else {
+      c0 = 2 * n8 + (l - n8);
+      c1 = c0 + (HD - 16 * n8) / 16;
+      a0 = HD / 2;               // past the angles: not turned
+    }
+  }
+};
+
+// A token's angles: computed by the warp, 8 pairs handed to each lane
+template <int HD, bool NB>
+struct Angles {
+  float c[8], s[8];
+  __device__ __forceinline__ void take(const Args& a, float2* tab, const Place<HD, NB>& pl, int pos, int lane) {
+    __syncwarp();                // (the token before is through with them)
+#pragma unroll
+    for (int i = lane; i < HD / 2; i += 32) {
+      float2 v = make_float2(1.f, 0.f);
+      if (i < a.n) {
+        bool bad;
+        const uint64_t t = turns_of(__ldg(a.freq + i), &bad);
+        v = turn(pos, t, bad);
+        v.y *= a.sign;
+      }
+      tab[i] = v;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const int i = NB ? pl.a0 + (e < 4 ? e : HD / 4 + e - 4) : pl.a0 + e;
+      float4 v = make_float4(1.f, 0.f, 1.f, 0.f);
+      if (i < HD / 2) v = *reinterpret_cast<const float4*>(tab + i);
+      c[e] = v.x;
+      s[e] = v.y;
+      c[e + 1] = v.z;
+      s[e + 1] = v.w;
+    }
+  }
+  // x: the lane's 16 elements of a head
+  __device__ __forceinline__ void turn_head(float* x) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float& a = x[NB ? 2 * e : e];
+      float& b = x[NB ? 2 * e + 1 : e + 8];
+      const float y = fmaf(a, c[e], -b * s[e]);
+      b = fmaf(b, c[e], a * s[e]);
+      a = y;
+    }
+  }
+};
+template <int LANES> __device__ __forceinline__ float sum_head(float v) {
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) v += __shfl_xor_sync(~0u, v, o);
+  return v;
+}
+template <typename T> __device__ __forceinline__ void unpack16(const uint4* u, float* x) {
+  Vec16<T>::unpack(u[0], x);
+  Vec16<T>::unpack(u[1], x + 8);
+}
+
+// The place of token t in its sequence's cache
+struct Where {
+  int pos;
+  int64_t row;                   // K's row of head 0 in the pool, in rows of hd; -1: not to be written
+  bool ok;                       // the position is known
+};
+__device__ __forceinline__ Where find(const Book& k, int Hkv, int64_t t, int lane, int* err) {
+  // the last sequence that starts at or before t: 32 starts a step
+  int lo = 0, left = k.n;
+  while (left > 1) {
+    const int step = (left + 31) / 32, at = lane * step;
+    const uint32_t m = __ballot_sync(~0u, at < left && __ldg(k.starts + lo + min(at, left - 1)) <= t);
+    const int i = max(0, 31 - __clz(m)) * step;
+    lo += i;
+    left = min(step, left - i);
+  }
+  const int first = __ldg(k.starts + lo), end = __ldg(k.starts + lo + 1), s = __ldg(k.which + lo);
+  Where w{0, -1, false};
+  int bad = 0;
+  if (t < first || t >= end || s < 0 || s >= k.slots) bad = KF_DEV_BAD_ROW;
+  else {
+    const int64_t pos = (int64_t)k.lens[s] - end + t;
+    if (pos < 0 || pos >= (int64_t)k.width * k.page) bad = KF_DEV_BAD_ROW;
+    else {
+      w.ok = true;
+      w.pos = (int)pos;
+      const int p = k.table[(int64_t)s * k.width + w.pos / k.page];
+      if (p < 0 || p >= k.n_pages) bad = KF_DEV_BAD_PAGE;
+      else w.row = (int64_t)p * 2 * Hkv * k.page + w.pos % k.page;
+    }
+  }
+  if (bad && lane == 0) atomicOr(err, bad);
+  return w;
+}
+
+template <typename T, int HD, bool NB, bool APPEND>
+__global__ void __launch_bounds__(kThreads) k_rotate(const Args a) {
+  __shared__ __align__(16) float2 tab[kWarps][HD / 2];
+  constexpr int LANES = HD / 16, PER = 32 / LANES;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane / LANES;
+  const int64_t w = (int64_t)blockIdx.x * kWarps + warp, t = w / a.split;
+  if (t >= a.T) return;
+  const int heads = a.Hq + a.Hkv * (APPEND ? 2 : 1), passes = (heads + PER - 1) / PER;
+  const Place<HD, NB> pl(lane, a.n);
+  const T* from[3] = {static_cast<const T*>(a.q.p) + t * a.q.row, static_cast<const T*>(a.k.p) + t * a.k.row,
+                      APPEND ? static_cast<const T*>(a.v.p) + t * a.v.row : nullptr};
+  const int p0 = (int)(w - t * a.split);
+  uint4 u[kAhead][2];
+  auto load = [&](int p, uint4* d) {
+    const int j = p * PER + grp;
+    if (j >= heads) return;
+    const T* x = j < a.Hq ? from[0] + j * a.q.head : !APPEND || j < a.Hq + a.Hkv ? from[1] + (j - a.Hq) * a.k.head
+                                                                                 : from[2] + (j - a.Hq - a.Hkv) * a.v.head;
+    d[0] = *reinterpret_cast<const uint4*>(x + 8 * pl.c0);
+    d[1] = *reinterpret_cast<const uint4*>(x + 8 * pl.c1);
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i)
+    if (p0 + i * a.split < passes) load(p0 + i * a.split, u[i]);
+  uint4 wq[2], wk[2];
+  if (a.wq) {
+    wq[0] = __ldg(reinterpret_cast<const uint4*>(a.wq) + pl.c0);
+    wq[1] = __ldg(reinterpret_cast<const uint4*>(a.wq) + pl.c1);
+  }
+  if (a.wk) {
+    wk[0] = __ldg(reinterpret_cast<const uint4*>(a.wk) + pl.c0);
+    wk[1] = __ldg(reinterpret_cast<const uint4*>(a.wk) + pl.c1);
+  }
+  Where at{0, -1, true};
+  if (APPEND) at = find(a.book, a.Hkv, t, lane, a.err);
+  else at.pos = __ldg(a.pos + t);
+  Angles<HD, NB> an;
+  an.take(a, tab[warp], pl, at.pos, lane);
+
+  for (int p = p0; p < passes; p += kAhead * a.split) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int pi = p + i * a.split, j = pi * PER + grp;
+      if (pi >= passes) break;                       // (uniform)
+      const bool is_q = j < a.Hq, is_v = APPEND && j >= a.Hq + a.Hkv;
+      uint4 o[2] = {u[i][0], u[i][1]};
+      if (p + (i + kAhead) * a.split < passes) load(p + (i + kAhead) * a.split, u[i]);
+      float x[16];
+      unpack16<T>(o, x);
+      if (a.eps >= 0.f) {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
+        const float r = rsqrtf(fmaf(sum_head<LANES>(ss), 1.f / HD, a.eps));
+        if (is_q ? a.wq != nullptr : a.wk != nullptr) {
+          float g[16];
+          const uint4 gw[2] = {is_q ? wq[0] : wk[0], is_q ? wq[1] : wk[1]};
+          unpack16<T>(gw, g);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] *= r * g[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] *= r;
+        }
+      }
+      an.turn_head(x);
+      if (!is_v) {
+        o[0] = Vec16<T>::pack(x);
+        o[1] = Vec16<T>::pack(x + 8);
+      }
+      if (j >= heads) continue;
+      T* to;
+      if (is_q) {
+        to = static_cast<T*>(a.oq.p) + t * a.oq.row + j * a.oq.head;
+        if (!at.ok) o[0] = o[1] = make_uint4(0u, 0u, 0u, 0u);
+      } else if (APPEND) {
+        // (V's heads follow K's in a page)
+        if (at.row < 0) continue;
+        to = static_cast<T*>(a.book.pool) + (at.row + (int64_t)(j - a.Hq) * a.book.page) * HD;
+      } else {
+        to = static_cast<T*>(a.ok.p) + t * a.ok.row + (j - a.Hq) * a.ok.head;
+      }
+      *reinterpret_cast<uint4*>(to + 8 * pl.c0) = o[0];
+      *reinterpret_cast<uint4*>(to + 8 * pl.c1) = o[1];
+    }
+  }
+}
+
+// Gradients: the warps walk over the tokens and keep the weights' sums in registers; each
+// CTA leaves its own, which k_join adds in one fixed order.
+template <typename T, int HD, bool NB>
+__global__ void __launch_bounds__(kThreads) k_back(const Args a) {
+  __shared__ __align__(16) float2 tab[kWarps][HD / 2];
+  __shared__ float sums[kWarps][2][HD];
+  constexpr int LANES = HD / 16, PER = 32 / LANES;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane / LANES;
+  const Place<HD, NB> pl(lane, a.n);
+  float acc[2][16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[0][e] = acc[1][e] = 0.f;
+  const int64_t step = (int64_t)gridDim.x * kWarps;
+  for (int64_t w = (int64_t)blockIdx.x * kWarps + warp; w < a.T * a.split; w += step) {
+    const int64_t t = w / a.split;
+    const int p0 = (int)(w - t * a.split);
+    Angles<HD, NB> an;
+    an.take(a, tab[warp], pl, __ldg(a.pos + t), lane);
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      const Rows &X = part ? a.k : a.q, &DY = part ? a.dk : a.dq;
+      const Out& O = part ? a.ok : a.oq;
+      const void* W = part ? a.wk : a.wq;
+      const int heads = part ? a.Hkv : a.Hq, passes = (heads + PER - 1) / PER;
+      float g[16];
+      if (W) {
+        const uint4 u[2] = {__ldg(reinterpret_cast<const uint4*>(W) + pl.c0), __ldg(reinterpret_cast<const uint4*>(W) + pl.c1)};
+        unpack16<T>(u, g);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) g[e] = 1.f;
+      }
+#pragma unroll 2
+      for (int p = p0; p < passes; p += a.split) {
+        const int j = p * PER + grp;
+        uint4 ux[2], ud[2];
+        if (j < heads) {
+          const T* x = static_cast<const T*>(X.p) + t * X.row + j * X.head;
+          const T* d = static_cast<const T*>(DY.p) + t * DY.row + j * DY.head;
+          ux[0] = *reinterpret_cast<const uint4*>(x + 8 * pl.c0);
+          ux[1] = *reinterpret_cast<const uint4*>(x + 8 * pl.c1);
+          ud[0] = *reinterpret_cast<const uint4*>(d + 8 * pl.c0);
+          ud[1] = *reinterpret_cast<const uint4*>(d + 8 * pl.c1);
+        } else {
+          ux[0] = ux[1] = ud[0] = ud[1] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        float x[16], d[16];
+        unpack16<T>(ux, x);
+        unpack16<T>(ud, d);
+        an.turn_head(d);
+        float ss = 0.f, sg = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          ss = fmaf(x[e], x[e], ss);
+          sg = fmaf(d[e] * g[e], x[e], sg);
+        }
+        const float r = rsqrtf(fmaf(sum_head<LANES>(ss), 1.f / HD, a.eps));
+        const float m = sum_head<LANES>(sg) * (1.f / HD) * r * r;
+        if (j >= heads) continue;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          acc[part][e] = fmaf(d[e] * r, x[e], acc[part][e]);
+          d[e] = r * fmaf(d[e], g[e], -m * x[e]);
+        }
+        T* to = static_cast<T*>(O.p) + t * O.row + j * O.head;
+        *reinterpret_cast<uint4*>(to + 8 * pl.c0) = Vec16<T>::pack(d);
+        *reinterpret_cast<uint4*>(to + 8 * pl.c1) = Vec16<T>::pack(d + 8);
+      }
+    }
+  }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (!a.part) return;
+#pragma unroll
+  for (int part = 0; part < 2; ++part)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float v = acc[part][e];
+#pragma unroll
+      for (int o = LANES; o < 32; o <<= 1) v += __shfl_xor_sync(~0u, v, o);
+      if (grp == 0) sums[warp][part][8 * (e < 8 ? pl.c0 : pl.c1) + (e & 7)] = v;
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * HD; i += kThreads) {
+    float v = 0.f;
+#pragma unroll
+    for (int x = 0; x < kWarps; ++x) v += sums[x][i / HD][i % HD];
+    a.part[(int64_t)blockIdx.x * 2 * HD + i] = v;
+  }
+}
+// Block b: columns 8 b .. 8 b + 7 of the weights' gradients, the CTAs' parts added in fixed order
+template <int HD>
+__global__ void __launch_bounds__(kJoinThreads) k_join(const float* part, int ctas, float* dwq, float* dwk) {
+  __shared__ float s[kJoinThreads / 8][8];
+  const int c = threadIdx.x % 8, y = threadIdx.x / 8, col = blockIdx.x * 8 + c;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  float v = 0.f;
+#pragma unroll 8
+  for (int i = y; i < ctas; i += kJoinThreads / 8) v += __ldcg(part + (int64_t)i * 2 * HD + col);
+  s[y][c] = v;
+  __syncthreads();
+#pragma unroll
+  for (int o = kJoinThreads / 16; o; o >>= 1) {
+    if (y < o) s[y][c] += s[y + o][c];
+    __syncthreads();
+  }
+  float* to = col < HD ? dwq : dwk;
+  if (y == 0 && to) to[col % HD] = s[0][c];
+}
+
+// ------------------------------------------------------------------ host
+constexpr int kBackCtasPerSm = 3;
+// Warps of a token: its passes over the heads are split while the SMs' warps are not filled
+int split_of(int64_t T, int passes, int warps_per_sm) {
+  const int64_t want = (int64_t)device_sms() * warps_per_sm;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(passes, want / std::max<int64_t>(T, 1)));
+}
+template <typename T, int HD, bool NB, bool APPEND>
+void launch_rotate(Args a, cudaStream_t s) {
+  const int heads = a.Hq + a.Hkv * (APPEND ? 2 : 1), per = 32 / (HD / 16);
+  a.split = split_of(a.T, ceil_div(heads, per), 32);
+  const int64_t warps = a.T * a.split;
+  launch_cluster(k_rotate<T, HD, NB, APPEND>, dim3((unsigned)((warps + kWarps - 1) / kWarps)), dim3(kThreads), 0, 1, false, s, a);
+}
+int back_ctas(int64_t T, int Hq, int Hkv, int hd, int* split) {
+  const int per = 32 / (hd / 16);
+  *split = split_of(T, std::max(ceil_div(Hq, per), ceil_div(Hkv, per)), kWarps * kBackCtasPerSm);
+  return (int)std::min<int64_t>((int64_t)kBackCtasPerSm * device_sms(), (T * *split + kWarps - 1) / kWarps);
+}
+template <typename T, int HD, bool NB>
+void launch_back(Args a, float* dwq, float* dwk, cudaStream_t s) {
+  const int grid = back_ctas(a.T, a.Hq, a.Hkv, HD, &a.split);
+  launch_cluster(k_back<T, HD, NB>, dim3(grid), dim3(kThreads), 0, 1, false, s, a);
+  if (a.part) launch_cluster(k_join<HD>, dim3(2 * HD / 8), dim3(kJoinThreads), 0, 1, true, s, (const float*)a.part, grid, dwq, dwk);
+}
+template <bool APPEND>
+void rotate_any(int type, int hd, bool nb, const Args& a, cudaStream_t s) {
+  auto by_type = [&](auto x) {
+    using T = decltype(x);
+    if (hd == 64) nb ? launch_rotate<T, 64, true, APPEND>(a, s) : launch_rotate<T, 64, false, APPEND>(a, s);
+    else nb ? launch_rotate<T, 128, true, APPEND>(a, s) : launch_rotate<T, 128, false, APPEND>(a, s);
+  };
+  if (type == KF_TYPE_BF16) by_type(__nv_bfloat16{});
+  else by_type(__half{});
+}
+void back_any(int type, int hd, bool nb, const Args& a, float* dwq, float* dwk, cudaStream_t s) {
+  auto by_type = [&](auto x) {
+    using T = decltype(x);
+    if (hd == 64) nb ? launch_back<T, 64, true>(a, dwq, dwk, s) : launch_back<T, 64, false>(a, dwq, dwk, s);
+    else nb ? launch_back<T, 128, true>(a, dwq, dwk, s) : launch_back<T, 128, false>(a, dwq, dwk, s);
+  };
+  if (type == KF_TYPE_BF16) by_type(__nv_bfloat16{});
+  else by_type(__half{});
+}
+
+// what all three entries ask for; nullptr if it is fine
+const char* fault(int32_t type, int64_t T, int32_t Hq, int32_t Hkv, int32_t hd, const double* freq, int32_t n_freq, float eps,
+                  const void* wq, const void* wk) {
+  if (type != KF_TYPE_BF16 && type != KF_TYPE_FP16) return "the type is bf16 or fp16";
+  if (hd != 64 && hd != 128) return "head_dim is 64 or 128";
+  if (T < 0 || T > 0x7fffffffll || Hq < 1 || Hkv < 1 || Hq > 4096 || Hkv > 4096) return "tokens or heads out of range";
+  if (n_freq < 0 || n_freq % 8 || 2 * n_freq > hd) return "frequencies: a multiple of 8, at most head_dim / 2";
+  if (!(eps < 0.f) && !(eps >= 0.f && !std::isinf(eps))) return "eps is a finite number (negative: no norms)";
+  if (eps < 0.f && (wq || wk)) return "weights belong to norms (eps is negative)";
+  if (n_freq && (!freq || !aligned(freq, 8))) return "frequencies: null or misaligned";
+  if (!aligned(wq, 16) || !aligned(wk, 16)) return "weights are 16-byte aligned";
+  return nullptr;
+}
+// one array of heads
+const char* rows_fault(const void* p, int64_t row, int64_t head) {
+  if (!p) return "a null array";
+  if (!aligned(p, 16)) return "arrays of heads are 16-byte aligned";
+  for (const int64_t s : {row, head})
+    if (s % 8 || s < 0 || s > (1ll << 37)) return "strides are multiples of 8 elements";
+  return nullptr;
+}
+
+}  // namespace
+}  // namespace kf
+
+using namespace kf;
+
+extern "C" int kf_op_rotate_heads(int32_t type, int64_t T, int32_t Hq, int32_t Hkv, int32_t hd, const void* q, int64_t q_row,
+                                  int64_t q_head, const void* k, int64_t k_row, int64_t k_head, const int32_t* pos,
+                                  const double* freq, int32_t n_freq, int32_t neighbours, float eps, const void* q_weight,
+                                  const void* k_weight, void* q_out, int64_t q_out_row, int64_t q_out_head, void* k_out,
+                                  int64_t k_out_row, int64_t k_out_head, void* stream) {
+  const char* what = "kf_op_rotate_heads";
+  if (const char* f = fault(type, T, Hq, Hkv, hd, freq, n_freq, eps, q_weight, k_weight)) return refuse(what, f);
+  if (T == 0) return KF_OK;
+  if (const char* f = rows_fault(q, q_row, q_head)) return refuse(what, f);
+  if (const char* f = rows_fault(k, k_row, k_head)) return refuse(what, f);
+  if (const char* f = rows_fault(q_out, q_out_row, q_out_head)) return refuse(what, f);
+  if (const char* f = rows_fault(k_out, k_out_row, k_out_head)) return refuse(what, f);
+  if (!pos || !aligned(pos, 4)) return refuse(what, "positions: null or misaligned");
+  if ((q_out == q && (q_out_row != q_row || q_out_head != q_head)) || (k_out == k && (k_out_row != k_row || k_out_head != k_head)))
+    return refuse(what, "an output over its input has its strides");
+  Args a{};
+  a.q = Rows{q, q_row, q_head};
+  a.k = Rows{k, k_row, k_head};
+  a.oq = Out{q_out, q_out_row, q_out_head};
+  a.ok = Out{k_out, k_out_row, k_out_head};
+  a.wq = q_weight;
+  a.wk = k_weight;
+  a.pos = pos;
+  a.freq = freq;
+  a.T = T;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.n = n_freq;
+  a.eps = eps;
+  a.sign = 1.f;
+  rotate_any<false>(type, hd, neighbours != 0, a, (cudaStream_t)stream);
+  return launched(what);
+}
+
+extern "C" int kf_op_rotate_append(int32_t type, int32_t n, const int32_t* which, const int32_t* starts, int64_t T, int32_t Hq,
+                                   int32_t Hkv, int32_t hd, const void* q, int64_t q_row, int64_t q_head, const void* k,
+                                   int64_t k_row, int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
+                                   const double* freq, int32_t n_freq, int32_t neighbours, float eps, const void* q_weight,
+                                   const void* k_weight, void* q_out, void* pool, int32_t n_pages, int32_t page,
+                                   const int32_t* table, int32_t slots, int32_t width, const int32_t* lens, void* stream) {
+  const char* what = "kf_op_rotate_append";
+  if (const char* f = fault(type, T, Hq, Hkv, hd, freq, n_freq, eps, q_weight, k_weight)) return refuse(what, f);
+  if (n < 0 || n_pages < 1 || slots < 1 || width < 0) return refuse(what, "sequences, pages, slots or width out of range");
+  if (page < 1 || page > (1 << 20) || (int64_t)width * page > 0x7fffffffll) return refuse(what, "page, or width * page, out of range");
+  if (T == 0) return KF_OK;
+  if (n == 0) return refuse(what, "tokens of no sequence");
+  if (!which || !starts || !pool || !lens || (width && !table)) return refuse(what, "a null array");
+  if (const char* f = rows_fault(q, q_row, q_head)) return refuse(what, f);
+  if (const char* f = rows_fault(k, k_row, k_head)) return refuse(what, f);
+  if (const char* f = rows_fault(v, v_row, v_head)) return refuse(what, f);
+  if (const char* f = rows_fault(q_out, (int64_t)Hq * hd, hd)) return refuse(what, f);
+  if (!aligned(pool, 16) || !aligned(which, 4) || !aligned(starts, 4) || !aligned(table, 4) || !aligned(lens, 4))
+    return refuse(what, "the pool is 16-byte aligned, the book's lists 4-byte");
+  Args a{};
+  a.q = Rows{q, q_row, q_head};
+  a.k = Rows{k, k_row, k_head};
+  a.v = Rows{v, v_row, v_head};
+  a.oq = Out{q_out, (int64_t)Hq * hd, hd};
+  a.wq = q_weight;
+  a.wk = k_weight;
+  a.freq = freq;
+  a.book = Book{which, starts, table, lens, pool, n_pages, n, page, slots, width};
+  a.T = T;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.n = n_freq;
+  a.eps = eps;
+  a.sign = 1.f;
+  if (!(a.err = serving_error_word())) return refuse(what, "no error word", KF_E_CUDA);
+  rotate_any<true>(type, hd, neighbours != 0, a, (cudaStream_t)stream);
+  return launched(what);
+}
+
+extern "C" int64_t kf_op_rotate_heads_grad_work(int64_t T, int32_t Hq, int32_t Hkv, int32_t hd) {
+  if (T < 1 || Hq < 1 || Hkv < 1 || (hd != 64 && hd != 128)) return 0;
+  int split;
+  return (int64_t)back_ctas(T, Hq, Hkv, hd, &split) * 2 * hd * (int64_t)sizeof(float);
+}
+
+extern "C" int kf_op_rotate_heads_grad(int32_t type, int64_t T, int32_t Hq, int32_t Hkv, int32_t hd, const void* dq, int64_t dq_row,
+                                       int64_t dq_head, const void* dk, int64_t dk_row, int64_t dk_head, const void* q,
+                                       int64_t q_row, int64_t q_head, const void* k, int64_t k_row, int64_t k_head,
+                                       const int32_t* pos, const double* freq, int32_t n_freq, int32_t neighbours, float eps,
+                                       const void* q_weight, const void* k_weight, void* q_grad, void* k_grad,
+                                       float* q_weight_grad, float* k_weight_grad, void* work, void* stream) {
+  const char* what = "kf_op_rotate_heads_grad";
+  if (const char* f = fault(type, T, Hq, Hkv, hd, freq, n_freq, eps, q_weight, k_weight)) return refuse(what, f);
+  const bool norm = !(eps < 0.f);
+  if ((q_weight_grad && !q_weight) || (k_weight_grad && !k_weight)) return refuse(what, "a weight's gradient wants the weight");
+  if (!aligned(q_weight_grad, 4) || !aligned(k_weight_grad, 4)) return refuse(what, "a weight's gradient is misaligned");
+  cudaStream_t s = (cudaStream_t)stream;
+  if (T == 0) {
+    for (float* g : {q_weight_grad, k_weight_grad})
+      if (g && cudaMemsetAsync(g, 0, hd * sizeof(float), s) != cudaSuccess) return launched(what);
+    return KF_OK;
+  }
+  if (const char* f = rows_fault(dq, dq_row, dq_head)) return refuse(what, f);
+  if (const char* f = rows_fault(dk, dk_row, dk_head)) return refuse(what, f);
+  if (norm)
+    if (const char* f = rows_fault(q, q_row, q_head)) return refuse(what, f);
+  if (norm)
+    if (const char* f = rows_fault(k, k_row, k_head)) return refuse(what, f);
+  if (const char* f = rows_fault(q_grad, (int64_t)Hq * hd, hd)) return refuse(what, f);
+  if (const char* f = rows_fault(k_grad, (int64_t)Hkv * hd, hd)) return refuse(what, f);
+  if (!pos || !aligned(pos, 4)) return refuse(what, "positions: null or misaligned");
+  const bool weights = q_weight_grad || k_weight_grad;
+  if (weights && (!work || !aligned(work, 256))) return refuse(what, "work is 256-byte aligned");
+  Args a{};
+  a.oq = Out{q_grad, (int64_t)Hq * hd, hd};
+  a.ok = Out{k_grad, (int64_t)Hkv * hd, hd};
+  a.pos = pos;
+  a.freq = freq;
+  a.T = T;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.n = n_freq;
+  a.eps = eps;
+  a.sign = -1.f;
+  if (!norm) {
+    // the gradient of a rotation is the rotation back
+    a.q = Rows{dq, dq_row, dq_head};
+    a.k = Rows{dk, dk_row, dk_head};
+    rotate_any<false>(type, hd, neighbours != 0, a, s);
+    return launched(what);
+  }
+  a.q = Rows{q, q_row, q_head};
+  a.k = Rows{k, k_row, k_head};
+  a.dq = Rows{dq, dq_row, dq_head};
+  a.dk = Rows{dk, dk_row, dk_head};
+  a.wq = q_weight;
+  a.wk = k_weight;
+  a.part = weights ? static_cast<float*>(work) : nullptr;
+  back_any(type, hd, neighbours != 0, a, q_weight_grad, k_weight_grad, s);
+  return launched(what);
+}

@@ -1,5 +1,6 @@
-// Scores of tokens under rows of logits (kf_op_token_scores) and their
-// gradient (kf_op_token_scores_grad).
+// Scores of tokens under rows of logits (kf_op_token_scores), their
+// gradient (kf_op_token_scores_grad), and the clipped policy loss with its gradient
+// (kf_op_policy_loss).
 //
 // With x = logits / tau and a reference m near max x, one pass over a row gives
 //   S = sum exp(x - m),  T = sum (x - m) exp(x - m),
@@ -60,6 +61,13 @@ constexpr float kLeast = -300.f;   // 2^-300 is 0 in fp32: stands for -inf where
 constexpr float kRaise = 20.f;
 constexpr float kLarge = 16777216.f;      // 2^24: from there on the rounding of a reference in base-2 units passes 1
 
+// the policy loss: its inputs and outputs of a row, its constants
+struct Policy {
+  const float *old_logp, *advantage, *ref_logp, *weight;
+  float *loss, *ratio, *kl;
+  float low, high;                 // the ratio's ends
+  float kl_weight, entropy_weight, c2_low;      // c2_low: what c2 lost in rounding
+};
 struct Args {
   const void* logits;
   int64_t stride;
@@ -72,6 +80,7 @@ struct Args {
   int V, top;
   float inv_tau, c2, margin;       // 1 / tau, log2(e) / tau, kRaise / c2
   int* err;
+  Policy pol;
 };
 
 // 2^x on the special-function unit: relative error about 2^-22
@@ -211,7 +220,7 @@ struct Shared {
 // A row's numbers, the same in all of its threads
 struct Scores {
   Ref ref;
-  float logs, lse, H;              // log2 S; H: the entropy
+  float s, logs, lse, H;           // S, log2 S; H: the entropy
   bool none, bad;                  // every token closed; a NaN or +inf in the row
   // log p of a logit: from the difference to the reference, not from lse, which loses log S where the
   // reference is large (the last form where a difference leaves fp32's range before it is scaled)
@@ -285,11 +294,86 @@ __device__ __forceinline__ Scores reduce_row(const Args& a, Shared<THREADS>& sh,
   }
   o.none = !o.ref.open(a) && x.x == 0.f;
   o.bad = !(x.x > 0.f) && !o.none;
+  o.s = x.x;
   o.logs = log2f(x.x);
   o.lse = o.none ? -INFINITY : o.bad ? NAN : o.ref.raw * a.inv_tau + o.logs * kLn2;
   o.H = o.none ? 0.f : o.bad ? NAN : (o.logs - x.y / x.x) * kLn2;
   return o;
 }
+// Sum of two numbers, and what its rounding lost
+__device__ __forceinline__ float2 two_sum(float x, float y) {
+  const float s = __fadd_rn(x, y), z = __fsub_rn(s, x);
+  return make_float2(s, __fadd_rn(__fsub_rn(x, __fsub_rn(s, z)), __fsub_rn(y, z)));
+}
+// The policy loss of a row: ratio = exp(lp - old), u = ref - lp,
+//   loss = w (kl_weight (e^u - 1 - u) - min(ratio A, clip(ratio) A) - entropy_weight H),
+// and its derivatives by lp and H.  The exponents are small differences of numbers of size ten and more, so
+// lp is kept in two parts: in one it would carry 5e-7 of rounding into ratio, and ten times as
+// much of its own size into the KL term.
+struct PolicyRow {
+  float logp, ratio, kl, loss, gl, gh;
+  bool left_out;                   // no part in the loss: padding, a weight of 0 (or a token outside the vocabulary)
+  __device__ __forceinline__ PolicyRow(const Args& a, const Scores& o, int64_t r, int64_t token, float at_logit) {
+    const Policy& p = a.pol;
+    const float w = p.weight ? p.weight[r] : 1.f;
+    const bool has = token >= 0 && token < a.V;
+    left_out = !has || w == 0.f;
+    logp = kl = gl = gh = loss = 0.f;
+    ratio = 1.f;
+    if (token >= a.V) logp = ratio = kl = loss = NAN;
+    if (!has) return;
+    // log2 p = (v - m) c - log2 S; S = 2^e f, 1 <= f < 2
+    float2 x;
+    if (o.bad) x = make_float2(NAN, 0.f);
+    else if (o.none) x = make_float2(-INFINITY, 0.f);
+    else {
+      const int bits = __float_as_int(o.s);       // (S is 1 at least: the reference is an element)
+      const float e = (float)((bits >> 23) - 127), f = __int_as_float((bits & 0x7fffff) | 0x3f800000);
+      float lo;
+      if (!o.ref.big) {
+        const float v = __fmul_rn(at_logit, a.c2);
+        x = two_sum(v, o.ref.nm);
+        lo = fmaf(at_logit, a.c2, -v);
+      } else {
+        const float d = at_logit + o.ref.nm;
+        x = make_float2(__fmul_rn(d, a.c2), 0.f);
+        lo = fmaf(d, a.c2, -x.x);
+      }
+      lo += x.y + fmaf(at_logit - o.ref.raw, p.c2_low, -log2f(f));
+      x = two_sum(x.x, -e);
+      x = two_sum(x.x, x.y + lo);
+      if (!(fabsf(x.x) < INFINITY)) x = make_float2(o.lp(a, at_logit) * kLog2e, 0.f);
+      // in natural units
+      constexpr float kLn2Low = -1.9046543e-9f;   // what kLn2 lost in rounding
+      const float h = __fmul_rn(x.x, kLn2);
+      if (fabsf(h) < INFINITY) x = make_float2(h, fmaf(x.x, kLn2, -h) + fmaf(x.y, kLn2, x.x * kLn2Low));
+      else x = make_float2(h, 0.f);
+    }
+    logp = x.x + x.y;
+    const float A = p.advantage[r];
+    ratio = expf((x.x - p.old_logp[r]) + x.y);
+    float em1 = 0.f;               // e^u - 1
+    if (p.ref_logp) {
+      const float u = (p.ref_logp[r] - x.x) - x.y;
+      if (fabsf(u) < 0.25f) {
+        // u^2 / 2 + u^3 / 6 + ... to u^8
+        kl = u * u * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, 1.f / 40320, 1.f / 5040), 1.f / 720), 1.f / 120), 1.f / 24), 1.f / 6), 0.5f);
+        em1 = u + kl;
+      } else {
+        em1 = expm1f(u);
+        kl = em1 == INFINITY ? em1 : em1 - u;
+      }
+    }
+    if (w == 0.f) return;
+    const float gain = A > 0.f ? fminf(ratio, p.high) * A : fmaxf(ratio, p.low) * A;
+    const bool open = A > 0.f ? ratio <= p.high : ratio >= p.low;
+    const float k = p.kl_weight == 0.f ? 0.f : p.kl_weight * kl, gk = p.kl_weight == 0.f ? 0.f : p.kl_weight * em1;
+    const float c = p.entropy_weight == 0.f ? 0.f : p.entropy_weight * o.H;
+    loss = w * (k - gain - c);
+    gl = w * (-gk - (open ? ratio * A : 0.f));
+    gh = -w * p.entropy_weight;
+  }
+};
 __device__ __forceinline__ void write_numbers(const Args& a, int64_t r, const Scores& o, int64_t token, float at_logit) {
   if (a.lse) a.lse[r] = o.lse;
   if (a.entropy) a.entropy[r] = o.H;
@@ -304,10 +388,10 @@ struct Extra {
   float at_logit, edge_logit;
   int edge_id;
   bool edge;
-  __device__ __forceinline__ Extra(const Args& a, const Row<T>& row, int64_t r, bool first_cta) {
+  __device__ __forceinline__ Extra(const Args& a, const Row<T>& row, int64_t r, bool first_cta, bool all = false) {
     const int t = threadIdx.x;
     token = a.tokens[r];
-    at_logit = t == 0 && token >= 0 && token < a.V ? to_f(row.p[token]) : 0.f;
+    at_logit = (all || t == 0) && token >= 0 && token < a.V ? to_f(row.p[token]) : 0.f;
     edge = first_cta && t < row.edge();
     edge_id = edge ? row.edge_id(t) : 0;
     edge_logit = edge ? to_f(row.p[edge_id]) : -INFINITY;
@@ -565,7 +649,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
 
 // ---------------------------------------------------------------- gradient
 static_assert(2 * (kPairBytes + sizeof(Shared<512>) + 1024) <= 233472, "two CTAs on an SM");
-template <typename T, int THREADS, int CS>
+template <typename T, int THREADS, int CS, bool POLICY>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const Args a) {
   extern __shared__ __align__(16) uint4 slots[];         // [vector][thread]
   __shared__ Shared<THREADS> sh;
@@ -591,7 +675,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
     const Row<T> row = row_at<T>(a, r);
     const bool more = r + step < a.R;
     const Row<T> next = row_at<T>(a, more ? r + step : r);
-    const Extra<T> ex(a, row, r, rank == 0);
+    const Extra<T> ex(a, row, r, rank == 0, POLICY);
     const int n = mine.have(row), n_next = mine.have(next);
     Pass ps;
 #pragma unroll
@@ -617,10 +701,27 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
     }
     if (ex.edge) ps.add_one(a, ex.edge_logit);
     const Scores o = reduce_row<THREADS, CS, false>(a, sh, ps);
-    if (rank == 0 && t == 0) write_numbers(a, r, o, ex.token, ex.at_logit);
-
-    const bool has = ex.token >= 0 && ex.token < a.V;
-    const float gl = has && a.g_logp ? a.g_logp[r] : 0.f, gh = a.g_entropy ? a.g_entropy[r] : 0.f;
+    float gl, gh;
+    bool zeros = false;                   // (uniform) a row that the loss leaves out, whatever it holds
+    if constexpr (POLICY) {
+      const PolicyRow p(a, o, r, ex.token, ex.at_logit);
+      gl = p.gl;
+      gh = p.gh;
+      zeros = p.left_out || o.none;
+      if (rank == 0 && t == 0) {
+        if (ex.token >= a.V) atomicOr(a.err, KF_DEV_BAD_TOKEN);
+        a.logp[r] = p.logp;
+        a.entropy[r] = o.H;
+        a.pol.loss[r] = p.loss;
+        a.pol.ratio[r] = p.ratio;
+        if (a.pol.kl) a.pol.kl[r] = p.kl;
+      }
+    } else {
+      if (rank == 0 && t == 0) write_numbers(a, r, o, ex.token, ex.at_logit);
+      const bool has = ex.token >= 0 && ex.token < a.V;
+      gl = has && a.g_logp ? a.g_logp[r] : 0.f;
+      gh = a.g_entropy ? a.g_entropy[r] : 0.f;
+    }
     // grad = p (A + B log2 p) + (v == token) gl / tau.  A row with a NaN has A = NaN; one
     // without open tokens p = 0
     const float A = (-gl - gh * o.H) * a.inv_tau, B = -gh * a.inv_tau * kLn2;
@@ -641,6 +742,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
     if (ex.edge) {
       float x = ex.edge_logit, y = -INFINITY;
       pair(x, y);
+      if (POLICY && zeros) x = 0.f;
       out[ex.edge_id] = from_f<T>(ex.edge_id == ex.token ? x + at_token : x);
     }
 #pragma unroll
@@ -653,6 +755,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
         const int id0 = row.head + (mine.first + j * THREADS) * N;
 #pragma unroll
         for (int e = 0; e < N; e += 2) pair(v[e], v[e + 1]);
+        if (POLICY && zeros) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) v[e] = 0.f;
+        }
         if (ex.token >= id0 && ex.token < id0 + N) {
 #pragma unroll
           for (int e = 0; e < N; ++e)
@@ -684,13 +790,15 @@ void launch_scores(const Args& a, cudaStream_t s) {
   static PerDevice attr;
   launch_rows<THREADS, CS>(k_scores<T, THREADS, CS>, attr, a, (size_t)kRing<THREADS> * kBatch * THREADS * 16, s);
 }
-template <typename T, int THREADS, int CS>
+template <typename T, int THREADS, int CS, bool POLICY>
 void launch_grad(const Args& a, cudaStream_t s) {
   static PerDevice attr;
   const int k = (a.V / Vec16<T>::N + CS * THREADS - 1) / (CS * THREADS);
-  launch_rows<THREADS, CS>(k_scores_grad<T, THREADS, CS>, attr, a, (size_t)k * THREADS * 16, s);
+  launch_rows<THREADS, CS>(k_scores_grad<T, THREADS, CS, POLICY>, attr, a, (size_t)k * THREADS * 16, s);
 }
-template <typename T, bool GRAD>
+enum Kind { SCORES, GRAD, POLICY };
+constexpr const char* kNames[] = {"kf_op_token_scores", "kf_op_token_scores_grad", "kf_op_policy_loss"};
+template <typename T, Kind K>
 int launch(const Args& a, cudaStream_t s) {
   // Many rows that are not wide take CTAs of two warps, sixteen a SM (the gradient's ten): less of
   // a row's time goes to its joins (up to kFew alternatives, see there).  Measured on bf16 with two warps against wide CTAs, us:
@@ -704,13 +812,13 @@ int launch(const Args& a, cudaStream_t s) {
   // also until they fit the slots
   const int64_t bytes = (int64_t)a.V * sizeof(T), sms = device_sms();
   int cs = 1;
-  if constexpr (GRAD) {
+  if constexpr (K != SCORES) {
     while (cs < 8 && (bytes > (int64_t)cs * kPairBytes || (a.R * cs * 2 <= sms && bytes >= cs * 2 * 2 * 512 * 16))) cs *= 2;
-    if (bytes <= 12288 && a.R > 2 * sms) launch_grad<T, 64, 1>(a, s);
-    else if (cs == 1) launch_grad<T, 512, 1>(a, s);
-    else if (cs == 2) launch_grad<T, 512, 2>(a, s);
-    else if (cs == 4) launch_grad<T, 512, 4>(a, s);
-    else launch_grad<T, 512, 8>(a, s);
+    if (bytes <= 12288 && a.R > 2 * sms) launch_grad<T, 64, 1, K == POLICY>(a, s);
+    else if (cs == 1) launch_grad<T, 512, 1, K == POLICY>(a, s);
+    else if (cs == 2) launch_grad<T, 512, 2, K == POLICY>(a, s);
+    else if (cs == 4) launch_grad<T, 512, 4, K == POLICY>(a, s);
+    else launch_grad<T, 512, 8, K == POLICY>(a, s);
   } else {
     while (cs < 8 && a.R * cs * 2 <= sms && bytes >= cs * 2 * 2 * 256 * 16) cs *= 2;
     if (a.R > 4 * sms && a.top <= kFew && bytes <= (a.top ? 49152 : 114688)) launch_scores<T, 64, 1>(a, s);
@@ -719,11 +827,12 @@ int launch(const Args& a, cudaStream_t s) {
     else if (cs == 4) launch_scores<T, 256, 4>(a, s);
     else launch_scores<T, 256, 8>(a, s);
   }
-  return launched(GRAD ? "kf_op_token_scores_grad" : "kf_op_token_scores");
+  return launched(kNames[K]);
 }
 
-template <bool GRAD>
-int scores(const char* what, int32_t type, int64_t R, Args a, float tau, cudaStream_t s) {
+template <Kind K>
+int scores(int32_t type, int64_t R, Args a, float tau, cudaStream_t s) {
+  const char* what = kNames[K];
   const int size = type == KF_TYPE_FP32 ? 4 : 2;
   if (type != KF_TYPE_FP32 && type != KF_TYPE_BF16 && type != KF_TYPE_FP16)
     return refuse(what, "the logits' type is fp32, bf16 or fp16");
@@ -734,15 +843,15 @@ int scores(const char* what, int32_t type, int64_t R, Args a, float tau, cudaStr
   if (R == 0) return KF_OK;
   if (!a.logits || !a.tokens || (a.top && (!a.top_ids || !a.top_logp))) return refuse(what, "a null array");
   if (!aligned(a.logits, size) || !aligned(a.tokens, 8)) return refuse(what, "an array is not aligned to its elements");
-  if (GRAD && (!a.grad || !aligned(a.grad, size) || a.grad_stride < a.V)) return refuse(what, "grad: null, misaligned or rows too near");
-  if (GRAD && a.grad == a.logits && a.grad_stride != a.stride) return refuse(what, "grad over the logits has their row stride");
+  if (K != SCORES && (!a.grad || !aligned(a.grad, size) || a.grad_stride < a.V)) return refuse(what, "grad: null, misaligned or rows too near");
+  if (K != SCORES && a.grad == a.logits && a.grad_stride != a.stride) return refuse(what, "grad over the logits has their row stride");
   a.inv_tau = 1.f / tau;
   a.c2 = a.inv_tau * kLog2e;
   a.margin = kRaise / a.c2;
   if (!(a.err = serving_error_word())) return refuse(what, "no error word", KF_E_CUDA);
-  if (type == KF_TYPE_FP32) return launch<float, GRAD>(a, s);
-  if (type == KF_TYPE_BF16) return launch<__nv_bfloat16, GRAD>(a, s);
-  return launch<__half, GRAD>(a, s);
+  if (type == KF_TYPE_FP32) return launch<float, K>(a, s);
+  if (type == KF_TYPE_BF16) return launch<__nv_bfloat16, K>(a, s);
+  return launch<__half, K>(a, s);
 }
 
 }  // namespace
@@ -753,14 +862,36 @@ using namespace kf;
 extern "C" int kf_op_token_scores(int32_t type, int64_t R, int32_t V, const void* logits, int64_t stride,
                                   const int64_t* tokens, float tau, int32_t top, float* logp, float* entropy,
                                   float* lse, int32_t* top_ids, float* top_logp, void* stream) {
-  Args a{logits, stride, tokens, nullptr, nullptr, logp, entropy, lse, top_logp, top_ids, nullptr, 0, R, V, top, 1.f, 1.f, 1.f, nullptr};
-  return scores<false>("kf_op_token_scores", type, R, a, tau, (cudaStream_t)stream);
+  Args a{logits, stride, tokens, nullptr, nullptr, logp, entropy, lse, top_logp, top_ids, nullptr, 0, R, V, top, 1.f, 1.f, 1.f, nullptr, {}};
+  return scores<SCORES>(type, R, a, tau, (cudaStream_t)stream);
 }
 
 extern "C" int kf_op_token_scores_grad(int32_t type, int64_t R, int32_t V, const void* logits, int64_t stride,
                                        const int64_t* tokens, float tau, const float* g_logp,
                                        const float* g_entropy, float* logp, float* entropy, float* lse,
                                        void* grad, int64_t grad_stride, void* stream) {
-  Args a{logits, stride, tokens, g_logp, g_entropy, logp, entropy, lse, nullptr, nullptr, grad, grad_stride, R, V, 0, 1.f, 1.f, 1.f, nullptr};
-  return scores<true>("kf_op_token_scores_grad", type, R, a, tau, (cudaStream_t)stream);
+  Args a{logits, stride, tokens, g_logp, g_entropy, logp, entropy, lse, nullptr, nullptr, grad, grad_stride, R, V, 0, 1.f, 1.f, 1.f, nullptr, {}};
+  return scores<GRAD>(type, R, a, tau, (cudaStream_t)stream);
+}
+
+extern "C" int kf_op_policy_loss(int32_t type, int64_t R, int32_t V, const void* logits, int64_t stride, const int64_t* tokens,
+                                 double tau, const float* old_logp, const float* advantage, const float* ref_logp,
+                                 const float* weight, float clip_low, float clip_high, float kl_weight, float entropy_weight,
+                                 float* loss, float* logp, float* entropy, float* ratio, float* kl, void* grad, int64_t grad_stride,
+                                 void* stream) {
+  const char* what = "kf_op_policy_loss";
+  if (!(clip_low >= 0.f) || !(clip_low <= 1.f) || !(clip_high >= 0.f)) return refuse(what, "clip: 0 to 1 below, 0 or more above");
+  if (!(std::fabs(kl_weight) < INFINITY) || !(std::fabs(entropy_weight) < INFINITY)) return refuse(what, "the terms' weights are finite");
+  if (kl_weight != 0.f && !ref_logp) return refuse(what, "the KL term wants ref_logp");
+  if (R > 0 && (!old_logp || !advantage || !loss || !logp || !entropy || !ratio || (ref_logp && !kl))) return refuse(what, "a null array");
+  for (const void* p : {(const void*)old_logp, (const void*)advantage, (const void*)ref_logp, (const void*)weight, (const void*)loss,
+                        (const void*)logp, (const void*)entropy, (const void*)ratio, (const void*)kl})
+    if (!aligned(p, 4)) return refuse(what, "an array is not aligned to its elements");
+  const double c = 1.4426950408889634074 / tau;
+  Args a{logits, stride, tokens, nullptr, nullptr, logp, entropy, nullptr, nullptr, nullptr, grad, grad_stride, R, V, 0, 1.f, 1.f, 1.f, nullptr,
+         Policy{old_logp, advantage, ref_logp, weight, loss, ratio, ref_logp ? kl : nullptr, 1.f - clip_low, 1.f + clip_high, kl_weight,
+                entropy_weight, 0.f}};
+  const float t32 = (float)tau;
+  if (t32 > 0.f) a.pol.c2_low = (float)(c - (double)(float)((1.f / t32) * kLog2e));
+  return scores<POLICY>(type, R, a, t32, (cudaStream_t)stream);
 }

@@ -45,14 +45,15 @@ int64_t integer(PyObject* o, const char* name, int64_t lo, int64_t hi) {
   return v;
 }
 int32_t int32(PyObject* o, const char* name) { return (int32_t)integer(o, name, INT32_MIN, INT32_MAX); }
-float number(PyObject* o, const char* name) {
+double real(PyObject* o, const char* name) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) {
     PyErr_Clear();
     throw Refused{std::string(name) + ": a number is wanted"};
   }
-  return (float)v;
+  return v;
 }
+float number(PyObject* o, const char* name) { return (float)real(o, name); }
 int32_t narrow(int64_t v, const char* name) {
   if (v > INT32_MAX) throw Refused{std::string(name) + ": too long"};
   return (int32_t)v;
@@ -83,6 +84,12 @@ void* on(const at::Tensor& t, c10::Device dev, at::ScalarType type, at::IntArray
 }
 int32_t* ints(PyObject* o, c10::Device dev, at::IntArrayRef shape, const char* name) {
   return static_cast<int32_t*>(on(tensor(o, name), dev, at::kInt, shape, name));
+}
+// a list of int32 on the device; its length
+int32_t length(PyObject* o, const char* name) {
+  const at::Tensor& t = tensor(o, name);
+  if (t.dim() != 1) throw Refused{std::string(name) + ": a list of int32 on the GPU is wanted"};
+  return narrow(t.size(0), name);
 }
 // the stride of a dimension; of one of a single element any will do, whatever the tensor says
 int64_t step(const at::Tensor& t, int64_t d) { return t.size(d) == 1 ? t.size(-1) : t.stride(d); }
@@ -147,6 +154,124 @@ KF_PY(set_check, 1) {
   Py_XDECREF(g_check);
   g_check = a[0];
   return done();
+}
+
+// ------------------------------------------------------ rotary positions
+// heads [T, H, hd] of contiguous elements; `like`: of its tokens, head size, type and device
+void heads(const at::Tensor& t, const at::Tensor* like, const char* name, const char* want) {
+  need(t.is_cuda() && t.dim() == 3 && t.stride(2) == 1, want);
+  if (like)
+    need(t.size(0) == like->size(0) && t.size(2) == like->size(2) && t.scalar_type() == like->scalar_type() && t.device() == like->device(), want);
+  plain(t, name);
+}
+// q, k, freq, q_weight | None, k_weight | None, eps | None, neighbours
+struct Turn {
+  const at::Tensor &q, &k;
+  c10::Device dev;
+  int64_t T;
+  int32_t type, Hq, Hkv, hd, n, neighbours;
+  const double* freq;
+  float eps;
+  const void* w[2];
+  Turn(PyObject* q_, PyObject* k_, PyObject* f, PyObject* wq, PyObject* wk, PyObject* e, PyObject* nb) : q(tensor(q_, "q")), k(tensor(k_, "k")), dev(q.device()) {
+    heads(q, nullptr, "q", "q: [T, Hq, hd] on a GPU, heads of contiguous elements");
+    type = type_of(q, false, "q and k: bf16 or fp16");
+    heads(k, &q, "k", "k: [T, Hkv, hd] of q's type and device, heads of contiguous elements");
+    T = q.size(0);
+    Hq = narrow(q.size(1), "q");
+    Hkv = narrow(k.size(1), "k");
+    hd = narrow(q.size(2), "q");
+    const at::Tensor& ft = tensor(f, "freq");
+    need(ft.dim() == 1, "freq: a list of fp64 on the GPU");
+    n = narrow(ft.size(0), "freq");
+    freq = static_cast<const double*>(on(ft, dev, at::kDouble, {(int64_t)n}, "freq"));
+    plain(ft, "freq");
+    int i = 0;
+    for (PyObject* o : {wq, wk}) {
+      const char* name = i ? "k_weight" : "q_weight";
+      w[i] = none(o) ? nullptr : on(tensor(o, name), dev, q.scalar_type(), {(int64_t)hd}, name);
+      if (w[i++]) plain(THPVariable_Unpack(o), name);
+    }
+    eps = none(e) ? -1.f : number(e, "eps");
+    need(none(e) || eps >= 0.f, "eps: 0 or more (None: no norms)");
+    neighbours = PyObject_IsTrue(nb);
+    if (neighbours < 0) throw python_error();
+  }
+  const int32_t* positions(PyObject* o) const { return ints(o, dev, {T}, "pos"); }
+};
+at::Tensor heads_out(PyObject* o, const at::Tensor& like, const char* name) {
+  if (none(o)) return make({like.size(0), like.size(1), like.size(2)}, like.scalar_type(), like.device());
+  const at::Tensor& t = tensor(o, name);
+  if (t.sizes() != like.sizes() || t.scalar_type() != like.scalar_type() || t.device() != like.device() || t.stride(2) != 1)
+    throw Refused{std::string(name) + ": a tensor like its input"};
+  plain(t, name);
+  return t;
+}
+// q, k, pos, freq, q_weight, k_weight, eps, neighbours, q_out | None, k_out | None
+KF_PY(rotate_heads, 10) {
+  const Turn x(a[0], a[1], a[3], a[4], a[5], a[6], a[7]);
+  const int32_t* pos = x.positions(a[2]);
+  const On at(x.dev);
+  const at::Tensor oq = heads_out(a[8], x.q, "q_out"), ok = heads_out(a[9], x.k, "k_out");
+  if (failed(kf_op_rotate_heads(x.type, x.T, x.Hq, x.Hkv, x.hd, addr(x.q), step(x.q, 0), step(x.q, 1), addr(x.k), step(x.k, 0), step(x.k, 1),
+                                pos, x.freq, x.n, x.neighbours, x.eps, x.w[0], x.w[1], addr(oq), step(oq, 0), step(oq, 1), addr(ok),
+                                step(ok, 0), step(ok, 1), at.stream)))
+    return nullptr;
+  if (!none(a[8])) changed(oq);
+  if (!none(a[9])) changed(ok);
+  PyObject *pq = THPVariable_Wrap(oq), *pk = THPVariable_Wrap(ok), *both = pq && pk ? PyTuple_Pack(2, pq, pk) : nullptr;
+  Py_XDECREF(pq);
+  Py_XDECREF(pk);
+  return both;
+}
+// q, k, v, pool, starts, table, lens, slots, freq, q_weight, k_weight, eps, neighbours
+KF_PY(rotate_append, 13) {
+  const Turn x(a[0], a[1], a[8], a[9], a[10], a[11], a[12]);
+  const at::Tensor &v = tensor(a[2], "v"), &pool = tensor(a[3], "pool"), &table = tensor(a[5], "table");
+  heads(v, &x.q, "v", "v: [T, Hkv, hd] of q's type and device, heads of contiguous elements");
+  need(v.size(1) == x.Hkv, "v: k's heads");
+  need(pool.dim() == 5 && pool.size(1) == 2 && table.dim() == 2, "pool: [pages, 2, Hkv, page, hd], table: [slots, width]");
+  void* pp = on(pool, x.dev, x.q.scalar_type(), {pool.size(0), 2, x.Hkv, pool.size(3), x.hd}, "pool");
+  plain(pool, "pool");
+  const int32_t n = length(a[7], "slots"), slots = narrow(table.size(0), "table"), width = narrow(table.size(1), "table");
+  const int32_t *which = ints(a[7], x.dev, {(int64_t)n}, "slots"), *starts = ints(a[4], x.dev, {(int64_t)n + 1}, "starts");
+  const int32_t *tp = ints(a[5], x.dev, {(int64_t)slots, (int64_t)width}, "table"), *lens = ints(a[6], x.dev, {(int64_t)slots}, "lens");
+  const On at(x.dev);
+  const at::Tensor oq = make({x.T, x.Hq, x.hd}, x.q.scalar_type(), x.dev);
+  if (failed(kf_op_rotate_append(x.type, n, which, starts, x.T, x.Hq, x.Hkv, x.hd, addr(x.q), step(x.q, 0), step(x.q, 1), addr(x.k),
+                                 step(x.k, 0), step(x.k, 1), addr(v), step(v, 0), step(v, 1), x.freq, x.n, x.neighbours, x.eps, x.w[0],
+                                 x.w[1], addr(oq), pp, narrow(pool.size(0), "pool"), narrow(pool.size(3), "pool"), tp, slots, width, lens,
+                                 at.stream)))
+    return nullptr;
+  changed(pool);
+  return THPVariable_Wrap(oq);
+}
+// dq, dk, q, k, pos, freq, q_weight, k_weight, eps, neighbours
+KF_PY(rotate_heads_grad, 10) {
+  const Turn x(a[2], a[3], a[5], a[6], a[7], a[8], a[9]);
+  const at::Tensor &dq = tensor(a[0], "dq"), &dk = tensor(a[1], "dk");
+  heads(dq, &x.q, "dq", "dq: a tensor like q");
+  heads(dk, &x.q, "dk", "dk: a tensor like k");
+  need(dq.size(1) == x.Hq && dk.size(1) == x.Hkv, "dq and dk: the heads of q and k");
+  const int32_t* pos = x.positions(a[4]);
+  const On at(x.dev);
+  const at::Tensor gq = make({x.T, x.Hq, x.hd}, x.q.scalar_type(), x.dev), gk = make({x.T, x.Hkv, x.hd}, x.q.scalar_type(), x.dev);
+  at::Tensor gw[2];
+  for (int i = 0; i < 2; ++i)
+    if (x.w[i]) gw[i] = make({x.hd}, at::kFloat, x.dev);
+  auto p = [&](int i) { return x.w[i] ? static_cast<float*>(gw[i].data_ptr()) : nullptr; };
+  const Scratch work(x.w[0] || x.w[1] ? kf_op_rotate_heads_grad_work(x.T, x.Hq, x.Hkv, x.hd) : 0, x.dev);
+  if (failed(kf_op_rotate_heads_grad(x.type, x.T, x.Hq, x.Hkv, x.hd, addr(dq), step(dq, 0), step(dq, 1), addr(dk), step(dk, 0), step(dk, 1),
+                                     addr(x.q), step(x.q, 0), step(x.q, 1), addr(x.k), step(x.k, 0), step(x.k, 1), pos, x.freq, x.n,
+                                     x.neighbours, x.eps, x.w[0], x.w[1], addr(gq), addr(gk), p(0), p(1), work.ptr(), at.stream)))
+    return nullptr;
+  PyObject* d = PyDict_New();
+  if (!d) throw python_error();
+  put(d, "q", gq);
+  put(d, "k", gk);
+  if (x.w[0]) put(d, "q_weight", gw[0]);
+  if (x.w[1]) put(d, "k_weight", gw[1]);
+  return d;
 }
 
 // --------------------------------------------------------------- attention
@@ -242,12 +367,6 @@ struct Book {
       if (o) changed(THPVariable_Unpack(o));
   }
 };
-// a list of int32 on the device; its length
-int32_t length(PyObject* o, const char* name) {
-  const at::Tensor& t = tensor(o, name);
-  if (t.dim() != 1) throw Refused{std::string(name) + ": a list of int32 on the GPU is wanted"};
-  return narrow(t.size(0), name);
-}
 struct Pool {
   const at::Tensor& t;
   void* p;
@@ -377,10 +496,10 @@ struct Logits {
     need(stride >= V, "logits: rows that do not overlap");
     tokens = static_cast<const int64_t*>(on(tensor(tok, "tokens"), dev, at::kLong, {R}, "tokens"));
   }
-  void outputs() {
+  void outputs(bool with_lse = true) {
     logp = make({R}, at::kFloat, dev);
     entropy = make({R}, at::kFloat, dev);
-    lse = make({R}, at::kFloat, dev);
+    if (with_lse) lse = make({R}, at::kFloat, dev);
   }
   float* p(const at::Tensor& x) const { return static_cast<float*>(x.data_ptr()); }
   PyObject* dict() const {
@@ -415,6 +534,15 @@ KF_PY(token_scores, 4) {
   }
   return d;
 }
+// the gradient's tensor: `o`, or a new one
+at::Tensor grad_like(const Logits& x, PyObject* o) {
+  if (none(o)) return make({x.R, x.V}, x.t.scalar_type(), x.dev);
+  const at::Tensor& grad = tensor(o, "out");
+  need(grad.scalar_type() == x.t.scalar_type() && grad.device() == x.dev && grad.sizes() == x.t.sizes() && (grad.stride(1) == 1 || x.V == 1),
+       "out: a tensor like the logits");
+  need(!wants_gradient(grad) || !grad.is_leaf(), "out: a leaf that requires a gradient cannot be written (detach it, or call under torch.no_grad())");
+  return grad;
+}
 // logits, tokens, g_logp | None, g_entropy | None, tau, out | None
 KF_PY(token_scores_grad, 6) {
   Logits x(a[0], a[1]);
@@ -426,15 +554,7 @@ KF_PY(token_scores_grad, 6) {
   }
   const float tau = number(a[4], "tau");
   const On at(x.dev);
-  at::Tensor grad;
-  if (none(a[5])) {
-    grad = make({x.R, x.V}, x.t.scalar_type(), x.dev);
-  } else {
-    grad = tensor(a[5], "out");
-    need(grad.scalar_type() == x.t.scalar_type() && grad.device() == x.dev && grad.sizes() == x.t.sizes() && (grad.stride(1) == 1 || x.V == 1),
-         "out: a tensor like the logits");
-    need(!wants_gradient(grad) || !grad.is_leaf(), "out: a leaf that requires a gradient cannot be written (detach it, or call under torch.no_grad())");
-  }
+  const at::Tensor grad = grad_like(x, a[5]);
   x.outputs();
   if (failed(kf_op_token_scores_grad(x.type, x.R, x.V, addr(x.t), x.stride, x.tokens, tau, g[0], g[1], x.p(x.logp), x.p(x.entropy),
                                      x.p(x.lse), addr(grad), x.R > 1 ? grad.stride(0) : x.V, at.stream)))
@@ -445,10 +565,44 @@ KF_PY(token_scores_grad, 6) {
   return d;
 }
 
+// logits, tokens, old_logp, advantage, ref_logp | None, weight | None, clip below, above, kl_weight, entropy_weight, tau, out | None
+KF_PY(policy_loss, 12) {
+  Logits x(a[0], a[1]);
+  const char* names[4] = {"old_logp", "advantage", "ref_logp", "weight"};
+  const float* rows[4];
+  for (int i = 0; i < 4; ++i) {
+    rows[i] = i >= 2 && none(a[2 + i]) ? nullptr : static_cast<const float*>(on(tensor(a[2 + i], names[i]), x.dev, at::kFloat, {x.R}, names[i]));
+    if (rows[i]) plain(THPVariable_Unpack(a[2 + i]), names[i]);
+  }
+  const float low = number(a[6], "clip"), high = number(a[7], "clip"), kl_weight = number(a[8], "kl_weight"), entropy_weight = number(a[9], "entropy_weight");
+  const double tau = real(a[10], "tau");
+  const On at(x.dev);
+  const at::Tensor grad = grad_like(x, a[11]);
+  x.outputs(false);
+  const at::Tensor loss = make({x.R}, at::kFloat, x.dev), ratio = make({x.R}, at::kFloat, x.dev);
+  at::Tensor kl;
+  if (rows[2]) kl = make({x.R}, at::kFloat, x.dev);
+  if (failed(kf_op_policy_loss(x.type, x.R, x.V, addr(x.t), x.stride, x.tokens, tau, rows[0], rows[1], rows[2], rows[3], low, high, kl_weight,
+                               entropy_weight, x.p(loss), x.p(x.logp), x.p(x.entropy), x.p(ratio), rows[2] ? x.p(kl) : nullptr, addr(grad),
+                               x.R > 1 ? grad.stride(0) : x.V, at.stream)))
+    return nullptr;
+  if (!none(a[11])) changed(grad);
+  PyObject* d = PyDict_New();
+  if (!d) throw python_error();
+  put(d, "loss", loss);
+  put(d, "logp", x.logp);
+  put(d, "entropy", x.entropy);
+  put(d, "ratio", ratio);
+  if (rows[2]) put(d, "kl", kl);
+  put(d, "grad", grad);
+  return d;
+}
+
 #define KF_ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
-PyMethodDef g_methods[] = {KF_ENTRY(set_check),     KF_ENTRY(prompt_attention), KF_ENTRY(paged_attention), KF_ENTRY(pages_grow),
+PyMethodDef g_methods[] = {KF_ENTRY(set_check),     KF_ENTRY(rotate_heads),     KF_ENTRY(rotate_append),   KF_ENTRY(rotate_heads_grad),
+                           KF_ENTRY(prompt_attention), KF_ENTRY(paged_attention), KF_ENTRY(pages_grow),
                            KF_ENTRY(pages_free),    KF_ENTRY(pages_fork),       KF_ENTRY(pages_compact),   KF_ENTRY(pages_copy),
-                           KF_ENTRY(pages_append),  KF_ENTRY(token_scores),     KF_ENTRY(token_scores_grad), {nullptr, nullptr, 0, nullptr}};
+                           KF_ENTRY(pages_append),  KF_ENTRY(token_scores),     KF_ENTRY(token_scores_grad), KF_ENTRY(policy_loss), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_serving", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

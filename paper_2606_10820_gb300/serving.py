@@ -9,8 +9,8 @@ stream; tensors that are made on another stream need that stream's work
 to be waited for, as with any torch operator.
 
 The operators have no backward pass of their own: a tensor that requires a gradient raises ``ValueError``
-while torch records gradients, instead of losing it.  ``token_scores_grad`` gives the logits' gradient
-explicitly, so its logits may require one (``logits.backward(out["grad"])``).  What a call changes in
+while torch records gradients, instead of losing it.  ``token_scores_grad`` and ``policy_loss`` give the logits' gradient
+explicitly, so their logits may require one (``logits.backward(out["grad"])``); ``rotate_heads_grad`` gives that of heads.  What a call changes in
 place counts up its version, so autograd notices a saved tensor that was written.
 """
 from __future__ import annotations
@@ -45,6 +45,32 @@ def status(device=None):
     _m or _load()
     with torch.cuda.device(device if device is not None else torch.cuda.current_device()):
         kf._check(kf.load_library().kf_op_status(torch.cuda.current_stream().cuda_stream))
+
+
+# -------------------------------------------------------- rotary positions
+
+def rotate_heads(q, k, pos, freq, q_weight=None, k_weight=None, eps=None, neighbours=False, q_out=None, k_out=None):
+    """Rotary positions of query and key heads, and with ``eps`` their norms first, in one pass: (q, k), new tensors
+    unless ``q_out`` and ``k_out`` (which may be q and k themselves) are given.
+
+    q [T, Hq, hd], k [T, Hkv, hd] (bf16 or fp16, hd 64 or 128; any strides but the last, so they may be parts of one
+    projection's output); pos [T] int32; freq [n] fp64 on the GPU, n a multiple of 8: pair i of a head, of its elements i and i + n
+    (``neighbours``: 2 i and 2 i + 1), turns by pos * freq[i]; elements from 2 n on stay.  eps: each head is divided by
+    sqrt(mean(x^2) + eps) and multiplied by its weight [hd] (of q's type; None: ones)."""
+    return (_m or _load()).rotate_heads(q, k, pos, freq, q_weight, k_weight, eps, neighbours, q_out, k_out)
+
+
+def rotate_append(q, k, v, pool, starts, table, lens, slots, freq, q_weight=None, k_weight=None, eps=None, neighbours=False):
+    """``rotate_heads`` of a cache's new tokens and ``pages_append`` of their K and V in one pass: rows starts[i] ..
+    starts[i + 1] - 1 of q, k and v are the last tokens of slot slots[i], and turn by their positions in it.  Returns the
+    queries [T, Hq, hd]; the keys and v [T, Hkv, hd] go to pool [pages, 2, Hkv, page, hd]."""
+    return (_m or _load()).rotate_append(q, k, v, pool, starts, table, lens, slots, freq, q_weight, k_weight, eps, neighbours)
+
+
+def rotate_heads_grad(dq, dk, q, k, pos, freq, q_weight=None, k_weight=None, eps=None, neighbours=False):
+    """Gradients of ``rotate_heads`` from those of its outputs, dq and dk: a dict of ``q``, ``k`` (in their type) and, where
+    the weights are given, ``q_weight`` and ``k_weight`` [hd] fp32."""
+    return (_m or _load()).rotate_heads_grad(dq, dk, q, k, pos, freq, q_weight, k_weight, eps, neighbours)
 
 
 # --------------------------------------------------------------- attention
@@ -122,3 +148,17 @@ def token_scores_grad(logits, tokens, g_logp=None, g_entropy=None, tau=1.0, out=
     ``logp``, ``entropy``, ``lse`` [R] fp32 and ``grad`` [R, V] in the logits' type (``out``, which may be
     the logits themselves, where it is given)."""
     return (_m or _load()).token_scores_grad(logits, tokens, g_logp, g_entropy, tau, out)
+
+
+def policy_loss(logits, tokens, old_logp, advantage, ref_logp=None, weight=None, clip=0.2, kl_weight=0.0, entropy_weight=0.0, tau=1.0, out=None):
+    """The clipped policy loss of ``tokens`` [R] (int64; negative: padding) under ``logits`` [R, V] / tau, and the logits'
+    gradient, in one pass: with ratio = exp(logp - old_logp), u = ref_logp - logp, kl = e^u - 1 - u and the row's entropy,
+
+        loss = weight * (kl_weight * kl - min(ratio * advantage, clamp(ratio, 1 - clip, 1 + clip) * advantage) - entropy_weight * entropy)
+
+    old_logp, advantage, ref_logp (None: no KL term) and weight (None: ones; 0: the row is left out) are [R] fp32; clip: a number,
+    or those below and above.  A dict of ``loss``, ``logp``, ``entropy``, ``ratio``, ``kl`` (with ref_logp) [R] fp32 and
+    ``grad`` [R, V], the gradient of ``loss.sum()`` in the logits' type (``out``, which may be the logits themselves,
+    where it is given)."""
+    low, high = clip if isinstance(clip, (tuple, list)) else (clip, clip)
+    return (_m or _load()).policy_loss(logits, tokens, old_logp, advantage, ref_logp, weight, low, high, kl_weight, entropy_weight, tau, out)
