@@ -133,6 +133,27 @@ int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int
                           const int32_t* lens, float scale, void* out, void* work, void* stream);
 
 /*
+ * Paged attention of groups of sequences that begin with the same tokens (candidates of one prompt, questions about one
+ * document): as kf_op_paged_attention, but the keys that a group shares are read once for all of its rows.
+ * Sequences groups[g] .. groups[g+1]-1 are group g, and their first shared[g] tokens are the same: groups int32 [n+1] on the
+ * device, groups[0] = 0, not falling, groups[n] = B; shared int32 [n], 0 .. width * page, at most the lengths of the group's
+ * sequences.  Keys below shared[g] are read through the table row of the group's first sequence, keys from there on
+ * through each sequence's own (whose pages below are not looked at; kf_op_pages_fork leaves tables so that both are the same).
+ * A group of one, or of none, and a prefix of no tokens are allowed.  Where every sequence is a group by itself (n >= B) the call is
+ * kf_op_paged_attention.  What a row sees does not depend on shared: row i keys 0 .. len - rows + i.
+ * The same lengths, groups and prefixes in a table of the same width and a pool of the same size give the same bits.
+ * A prefix outside 0 .. width * page: KF_DEV_BAD_ROW, and it counts as none.  Groups that are not as said: KF_DEV_BAD_ROW, and
+ * out holds anything.
+ * work: kf_op_shared_attention_work bytes of the call's own sizes.  Errors: KF_E_ARG, KF_E_CUDA.
+ */
+int64_t kf_op_shared_attention_work(int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, int64_t n_pages, int32_t page,
+                                    int32_t width, int32_t n);
+int kf_op_shared_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, const void* q,
+                           int64_t q_seq, int64_t q_row, int64_t q_head, const void* pool, int64_t n_pages, int32_t page,
+                           const int32_t* table, int32_t width, const int32_t* lens, int32_t n, const int32_t* groups,
+                           const int32_t* shared, float scale, void* out, void* work, void* stream);
+
+/*
  * The book of a cache: ref int32 [n_pages], the references to each page (0:
  * free); table int32 [slots][width], the pages of each sequence in order (-1:
  * none); lens int32 [slots], its tokens.  A sequence of len tokens has

@@ -25,6 +25,7 @@
 
 #include "kf_mma.cuh"
 #include "kf_serving.cuh"
+#include "kf_shared.cuh"
 
 namespace kf {
 namespace {
@@ -62,6 +63,9 @@ struct Args {
   int B, rows, Hq, Hkv, G, MT, page, page_shift, width;    // page_shift: -1 where page is no power of two
   int direct;           // a CTA per segment
   float scale2;         // scale log2(e): scores in base-2 units
+  // SHARED: the keys from the group's prefix on, and partial outputs of every row
+  Sharing sh;
+  Partials part;
   __device__ __forceinline__ int page_of(int key) const { return page_shift >= 0 ? key >> page_shift : key / page; }
 };
 
@@ -89,9 +93,29 @@ __device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b
 __device__ __forceinline__ int seq_len(const Args& a, int b) {
   return min(max(__ldg(a.lens + b), 0), a.width * a.page);
 }
+// The first key of a sequence: 0, or where its group's prefix ends
+template <bool SHARED>
+struct First {
+  int g, key;
+  __device__ __forceinline__ void at(const Args& a, int b) {
+    key = 0;
+    if constexpr (SHARED) {
+      g = group_of(a.sh, b);
+      key = prefix_of(a.sh, g, a.width * a.page);
+    }
+  }
+  // of the sequence after it
+  __device__ __forceinline__ void next(const Args& a, int b) {
+    if constexpr (SHARED) {
+      while (g + 1 < a.sh.n && __ldg(a.sh.groups + g + 1) <= b) ++g;
+      key = prefix_of(a.sh, g, a.width * a.page);
+    }
+  }
+  __device__ __forceinline__ int unit0() const { return SHARED ? key & ~15 : 0; }      // (units begin where 16 keys of a page do)
+};
 // units of each of a sequence's segments (one without keys has a unit too: its rows are written)
-template <int HD> __device__ __forceinline__ int units_of(const Args& a, int b) {
-  return max(1, (seq_len(a, b) + kUnit<HD> - 1) / kUnit<HD>);
+template <int HD, bool SHARED> __device__ __forceinline__ int units_of(const Args& a, int b, const First<SHARED>& f) {
+  return max(1, (seq_len(a, b) - f.unit0() + kUnit<HD> - 1) / kUnit<HD>);
 }
 
 // The list: sequence by sequence, each one's Hkv * MT segments, each one's units and kExtra
@@ -101,17 +125,22 @@ struct Part {
   long long total, x0, x1, base;
   int b, parts;
 };
-template <int HD, int TILES>
-__device__ __forceinline__ int places_of(const Args& a, int b) { return units_of<HD>(a, b) * (kTurns<HD, TILES> ? 2 : 1); }
+template <int HD, int TILES, bool SHARED>
+__device__ __forceinline__ int places_of(const Args& a, int b, const First<SHARED>& f) { return units_of<HD>(a, b, f) * (kTurns<HD, TILES> ? 2 : 1); }
 __device__ __forceinline__ long long part_begin(long long total, int parts, int c) { return total * c / parts; }
-template <int HD, int TILES>
+template <int HD, int TILES, bool SHARED>
 __device__ Part find_part(const Args& a, int c, int ctas) {
   __shared__ long long warp_sum[NW];
   __shared__ Part found;
   const int t = threadIdx.x, per = (a.B + kThreads - 1) / kThreads, sb = a.Hkv * a.MT;
   const int first = min(a.B, t * per), last = min(a.B, first + per);
   long long mine = 0;
-  for (int b = first; b < last; ++b) mine += places_of<HD, TILES>(a, b) + kExtra;
+  First<SHARED> f;
+  if (first < last) f.at(a, first);
+  for (int b = first; b < last; ++b) {
+    if (b > first) f.next(a, b);
+    mine += places_of<HD, TILES>(a, b, f) + kExtra;
+  }
   mine *= sb;
   long long incl = mine;
 #pragma unroll
@@ -131,9 +160,10 @@ __device__ Part find_part(const Args& a, int c, int ctas) {
   if (c < parts && x0 >= lo && x0 < lo + mine) {
     long long base = lo;
     int b = first;
-    for (long long n = (long long)(places_of<HD, TILES>(a, b) + kExtra) * sb; x0 >= base + n; n = (long long)(places_of<HD, TILES>(a, b) + kExtra) * sb) {
+    f.at(a, b);
+    for (long long n = (long long)(places_of<HD, TILES>(a, b, f) + kExtra) * sb; x0 >= base + n; n = (long long)(places_of<HD, TILES>(a, b, f) + kExtra) * sb) {
       base += n;
-      ++b;
+      f.next(a, ++b);
     }
     found = Part{total, x0, part_begin(total, parts, c + 1), base, b, parts};
   }
@@ -143,11 +173,13 @@ __device__ Part find_part(const Args& a, int c, int ctas) {
 }
 
 // one segment's places within a CTA's part
-template <int HD, int TILES>
+template <int HD, int TILES, bool SHARED>
 struct Piece {
   long long xs, xa, xb, xe;    // the segment's first unit; the piece's units [xa, xb) (or none) and its end
   int b, s, n, len;            // sequence, segment of it, units of the segment, tokens
-  __device__ __forceinline__ int unit(long long x) const { return (int)(x - xs) >> (kTurns<HD, TILES> ? 1 : 0); }
+  First<SHARED> f;
+  // the first key of place x
+  __device__ __forceinline__ int key(long long x) const { return f.unit0() + ((int)(x - xs) >> (kTurns<HD, TILES> ? 1 : 0)) * kUnit<HD>; }
   __device__ __forceinline__ void cut(const Part& p) {
     xa = max(xs, p.x0);
     xb = min(xs + n, p.x1);
@@ -155,7 +187,8 @@ struct Piece {
   }
   __device__ __forceinline__ void at(const Args& a, const Part& p) {
     b = p.b;
-    n = places_of<HD, TILES>(a, b);
+    f.at(a, b);
+    n = places_of<HD, TILES>(a, b, f);
     len = seq_len(a, b);
     s = (int)((p.x0 - p.base) / (n + kExtra));
     xs = p.base + (long long)s * (n + kExtra);
@@ -166,8 +199,8 @@ struct Piece {
     if (xe >= p.x1) return false;
     if (++s == a.Hkv * a.MT) {
       s = 0;
-      ++b;
-      n = places_of<HD, TILES>(a, b);
+      f.next(a, ++b);
+      n = places_of<HD, TILES>(a, b, f);
       len = seq_len(a, b);
     }
     xs = xe;
@@ -177,17 +210,17 @@ struct Piece {
 };
 
 // a warp's copies: unit after unit of its own, ahead of the products
-template <typename T, int HD, int TILES>
+template <typename T, int HD, int TILES, bool SHARED>
 struct Feed {
   static constexpr int U = kUnit<HD>, kHalves = U / 16;
-  Piece<HD, TILES> pc;
+  Piece<HD, TILES, SHARED> pc;
   long long x;
   int page[kHalves];       // pages of unit x
   bool more;
   __device__ __forceinline__ void look(const Args& a) {
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
-      const int key = pc.unit(x) * U + 16 * h;
+      const int key = pc.key(x) + 16 * h;
       page[h] = key < pc.len ? __ldg(a.table + (size_t)pc.b * a.width + a.page_of(key)) : -1;
     }
   }
@@ -213,7 +246,7 @@ struct Feed {
       uint32_t ok = 0;
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
-        const int key0 = pc.unit(x) * U + 16 * h, left = pc.len - key0;
+        const int key0 = pc.key(x) + 16 * h, left = pc.len - key0;
         const bool in = page[h] >= 0 && page[h] < a.n_pages;
         if (in) ok |= 1u << h;
         else if (left > 0 && lane == 0) atomicOr(a.err, KF_DEV_BAD_PAGE);
@@ -223,7 +256,7 @@ struct Feed {
 #pragma unroll
         for (int i = 0; i < 16 / RP; ++i) {
           const int r = i * RP + lane / CH, row = 16 * h + r;
-          const int bytes = in && r < left ? 16 : 0;      // (0: zeros, nothing is read)
+          const int bytes = in && r < left && (!SHARED || r >= pc.f.key - key0) ? 16 : 0;      // (0: zeros, nothing is read)
           const uint32_t d = stage + row * (HD * 2) + ((c ^ (row & 7)) << 4);
           mma::cp_async16(d, bytes ? kb + r * HD : static_cast<const T*>(a.pool), bytes);
           mma::cp_async16(d + kUnitBytes / 2, bytes ? vb + r * HD : static_cast<const T*>(a.pool), bytes);
@@ -245,7 +278,7 @@ template <int HD, int TILES> constexpr bool kFits = kCtasPerSm<HD, TILES> * (kSm
 static_assert(sizeof(Part) + NW * sizeof(long long) <= 128, "the static arrays");
 static_assert(kFits<64, 1> && kFits<64, 2> && kFits<128, 1> && kFits<128, 2>, "the CTAs of an SM");
 
-template <typename T, int HD, int TILES>
+template <typename T, int HD, int TILES, bool SHARED>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const Args a) {
   extern __shared__ __align__(128) uint8_t sm[];
   constexpr int ST = kStages<HD, TILES>, ROWS = 16 * TILES, HELD = kHeld<HD, TILES>;
@@ -262,22 +295,24 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
       if (n < 0 || n > a.width * a.page) atomicOr(a.err, KF_DEV_BAD_ROW);
     }
   Part part;
-  if (a.direct) {
+  if (!SHARED && a.direct) {
     // this segment's places are the whole list: [0, n + kExtra)
-    const int sb = a.Hkv * a.MT, b = blockIdx.x / sb, n = places_of<HD, TILES>(a, b) + kExtra;
+    First<SHARED> f;
+    f.at(a, 0);
+    const int sb = a.Hkv * a.MT, b = blockIdx.x / sb, n = places_of<HD, TILES>(a, b, f) + kExtra;
     part = Part{n, 0, n, -(long long)(blockIdx.x - b * sb) * n, b, 1};
   } else {
-    if (t == 0) a.split[blockIdx.x].pieces = 0;
-    part = find_part<HD, TILES>(a, blockIdx.x, gridDim.x);
+    if (!SHARED && t == 0) a.split[blockIdx.x].pieces = 0;
+    part = find_part<HD, TILES, SHARED>(a, blockIdx.x, gridDim.x);
   }
   if (part.x0 < part.x1) {
-    Feed<T, HD, TILES> feed;
+    Feed<T, HD, TILES, SHARED> feed;
     feed.start(a, part, warp);
 #pragma unroll
     for (int i = 0; i < ST - 1; ++i) feed.copy(a, part, ring + i * kUnitBytes, open + i, lane);
     int st = 0;
 
-    Piece<HD, TILES> pc;
+    Piece<HD, TILES, SHARED> pc;
     pc.at(a, part);
     do {
       if (pc.xa >= pc.xb) continue;                // (uniform) only places without units
@@ -338,15 +373,15 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
                 mma16816<T>(s[i][n + 1], q[i][k], kb[2], kb[3]);
               }
             }
-          const int key0 = pc.unit(x) * U;
-          if (key0 + U - 1 > free_to || ok != (1u << (U / 16)) - 1) {       // (uniform)
+          const int key0 = pc.key(x);
+          if (key0 + U - 1 > free_to || (SHARED && key0 < pc.f.key) || ok != (1u << (U / 16)) - 1) {       // (uniform)
 #pragma unroll
             for (int i = 0; i < HELD; ++i)
 #pragma unroll
               for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                  if (key0 + 8 * n + 2 * c + (e & 1) > last[i][e >> 1] || !((ok >> (n >> 1)) & 1u)) s[i][n][e] = -INFINITY;
+                  if (key0 + 8 * n + 2 * c + (e & 1) > last[i][e >> 1] || (SHARED && key0 + 8 * n + 2 * c + (e & 1) < pc.f.key) || !((ok >> (n >> 1)) & 1u)) s[i][n][e] = -INFINITY;
           }
 #pragma unroll
           for (int i = 0; i < HELD; ++i) {
@@ -464,15 +499,25 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
         const bool whole = pc.xa == pc.xs && pc.xb == end;
         const int slot = 2 * blockIdx.x + (pc.xa == pc.xs);       // 0: a segment begun elsewhere, 1: one that goes on elsewhere
         // (parts up to the last that begins before the segment's end: total p / parts < end)
-        if (!whole && pc.xa == pc.xs && j == 0 && lane == 0)
-          a.split[blockIdx.x] = Split{pc.b, pc.s, (int)((end * part.parts + part.total - 1) / part.total) - (int)blockIdx.x, 0};
+        if ((SHARED || !whole) && pc.xa == pc.xs && j == 0 && lane == 0) {
+          const int pieces = (int)((end * part.parts + part.total - 1) / part.total) - (int)blockIdx.x;
+          if (SHARED) a.part.rec[(int64_t)pc.b * a.Hkv * a.MT + pc.s] = Record{(int)blockIdx.x, pieces};
+          else a.split[blockIdx.x] = Split{pc.b, pc.s, pieces, 0};
+        }
 #pragma unroll
         for (int i = 0; i < HELD; ++i)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const int rr = 16 * (tile + i) + g + 8 * h, r = seg0 + rr, tok = r / a.G;
             if (r >= R) continue;
-            if (whole) {
+            if constexpr (SHARED) {
+              const bool first = pc.xa == pc.xs;
+              const int64_t at = first ? ((int64_t)pc.b * a.rows + tok) * a.Hq + hk * a.G + r - tok * a.G : (int64_t)blockIdx.x * ROWS + rr;
+              float* op = (first ? a.part.first_o : a.part.more_o) + at * HD;
+#pragma unroll
+              for (int d = 0; d < DT; ++d) *reinterpret_cast<float2*>(op + 8 * d + 2 * c) = make_float2(o[i][d][2 * h], o[i][d][2 * h + 1]);
+              if (c == 0) (first ? a.part.first_ml : a.part.more_ml)[at] = make_float2(m[i][h], l[i][h]);
+            } else if (whole) {
               const float inv = l[i][h] == 0.f ? 0.f : 1.f / l[i][h];     // (no key seen: zeros)
               T* op = static_cast<T*>(a.out) + (((int64_t)pc.b * a.rows + tok) * a.Hq + hk * a.G + r - tok * a.G) * HD;
 #pragma unroll
@@ -489,6 +534,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
     } while (pc.next(a, part));
     mma::cp_wait<0>();
   }
+  // (the prefixes' kernel before this one: what comes after is to see both)
+  if (SHARED) asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
@@ -582,8 +629,8 @@ int launch(Args a, const Shape& sh, void* work, cudaStream_t s) {
   // and 16 blocks: 20.2, 15.1, 13.1 us; 128 of 512 to 8192, 32 heads over 8: 685, 686, 691)
   const int by = (int)std::min<long long>(16, std::max(4ll, 2 * grid / sh.segments));
   static PerDevice attr;
-  set_smem_attr(attr, k_paged<T, HD, TILES>, kSmem<HD, TILES>);
-  launch_cluster(k_paged<T, HD, TILES>, dim3(grid), dim3(kThreads), kSmem<HD, TILES>, 1, false, s, a);
+  set_smem_attr(attr, k_paged<T, HD, TILES, false>, kSmem<HD, TILES>);
+  launch_cluster(k_paged<T, HD, TILES, false>, dim3(grid), dim3(kThreads), kSmem<HD, TILES>, 1, false, s, a);
   if (!sh.direct && grid > 1) launch_cluster(k_join<T, HD, TILES>, dim3(grid, std::min(by, a.rows * a.G)), dim3(kJoinThreads), 0, 1, true, s, a);
   return launched("kf_op_paged_attention");
 }
@@ -591,6 +638,23 @@ template <typename T>
 int launch_any(int hd, const Args& a, const Shape& sh, void* work, cudaStream_t s) {
   if (hd == 128) return sh.tiles == 2 ? launch<T, 128, 2>(a, sh, work, s) : launch<T, 128, 1>(a, sh, work, s);
   return sh.tiles == 2 ? launch<T, 64, 2>(a, sh, work, s) : launch<T, 64, 1>(a, sh, work, s);
+}
+template <typename T, int HD, int TILES>
+void launch_own(const Args& a, int grid, cudaStream_t s) {
+  static PerDevice attr;
+  set_smem_attr(attr, k_paged<T, HD, TILES, true>, kSmem<HD, TILES>);
+  launch_cluster(k_paged<T, HD, TILES, true>, dim3(grid), dim3(kThreads), kSmem<HD, TILES>, 1, true, s, a);
+}
+template <typename T>
+void launch_own_any(int hd, int tiles, const Args& a, int grid, cudaStream_t s) {
+  if (hd == 128) tiles == 2 ? launch_own<T, 128, 2>(a, grid, s) : launch_own<T, 128, 1>(a, grid, s);
+  else tiles == 2 ? launch_own<T, 64, 2>(a, grid, s) : launch_own<T, 64, 1>(a, grid, s);
+}
+int shift_of(int page) {
+  int shift = -1;
+  if ((page & (page - 1)) == 0)
+    for (shift = 0; (1 << shift) < page;) ++shift;
+  return shift;
 }
 // the arguments' sizes; nullptr if they are fine
 const char* sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int width) {
@@ -602,6 +666,21 @@ const char* sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int 
 }
 
 }  // namespace
+
+const char* paged_sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int width) { return sizes_fault(B, rows, Hq, Hkv, hd, page, width); }
+
+OwnPlan plan_own(int B, int rows, int G, int Hkv, int hd, int page, int width, int64_t n_pages) {
+  const Shape sh = shape_of(B, rows, G, Hkv, hd, page, width, std::min((int64_t)B * width, n_pages) * page);
+  const int per_sm = hd == 64 && sh.tiles == 1 ? kCtasPerSm<64, 1> : 2;
+  return OwnPlan{(int)std::min<long long>((long long)per_sm * device_sms(), std::max(1ll, sh.segments * (sh.longest + kExtra) / kMinUnits)),
+                 16 * sh.tiles, (int)sh.segments};
+}
+void launch_own(int32_t type, const SharedCall& c, cudaStream_t s) {
+  Args a{c.q, c.q_seq, c.q_row, c.q_head, c.pool, c.table, c.lens, nullptr, nullptr, nullptr, nullptr, c.err, c.n_pages,
+         c.B, c.rows, c.Hq, c.Hkv, c.G, ceil_div(c.rows * c.G, c.own.seg_rows), c.page, shift_of(c.page), c.width, 0, c.scale2, c.sh, c.own};
+  if (type == KF_TYPE_BF16) launch_own_any<__nv_bfloat16>(c.hd, c.own.seg_rows / 16, a, c.own.ctas, s);
+  else launch_own_any<__half>(c.hd, c.own.seg_rows / 16, a, c.own.ctas, s);
+}
 }  // namespace kf
 
 using namespace kf;
@@ -628,12 +707,9 @@ extern "C" int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int3
   if (!aligned(q, 16) || !aligned(pool, 16) || !aligned(out, 16) || !aligned(work, 256) || !aligned(table, 4) || !aligned(lens, 4))
     return refuse(what, "q, pool and out are 16-byte aligned, work 256-byte");
   if (q_seq % 8 || q_row % 8 || q_head % 8) return refuse(what, "q's strides are multiples of 8 elements");
-  int shift = -1;
-  if ((page & (page - 1)) == 0)
-    for (shift = 0; (1 << shift) < page;) ++shift;
   if (!n_pages) pool = q;      // (nothing of it is read)
   const Args a{q, q_seq, q_row, q_head, pool, table, lens, out, nullptr, nullptr, nullptr, serving_error_word(), n_pages,
-               B, rows, Hq, Hkv, G, 0, page, shift, width, 0, scale * 1.4426950408889634f};
+               B, rows, Hq, Hkv, G, 0, page, shift_of(page), width, 0, scale * 1.4426950408889634f, {}, {}};
   if (!a.err) return refuse(what, "no error word", KF_E_CUDA);
   cudaStream_t s = (cudaStream_t)stream;
   return type == KF_TYPE_BF16 ? launch_any<__nv_bfloat16>(hd, a, sh, work, s) : launch_any<__half>(hd, a, sh, work, s);

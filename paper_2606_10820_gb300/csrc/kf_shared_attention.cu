@@ -1,0 +1,491 @@
+// The keys that groups of sequences share (kf_op_shared_attention): head_dim 64 or 128, bf16 or fp16,
+// on tcgen05 (kf_attn_pair.cuh).
+//
+// The query rows that read a group's prefix under one KV head are its sequences' rows x group heads: a
+// segment is up to 256 of them, two sub-tiles of 128, over all key tiles of 128 of the prefix.  So
+// a prefix comes from memory once for all of a group's sequences.  The segments' tiles form one list which the
+// CTAs (one a SM) share evenly, kExtra tiles more a segment for its start and end; what a part leaves
+// unfinished the join adds (kf_shared.cuh).  K and V come by TMA, in boxes of the 16 keys that a page is a multiple of;
+// a page outside of the pool is a box outside of the map, which is zeros and closed by the softmax.  Each
+// row sees keys up to its own position.
+// What bounds it: the prefixes' bytes; from about 200 rows a group on the tensor cores and exponentials beside them.
+#include <algorithm>
+
+#include "kf_attn_pair.cuh"
+#include "kf_shared.cuh"
+
+namespace kf {
+namespace {
+using namespace pair;
+
+constexpr int kGran = 16, kGrans = kKeys / kGran;    // keys of a box; boxes of a tile
+constexpr int kExtra = 2;                            // a segment's start and end, in tiles
+constexpr int kMinTiles = 2;                         // places of a CTA, at least
+
+struct Item {
+  int b0, first, rows;                               // the group's first sequence; the segment's first row, and its rows
+  int hk, t0, len;                                   // KV head, first key tile, the prefix's tokens
+  int n[2];                                          // key tiles (0: no sub-tile)
+  int more;                                          // a later piece of its segment
+};
+using Bars = PairBars<Item>;
+static_assert(sizeof(Bars) <= kBarBytes, "the barriers' part of the shared memory");
+
+// Places of a group: pairs of sub-tiles x KV heads x (tiles + kExtra)
+struct Group {
+  int b0, rows, len, tiles, pairs;
+  int64_t before;                                    // rows a head before the group
+  __device__ __forceinline__ Group(const SharedCall& a, int g) {
+    const int2 m = members(a.sh, g, a.B);
+    b0 = m.x;
+    rows = (m.y - m.x) * a.rows * a.G;
+    before = (int64_t)m.x * a.rows * a.G;
+    len = prefix_of(a.sh, g, a.width * a.page);
+    tiles = (len + kKeys - 1) / kKeys;
+    pairs = tiles > 0 ? (rows + kPrefixRows - 1) / kPrefixRows : 0;
+  }
+  __device__ __forceinline__ int64_t places(const SharedCall& a) const { return (int64_t)pairs * a.Hkv * (tiles + kExtra); }
+};
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ CUtensorMap map, const SharedCall a) {
+  extern __shared__ __align__(1024) uint8_t sm[];
+  constexpr int ST = kStages<HD>, AT = HD / 64;
+  constexpr uint32_t TILE = kTile<HD>;
+  Bars& b = *reinterpret_cast<Bars*>(sm + (2 + ST) * TILE);
+  const uint32_t sQ = smem_u32(sm), sKV = sQ + 2 * TILE;
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (sQ & 1023) {                              // (uniform) swizzle atoms need the alignment
+    if (t == 0) atomicOr(a.err, kErrInternal);
+    return;
+  }
+  if (t == 0) {
+    auto init = [](uint64_t* p, uint32_t n) { mbar_init(smem_u32(p), n); };
+    init(&b.q_full, 8);                         // the softmax warps, which copy Q
+    init(&b.q_empty, 1);
+    for (int i = 0; i < 2; ++i) {
+      init(&b.item_full[i], 1);
+      init(&b.item_empty[i], 9);                // the MMA warp and eight softmax warps
+      init(&b.s_full[i], 1);
+      init(&b.s_free[i], 4);
+      init(&b.p_full[i][0], 4);
+      init(&b.p_full[i][1], 4);
+      init(&b.o_full[i], 1);
+      init(&b.o_free[i], 4);
+    }
+    init(&b.tail, 1);
+    for (int i = 0; i < ST; ++i) {
+      init(&b.kv_full[i], 1);
+      init(&b.kv_empty[i], 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&b.tmem)), "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = b.tmem;
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+    if (warp == 0) {
+      // ------------------------------------------------------ items and copies
+      // this CTA's part [x0, x1) of the list, and the group that it begins in (its places begin at `base`)
+      if (blockIdx.x == 0) {
+        bool bad = false;
+        for (int g = lane; g < a.sh.n; g += 32) {
+          const int p = a.sh.groups[g], e = a.sh.groups[g + 1], n = a.sh.shared[g];
+          bad |= p < 0 || e < p || e > a.B || (g == 0 && p != 0) || (g == a.sh.n - 1 && e != a.B) || n < 0 || n > a.width * a.page;
+        }
+        if (__any_sync(~0u, bad) && lane == 0) atomicOr(a.err, KF_DEV_BAD_ROW);
+      }
+      int64_t total = 0;
+      for (int g0 = 0; g0 < a.sh.n; g0 += 32) {
+        const int g = g0 + lane;
+        int64_t v = g < a.sh.n ? Group(a, g).places(a) : 0;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+        total += v;
+      }
+      const int parts = (int)min((int64_t)gridDim.x, max((int64_t)1, total / kMinTiles)), c = blockIdx.x;
+      const int64_t x0 = c < parts ? total * c / parts : total, x1 = c < parts ? total * (c + 1) / parts : total;
+      int64_t base = 0;
+      int g = 0;
+      for (int g0 = 0; x0 < x1 && g0 < a.sh.n; g0 += 32) {
+        const int64_t v = g0 + lane < a.sh.n ? Group(a, g0 + lane).places(a) : 0;
+        int64_t incl = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int64_t u = __shfl_up_sync(~0u, incl, o);
+          if (lane >= o) incl += u;
+        }
+        const uint32_t past = __ballot_sync(~0u, base + incl > x0);
+        if (past) {
+          const int l = __ffs(past) - 1;
+          base += __shfl_sync(~0u, incl - v, l);
+          g = g0 + l;
+          break;
+        }
+        base += __shfl_sync(~0u, incl, 31);
+      }
+      bool ok = true;
+      int it = 0, ring = 0, tails = 0;
+      auto wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, a.err)); };
+      auto publish = [&](const Item& im) -> bool {
+        const int slot = it & 1;
+        if (!wait(&b.item_empty[slot], ((it >> 1) & 1) ^ 1)) return false;
+        if (lane == 0) {
+          b.item[slot] = im;
+          mbar_arrive(smem_u32(&b.item_full[slot]));
+        }
+        __syncwarp();
+        ++it;
+        return true;
+      };
+      for (int64_t x = x0; ok && x < x1;) {
+        Group gr(a, g);
+        const int per = gr.tiles + kExtra;
+        const int64_t places = gr.places(a);
+        if (x >= base + places) {               // (also a group without places)
+          base += places;
+          if (++g >= a.sh.n) break;
+          continue;
+        }
+        // a segment: pair by pair, head by head
+        const int s = (int)((x - base) / per), pair = s / a.Hkv, hk = s - pair * a.Hkv;
+        const int64_t xs = base + (int64_t)s * per, end = xs + gr.tiles;
+        const int t0 = (int)(x - xs), n = (int)(min(end, x1) - x);
+        x = min(xs + per, x1);
+        if (n <= 0) continue;                   // only places of its end
+        Item im;
+        im.b0 = gr.b0;
+        im.first = pair * kPrefixRows;
+        im.rows = min(kPrefixRows, gr.rows - im.first);
+        im.hk = hk;
+        im.t0 = t0;
+        im.len = gr.len;
+        im.n[0] = n;
+        im.n[1] = im.rows > kRows ? n : 0;
+        im.more = t0 > 0;
+        if (lane == 0 && t0 == 0) {
+          // (parts up to the last that begins before the segment's end)
+          const int at = prefix_record(gr.before, g, pair, hk, a.Hkv);
+          if (at < a.pre.segments) a.pre.rec[at] = Record{c, (int)((end * parts + total - 1) / total) - c};
+        }
+        ok = publish(im);
+        if (!ok) break;
+        // lane x < 8 looks up box x of a tile
+        const int32_t* ids = a.table + (int64_t)gr.b0 * a.width;
+        auto look = [&](int tile) -> int {
+          const int key = tile * kKeys + lane * kGran;
+          return lane < kGrans && key < gr.len ? __ldg(ids + key / a.page) : -1;
+        };
+        int id = look(t0);
+        for (int j = t0; ok && j < t0 + n; ++j) {
+          const int key = j * kKeys + lane * kGran, left = gr.len - j * kKeys;
+          // (a box outside of the map: zeros)
+          const bool in = id >= 0 && id < a.n_pages;
+          const int page = in ? id : (int)a.n_pages, row = in ? key % a.page : 0;
+          if (lane < kGrans && key < gr.len && !in) atomicOr(a.err, KF_DEV_BAD_PAGE);
+          if (j + 1 < t0 + n) id = look(j + 1);
+          for (int kv = 0; kv < 2; ++kv, ++ring) {
+            const int st = ring % ST;
+            ok = wait(&b.kv_empty[st], ((ring / ST) & 1) ^ 1);
+            if (!ok) break;
+            const uint32_t dst = sKV + st * TILE;
+            // V rows past the prefix's end: their probabilities are 0, and 0 times them has to be 0
+            const bool tail = kv == 1 && left < kKeys && left % kGran != 0;
+            uint64_t* bar = tail ? &b.tail : &b.kv_full[st];
+            if (lane == 0) mbar_expect_tx(smem_u32(bar), TILE);
+            __syncwarp();
+            if (lane < kGrans)
+              for (int y = 0; y < AT; ++y)
+                tma_load_4d(dst + y * kAtom + lane * kGran * 128, &map, smem_u32(bar), 64 * y, row, kv * a.Hkv + hk, page);
+            __syncwarp();
+            if (tail) {
+              ok = wait(&b.tail, tails++ & 1);
+              if (!ok) break;
+              uint8_t* p = sm + (2 + st) * TILE;
+              const int to = (left + kGran - 1) / kGran * kGran * 128;
+              for (int y = 0; y < AT; ++y)
+                for (int i = left * 128 + lane * 16; i < to; i += 32 * 16)
+                  *reinterpret_cast<uint4*>(p + y * kAtom + i) = make_uint4(0u, 0u, 0u, 0u);
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) mbar_arrive(smem_u32(&b.kv_full[st]));
+            }
+          }
+        }
+      }
+      if (ok) {
+        Item im{};                              // (an item without sub-tiles ends the others)
+        ok = publish(im);
+      }
+      if (!ok && lane == 0)
+        // let the copies still in flight land before the CTA ends (bounded)
+        for (int i = max(0, ring - ST); i < ring; ++i) mbar_wait(smem_u32(&b.kv_full[i % ST]), (i / ST) & 1, a.err);
+      __syncwarp();
+    } else if (warp == 1) {
+      product_warp<T, HD>(b, tmem, sQ, sKV, lane, a.err);
+      __syncwarp();
+    }
+  } else {
+    // ------------------------------------------------------------- softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    const int sub = warp >= 8, quarter = warp & 3, row = 32 * quarter + lane;
+    const Softmax<T, HD> sx(tmem, sub, quarter, lane);
+    const float sc = a.scale2;
+    auto wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, a.err)); };
+    auto arrive = [&](uint64_t* bar) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(bar));
+    };
+    int g = 0;                                  // this sub-tile's key tiles so far
+    bool ok = true;
+    for (int it = 0; ok; ++it) {
+      const int slot = it & 1;
+      if (!wait(&b.item_full[slot], (it >> 1) & 1)) break;
+      const Item im = b.item[slot];
+      arrive(&b.item_empty[slot]);
+      if (im.n[0] == 0) break;
+      const int n = im.n[sub], per = a.rows * a.G;
+      if (it > 0) ok = wait(&b.q_empty, (it - 1) & 1);
+      if (!ok) break;
+      if (n > 0) {
+        // this warp's 32 rows of Q, swizzled; rows that the segment does not have are zeros
+        constexpr int CH = HD / 8, RP = 32 / CH;
+        const int ch = lane % CH;
+        uint4 v[CH];
+#pragma unroll
+        for (int p = 0; p < CH; ++p) {
+          const int r = sub * kRows + 32 * quarter + p * RP + lane / CH, R = im.first + r, seq = R / per, x = R - seq * per, tok = x / a.G;
+          v[p] = r < im.rows ? __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (im.b0 + seq) * a.q_seq + tok * a.q_row +
+                                                                    (int64_t)(im.hk * a.G + x - tok * a.G) * a.q_head) + ch)
+                             : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int p = 0; p < CH; ++p) {
+          const int r = 32 * quarter + p * RP + lane / CH;
+          *reinterpret_cast<uint4*>(sm + sub * TILE + (ch / 8) * kAtom + r * 128 + (((ch % 8) ^ (r & 7)) << 4)) = v[p];
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      }
+      arrive(&b.q_full);
+      if (n == 0) continue;
+      // this thread's row: its place among all rows, and the keys that it sees
+      const int r = sub * kRows + row, R = im.first + r, seq = R / per, x = R - seq * per, tok = x / a.G;
+      const bool mine = r < im.rows;
+      int see = 0;
+      if (mine) see = min(im.len, min(max(__ldg(a.lens + im.b0 + seq), 0), a.width * a.page) - a.rows + tok + 1);
+      const int32_t* ids = a.table + (int64_t)im.b0 * a.width;
+      auto look = [&](int tile) -> int {        // the tile's page of box `lane`
+        const int key = tile * kKeys + lane * kGran;
+        return lane < kGrans && key < im.len ? __ldg(ids + key / a.page) : 0;
+      };
+      int id = look(im.t0);
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < n; ++j, ++g) {
+        const uint32_t open = __ballot_sync(~0u, id >= 0 && id < a.n_pages);
+        if (j + 1 < n) id = look(im.t0 + j + 1);
+        const int lim = see - (im.t0 + j) * kKeys;      // keys below it are seen
+        const bool all = open == ~0u && __all_sync(~0u, lim >= kKeys);
+        ok = sx.tile(b, sc, j == 0, g, m, l, a.err, [&](int c, uint32_t* s) {
+          if (!all) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) s[e] = 32 * c + e < lim && ((open >> (2 * c + e / 16)) & 1u) ? s[e] : 0xff800000u;
+          }
+        });
+        if (!ok) break;
+      }
+      if (!ok) break;
+      if (!wait(&b.o_full[sub], (g - 1) & 1)) { ok = false; break; }
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const int64_t at = im.more ? (int64_t)blockIdx.x * kPrefixRows + r
+                                 : ((int64_t)(im.b0 + seq) * a.rows + tok) * a.Hq + im.hk * a.G + x - tok * a.G;
+      float* dst = (im.more ? a.pre.more_o : a.pre.first_o) + at * HD;
+      if (mine) (im.more ? a.pre.more_ml : a.pre.first_ml)[at] = make_float2(m, l);
+#pragma unroll
+      for (int c = 0; c < HD / 32; ++c) {
+        float o[32];
+        tmem_ld32(sx.tO + 32 * c, o);
+        if (c == HD / 32 - 1) {
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          arrive(&b.o_free[sub]);
+        }
+        if (mine) {
+#pragma unroll
+          for (int d = 0; d < 32; d += 8) st_32(dst + 32 * c + d, reinterpret_cast<const uint32_t*>(o + d));
+        }
+      }
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+}
+
+// A warp per query row: the pieces of its group's prefix and of its sequence's own keys added, in one order
+constexpr int kJoinThreads = 256;
+template <typename T, int HD>
+__global__ void __launch_bounds__(kJoinThreads) k_add(const SharedCall a) {
+  constexpr int N = HD / 32;                    // values of a lane
+  using V = typename std::conditional<N == 4, float4, float2>::type;
+  const int lane = threadIdx.x & 31;
+  const int64_t at = (int64_t)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
+  const int64_t tokens = (int64_t)a.B * a.rows;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (at >= tokens * a.Hq) return;
+  const int64_t bt = at / a.Hq;
+  const int h = (int)(at - bt * a.Hq), b = (int)(bt / a.rows), tok = (int)(bt - (int64_t)b * a.rows), hk = h / a.G, r = tok * a.G + h - hk * a.G;
+  float m = -INFINITY, l = 0.f, o[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = 0.f;
+  auto add = [&](float2 ml, V x) {
+    const float mm = fmaxf(m, ml.x);
+    const float fa = m == -INFINITY ? 0.f : mma::ex2((m - mm) * a.scale2), fb = ml.x == -INFINITY ? 0.f : mma::ex2((ml.x - mm) * a.scale2);
+    m = mm;
+    l = l * fa + ml.y * fb;
+    const float* v = reinterpret_cast<const float*>(&x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = o[i] * fa + v[i] * fb;
+  };
+  // (written by the kernels before this one: not through the read-only path; a record of groups that are not as they
+  // should be may hold anything)
+  auto pieces = [&](const Partials& p, int64_t rec, int row) {
+    const int2 rc = __ldcg(reinterpret_cast<const int2*>(p.rec) + rec);
+    add(__ldcg(p.first_ml + at), __ldcg(reinterpret_cast<const V*>(p.first_o + at * HD) + lane));
+    const int c0 = max(rc.x, 0) + 1, c1 = min(p.ctas, max(rc.x, 0) + rc.y);
+#pragma unroll 4
+    for (int c = c0; c < c1; ++c) {
+      const int64_t q = (int64_t)c * p.seg_rows + row;
+      add(__ldcg(p.more_ml + q), __ldcg(reinterpret_cast<const V*>(p.more_o + q * HD) + lane));
+    }
+  };
+  const int g = group_of(a.sh, b);
+  const int2 in = members(a.sh, g, a.B);
+  if (b >= in.x && b < in.y && prefix_of(a.sh, g, a.width * a.page) > 0) {
+    const int64_t x = (int64_t)(b - in.x) * a.rows * a.G + r;
+    const int rec = prefix_record((int64_t)in.x * a.rows * a.G, g, (int)(x / kPrefixRows), hk, a.Hkv);
+    if (rec < a.pre.segments) pieces(a.pre, rec, (int)(x % kPrefixRows));
+  }
+  const int MT = (a.rows * a.G + a.own.seg_rows - 1) / a.own.seg_rows;
+  pieces(a.own, ((int64_t)b * a.Hkv + hk) * MT + r / a.own.seg_rows, r % a.own.seg_rows);
+  const float inv = l == 0.f ? 0.f : 1.f / l;   // (no key seen: zeros)
+  T* out = static_cast<T*>(a.out) + at * HD + lane * N;
+  if constexpr (N == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv));
+  else *reinterpret_cast<uint32_t*>(out) = pack2<T>(o[0] * inv, o[1] * inv);
+}
+
+// ------------------------------------------------------------------ host
+template <typename T, int HD>
+int launch(int32_t type, const SharedCall& c, const CUtensorMap& map, cudaStream_t s) {
+  static PerDevice attr;
+  set_smem_attr(attr, k_prefix<T, HD>, kSmem<HD>);
+  launch_cluster(k_prefix<T, HD>, dim3(c.pre.ctas), dim3(kThreads), kSmem<HD>, 1, false, s, map, c);
+  launch_own(type, c, s);
+  const int64_t rows = (int64_t)c.B * c.rows * c.Hq, per = kJoinThreads / 32;
+  launch_cluster(k_add<T, HD>, dim3((unsigned)((rows + per - 1) / per)), dim3(kJoinThreads), 0, 1, true, s, c);
+  return launched("kf_op_shared_attention");
+}
+
+// pages of K and V heads of rows, in boxes of 16 rows x 64 elements
+bool pool_map(CUtensorMap* m, const void* pool, int64_t n_pages, int Hkv, int page, int hd) {
+  const uint64_t dims[4] = {(uint64_t)hd, (uint64_t)page, (uint64_t)2 * Hkv, (uint64_t)n_pages};
+  const uint64_t strides[3] = {(uint64_t)hd * 2, (uint64_t)page * hd * 2, (uint64_t)2 * Hkv * page * hd * 2};
+  const uint32_t box[4] = {64, kGran, 1, 1};
+  return encode_map_bf16(m, pool, 4, dims, strides, box);      // (fp16 is copied the same way)
+}
+
+// The scratch, in 256-byte pieces; its size where work is NULL
+int64_t layout(SharedCall& c, void* work) {
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) -> void* {
+    const int64_t p = at;
+    at += (bytes + 255) / 256 * 256;
+    return static_cast<uint8_t*>(work) + p;
+  };
+  const int64_t rows = (int64_t)c.B * c.rows * c.Hq;
+  const OwnPlan own = plan_own(c.B, c.rows, c.G, c.Hkv, c.hd, c.page, c.width, c.n_pages);
+  // no more CTAs than the longest list that the table could hold fills
+  const int64_t pairs = (int64_t)c.B * c.rows * c.G / kPrefixRows + c.sh.n, tiles = ((int64_t)c.width * c.page + kKeys - 1) / kKeys + kExtra;
+  c.pre.ctas = (int)std::max<int64_t>(1, std::min<int64_t>(device_sms(), pairs * c.Hkv * tiles / kMinTiles));
+  c.pre.seg_rows = kPrefixRows;
+  c.pre.segments = (int)((pairs + 1) * c.Hkv);
+  c.own.ctas = own.ctas;
+  c.own.seg_rows = own.seg_rows;
+  c.own.segments = own.segments;
+  for (Partials* p : {&c.pre, &c.own}) {
+    p->first_o = static_cast<float*>(take(rows * c.hd * (int64_t)sizeof(float)));
+    p->first_ml = static_cast<float2*>(take(rows * (int64_t)sizeof(float2)));
+    p->more_o = static_cast<float*>(take((int64_t)p->ctas * p->seg_rows * c.hd * (int64_t)sizeof(float)));
+    p->more_ml = static_cast<float2*>(take((int64_t)p->ctas * p->seg_rows * (int64_t)sizeof(float2)));
+    p->rec = static_cast<Record*>(take(p->segments * (int64_t)sizeof(Record)));
+  }
+  return at;
+}
+const char* sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int width, int n) {
+  if (const char* f = paged_sizes_fault(B, rows, Hq, Hkv, hd, page, width)) return f;
+  if (n < 0 || (B > 0 && n < 1)) return "groups out of range";
+  if ((int64_t)B * rows * Hq > (1 << 30) || ((int64_t)B * rows * (Hq / Hkv) / kPrefixRows + n + 1) * Hkv > (1 << 30) || (int64_t)B * Hkv * rows * (Hq / Hkv) > (1 << 30))
+    return "too many rows and heads";
+  return nullptr;
+}
+// Nothing to share: each sequence a group, or no pages
+bool plain(int B, int n, int64_t n_pages) { return n >= B || n_pages == 0; }
+
+}  // namespace
+}  // namespace kf
+
+using namespace kf;
+
+extern "C" int64_t kf_op_shared_attention_work(int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, int64_t n_pages, int32_t page,
+                                               int32_t width, int32_t n) {
+  if (B <= 0 || n_pages < 0 || sizes_fault(B, rows, Hq, Hkv, hd, page, width, n)) return 0;
+  if (plain(B, n, n_pages)) return kf_op_paged_attention_work(B, rows, Hq, Hkv, hd, page, width);
+  SharedCall c{};
+  c.B = B;
+  c.rows = rows;
+  c.Hq = Hq;
+  c.Hkv = Hkv;
+  c.G = Hq / Hkv;
+  c.hd = hd;
+  c.n_pages = n_pages;
+  c.page = page;
+  c.width = width;
+  c.sh.n = n;
+  return layout(c, nullptr);
+}
+
+extern "C" int kf_op_shared_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, const void* q, int64_t q_seq,
+                                      int64_t q_row, int64_t q_head, const void* pool, int64_t n_pages, int32_t page, const int32_t* table,
+                                      int32_t width, const int32_t* lens, int32_t n, const int32_t* groups, const int32_t* shared,
+                                      float scale, void* out, void* work, void* stream) {
+  const char* what = "kf_op_shared_attention";
+  if (type != KF_TYPE_BF16 && type != KF_TYPE_FP16) return refuse(what, "the type is bf16 or fp16");
+  if (const char* f = sizes_fault(B, rows, Hq, Hkv, hd, page, width, n)) return refuse(what, f);
+  if (n_pages < 0 || n_pages > 0x7fffffffll) return refuse(what, "pages out of range");
+  if (!(scale > 0.f) || std::isinf(scale)) return refuse(what, "scale is a positive number");
+  if (B == 0) return KF_OK;
+  if (!groups || !shared || !aligned(groups, 4) || !aligned(shared, 4)) return refuse(what, "groups or shared: null or misaligned");
+  if (plain(B, n, n_pages))
+    return kf_op_paged_attention(type, B, rows, Hq, Hkv, hd, q, q_seq, q_row, q_head, pool, n_pages, page, table, width, lens, scale, out, work, stream);
+  if (!q || !out || !lens || !work || !pool || (width && !table)) return refuse(what, "a null array");
+  if (!aligned(q, 16) || !aligned(pool, 16) || !aligned(out, 16) || !aligned(work, 256) || !aligned(table, 4) || !aligned(lens, 4))
+    return refuse(what, "q, pool and out are 16-byte aligned, work 256-byte");
+  if (q_seq % 8 || q_row % 8 || q_head % 8) return refuse(what, "q's strides are multiples of 8 elements");
+  SharedCall c{q, q_seq, q_row, q_head, pool, table, lens, out, n_pages, Sharing{groups, shared, n}, {}, {}, serving_error_word(),
+               B, rows, Hq, Hkv, Hq / Hkv, hd, page, width, scale * 1.4426950408889634f};
+  if (!c.err) return refuse(what, "no error word", KF_E_CUDA);
+  layout(c, work);
+  CUtensorMap map;
+  if (!pool_map(&map, pool, n_pages, Hkv, page, hd)) return refuse(what, "a tensor map is refused (the pool)");
+  cudaStream_t s = (cudaStream_t)stream;
+  if (type == KF_TYPE_BF16) return hd == 64 ? launch<__nv_bfloat16, 64>(type, c, map, s) : launch<__nv_bfloat16, 128>(type, c, map, s);
+  return hd == 64 ? launch<__half, 64>(type, c, map, s) : launch<__half, 128>(type, c, map, s);
+}

@@ -315,33 +315,66 @@ KF_PY(prompt_attention, 7) {
   return THPVariable_Wrap(out);
 }
 
-// q, pool, table, lens, scale | None, out | None
+// q, pool, table, lens, scale | None, out | None: what both attentions over a cache take
+struct Paged {
+  const at::Tensor &q, &pool, &table;
+  c10::Device dev;
+  int32_t type, B, rows, Hq, Hkv, hd, page, width;
+  int64_t n_pages;
+  void *pp;
+  const int32_t *tp, *lp;
+  float scale;
+  Paged(PyObject* q_, PyObject* p, PyObject* t, PyObject* l, PyObject* s)
+      : q(tensor(q_, "q")), pool(tensor(p, "pool")), table(tensor(t, "table")), dev(q.device()) {
+    need(q.is_cuda() && q.dim() == 4 && pool.dim() == 5 && table.dim() == 2,
+         "q: [B, rows, Hq, hd], pool: [pages, 2, Hkv, page, hd], table: [B, width], on a GPU");
+    type = type_of(q, false, "q and pool: bf16 or fp16");
+    n_pages = pool.size(0);
+    need(pool.size(1) == 2 && q.stride(3) == 1, "pool: K and V of each page; q: heads of contiguous elements");
+    pp = on(pool, dev, q.scalar_type(), {n_pages, 2, pool.size(2), pool.size(3), q.size(3)}, "pool");
+    tp = ints(t, dev, {q.size(0), table.size(1)}, "table");
+    lp = ints(l, dev, {q.size(0)}, "lens");
+    scale = scale_of(s, q.size(3));
+    plain(q, "q");
+    plain(pool, "pool");
+    B = narrow(q.size(0), "q");
+    rows = narrow(q.size(1), "q");
+    Hq = narrow(q.size(2), "q");
+    Hkv = narrow(pool.size(2), "pool");
+    hd = narrow(q.size(3), "q");
+    page = narrow(pool.size(3), "pool");
+    width = narrow(table.size(1), "table");
+  }
+  at::Tensor output(PyObject* o) const {
+    at::Tensor out = none(o) ? make({B, rows, Hq, hd}, q.scalar_type(), dev) : tensor(o, "out");
+    on(out, dev, q.scalar_type(), q.sizes(), "out");
+    plain(out, "out");
+    return out;
+  }
+};
 KF_PY(paged_attention, 6) {
-  const at::Tensor &q = tensor(a[0], "q"), &pool = tensor(a[1], "pool"), &table = tensor(a[2], "table");
-  need(q.is_cuda() && q.dim() == 4 && pool.dim() == 5 && table.dim() == 2,
-       "q: [B, rows, Hq, hd], pool: [pages, 2, Hkv, page, hd], table: [B, width], on a GPU");
-  const int32_t type = type_of(q, false, "q and pool: bf16 or fp16");
-  const int64_t B = q.size(0), rows = q.size(1), Hq = q.size(2), hd = q.size(3);
-  const int64_t n_pages = pool.size(0), Hkv = pool.size(2), page = pool.size(3), width = table.size(1);
-  const c10::Device dev = q.device();
-  need(pool.size(1) == 2 && q.stride(3) == 1, "pool: K and V of each page; q: heads of contiguous elements");
-  void* pp = on(pool, dev, q.scalar_type(), {n_pages, 2, Hkv, page, hd}, "pool");
-  const int32_t* tp = ints(a[2], dev, {B, width}, "table");
-  const int32_t* lp = ints(a[3], dev, {B}, "lens");
-  const float scale = scale_of(a[4], hd);
-  plain(q, "q");
-  plain(pool, "pool");
-  const On at(dev);
-  at::Tensor out = none(a[5]) ? make({B, rows, Hq, hd}, q.scalar_type(), dev) : tensor(a[5], "out");
-  void* op = on(out, dev, q.scalar_type(), q.sizes(), "out");
-  plain(out, "out");
-  const int32_t b = narrow(B, "q"), r = narrow(rows, "q"), hq = narrow(Hq, "q"), hk = narrow(Hkv, "pool"), d = narrow(hd, "q"),
-                pg = narrow(page, "pool"), w = narrow(width, "table");
-  const Scratch work(kf_op_paged_attention_work(b, r, hq, hk, d, pg, w), dev);
-  if (failed(kf_op_paged_attention(type, b, r, hq, hk, d, addr(q), step(q, 0), step(q, 1), step(q, 2), pp, n_pages, pg, tp, w, lp, scale,
-                                   op, work.ptr(), at.stream)))
+  const Paged x(a[0], a[1], a[2], a[3], a[4]);
+  const On at(x.dev);
+  const at::Tensor out = x.output(a[5]);
+  const Scratch work(kf_op_paged_attention_work(x.B, x.rows, x.Hq, x.Hkv, x.hd, x.page, x.width), x.dev);
+  if (failed(kf_op_paged_attention(x.type, x.B, x.rows, x.Hq, x.Hkv, x.hd, addr(x.q), step(x.q, 0), step(x.q, 1), step(x.q, 2), x.pp, x.n_pages,
+                                   x.page, x.tp, x.width, x.lp, x.scale, addr(out), work.ptr(), at.stream)))
     return nullptr;
   if (!none(a[5])) changed(out);
+  return THPVariable_Wrap(out);
+}
+// q, pool, table, lens, groups, shared, scale | None, out | None
+KF_PY(shared_attention, 8) {
+  const Paged x(a[0], a[1], a[2], a[3], a[6]);
+  const int32_t n = length(a[5], "shared");
+  const int32_t *groups = ints(a[4], x.dev, {(int64_t)n + 1}, "groups"), *shared = ints(a[5], x.dev, {(int64_t)n}, "shared");
+  const On at(x.dev);
+  const at::Tensor out = x.output(a[7]);
+  const Scratch work(kf_op_shared_attention_work(x.B, x.rows, x.Hq, x.Hkv, x.hd, x.n_pages, x.page, x.width, n), x.dev);
+  if (failed(kf_op_shared_attention(x.type, x.B, x.rows, x.Hq, x.Hkv, x.hd, addr(x.q), step(x.q, 0), step(x.q, 1), step(x.q, 2), x.pp, x.n_pages,
+                                    x.page, x.tp, x.width, x.lp, n, groups, shared, x.scale, addr(out), work.ptr(), at.stream)))
+    return nullptr;
+  if (!none(a[7])) changed(out);
   return THPVariable_Wrap(out);
 }
 
@@ -600,7 +633,7 @@ KF_PY(policy_loss, 12) {
 
 #define KF_ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {KF_ENTRY(set_check),     KF_ENTRY(rotate_heads),     KF_ENTRY(rotate_append),   KF_ENTRY(rotate_heads_grad),
-                           KF_ENTRY(prompt_attention), KF_ENTRY(paged_attention), KF_ENTRY(pages_grow),
+                           KF_ENTRY(prompt_attention), KF_ENTRY(paged_attention), KF_ENTRY(shared_attention), KF_ENTRY(pages_grow),
                            KF_ENTRY(pages_free),    KF_ENTRY(pages_fork),       KF_ENTRY(pages_compact),   KF_ENTRY(pages_copy),
                            KF_ENTRY(pages_append),  KF_ENTRY(token_scores),     KF_ENTRY(token_scores_grad), KF_ENTRY(policy_loss), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_serving", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
