@@ -7,9 +7,13 @@ shared, the last one copied), and every candidate draws its own tokens, one nois
 token, by the noise -> token map of the LM head (kf_op_head_tokens).  Each
 token is scored under the model; the best candidate of each prompt stays, the others' pages
 go back, and what is left of the cache is moved together.  ``head_step`` gives the
-loss of the kept tokens and the LM head's gradient, the step that would train on them.
+loss of the kept tokens and the LM head's gradient, the step that would train on them;
+``policy_step`` that of all candidates under a reward of each, clipped to the policy that drew them.
 
-    python -m paper_2606_10820_gb300.best_of_n --prompts 4 --n 8 --tokens 32
+``shared`` reads a prompt's keys once for all of its candidates, and rotates heads on their way to the
+pages; Config.qk_norm gives the model norms of its query and key heads.
+
+    python -m paper_2606_10820_gb300.best_of_n --prompts 4 --n 8 --tokens 32 [--shared] [--policy] [--qk-norm]
 """
 from __future__ import annotations
 
@@ -35,6 +39,7 @@ class Config:
     hd: int = 64
     ff: int = 2048
     vocab: int = 30522
+    qk_norm: bool = False
 
 
 class Model:
@@ -50,6 +55,9 @@ class Model:
         self.head = w(c.vocab, c.d)
         self.layers = [(w((c.heads + 2 * c.kv_heads) * c.hd, c.d), w(c.d, c.heads * c.hd), w(c.ff, c.d), w(c.d, c.ff))
                        for _ in range(c.layers)]
+        self.freq = 1e4 ** (-2.0 * torch.arange(c.hd // 2, dtype=torch.float64, device="cuda") / c.hd)
+        # what rotate_heads and rotate_append take beside the heads, a dict a layer
+        self.turn = [{"eps": 1e-6, "q_weight": 1 + 10 * w(c.hd), "k_weight": 1 + 10 * w(c.hd)} if c.qk_norm else {} for _ in range(c.layers)]
 
     @staticmethod
     def norm(h):
@@ -63,14 +71,23 @@ class Model:
         a, b = x[..., :half].float(), x[..., half:].float()
         return torch.cat([a * cos - b * sin, b * cos + a * sin], -1).bfloat16()
 
-    def run(self, tokens, pos, attend):
-        """The final hidden rows [T, d] bf16 of tokens at pos; attend(layer, q, k, v) -> [T, heads, hd]."""
+    def heads(self, layer, q, k, pos):
+        """The rotated query and key heads."""
+        if self.turn[layer]:
+            return serving.rotate_heads(q, k, pos.int(), self.freq, **self.turn[layer])
+        return self.rotate(q, pos), self.rotate(k, pos)
+
+    def run(self, tokens, pos, attend, raw=False):
+        """The final hidden rows [T, d] bf16 of tokens at pos; attend(layer, q, k, v) -> [T, heads, hd], of rotated heads
+        (raw: of the projections' own)."""
         c = self.cfg
         h = self.emb[tokens].float()
         for i, (wqkv, wo, up, down) in enumerate(self.layers):
             qkv = (self.norm(h) @ wqkv.T).view(len(h), -1, c.hd)
             q, k, v = qkv.split([c.heads, c.kv_heads, c.kv_heads], 1)
-            o = attend(i, self.rotate(q, pos), self.rotate(k, pos), v)
+            if not raw:
+                q, k = self.heads(i, q, k, pos)
+            o = attend(i, q, k, v)
             h = h + (o.reshape(len(h), -1) @ wo.T).float()
             h = h + (torch.nn.functional.gelu(self.norm(h) @ up.T, approximate="tanh") @ down.T).float()
         return self.norm(h)
@@ -103,8 +120,9 @@ def _ints(x):
     return torch.as_tensor(x, dtype=torch.int32, device="cuda")
 
 
-def best_of_n(model: Model, prompts, n, steps, noise, tau=1.0):
+def best_of_n(model: Model, prompts, n, steps, noise, tau=1.0, shared=False):
     """n answers of `steps` tokens to each prompt (lists of ids), noise [steps, prompts * n] in [0, 1).
+    shared: the candidates' attention reads their prompt's keys once, and heads are rotated on their way to the pages.
 
     A dict: tokens [prompts, n, steps]; logp [prompts, n, steps], their scores; best [prompts], the
     answer of the highest total; rows, the hidden rows that the tokens were drawn from; cache, with
@@ -125,6 +143,7 @@ def best_of_n(model: Model, prompts, n, steps, noise, tau=1.0):
         cache.append(layer, k, v, starts, owners)
         return serving.prompt_attention(q, k, v, starts, max(lens))
 
+    # (the prompts' rotated keys are read by their own attention: they are wanted as rows, not in pages alone)
     rows = model.run(ids, pos, whole)[(starts[1:] - 1).long()]
 
     # candidate i of prompt p in slot P + p n + i
@@ -140,13 +159,19 @@ def best_of_n(model: Model, prompts, n, steps, noise, tau=1.0):
         cache.append(layer, k, v, one_each, slots)
         return serving.paged_attention(q[:, None], cache.pool[layer], table, at + 1)[:, 0]
 
+    groups, prompt_lens = _ints(range(0, P * n + 1, n)), _ints(lens)
+
+    def newest_shared(layer, q, k, v):
+        q = serving.rotate_append(q, k, v, cache.pool[layer], one_each, cache.table, cache.lens, slots, model.freq, **model.turn[layer])
+        return serving.shared_attention(q[:, None], cache.pool[layer], table, at + 1, groups, prompt_lens)[:, 0]
+
     for step in range(steps):
         drawn_from.append(rows)
         tokens.append(draw_tokens(rows, model.head, noise[step].contiguous(), tau))
         logp.append(serving.token_scores(rows @ model.head.T, tokens[-1], tau=tau)["logp"])
         serving.pages_grow(*cache.book, slots, at + 1)
         table = cache.table[P:]
-        rows = model.run(tokens[-1], at, newest)
+        rows = model.run(tokens[-1], at, newest_shared, raw=True) if shared else model.run(tokens[-1], at, newest)
         at = at + 1
 
     logp = torch.stack(logp, 1).view(P, n, steps)
@@ -170,22 +195,43 @@ def head_step(model: Model, answer, tau=1.0):
     return -out["logp"].mean(), out["grad"].T @ rows
 
 
+def policy_step(model: Model, answer, reward, clip=(0.2, 0.28), kl_weight=0.01, entropy_weight=0.0, ref_logp=None, tau=1.0):
+    """The clipped policy loss of all answers' tokens under reward [prompts, n], and the LM head's gradient [V, d].
+
+    An answer's advantage is its reward against its prompt's other answers (their mean, in units of their deviation); the tokens'
+    scores as they were drawn are the old policy's, and the reference's where ref_logp [prompts, n, steps] is not given."""
+    P, n, steps = answer["tokens"].shape
+    advantage = (reward - reward.mean(1, keepdim=True)) / (reward.std(1, keepdim=True) + 1e-6)
+    old = answer["logp"].flatten()
+    rows = answer["rows"].flatten(0, 1)
+    out = serving.policy_loss(rows @ model.head.T, answer["tokens"].flatten(), old, advantage.float().repeat_interleave(steps),
+                              ref_logp=old if ref_logp is None else ref_logp.flatten(), weight=torch.full_like(old, 1.0 / len(old)), clip=clip,
+                              kl_weight=kl_weight, entropy_weight=entropy_weight, tau=tau)
+    return out["loss"].sum(), out["grad"].T @ rows
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--prompts", type=int, default=4)
     ap.add_argument("--n", type=int, default=8)
     ap.add_argument("--tokens", type=int, default=32)
+    ap.add_argument("--shared", action="store_true", help="read a prompt's keys once for all of its candidates")
+    ap.add_argument("--policy", action="store_true", help="a policy step on all candidates too, the mean score as their reward")
+    ap.add_argument("--qk-norm", action="store_true", help="a model with norms of its query and key heads")
     a = ap.parse_args()
-    model, g = Model(Config()), torch.Generator().manual_seed(1)
+    model, g = Model(Config(qk_norm=a.qk_norm)), torch.Generator().manual_seed(1)
     lens = torch.randint(20, 400, (a.prompts,), generator=g).tolist()
     prompts = [torch.randint(0, model.cfg.vocab, (x,), generator=g).tolist() for x in lens]
     noise = torch.rand(a.tokens, a.prompts * a.n, generator=g).cuda()
-    out = best_of_n(model, prompts, a.n, a.tokens, noise)
+    out = best_of_n(model, prompts, a.n, a.tokens, noise, shared=a.shared)
     loss, grad = head_step(model, out)
     for p in range(a.prompts):
         total = out["logp"][p].sum(-1)
         print(f"prompt of {lens[p]}: best of {a.n} is {int(out['best'][p])}, log p {total.max():.2f} (mean {total.mean():.2f})")
     print(f"{out['live']} pages live; loss of the kept tokens {loss:.4f}, head gradient norm {grad.float().norm():.4f}")
+    if a.policy:
+        loss, grad = policy_step(model, out, out["logp"].mean(-1))
+        print(f"policy loss of all tokens {loss:.4f}, head gradient norm {grad.float().norm():.4f}")
 
 
 if __name__ == "__main__":

@@ -279,7 +279,7 @@ static_assert(sizeof(Part) + NW * sizeof(long long) <= 128, "the static arrays")
 static_assert(kFits<64, 1> && kFits<64, 2> && kFits<128, 1> && kFits<128, 2>, "the CTAs of an SM");
 
 template <typename T, int HD, int TILES, bool SHARED>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const Args a) {
+__device__ __forceinline__ void attend(const Args& a) {
   extern __shared__ __align__(128) uint8_t sm[];
   constexpr int ST = kStages<HD, TILES>, ROWS = 16 * TILES, HELD = kHeld<HD, TILES>;
   constexpr int PARTS = kTurns<HD, TILES> ? 2 : 1;      // warps of a piece that hold its rows in the end
@@ -539,6 +539,12 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+template <typename T, int HD, int TILES>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const __grid_constant__ Args a) { attend<T, HD, TILES, false>(a); }
+// the keys from the groups' prefixes on (kf_shared.cuh)
+template <typename T, int HD, int TILES>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_own(const __grid_constant__ Args a) { attend<T, HD, TILES, true>(a); }
+
 // Block (c, y): rows y, y + gridDim.y, ... of the segment that CTA c began and others went on
 // with: its pieces (slot 1 of c, slot 0 of c + 1, c + 2, ...) added in order
 constexpr int kJoinThreads = 256;
@@ -629,8 +635,8 @@ int launch(Args a, const Shape& sh, void* work, cudaStream_t s) {
   // and 16 blocks: 20.2, 15.1, 13.1 us; 128 of 512 to 8192, 32 heads over 8: 685, 686, 691)
   const int by = (int)std::min<long long>(16, std::max(4ll, 2 * grid / sh.segments));
   static PerDevice attr;
-  set_smem_attr(attr, k_paged<T, HD, TILES, false>, kSmem<HD, TILES>);
-  launch_cluster(k_paged<T, HD, TILES, false>, dim3(grid), dim3(kThreads), kSmem<HD, TILES>, 1, false, s, a);
+  set_smem_attr(attr, k_paged<T, HD, TILES>, kSmem<HD, TILES>);
+  launch_cluster(k_paged<T, HD, TILES>, dim3(grid), dim3(kThreads), kSmem<HD, TILES>, 1, false, s, a);
   if (!sh.direct && grid > 1) launch_cluster(k_join<T, HD, TILES>, dim3(grid, std::min(by, a.rows * a.G)), dim3(kJoinThreads), 0, 1, true, s, a);
   return launched("kf_op_paged_attention");
 }
@@ -642,8 +648,8 @@ int launch_any(int hd, const Args& a, const Shape& sh, void* work, cudaStream_t 
 template <typename T, int HD, int TILES>
 void launch_own(const Args& a, int grid, cudaStream_t s) {
   static PerDevice attr;
-  set_smem_attr(attr, k_paged<T, HD, TILES, true>, kSmem<HD, TILES>);
-  launch_cluster(k_paged<T, HD, TILES, true>, dim3(grid), dim3(kThreads), kSmem<HD, TILES>, 1, true, s, a);
+  set_smem_attr(attr, k_own<T, HD, TILES>, kSmem<HD, TILES>);
+  launch_cluster(k_own<T, HD, TILES>, dim3(grid), dim3(kThreads), kSmem<HD, TILES>, 1, true, s, a);
 }
 template <typename T>
 void launch_own_any(int hd, int tiles, const Args& a, int grid, cudaStream_t s) {
