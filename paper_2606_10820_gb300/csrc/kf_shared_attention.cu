@@ -28,6 +28,17 @@ struct Item {
   int n[2];                                          // key tiles (0: no sub-tile)
   int more;                                          // a later piece of its segment
 };
+// row r of an item: its sequence of the group, token of that and head of the KV head's
+struct Row {
+  int seq, tok, j;
+  __device__ __forceinline__ Row(const SharedCall& a, const Item& im, int r) {
+    const int R = im.first + r;
+    seq = a.by_seq.of(R);
+    const int x = R - seq * (int)a.by_seq.d;
+    tok = a.by_group.of(x);
+    j = x - tok * a.G;
+  }
+};
 using Bars = PairBars<Item>;
 static_assert(sizeof(Bars) <= kBarBytes, "the barriers' part of the shared memory");
 
@@ -44,7 +55,87 @@ struct Group {
     tiles = (len + kKeys - 1) / kKeys;
     pairs = tiles > 0 ? (rows + kPrefixRows - 1) / kPrefixRows : 0;
   }
-  __device__ __forceinline__ int64_t places(const SharedCall& a) const { return (int64_t)pairs * a.Hkv * (tiles + kExtra); }
+  __device__ __forceinline__ int places(const SharedCall& a) const { return pairs * a.Hkv * (tiles + kExtra); }
+};
+
+// The list of `total` places in `parts` even parts: the first `more` have one more than the others
+struct Parts {
+  int total, parts, each, more;
+  Parts() = default;
+  __device__ __forceinline__ Parts(int total_, int most) : total(total_) {
+    parts = min(most, max(1, total / kMinTiles));
+    each = total / parts;
+    more = total - each * parts;
+  }
+  __device__ __forceinline__ int begin(int c) const { return c < parts ? c * each + min(c, more) : total; }
+  __device__ __forceinline__ int part_of(int x) const {
+    const int split = more * (each + 1);
+    return x < split ? x / (each + 1) : more + (x - split) / each;
+  }
+};
+
+// A CTA's pieces of segments, in order (by the load warp, uniform)
+struct Walk {
+  Parts parts;
+  int x, x1, base, g;            // the next place, the part's end; the group that it lies in, whose places begin at base
+  int at, pieces;                // of the piece: its segment's record, and the CTAs that have pieces of it
+  __device__ __forceinline__ void start(const SharedCall& a, int lane) {
+    base = g = 0;
+    const int mine = lane < a.sh.n ? Group(a, lane).places(a) : 0;
+    int total = __reduce_add_sync(~0u, mine);
+    for (int i = 32; i < a.sh.n; i += 32) total += __reduce_add_sync(~0u, i + lane < a.sh.n ? Group(a, i + lane).places(a) : 0);
+    parts = Parts(total, gridDim.x);
+    x = parts.begin(blockIdx.x);
+    x1 = parts.begin(blockIdx.x + 1);
+    for (int i = 0; x < x1 && i < a.sh.n; i += 32) {
+      const int v = i == 0 ? mine : i + lane < a.sh.n ? Group(a, i + lane).places(a) : 0;
+      int incl = v;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(~0u, incl, o);
+        if (lane >= o) incl += u;
+      }
+      const uint32_t past = __ballot_sync(~0u, base + incl > x);
+      if (past) {
+        const int l = __ffs(past) - 1;
+        base += __shfl_sync(~0u, incl - v, l);
+        g = i + l;
+        break;
+      }
+      base += __shfl_sync(~0u, incl, 31);
+    }
+  }
+  // the next piece; one without tiles past the last
+  __device__ __forceinline__ Item next(const SharedCall& a) {
+    Item im{};
+    while (x < x1) {
+      const Group gr(a, g);
+      const int per = gr.tiles + kExtra, places = gr.places(a);
+      if (x >= base + places) {                 // (also a group without places)
+        base += places;
+        if (++g >= a.sh.n) break;
+        continue;
+      }
+      // a segment: pair by pair, head by head
+      const int s = (x - base) / per, pair = s / a.Hkv, hk = s - pair * a.Hkv;
+      const int xs = base + s * per, end = xs + gr.tiles, t0 = x - xs, n = min(end, x1) - x;
+      x = min(xs + per, x1);
+      if (n <= 0) continue;                     // only places of its end
+      im.b0 = gr.b0;
+      im.first = pair * kPrefixRows;
+      im.rows = min(kPrefixRows, gr.rows - im.first);
+      im.hk = hk;
+      im.t0 = t0;
+      im.len = gr.len;
+      im.n[0] = n;
+      im.n[1] = im.rows > kRows ? n : 0;
+      im.more = t0 > 0;
+      at = prefix_record(gr.before, g, pair, hk, a.Hkv);
+      pieces = parts.part_of(end - 1) - blockIdx.x + 1;      // (parts up to the one of the segment's last tile)
+      break;
+    }
+    return im;
+  }
 };
 
 template <typename T, int HD>
@@ -60,7 +151,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
     if (t == 0) atomicOr(a.err, kErrInternal);
     return;
   }
-  if (t == 0) {
+  if (t == 64) {
     auto init = [](uint64_t* p, uint32_t n) { mbar_init(smem_u32(p), n); };
     init(&b.q_full, 8);                         // the softmax warps, which copy Q
     init(&b.q_empty, 1);
@@ -81,6 +172,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  // the load warp finds the first item, and its first tile's pages, before the barrier
+  Walk walk;
+  Item im;
+  int id = -1;
+  // lane x < 8 looks up box x of a tile
+  auto look = [&](int tile) -> int {
+    const int key = tile * kKeys + lane * kGran;
+    return lane < kGrans && key < im.len ? __ldg(a.table + (int64_t)im.b0 * a.width + a.by_page.of(key)) : -1;
+  };
+  if (warp == 0) {
+    walk.start(a, lane);
+    im = walk.next(a);
+    if (lane == 0) b.item[0] = im;
+    if (im.n[0] > 0) id = look(im.t0);
+  }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&b.tmem)), "r"(kTmemCols)
                  : "memory");
@@ -95,105 +201,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
     if (warp == 0) {
       // ------------------------------------------------------ items and copies
-      // this CTA's part [x0, x1) of the list, and the group that it begins in (its places begin at `base`)
-      if (blockIdx.x == 0) {
-        bool bad = false;
-        for (int g = lane; g < a.sh.n; g += 32) {
-          const int p = a.sh.groups[g], e = a.sh.groups[g + 1], n = a.sh.shared[g];
-          bad |= p < 0 || e < p || e > a.B || (g == 0 && p != 0) || (g == a.sh.n - 1 && e != a.B) || n < 0 || n > a.width * a.page;
-        }
-        if (__any_sync(~0u, bad) && lane == 0) atomicOr(a.err, KF_DEV_BAD_ROW);
-      }
-      int64_t total = 0;
-      for (int g0 = 0; g0 < a.sh.n; g0 += 32) {
-        const int g = g0 + lane;
-        int64_t v = g < a.sh.n ? Group(a, g).places(a) : 0;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
-        total += v;
-      }
-      const int parts = (int)min((int64_t)gridDim.x, max((int64_t)1, total / kMinTiles)), c = blockIdx.x;
-      const int64_t x0 = c < parts ? total * c / parts : total, x1 = c < parts ? total * (c + 1) / parts : total;
-      int64_t base = 0;
-      int g = 0;
-      for (int g0 = 0; x0 < x1 && g0 < a.sh.n; g0 += 32) {
-        const int64_t v = g0 + lane < a.sh.n ? Group(a, g0 + lane).places(a) : 0;
-        int64_t incl = v;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int64_t u = __shfl_up_sync(~0u, incl, o);
-          if (lane >= o) incl += u;
-        }
-        const uint32_t past = __ballot_sync(~0u, base + incl > x0);
-        if (past) {
-          const int l = __ffs(past) - 1;
-          base += __shfl_sync(~0u, incl - v, l);
-          g = g0 + l;
-          break;
-        }
-        base += __shfl_sync(~0u, incl, 31);
-      }
       bool ok = true;
-      int it = 0, ring = 0, tails = 0;
+      int ring = 0, tails = 0;
       auto wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, a.err)); };
-      auto publish = [&](const Item& im) -> bool {
+      for (int it = 0;; ++it) {
         const int slot = it & 1;
-        if (!wait(&b.item_empty[slot], ((it >> 1) & 1) ^ 1)) return false;
-        if (lane == 0) {
-          b.item[slot] = im;
-          mbar_arrive(smem_u32(&b.item_full[slot]));
+        if (it > 0) {
+          im = walk.next(a);
+          ok = wait(&b.item_empty[slot], ((it >> 1) & 1) ^ 1);
+          if (!ok) break;
+          if (lane == 0) b.item[slot] = im;
+          __syncwarp();
         }
-        __syncwarp();
-        ++it;
-        return true;
-      };
-      for (int64_t x = x0; ok && x < x1;) {
-        Group gr(a, g);
-        const int per = gr.tiles + kExtra;
-        const int64_t places = gr.places(a);
-        if (x >= base + places) {               // (also a group without places)
-          base += places;
-          if (++g >= a.sh.n) break;
-          continue;
-        }
-        // a segment: pair by pair, head by head
-        const int s = (int)((x - base) / per), pair = s / a.Hkv, hk = s - pair * a.Hkv;
-        const int64_t xs = base + (int64_t)s * per, end = xs + gr.tiles;
-        const int t0 = (int)(x - xs), n = (int)(min(end, x1) - x);
-        x = min(xs + per, x1);
-        if (n <= 0) continue;                   // only places of its end
-        Item im;
-        im.b0 = gr.b0;
-        im.first = pair * kPrefixRows;
-        im.rows = min(kPrefixRows, gr.rows - im.first);
-        im.hk = hk;
-        im.t0 = t0;
-        im.len = gr.len;
-        im.n[0] = n;
-        im.n[1] = im.rows > kRows ? n : 0;
-        im.more = t0 > 0;
-        if (lane == 0 && t0 == 0) {
-          // (parts up to the last that begins before the segment's end)
-          const int at = prefix_record(gr.before, g, pair, hk, a.Hkv);
-          if (at < a.pre.segments) a.pre.rec[at] = Record{c, (int)((end * parts + total - 1) / total) - c};
-        }
-        ok = publish(im);
-        if (!ok) break;
-        // lane x < 8 looks up box x of a tile
-        const int32_t* ids = a.table + (int64_t)gr.b0 * a.width;
-        auto look = [&](int tile) -> int {
-          const int key = tile * kKeys + lane * kGran;
-          return lane < kGrans && key < gr.len ? __ldg(ids + key / a.page) : -1;
-        };
-        int id = look(t0);
+        if (lane == 0) mbar_arrive(smem_u32(&b.item_full[slot]));
+        if (im.n[0] == 0) break;                // (an item without sub-tiles ends the others)
+        if (it > 0) id = look(im.t0);
+        if (lane == 0 && !im.more && walk.at < a.pre.segments) a.pre.rec[walk.at] = Record{(int)blockIdx.x, walk.pieces};
+        const int t0 = im.t0, n = im.n[0], hk = im.hk;
         for (int j = t0; ok && j < t0 + n; ++j) {
-          const int key = j * kKeys + lane * kGran, left = gr.len - j * kKeys;
+          const int key = j * kKeys + lane * kGran, left = im.len - j * kKeys;
           // (a box outside of the map: zeros)
           const bool in = id >= 0 && id < a.n_pages;
-          const int page = in ? id : (int)a.n_pages, row = in ? key % a.page : 0;
-          if (lane < kGrans && key < gr.len && !in) atomicOr(a.err, KF_DEV_BAD_PAGE);
+          const int page = in ? id : (int)a.n_pages, row = in ? key - a.by_page.of(key) * a.page : 0;
+          if (lane < kGrans && key < im.len && !in) atomicOr(a.err, KF_DEV_BAD_PAGE);
           if (j + 1 < t0 + n) id = look(j + 1);
-          for (int kv = 0; kv < 2; ++kv, ++ring) {
+          // (the first Q comes before the bulk of the first K and V: behind them it took 7 us)
+          if (it == 0 && j == t0 + 1) ok = wait(&b.q_full, 0);
+          for (int kv = 0; ok && kv < 2; ++kv, ++ring) {
             const int st = ring % ST;
             ok = wait(&b.kv_empty[st], ((ring / ST) & 1) ^ 1);
             if (!ok) break;
@@ -221,10 +255,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
             }
           }
         }
+        if (!ok) break;
       }
-      if (ok) {
-        Item im{};                              // (an item without sub-tiles ends the others)
-        ok = publish(im);
+      if (blockIdx.x == 0) {
+        bool bad = false;
+        for (int i = lane; i < a.sh.n; i += 32) {
+          const int p = a.sh.groups[i], e = a.sh.groups[i + 1], n = a.sh.shared[i];
+          bad |= p < 0 || e < p || e > a.B || (i == 0 && p != 0) || (i == a.sh.n - 1 && e != a.B) || n < 0 || n > a.width * a.page;
+        }
+        if (__any_sync(~0u, bad) && lane == 0) atomicOr(a.err, KF_DEV_BAD_ROW);
       }
       if (!ok && lane == 0)
         // let the copies still in flight land before the CTA ends (bounded)
@@ -253,39 +292,37 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
       const Item im = b.item[slot];
       arrive(&b.item_empty[slot]);
       if (im.n[0] == 0) break;
-      const int n = im.n[sub], per = a.rows * a.G;
+      const int n = im.n[sub];
       if (it > 0) ok = wait(&b.q_empty, (it - 1) & 1);
       if (!ok) break;
       if (n > 0) {
         // this warp's 32 rows of Q, swizzled; rows that the segment does not have are zeros
         constexpr int CH = HD / 8, RP = 32 / CH;
         const int ch = lane % CH;
-        uint4 v[CH];
 #pragma unroll
         for (int p = 0; p < CH; ++p) {
-          const int r = sub * kRows + 32 * quarter + p * RP + lane / CH, R = im.first + r, seq = R / per, x = R - seq * per, tok = x / a.G;
-          v[p] = r < im.rows ? __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (im.b0 + seq) * a.q_seq + tok * a.q_row +
-                                                                    (int64_t)(im.hk * a.G + x - tok * a.G) * a.q_head) + ch)
-                             : make_uint4(0u, 0u, 0u, 0u);
+          const int lr = 32 * quarter + p * RP + lane / CH, r = sub * kRows + lr;
+          const Row w(a, im, r);
+          const T* from = static_cast<const T*>(a.q) + (im.b0 + w.seq) * a.q_seq + w.tok * a.q_row + (int64_t)(im.hk * a.G + w.j) * a.q_head + 8 * ch;
+          const bool in = r < im.rows;
+          mma::cp_async16(sQ + sub * TILE + (ch / 8) * kAtom + lr * 128 + (((ch % 8) ^ (lr & 7)) << 4), in ? from : static_cast<const T*>(a.q), in ? 16 : 0);
         }
-#pragma unroll
-        for (int p = 0; p < CH; ++p) {
-          const int r = 32 * quarter + p * RP + lane / CH;
-          *reinterpret_cast<uint4*>(sm + sub * TILE + (ch / 8) * kAtom + r * 128 + (((ch % 8) ^ (r & 7)) << 4)) = v[p];
-        }
+        mma::cp_commit();
+        mma::cp_wait<0>();
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       }
       arrive(&b.q_full);
       if (n == 0) continue;
       // this thread's row: its place among all rows, and the keys that it sees
-      const int r = sub * kRows + row, R = im.first + r, seq = R / per, x = R - seq * per, tok = x / a.G;
+      const int r = sub * kRows + row;
+      const Row w(a, im, r);
       const bool mine = r < im.rows;
       int see = 0;
-      if (mine) see = min(im.len, min(max(__ldg(a.lens + im.b0 + seq), 0), a.width * a.page) - a.rows + tok + 1);
+      if (mine) see = min(im.len, min(max(__ldg(a.lens + im.b0 + w.seq), 0), a.width * a.page) - a.rows + w.tok + 1);
       const int32_t* ids = a.table + (int64_t)im.b0 * a.width;
       auto look = [&](int tile) -> int {        // the tile's page of box `lane`
         const int key = tile * kKeys + lane * kGran;
-        return lane < kGrans && key < im.len ? __ldg(ids + key / a.page) : 0;
+        return lane < kGrans && key < im.len ? __ldg(ids + a.by_page.of(key)) : 0;
       };
       int id = look(im.t0);
       float m = -INFINITY, l = 0.f;
@@ -306,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
       if (!wait(&b.o_full[sub], (g - 1) & 1)) { ok = false; break; }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const int64_t at = im.more ? (int64_t)blockIdx.x * kPrefixRows + r
-                                 : ((int64_t)(im.b0 + seq) * a.rows + tok) * a.Hq + im.hk * a.G + x - tok * a.G;
+                                 : ((int64_t)(im.b0 + w.seq) * a.rows + w.tok) * a.Hq + im.hk * a.G + w.j;
       float* dst = (im.more ? a.pre.more_o : a.pre.first_o) + at * HD;
       if (mine) (im.more ? a.pre.more_ml : a.pre.first_ml)[at] = make_float2(m, l);
 #pragma unroll
@@ -330,19 +367,31 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
 }
 
-// A warp per query row: the pieces of its group's prefix and of its sequence's own keys added, in one order
-constexpr int kJoinThreads = 256;
+// The pieces of a query row added: those of its group's prefix and those of its sequence's own keys, by W warps (each
+// every W-th piece; their sums then in order)
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 template <typename T, int HD>
-__global__ void __launch_bounds__(kJoinThreads) k_add(const SharedCall a) {
+__global__ void __launch_bounds__(kJoinThreads) k_add(const __grid_constant__ SharedCall a, int W) {
   constexpr int N = HD / 32;                    // values of a lane
   using V = typename std::conditional<N == 4, float4, float2>::type;
-  const int lane = threadIdx.x & 31;
-  const int64_t at = (int64_t)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
-  const int64_t tokens = (int64_t)a.B * a.rows;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (at >= tokens * a.Hq) return;
+  __shared__ V so[kJoinWarps][32];
+  __shared__ float2 sml[kJoinWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % W;
+  const int64_t rows = (int64_t)a.B * a.rows * a.Hq, at = min(rows - 1, (int64_t)blockIdx.x * (kJoinWarps / W) + warp / W);
   const int64_t bt = at / a.Hq;
-  const int h = (int)(at - bt * a.Hq), b = (int)(bt / a.rows), tok = (int)(bt - (int64_t)b * a.rows), hk = h / a.G, r = tok * a.G + h - hk * a.G;
+  const int h = (int)(at - bt * a.Hq), b = (int)(bt / a.rows), tok = (int)(bt - (int64_t)b * a.rows), hk = a.by_group.of(h), r = tok * a.G + h - hk * a.G;
+  const int g = group_of(a.sh, b);
+  const int2 in = members(a.sh, g, a.B);
+  const bool prefixed = b >= in.x && b < in.y && prefix_of(a.sh, g, a.width * a.page) > 0;
+  const int64_t x = (int64_t)(b - in.x) * a.rows * a.G + r;
+  const int MT = (a.rows * a.G + a.own.seg_rows - 1) / a.own.seg_rows;
+  const int own_rec = (b * a.Hkv + hk) * MT + r / a.own.seg_rows;
+  const int pre_rec = prefixed ? min(a.pre.segments - 1, prefix_record((int64_t)in.x * a.rows * a.G, g, (int)(x / kPrefixRows), hk, a.Hkv)) : 0;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // (written by the kernels before this one: not through the read-only path; a record of groups that are not as they
+  // should be may hold anything)
+  const int2 own = __ldcg(reinterpret_cast<const int2*>(a.own.rec) + own_rec);
+  const int2 pre = prefixed ? __ldcg(reinterpret_cast<const int2*>(a.pre.rec) + pre_rec) : make_int2(0, 0);
   float m = -INFINITY, l = 0.f, o[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) o[i] = 0.f;
@@ -355,27 +404,23 @@ __global__ void __launch_bounds__(kJoinThreads) k_add(const SharedCall a) {
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = o[i] * fa + v[i] * fb;
   };
-  // (written by the kernels before this one: not through the read-only path; a record of groups that are not as they
-  // should be may hold anything)
-  auto pieces = [&](const Partials& p, int64_t rec, int row) {
-    const int2 rc = __ldcg(reinterpret_cast<const int2*>(p.rec) + rec);
-    add(__ldcg(p.first_ml + at), __ldcg(reinterpret_cast<const V*>(p.first_o + at * HD) + lane));
-    const int c0 = max(rc.x, 0) + 1, c1 = min(p.ctas, max(rc.x, 0) + rc.y);
+  auto pieces = [&](const Partials& p, int2 rc, int row) {
+    const int c = max(rc.x, 0), n = min(p.ctas - c, rc.y);
 #pragma unroll 4
-    for (int c = c0; c < c1; ++c) {
-      const int64_t q = (int64_t)c * p.seg_rows + row;
-      add(__ldcg(p.more_ml + q), __ldcg(reinterpret_cast<const V*>(p.more_o + q * HD) + lane));
+    for (int i = part; i < n; i += W) {
+      const int64_t q = i == 0 ? at : (int64_t)(c + i) * p.seg_rows + row;
+      add(__ldcg((i == 0 ? p.first_ml : p.more_ml) + q), __ldcg(reinterpret_cast<const V*>((i == 0 ? p.first_o : p.more_o) + q * HD) + lane));
     }
   };
-  const int g = group_of(a.sh, b);
-  const int2 in = members(a.sh, g, a.B);
-  if (b >= in.x && b < in.y && prefix_of(a.sh, g, a.width * a.page) > 0) {
-    const int64_t x = (int64_t)(b - in.x) * a.rows * a.G + r;
-    const int rec = prefix_record((int64_t)in.x * a.rows * a.G, g, (int)(x / kPrefixRows), hk, a.Hkv);
-    if (rec < a.pre.segments) pieces(a.pre, rec, (int)(x % kPrefixRows));
+  pieces(a.own, own, r % a.own.seg_rows);
+  if (prefixed) pieces(a.pre, pre, (int)(x % kPrefixRows));
+  if (W > 1) {                                  // (uniform)
+    so[warp][lane] = *reinterpret_cast<V*>(o);
+    if (lane == 0) sml[warp] = make_float2(m, l);
+    __syncthreads();
+    if (part != 0) return;
+    for (int i = 1; i < W; ++i) add(sml[warp + i], so[warp + i][lane]);
   }
-  const int MT = (a.rows * a.G + a.own.seg_rows - 1) / a.own.seg_rows;
-  pieces(a.own, ((int64_t)b * a.Hkv + hk) * MT + r / a.own.seg_rows, r % a.own.seg_rows);
   const float inv = l == 0.f ? 0.f : 1.f / l;   // (no key seen: zeros)
   T* out = static_cast<T*>(a.out) + at * HD + lane * N;
   if constexpr (N == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv));
@@ -389,8 +434,12 @@ int launch(int32_t type, const SharedCall& c, const CUtensorMap& map, cudaStream
   set_smem_attr(attr, k_prefix<T, HD>, kSmem<HD>);
   launch_cluster(k_prefix<T, HD>, dim3(c.pre.ctas), dim3(kThreads), kSmem<HD>, 1, false, s, map, c);
   launch_own(type, c, s);
-  const int64_t rows = (int64_t)c.B * c.rows * c.Hq, per = kJoinThreads / 32;
-  launch_cluster(k_add<T, HD>, dim3((unsigned)((rows + per - 1) / per)), dim3(kJoinThreads), 0, 1, true, s, c);
+  // as many warps a row as fit the SMs at once
+  const int64_t rows = (int64_t)c.B * c.rows * c.Hq;
+  int W = 1;
+  while (W < kJoinWarps && rows * W * 2 <= (int64_t)device_sms() * 64) W *= 2;
+  const int64_t per = kJoinWarps / W;
+  launch_cluster(k_add<T, HD>, dim3((unsigned)((rows + per - 1) / per)), dim3(kJoinThreads), 0, 1, true, s, c, W);
   return launched("kf_op_shared_attention");
 }
 
@@ -434,6 +483,7 @@ const char* sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int 
   if (n < 0 || (B > 0 && n < 1)) return "groups out of range";
   if ((int64_t)B * rows * Hq > (1 << 30) || ((int64_t)B * rows * (Hq / Hkv) / kPrefixRows + n + 1) * Hkv > (1 << 30) || (int64_t)B * Hkv * rows * (Hq / Hkv) > (1 << 30))
     return "too many rows and heads";
+  if (((int64_t)B * rows * (Hq / Hkv) / kPrefixRows + n + 1) * Hkv * (((int64_t)width * page + kKeys - 1) / kKeys + kExtra) > 0x7fffffff) return "too many keys";
   return nullptr;
 }
 // Nothing to share: each sequence a group, or no pages
@@ -480,7 +530,7 @@ extern "C" int kf_op_shared_attention(int32_t type, int32_t B, int32_t rows, int
     return refuse(what, "q, pool and out are 16-byte aligned, work 256-byte");
   if (q_seq % 8 || q_row % 8 || q_head % 8) return refuse(what, "q's strides are multiples of 8 elements");
   SharedCall c{q, q_seq, q_row, q_head, pool, table, lens, out, n_pages, Sharing{groups, shared, n}, {}, {}, serving_error_word(),
-               B, rows, Hq, Hkv, Hq / Hkv, hd, page, width, scale * 1.4426950408889634f};
+               B, rows, Hq, Hkv, Hq / Hkv, hd, page, width, scale * 1.4426950408889634f, Div(page), Div(Hq / Hkv), Div(rows * (Hq / Hkv))};
   if (!c.err) return refuse(what, "no error word", KF_E_CUDA);
   layout(c, work);
   CUtensorMap map;
