@@ -11,10 +11,11 @@
 // from positions of a few thousand on.  The nearest quarter turn comes off in whole numbers, so the
 // sine and cosine are taken of |t| <= pi / 4.
 //
-// What bounds it: the heads, read and written once.  A warp takes a token: hd / 16 lanes a head (two 16-byte
-// vectors a lane, both elements of a pair in one lane), 4 or 8 heads a pass, the
-// next pass' loads ahead of this one's arithmetic; the token's angles are computed once by the
-// warp's lanes and passed on through shared memory.
+// What bounds it: the heads, read and written once.  A warp's pass takes 4 or 8 heads of a token: hd / 16 lanes a head, two
+// 16-byte vectors a lane, so that both elements of a pair are in one lane.  The passes of all tokens form one list that
+// the warps share evenly.  Each lane streams its vectors through slots of shared memory that are its own (cp.async, kAhead
+// passes ahead, across tokens; no thread waits for another's), so the loads under way do not
+// cost registers; a token's angles are computed once by the warp's lanes and passed on through shared memory.
 #include <algorithm>
 
 #include "kf_mma.cuh"
@@ -24,7 +25,8 @@ namespace kf {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;      // of a CTA
-constexpr int kAhead = 4;                   // passes whose loads are under way
+constexpr int kAhead = 5;                   // slots of a warp: one in use, the others' loads under way
+constexpr int kBackAhead = 4;
 constexpr int kJoinThreads = 256;
 
 struct Rows {
@@ -51,7 +53,9 @@ struct Args {
   Book book;
   int* err;
   int64_t T;
-  int Hq, Hkv, n, split;         // n: pairs; split: warps of a token
+  int64_t each, more;            // passes of a warp; the first `more` warps have one more
+  Div by_passes;                 // (below 2^31 passes; else divided in 64 bits)
+  int Hq, Hkv, n, passes, warps; // n: pairs; passes: of a token; warps: that have passes
   float eps, sign;               // eps < 0: no norms; sign: -1 turns back
 };
 
@@ -170,9 +174,17 @@ struct Where {
   int64_t row;                   // K's row of head 0 in the pool, in rows of hd; -1: not to be written
   bool ok;                       // the position is known
 };
-__device__ __forceinline__ Where find(const Book& k, int Hkv, int64_t t, int lane, int* err) {
-  // the last sequence that starts at or before t: 32 starts a step
+__device__ __forceinline__ Where find(const Book& k, int Hkv, int64_t t, int lane, bool flags, int* err) {
+  // the last sequence that starts at or before t: up to 256 starts at once, 32 a step for more
   int lo = 0, left = k.n;
+  if (left <= 256) {
+    int below = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (32 * i < left) below += 32 * i + lane < left && __ldg(k.starts + 32 * i + lane) <= t;
+    lo = max(0, __reduce_add_sync(~0u, below) - 1);
+    left = 1;
+  }
   while (left > 1) {
     const int step = (left + 31) / 32, at = lane * step;
     const uint32_t m = __ballot_sync(~0u, at < left && __ldg(k.starts + lo + min(at, left - 1)) <= t);
@@ -195,168 +207,215 @@ __device__ __forceinline__ Where find(const Book& k, int Hkv, int64_t t, int lan
       else w.row = (int64_t)p * 2 * Hkv * k.page + w.pos % k.page;
     }
   }
-  if (bad && lane == 0) atomicOr(err, bad);
+  if (bad && flags && lane == 0) atomicOr(err, bad);
   return w;
 }
 
-template <typename T, int HD, bool NB, bool APPEND>
-__global__ void __launch_bounds__(kThreads) k_rotate(const Args a) {
-  __shared__ __align__(16) float2 tab[kWarps][HD / 2];
-  constexpr int LANES = HD / 16, PER = 32 / LANES;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane / LANES;
-  const int64_t w = (int64_t)blockIdx.x * kWarps + warp, t = w / a.split;
-  if (t >= a.T) return;
-  const int heads = a.Hq + a.Hkv * (APPEND ? 2 : 1), passes = (heads + PER - 1) / PER;
-  const Place<HD, NB> pl(lane, a.n);
-  const T* from[3] = {static_cast<const T*>(a.q.p) + t * a.q.row, static_cast<const T*>(a.k.p) + t * a.k.row,
-                      APPEND ? static_cast<const T*>(a.v.p) + t * a.v.row : nullptr};
-  const int p0 = (int)(w - t * a.split);
-  uint4 u[kAhead][2];
-  auto load = [&](int p, uint4* d) {
-    const int j = p * PER + grp;
-    if (j >= heads) return;
-    const T* x = j < a.Hq ? from[0] + j * a.q.head : !APPEND || j < a.Hq + a.Hkv ? from[1] + (j - a.Hq) * a.k.head
-                                                                                 : from[2] + (j - a.Hq - a.Hkv) * a.v.head;
-    d[0] = *reinterpret_cast<const uint4*>(x + 8 * pl.c0);
-    d[1] = *reinterpret_cast<const uint4*>(x + 8 * pl.c1);
-  };
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i)
-    if (p0 + i * a.split < passes) load(p0 + i * a.split, u[i]);
-  uint4 wq[2], wk[2];
-  if (a.wq) {
-    wq[0] = __ldg(reinterpret_cast<const uint4*>(a.wq) + pl.c0);
-    wq[1] = __ldg(reinterpret_cast<const uint4*>(a.wq) + pl.c1);
+// A warp's passes, first .. last - 1 of the list; pass x is pass x % passes of token x / passes
+struct Range {
+  int64_t t;
+  int p, left;                   // the token and pass that come next; how many are left
+  __device__ __forceinline__ Range(const Args& a, int w) {
+    const int64_t first = w * a.each + min((int64_t)w, a.more);
+    left = w < a.warps ? (int)(a.each + (w < a.more)) : 0;
+    t = first < 0x7fffffff ? a.by_passes.of((int)first) : first / a.passes;
+    p = (int)(first - t * a.passes);
   }
-  if (a.wk) {
-    wk[0] = __ldg(reinterpret_cast<const uint4*>(a.wk) + pl.c0);
-    wk[1] = __ldg(reinterpret_cast<const uint4*>(a.wk) + pl.c1);
-  }
-  Where at{0, -1, true};
-  if (APPEND) at = find(a.book, a.Hkv, t, lane, a.err);
-  else at.pos = __ldg(a.pos + t);
-  Angles<HD, NB> an;
-  an.take(a, tab[warp], pl, at.pos, lane);
-
-  for (int p = p0; p < passes; p += kAhead * a.split) {
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int pi = p + i * a.split, j = pi * PER + grp;
-      if (pi >= passes) break;                       // (uniform)
-      const bool is_q = j < a.Hq, is_v = APPEND && j >= a.Hq + a.Hkv;
-      uint4 o[2] = {u[i][0], u[i][1]};
-      if (p + (i + kAhead) * a.split < passes) load(p + (i + kAhead) * a.split, u[i]);
-      float x[16];
-      unpack16<T>(o, x);
-      if (a.eps >= 0.f) {
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
-        const float r = rsqrtf(fmaf(sum_head<LANES>(ss), 1.f / HD, a.eps));
-        if (is_q ? a.wq != nullptr : a.wk != nullptr) {
-          float g[16];
-          const uint4 gw[2] = {is_q ? wq[0] : wk[0], is_q ? wq[1] : wk[1]};
-          unpack16<T>(gw, g);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] *= r * g[e];
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] *= r;
-        }
-      }
-      an.turn_head(x);
-      if (!is_v) {
-        o[0] = Vec16<T>::pack(x);
-        o[1] = Vec16<T>::pack(x + 8);
-      }
-      if (j >= heads) continue;
-      T* to;
-      if (is_q) {
-        to = static_cast<T*>(a.oq.p) + t * a.oq.row + j * a.oq.head;
-        if (!at.ok) o[0] = o[1] = make_uint4(0u, 0u, 0u, 0u);
-      } else if (APPEND) {
-        // (V's heads follow K's in a page)
-        if (at.row < 0) continue;
-        to = static_cast<T*>(a.book.pool) + (at.row + (int64_t)(j - a.Hq) * a.book.page) * HD;
-      } else {
-        to = static_cast<T*>(a.ok.p) + t * a.ok.row + (j - a.Hq) * a.ok.head;
-      }
-      *reinterpret_cast<uint4*>(to + 8 * pl.c0) = o[0];
-      *reinterpret_cast<uint4*>(to + 8 * pl.c1) = o[1];
+  __device__ __forceinline__ void next(const Args& a) {
+    --left;
+    if (++p == a.passes) {
+      p = 0;
+      ++t;
     }
   }
-}
+};
 
-// Gradients: the warps walk over the tokens and keep the weights' sums in registers; each
-// CTA leaves its own, which k_join adds in one fixed order.
-template <typename T, int HD, bool NB>
-__global__ void __launch_bounds__(kThreads) k_back(const Args a) {
+template <typename T, int HD, bool NB, bool APPEND>
+__global__ void __launch_bounds__(kThreads, 6) k_rotate(const __grid_constant__ Args a) {
   __shared__ __align__(16) float2 tab[kWarps][HD / 2];
-  __shared__ float sums[kWarps][2][HD];
+  __shared__ uint4 slots[kWarps][kAhead][2][32];
   constexpr int LANES = HD / 16, PER = 32 / LANES;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane / LANES;
+  Range now(a, blockIdx.x * kWarps + warp), ahead = now;
+  if (now.left == 0) return;
+  const int heads = a.Hq + a.Hkv * (APPEND ? 2 : 1);
+  const Place<HD, NB> pl(lane, a.n);
+  const uint32_t slot0 = mma::smem_addr(&slots[warp][0][0][lane]);
+  int fslot = 0;
+  auto fill = [&] {              // one group of copies, empty past the last pass
+    const int j = ahead.p * PER + grp;
+    if (ahead.left > 0 && j < heads) {
+      const bool is_q = j < a.Hq, is_v = APPEND && j >= a.Hq + a.Hkv;
+      const Rows& r = is_q ? a.q : is_v ? a.v : a.k;
+      const T* x = static_cast<const T*>(r.p) + ahead.t * r.row + (j - (is_q ? 0 : is_v ? a.Hq + a.Hkv : a.Hq)) * r.head;
+      mma::cp_async16(slot0 + fslot * 1024, x + 8 * pl.c0, 16);
+      mma::cp_async16(slot0 + fslot * 1024 + 512, x + 8 * pl.c1, 16);
+    }
+    mma::cp_commit();
+    if (ahead.left > 0) ahead.next(a);
+    fslot = fslot + 1 == kAhead ? 0 : fslot + 1;
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead - 1; ++i) fill();
+  Angles<HD, NB> an;
+  Where at{0, -1, true};
+  int64_t token = -1;
+  int slot = 0;
+#pragma unroll 1
+  for (; now.left > 0; now.next(a)) {
+    const int64_t t = now.t;
+    const int j = now.p * PER + grp;
+    const bool is_q = j < a.Hq, is_v = APPEND && j >= a.Hq + a.Hkv;
+    if (t != token) {            // (uniform)
+      token = t;
+      if (APPEND) at = find(a.book, a.Hkv, t, lane, now.p == 0, a.err);
+      else at.pos = __ldg(a.pos + t);
+      an.take(a, tab[warp], pl, at.pos, lane);
+    }
+    mma::cp_wait<kAhead - 2>();
+    fill();                      // into the slot of the pass before
+    uint4 o[2] = {slots[warp][slot][0][lane], slots[warp][slot][1][lane]};
+    slot = slot + 1 == kAhead ? 0 : slot + 1;
+    float x[16];
+    unpack16<T>(o, x);
+    if (a.eps >= 0.f) {
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
+      const float r = rsqrtf(fmaf(sum_head<LANES>(ss), 1.f / HD, a.eps));
+      const uint4* w = static_cast<const uint4*>(is_q ? a.wq : a.wk);
+      if (w) {
+        float g[16];
+        const uint4 gw[2] = {__ldg(w + pl.c0), __ldg(w + pl.c1)};
+        unpack16<T>(gw, g);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] *= r * g[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] *= r;
+      }
+    }
+    an.turn_head(x);
+    if (!is_v) {
+      o[0] = Vec16<T>::pack(x);
+      o[1] = Vec16<T>::pack(x + 8);
+    }
+    if (j >= heads) continue;
+    T* to;
+    if (is_q) {
+      to = static_cast<T*>(a.oq.p) + t * a.oq.row + j * a.oq.head;
+      if (!at.ok) o[0] = o[1] = make_uint4(0u, 0u, 0u, 0u);
+    } else if (APPEND) {
+      // (V's heads follow K's in a page)
+      if (at.row < 0) continue;
+      to = static_cast<T*>(a.book.pool) + (at.row + (int64_t)(j - a.Hq) * a.book.page) * HD;
+    } else {
+      to = static_cast<T*>(a.ok.p) + t * a.ok.row + (j - a.Hq) * a.ok.head;
+    }
+    *reinterpret_cast<uint4*>(to + 8 * pl.c0) = o[0];
+    *reinterpret_cast<uint4*>(to + 8 * pl.c1) = o[1];
+  }
+  mma::cp_wait<0>();
+}
+
+// Gradients: a token's passes over its query heads, then over its key heads; a warp keeps the
+// weights' sums in registers, each CTA leaves its own, which k_join adds in one fixed order.
+template <typename T, int HD, bool NB>
+__global__ void __launch_bounds__(kThreads, 4) k_back(const __grid_constant__ Args a) {
+  __shared__ __align__(16) float2 tab[kWarps][HD / 2];
+  __shared__ float sums[kWarps][2][HD];
+  __shared__ uint4 slots[kWarps][kBackAhead][4][32];
+  constexpr int LANES = HD / 16, PER = 32 / LANES;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane / LANES, q_passes = (a.Hq + PER - 1) / PER;
   const Place<HD, NB> pl(lane, a.n);
   float acc[2][16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[0][e] = acc[1][e] = 0.f;
-  const int64_t step = (int64_t)gridDim.x * kWarps;
-  for (int64_t w = (int64_t)blockIdx.x * kWarps + warp; w < a.T * a.split; w += step) {
-    const int64_t t = w / a.split;
-    const int p0 = (int)(w - t * a.split);
-    Angles<HD, NB> an;
-    an.take(a, tab[warp], pl, __ldg(a.pos + t), lane);
+  Range now(a, blockIdx.x * kWarps + warp), ahead = now;
+  const uint32_t slot0 = mma::smem_addr(&slots[warp][0][0][lane]);
+  int fslot = 0;
+  auto fill = [&] {
+    const bool k = ahead.p >= q_passes;
+    const int j = (k ? ahead.p - q_passes : ahead.p) * PER + grp;
+    if (ahead.left > 0 && j < (k ? a.Hkv : a.Hq)) {
+      const Rows &rx = k ? a.k : a.q, &rd = k ? a.dk : a.dq;
+      const T* x = static_cast<const T*>(rx.p) + ahead.t * rx.row + j * rx.head;
+      const T* d = static_cast<const T*>(rd.p) + ahead.t * rd.row + j * rd.head;
+      mma::cp_async16(slot0 + fslot * 2048, x + 8 * pl.c0, 16);
+      mma::cp_async16(slot0 + fslot * 2048 + 512, x + 8 * pl.c1, 16);
+      mma::cp_async16(slot0 + fslot * 2048 + 1024, d + 8 * pl.c0, 16);
+      mma::cp_async16(slot0 + fslot * 2048 + 1536, d + 8 * pl.c1, 16);
+    }
+    mma::cp_commit();
+    if (ahead.left > 0) ahead.next(a);
+    fslot = fslot + 1 == kBackAhead ? 0 : fslot + 1;
+  };
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-      const Rows &X = part ? a.k : a.q, &DY = part ? a.dk : a.dq;
-      const Out& O = part ? a.ok : a.oq;
-      const void* W = part ? a.wk : a.wq;
-      const int heads = part ? a.Hkv : a.Hq, passes = (heads + PER - 1) / PER;
-      float g[16];
-      if (W) {
-        const uint4 u[2] = {__ldg(reinterpret_cast<const uint4*>(W) + pl.c0), __ldg(reinterpret_cast<const uint4*>(W) + pl.c1)};
-        unpack16<T>(u, g);
-      } else {
+  for (int i = 0; i < kBackAhead - 1; ++i) fill();
+  Angles<HD, NB> an;
+  int64_t token = -1;
+  int slot = 0;
+#pragma unroll 1
+  for (; now.left > 0; now.next(a)) {
+    const int64_t t = now.t;
+    const bool k = now.p >= q_passes;
+    const int j = (k ? now.p - q_passes : now.p) * PER + grp;
+    const bool has = j < (k ? a.Hkv : a.Hq);
+    if (t != token) {            // (uniform)
+      token = t;
+      an.take(a, tab[warp], pl, __ldg(a.pos + t), lane);
+    }
+    mma::cp_wait<kBackAhead - 2>();
+    fill();                      // into the slot of the pass before
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    const uint4 ux[2] = {has ? slots[warp][slot][0][lane] : zero, has ? slots[warp][slot][1][lane] : zero};
+    const uint4 ud[2] = {has ? slots[warp][slot][2][lane] : zero, has ? slots[warp][slot][3][lane] : zero};
+    slot = slot + 1 == kBackAhead ? 0 : slot + 1;
+    float x[16], d[16];
+    unpack16<T>(ux, x);
+    unpack16<T>(ud, d);
+    an.turn_head(d);
+    // one half of the weights' products at a time (registers): gw = d w
+    const uint4* w = static_cast<const uint4*>(k ? a.wk : a.wq);
+    float ss = 0.f, sg = 0.f;
+    uint4 gw[2] = {zero, zero};
+    if (w) {
+      gw[0] = __ldg(w + pl.c0);
+      gw[1] = __ldg(w + pl.c1);
+    }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) g[e] = 1.f;
-      }
-#pragma unroll 2
-      for (int p = p0; p < passes; p += a.split) {
-        const int j = p * PER + grp;
-        uint4 ux[2], ud[2];
-        if (j < heads) {
-          const T* x = static_cast<const T*>(X.p) + t * X.row + j * X.head;
-          const T* d = static_cast<const T*>(DY.p) + t * DY.row + j * DY.head;
-          ux[0] = *reinterpret_cast<const uint4*>(x + 8 * pl.c0);
-          ux[1] = *reinterpret_cast<const uint4*>(x + 8 * pl.c1);
-          ud[0] = *reinterpret_cast<const uint4*>(d + 8 * pl.c0);
-          ud[1] = *reinterpret_cast<const uint4*>(d + 8 * pl.c1);
-        } else {
-          ux[0] = ux[1] = ud[0] = ud[1] = make_uint4(0u, 0u, 0u, 0u);
-        }
-        float x[16], d[16];
-        unpack16<T>(ux, x);
-        unpack16<T>(ud, d);
-        an.turn_head(d);
-        float ss = 0.f, sg = 0.f;
+    for (int h = 0; h < 2; ++h) {
+      float g[8];
+      Vec16<T>::unpack(gw[h], g);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          ss = fmaf(x[e], x[e], ss);
-          sg = fmaf(d[e] * g[e], x[e], sg);
-        }
-        const float r = rsqrtf(fmaf(sum_head<LANES>(ss), 1.f / HD, a.eps));
-        const float m = sum_head<LANES>(sg) * (1.f / HD) * r * r;
-        if (j >= heads) continue;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          acc[part][e] = fmaf(d[e] * r, x[e], acc[part][e]);
-          d[e] = r * fmaf(d[e], g[e], -m * x[e]);
-        }
-        T* to = static_cast<T*>(O.p) + t * O.row + j * O.head;
-        *reinterpret_cast<uint4*>(to + 8 * pl.c0) = Vec16<T>::pack(d);
-        *reinterpret_cast<uint4*>(to + 8 * pl.c1) = Vec16<T>::pack(d + 8);
+      for (int e = 0; e < 8; ++e) {
+        ss = fmaf(x[8 * h + e], x[8 * h + e], ss);
+        sg = fmaf(w ? d[8 * h + e] * g[e] : d[8 * h + e], x[8 * h + e], sg);
       }
     }
+    const float r = rsqrtf(fmaf(sum_head<LANES>(ss), 1.f / HD, a.eps));
+    const float m = sum_head<LANES>(sg) * (1.f / HD) * r * r;
+    if (a.part && !k) {          // (uniform)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[0][e] = fmaf(d[e] * r, x[e], acc[0][e]);
+    } else if (a.part) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[1][e] = fmaf(d[e] * r, x[e], acc[1][e]);
+    }
+    if (!has) continue;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float g[8];
+      Vec16<T>::unpack(gw[h], g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[8 * h + e] = r * fmaf(-m, x[8 * h + e], w ? d[8 * h + e] * g[e] : d[8 * h + e]);
+    }
+    const Out& O = k ? a.ok : a.oq;
+    T* to = static_cast<T*>(O.p) + t * O.row + j * O.head;
+    *reinterpret_cast<uint4*>(to + 8 * pl.c0) = Vec16<T>::pack(d);
+    *reinterpret_cast<uint4*>(to + 8 * pl.c1) = Vec16<T>::pack(d + 8);
   }
+  mma::cp_wait<0>();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (!a.part) return;
 #pragma unroll
@@ -397,27 +456,28 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(const float* part, int ct
 }
 
 // ------------------------------------------------------------------ host
-constexpr int kBackCtasPerSm = 3;
-// Warps of a token: its passes over the heads are split while the SMs' warps are not filled
-int split_of(int64_t T, int passes, int warps_per_sm) {
-  const int64_t want = (int64_t)device_sms() * warps_per_sm;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(passes, want / std::max<int64_t>(T, 1)));
+// The list of T tokens' passes over as many warps as the SMs hold at once
+void share(Args& a, int passes, int ctas_per_sm) {
+  const int64_t total = a.T * passes;
+  a.passes = passes;
+  a.by_passes = Div(passes);
+  a.warps = (int)std::min<int64_t>(total, (int64_t)device_sms() * ctas_per_sm * kWarps);
+  a.each = total / a.warps;
+  a.more = total % a.warps;
 }
 template <typename T, int HD, bool NB, bool APPEND>
 void launch_rotate(Args a, cudaStream_t s) {
-  const int heads = a.Hq + a.Hkv * (APPEND ? 2 : 1), per = 32 / (HD / 16);
-  a.split = split_of(a.T, ceil_div(heads, per), 32);
-  const int64_t warps = a.T * a.split;
-  launch_cluster(k_rotate<T, HD, NB, APPEND>, dim3((unsigned)((warps + kWarps - 1) / kWarps)), dim3(kThreads), 0, 1, false, s, a);
+  share(a, ceil_div(a.Hq + a.Hkv * (APPEND ? 2 : 1), 32 / (HD / 16)), 6);
+  launch_cluster(k_rotate<T, HD, NB, APPEND>, dim3(ceil_div(a.warps, kWarps)), dim3(kThreads), 0, 1, false, s, a);
 }
-int back_ctas(int64_t T, int Hq, int Hkv, int hd, int* split) {
+void share_back(Args& a, int hd) {
   const int per = 32 / (hd / 16);
-  *split = split_of(T, std::max(ceil_div(Hq, per), ceil_div(Hkv, per)), kWarps * kBackCtasPerSm);
-  return (int)std::min<int64_t>((int64_t)kBackCtasPerSm * device_sms(), (T * *split + kWarps - 1) / kWarps);
+  share(a, ceil_div(a.Hq, per) + ceil_div(a.Hkv, per), 4);
 }
 template <typename T, int HD, bool NB>
 void launch_back(Args a, float* dwq, float* dwk, cudaStream_t s) {
-  const int grid = back_ctas(a.T, a.Hq, a.Hkv, HD, &a.split);
+  share_back(a, HD);
+  const int grid = ceil_div(a.warps, kWarps);
   launch_cluster(k_back<T, HD, NB>, dim3(grid), dim3(kThreads), 0, 1, false, s, a);
   if (a.part) launch_cluster(k_join<HD>, dim3(2 * HD / 8), dim3(kJoinThreads), 0, 1, true, s, (const float*)a.part, grid, dwq, dwk);
 }
@@ -543,8 +603,12 @@ extern "C" int kf_op_rotate_append(int32_t type, int32_t n, const int32_t* which
 
 extern "C" int64_t kf_op_rotate_heads_grad_work(int64_t T, int32_t Hq, int32_t Hkv, int32_t hd) {
   if (T < 1 || Hq < 1 || Hkv < 1 || (hd != 64 && hd != 128)) return 0;
-  int split;
-  return (int64_t)back_ctas(T, Hq, Hkv, hd, &split) * 2 * hd * (int64_t)sizeof(float);
+  Args a{};
+  a.T = T;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  share_back(a, hd);
+  return (int64_t)ceil_div(a.warps, kWarps) * 2 * hd * (int64_t)sizeof(float);
 }
 
 extern "C" int kf_op_rotate_heads_grad(int32_t type, int64_t T, int32_t Hq, int32_t Hkv, int32_t hd, const void* dq, int64_t dq_row,

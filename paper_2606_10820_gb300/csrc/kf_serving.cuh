@@ -55,6 +55,18 @@ inline void launch_cluster(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t
   cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 
+// Division of n < 2^31 by a number known on the host: floor(n (1 + m / 2^32) / 2^s), 2^s >= d the next power of two, m = floor(2^32
+// (2^s - d) / d) + 1
+struct Div {
+  uint32_t d, m, s;
+  Div() = default;
+  explicit Div(uint32_t d_) : d(d_), s(0) {
+    while ((1ull << s) < d) ++s;
+    m = (uint32_t)((((1ull << s) - d) << 32) / d + 1);
+  }
+  __device__ __forceinline__ int of(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
+};
+
 __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
 template <> __device__ __forceinline__ __half from_f<__half>(float x) { return __float2half_rn(x); }
 

@@ -51,19 +51,6 @@ __device__ __forceinline__ int prefix_record(int64_t before, int g, int pair, in
   return (int)((before / kPrefixRows + g + pair) * Hkv + hk);
 }
 
-// Division of n < 2^31 by a number known on the host: floor(n (1 + m / 2^32) / 2^s), 2^s >= d the next power of two, m = floor(2^32
-// (2^s - d) / d) + 1
-struct Div {
-  uint32_t d, m, s;
-  Div() = default;
-  explicit Div(uint32_t d_) : d(d_), s(0) {
-    while ((1ull << s) < d) ++s;
-    m = (uint32_t)((((1ull << s) - d) << 32) / d + 1);
-  }
-#ifdef __CUDACC__
-  __device__ __forceinline__ int of(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
-#endif
-};
 struct SharedCall {
   const void* q;
   int64_t q_seq, q_row, q_head;
