@@ -17,6 +17,7 @@
 // passes ahead, across tokens; no thread waits for another's), so the loads under way do not
 // cost registers; a token's angles are computed once by the warp's lanes and passed on through shared memory.
 #include <algorithm>
+#include <climits>
 
 #include "kf_mma.cuh"
 #include "kf_serving.cuh"
@@ -42,6 +43,7 @@ struct Book {
   void* pool;
   int64_t n_pages;
   int n, page, slots, width;
+  Div by_page;
 };
 struct Args {
   Rows q, k, v, dq, dk;          // v: append; dq, dk: gradient
@@ -168,48 +170,55 @@ template <typename T> __device__ __forceinline__ void unpack16(const uint4* u, f
   Vec16<T>::unpack(u[1], x + 8);
 }
 
-// The place of token t in its sequence's cache
-struct Where {
-  int pos;
+// The places of a warp's tokens in their sequences' caches, looked up 32 at a time: lane i holds that of token base + i, so the
+// chain of loads (starts, slot, length, page) is waited for once
+struct Places {
+  int64_t base;
+  int pos;                       // -1: not known
   int64_t row;                   // K's row of head 0 in the pool, in rows of hd; -1: not to be written
-  bool ok;                       // the position is known
-};
-__device__ __forceinline__ Where find(const Book& k, int Hkv, int64_t t, int lane, bool flags, int* err) {
-  // the last sequence that starts at or before t: up to 256 starts at once, 32 a step for more
-  int lo = 0, left = k.n;
-  if (left <= 256) {
-    int below = 0;
+  // tokens t .. t + n - 1 (n <= 32); `flags`: the first of them is this warp's to report
+  __device__ __forceinline__ void look(const Book& k, int Hkv, int64_t t, int n, bool flags, int lane, int* err) {
+    base = t;
+    pos = -1;
+    row = -1;
+    // the last sequence that starts at or before a lane's token
+    int lo = 0;
+    if (k.n <= 256) {
+      int start[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (32 * i < left) below += 32 * i + lane < left && __ldg(k.starts + 32 * i + lane) <= t;
-    lo = max(0, __reduce_add_sync(~0u, below) - 1);
-    left = 1;
-  }
-  while (left > 1) {
-    const int step = (left + 31) / 32, at = lane * step;
-    const uint32_t m = __ballot_sync(~0u, at < left && __ldg(k.starts + lo + min(at, left - 1)) <= t);
-    const int i = max(0, 31 - __clz(m)) * step;
-    lo += i;
-    left = min(step, left - i);
-  }
-  const int first = __ldg(k.starts + lo), end = __ldg(k.starts + lo + 1), s = __ldg(k.which + lo);
-  Where w{0, -1, false};
-  int bad = 0;
-  if (t < first || t >= end || s < 0 || s >= k.slots) bad = KF_DEV_BAD_ROW;
-  else {
-    const int64_t pos = (int64_t)k.lens[s] - end + t;
-    if (pos < 0 || pos >= (int64_t)k.width * k.page) bad = KF_DEV_BAD_ROW;
-    else {
-      w.ok = true;
-      w.pos = (int)pos;
-      const int p = k.table[(int64_t)s * k.width + w.pos / k.page];
-      if (p < 0 || p >= k.n_pages) bad = KF_DEV_BAD_PAGE;
-      else w.row = (int64_t)p * 2 * Hkv * k.page + w.pos % k.page;
+      for (int i = 0; i < 8; ++i) start[i] = 32 * i + lane < k.n ? __ldg(k.starts + 32 * i + lane) : INT_MAX;
+#pragma unroll 1
+      for (int x = 0; x < n; ++x) {
+        int below = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) below += start[i] <= t + x;
+        below = __reduce_add_sync(~0u, below);
+        if (x == lane) lo = max(0, below - 1);
+      }
+    } else if (lane < n) {
+      for (int hi = k.n - 1; lo < hi;) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (__ldg(k.starts + mid) <= t + lane) lo = mid;
+        else hi = mid - 1;
+      }
     }
+    if (lane >= n) return;
+    const int first = __ldg(k.starts + lo), end = __ldg(k.starts + lo + 1), s = __ldg(k.which + lo);
+    int bad = 0;
+    if (t + lane < first || t + lane >= end || s < 0 || s >= k.slots) bad = KF_DEV_BAD_ROW;
+    else {
+      const int64_t p = (int64_t)k.lens[s] - end + t + lane;
+      if (p < 0 || p >= (int64_t)k.width * k.page) bad = KF_DEV_BAD_ROW;
+      else {
+        pos = (int)p;
+        const int col = k.by_page.of(pos), id = k.table[(int64_t)s * k.width + col];
+        if (id < 0 || id >= k.n_pages) bad = KF_DEV_BAD_PAGE;
+        else row = (int64_t)id * 2 * Hkv * k.page + (pos - col * k.page);
+      }
+    }
+    if (bad && (flags || lane > 0)) atomicOr(err, bad);
   }
-  if (bad && flags && lane == 0) atomicOr(err, bad);
-  return w;
-}
+};
 
 // A warp's passes, first .. last - 1 of the list; pass x is pass x % passes of token x / passes
 struct Range {
@@ -258,8 +267,10 @@ __global__ void __launch_bounds__(kThreads, 6) k_rotate(const __grid_constant__ 
 #pragma unroll
   for (int i = 0; i < kAhead - 1; ++i) fill();
   Angles<HD, NB> an;
-  Where at{0, -1, true};
-  int64_t token = -1;
+  Places places;
+  places.base = -32;
+  int pos = 0;
+  int64_t row = -1, token = -1;
   int slot = 0;
 #pragma unroll 1
   for (; now.left > 0; now.next(a)) {
@@ -268,9 +279,17 @@ __global__ void __launch_bounds__(kThreads, 6) k_rotate(const __grid_constant__ 
     const bool is_q = j < a.Hq, is_v = APPEND && j >= a.Hq + a.Hkv;
     if (t != token) {            // (uniform)
       token = t;
-      if (APPEND) at = find(a.book, a.Hkv, t, lane, now.p == 0, a.err);
-      else at.pos = __ldg(a.pos + t);
-      an.take(a, tab[warp], pl, at.pos, lane);
+      if constexpr (APPEND) {
+        if (t >= places.base + 32) {
+          const int tokens = a.by_passes.of(min(now.p + now.left - 1, INT_MAX - 1)) + 1;      // of this warp, from t on
+          places.look(a.book, a.Hkv, t, min(tokens, 32), now.p == 0, lane, a.err);
+        }
+        pos = __shfl_sync(~0u, places.pos, (int)(t - places.base));
+        row = __shfl_sync(~0u, places.row, (int)(t - places.base));
+      } else {
+        pos = __ldg(a.pos + t);
+      }
+      an.take(a, tab[warp], pl, pos, lane);
     }
     mma::cp_wait<kAhead - 2>();
     fill();                      // into the slot of the pass before
@@ -304,11 +323,11 @@ __global__ void __launch_bounds__(kThreads, 6) k_rotate(const __grid_constant__ 
     T* to;
     if (is_q) {
       to = static_cast<T*>(a.oq.p) + t * a.oq.row + j * a.oq.head;
-      if (!at.ok) o[0] = o[1] = make_uint4(0u, 0u, 0u, 0u);
+      if (APPEND && pos < 0) o[0] = o[1] = make_uint4(0u, 0u, 0u, 0u);
     } else if (APPEND) {
       // (V's heads follow K's in a page)
-      if (at.row < 0) continue;
-      to = static_cast<T*>(a.book.pool) + (at.row + (int64_t)(j - a.Hq) * a.book.page) * HD;
+      if (row < 0) continue;
+      to = static_cast<T*>(a.book.pool) + (row + (int64_t)(j - a.Hq) * a.book.page) * HD;
     } else {
       to = static_cast<T*>(a.ok.p) + t * a.ok.row + (j - a.Hq) * a.ok.head;
     }
@@ -589,7 +608,7 @@ extern "C" int kf_op_rotate_append(int32_t type, int32_t n, const int32_t* which
   a.wq = q_weight;
   a.wk = k_weight;
   a.freq = freq;
-  a.book = Book{which, starts, table, lens, pool, n_pages, n, page, slots, width};
+  a.book = Book{which, starts, table, lens, pool, n_pages, n, page, slots, width, Div(page)};
   a.T = T;
   a.Hq = Hq;
   a.Hkv = Hkv;
