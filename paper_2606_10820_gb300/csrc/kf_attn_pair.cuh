@@ -315,6 +315,85 @@ struct Softmax {
     l += s2.x + s2.y;
     return true;
   }
+  // The same in a third of the code: the scores come from TMEM twice, 64 at a time, for their maximum and for P.  A call of a few
+  // tiles is mostly the first run through its code, at about 15 clocks an instruction: the first tile took 6,000 to 12,000 clocks as above.
+  // mask(c, s): closed scores among the 64 from 64 c on
+  template <typename B, typename M>
+  __device__ __forceinline__ bool short_tile(B& b, float sc, bool first, int g, float& m, float& l, int* err, M mask) const {
+    auto wait = [&](uint64_t* bar, uint32_t parity) -> bool { return __all_sync(~0u, mbar_wait(smem_u32(bar), parity, err)); };
+    auto arrive = [&](uint64_t* bar) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(bar));
+    };
+    uint32_t s[64];
+    auto load = [&](int c) {
+      tmem_ld32_async(tS + 64 * c, s);
+      tmem_ld32_async(tS + 64 * c + 32, s + 32);
+      tmem_wait32(s);
+      tmem_wait32(s + 32);
+      mask(c, s);
+    };
+    if (!wait(&b.s_full[sub], g & 1)) return false;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    float mq[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+    for (int c = 0; c < 2; ++c) {
+      load(c);
+#pragma unroll
+      for (int e = 0; e < 64; e += 8)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) mq[x] = max3f(mq[x], __uint_as_float(s[e + 2 * x]), __uint_as_float(s[e + 2 * x + 1]));
+    }
+    const float mx = fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3]));
+    const bool raise = first || (mx - m) * sc > kRaise;
+    if (g > 0 && (kOwnP<HD> || (!first && __any_sync(~0u, raise)))) {      // the product before has read P, and been added
+      if (!wait(&b.o_full[sub], (g - 1) & 1)) return false;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    }
+    if (!first && __any_sync(~0u, raise)) {
+      // O follows the new reference
+      const float f = raise ? mma::ex2((m - mx) * sc) : 1.f;
+#pragma unroll 1
+      for (int c = 0; c < HD / 32; ++c) {
+        float o[32];
+        tmem_ld32(tO + 32 * c, o);
+#pragma unroll
+        for (int d = 0; d < 32; ++d) o[d] *= f;
+        tmem_st32(tO + 32 * c, o);
+      }
+      l *= f;
+    }
+    if (raise) m = mx;
+    const float nm = m == -INFINITY ? 0.f : -m * sc;
+    const uint64_t sc2 = f2(sc, sc), nm2 = f2(nm, nm);
+    uint64_t ps[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll 1
+    for (int c = 0; c < 2; ++c) {
+      load(c);
+      if (kOwnP<HD> && c == 1) {            // (S may be written again under the last exponentials)
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        arrive(&b.s_free[sub]);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+          const float2 d = f2_split(fma_f2(f2(__uint_as_float(s[32 * h + 2 * u]), __uint_as_float(s[32 * h + 2 * u + 1])), sc2, nm2));
+          const float x = mma::ex2(d.x), y = mma::ex2(d.y);
+          ps[u & 3] = add_f2(ps[u & 3], f2(x, y));
+          pk[u] = pack2<T>(x, y);
+        }
+        tmem_st16(tP + 32 * c + 16 * h, pk);
+      }
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      arrive(&b.p_full[sub][c]);
+    }
+    const float2 s2 = f2_split(add_f2(add_f2(ps[0], ps[1]), add_f2(ps[2], ps[3])));
+    l += s2.x + s2.y;
+    return true;
+  }
 };
 
 }  // namespace pair

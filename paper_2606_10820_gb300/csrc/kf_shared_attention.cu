@@ -225,8 +225,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
           const int page = in ? id : (int)a.n_pages, row = in ? key - a.by_page.of(key) * a.page : 0;
           if (lane < kGrans && key < im.len && !in) atomicOr(a.err, KF_DEV_BAD_PAGE);
           if (j + 1 < t0 + n) id = look(j + 1);
-          // (the first Q comes before the bulk of the first K and V: behind them it took 7 us)
-          if (it == 0 && j == t0 + 1) ok = wait(&b.q_full, 0);
           for (int kv = 0; ok && kv < 2; ++kv, ++ring) {
             const int st = ring % ST;
             ok = wait(&b.kv_empty[st], ((ring / ST) & 1) ^ 1);
@@ -299,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
         // this warp's 32 rows of Q, swizzled; rows that the segment does not have are zeros
         constexpr int CH = HD / 8, RP = 32 / CH;
         const int ch = lane % CH;
-#pragma unroll
+#pragma unroll 2
         for (int p = 0; p < CH; ++p) {
           const int lr = 32 * quarter + p * RP + lane / CH, r = sub * kRows + lr;
           const Row w(a, im, r);
@@ -331,10 +329,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
         if (j + 1 < n) id = look(im.t0 + j + 1);
         const int lim = see - (im.t0 + j) * kKeys;      // keys below it are seen
         const bool all = open == ~0u && __all_sync(~0u, lim >= kKeys);
-        ok = sx.tile(b, sc, j == 0, g, m, l, a.err, [&](int c, uint32_t* s) {
+        ok = sx.short_tile(b, sc, j == 0, g, m, l, a.err, [&](int c, uint32_t* s) {
           if (!all) {
+            const int lc = lim - 64 * c;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) s[e] = 32 * c + e < lim && ((open >> (2 * c + e / 16)) & 1u) ? s[e] : 0xff800000u;
+            for (int e = 0; e < 64; ++e) s[e] = e < lc && ((open >> (4 * c + e / 16)) & 1u) ? s[e] : 0xff800000u;
           }
         });
         if (!ok) break;
@@ -346,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
                                  : ((int64_t)(im.b0 + w.seq) * a.rows + w.tok) * a.Hq + im.hk * a.G + w.j;
       float* dst = (im.more ? a.pre.more_o : a.pre.first_o) + at * HD;
       if (mine) (im.more ? a.pre.more_ml : a.pre.first_ml)[at] = make_float2(m, l);
-#pragma unroll
+#pragma unroll 1
       for (int c = 0; c < HD / 32; ++c) {
         float o[32];
         tmem_ld32(sx.tO + 32 * c, o);
