@@ -8,7 +8,7 @@
 // its operands are loaded, which keys a row sees and where its output goes is the kernels'.
 #pragma once
 
-#include "kf_mma.cuh"
+#include "kf_mma16.cuh"
 #include "kf_serving.cuh"
 #include "kf_tc.cuh"
 
@@ -105,15 +105,6 @@ __device__ __forceinline__ void st_32(void* p, const uint32_t* r) {
                "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  if constexpr (std::is_same<T, __half>::value) {
-    const __half2 h = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  } else {
-    return mma::pack_bf16(lo, hi);
-  }
-}
-
 // (I: an item, as the load warp hands it to the others; n[i]: key tiles of sub-tile i, 0: no sub-tile)
 template <typename I>
 struct PairBars {

@@ -23,8 +23,7 @@
 // of 64, eight rows, fp16, in 51 us (3.1 TB/s: the products of 24 rows, 32 with the padding).
 #include <algorithm>
 
-#include "kf_mma.cuh"
-#include "kf_serving.cuh"
+#include "kf_mma16.cuh"
 #include "kf_shared.cuh"
 
 namespace kf {
@@ -63,59 +62,17 @@ struct Args {
   int B, rows, Hq, Hkv, G, MT, page, page_shift, width;    // page_shift: -1 where page is no power of two
   int direct;           // a CTA per segment
   float scale2;         // scale log2(e): scores in base-2 units
-  // SHARED: the keys from the group's prefix on, and partial outputs of every row
-  Sharing sh;
-  Partials part;
   __device__ __forceinline__ int page_of(int key) const { return page_shift >= 0 ? key >> page_shift : key / page; }
 };
 
 template <int HD> constexpr int kUnit = kUnitBytes / (4 * HD);      // keys
 
-template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  if constexpr (std::is_same<T, __half>::value) {
-    const __half2 h = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  } else {
-    return mma::pack_bf16(lo, hi);
-  }
-}
-template <typename T>
-__device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  if constexpr (std::is_same<T, __half>::value)
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    mma::mma16816(d, a, b0, b1);
-}
-
 __device__ __forceinline__ int seq_len(const Args& a, int b) {
   return min(max(__ldg(a.lens + b), 0), a.width * a.page);
 }
-// The first key of a sequence: 0, or where its group's prefix ends
-template <bool SHARED>
-struct First {
-  int g, key;
-  __device__ __forceinline__ void at(const Args& a, int b) {
-    key = 0;
-    if constexpr (SHARED) {
-      g = group_of(a.sh, b);
-      key = prefix_of(a.sh, g, a.width * a.page);
-    }
-  }
-  // of the sequence after it
-  __device__ __forceinline__ void next(const Args& a, int b) {
-    if constexpr (SHARED) {
-      while (g + 1 < a.sh.n && __ldg(a.sh.groups + g + 1) <= b) ++g;
-      key = prefix_of(a.sh, g, a.width * a.page);
-    }
-  }
-  __device__ __forceinline__ int unit0() const { return SHARED ? key & ~15 : 0; }      // (units begin where 16 keys of a page do)
-};
 // units of each of a sequence's segments (one without keys has a unit too: its rows are written)
-template <int HD, bool SHARED> __device__ __forceinline__ int units_of(const Args& a, int b, const First<SHARED>& f) {
-  return max(1, (seq_len(a, b) - f.unit0() + kUnit<HD> - 1) / kUnit<HD>);
+template <int HD> __device__ __forceinline__ int units_of(const Args& a, int b) {
+  return max(1, (seq_len(a, b) + kUnit<HD> - 1) / kUnit<HD>);
 }
 
 // The list: sequence by sequence, each one's Hkv * MT segments, each one's units and kExtra
@@ -125,22 +82,17 @@ struct Part {
   long long total, x0, x1, base;
   int b, parts;
 };
-template <int HD, int TILES, bool SHARED>
-__device__ __forceinline__ int places_of(const Args& a, int b, const First<SHARED>& f) { return units_of<HD>(a, b, f) * (kTurns<HD, TILES> ? 2 : 1); }
+template <int HD, int TILES>
+__device__ __forceinline__ int places_of(const Args& a, int b) { return units_of<HD>(a, b) * (kTurns<HD, TILES> ? 2 : 1); }
 __device__ __forceinline__ long long part_begin(long long total, int parts, int c) { return total * c / parts; }
-template <int HD, int TILES, bool SHARED>
+template <int HD, int TILES>
 __device__ Part find_part(const Args& a, int c, int ctas) {
   __shared__ long long warp_sum[NW];
   __shared__ Part found;
   const int t = threadIdx.x, per = (a.B + kThreads - 1) / kThreads, sb = a.Hkv * a.MT;
   const int first = min(a.B, t * per), last = min(a.B, first + per);
   long long mine = 0;
-  First<SHARED> f;
-  if (first < last) f.at(a, first);
-  for (int b = first; b < last; ++b) {
-    if (b > first) f.next(a, b);
-    mine += places_of<HD, TILES>(a, b, f) + kExtra;
-  }
+  for (int b = first; b < last; ++b) mine += places_of<HD, TILES>(a, b) + kExtra;
   mine *= sb;
   long long incl = mine;
 #pragma unroll
@@ -160,10 +112,9 @@ __device__ Part find_part(const Args& a, int c, int ctas) {
   if (c < parts && x0 >= lo && x0 < lo + mine) {
     long long base = lo;
     int b = first;
-    f.at(a, b);
-    for (long long n = (long long)(places_of<HD, TILES>(a, b, f) + kExtra) * sb; x0 >= base + n; n = (long long)(places_of<HD, TILES>(a, b, f) + kExtra) * sb) {
+    for (long long n = (long long)(places_of<HD, TILES>(a, b) + kExtra) * sb; x0 >= base + n; n = (long long)(places_of<HD, TILES>(a, b) + kExtra) * sb) {
       base += n;
-      f.next(a, ++b);
+      ++b;
     }
     found = Part{total, x0, part_begin(total, parts, c + 1), base, b, parts};
   }
@@ -173,13 +124,11 @@ __device__ Part find_part(const Args& a, int c, int ctas) {
 }
 
 // one segment's places within a CTA's part
-template <int HD, int TILES, bool SHARED>
+template <int HD, int TILES>
 struct Piece {
   long long xs, xa, xb, xe;    // the segment's first unit; the piece's units [xa, xb) (or none) and its end
   int b, s, n, len;            // sequence, segment of it, units of the segment, tokens
-  First<SHARED> f;
-  // the first key of place x
-  __device__ __forceinline__ int key(long long x) const { return f.unit0() + ((int)(x - xs) >> (kTurns<HD, TILES> ? 1 : 0)) * kUnit<HD>; }
+  __device__ __forceinline__ int unit(long long x) const { return (int)(x - xs) >> (kTurns<HD, TILES> ? 1 : 0); }
   __device__ __forceinline__ void cut(const Part& p) {
     xa = max(xs, p.x0);
     xb = min(xs + n, p.x1);
@@ -187,8 +136,7 @@ struct Piece {
   }
   __device__ __forceinline__ void at(const Args& a, const Part& p) {
     b = p.b;
-    f.at(a, b);
-    n = places_of<HD, TILES>(a, b, f);
+    n = places_of<HD, TILES>(a, b);
     len = seq_len(a, b);
     s = (int)((p.x0 - p.base) / (n + kExtra));
     xs = p.base + (long long)s * (n + kExtra);
@@ -199,8 +147,8 @@ struct Piece {
     if (xe >= p.x1) return false;
     if (++s == a.Hkv * a.MT) {
       s = 0;
-      f.next(a, ++b);
-      n = places_of<HD, TILES>(a, b, f);
+      ++b;
+      n = places_of<HD, TILES>(a, b);
       len = seq_len(a, b);
     }
     xs = xe;
@@ -210,17 +158,17 @@ struct Piece {
 };
 
 // a warp's copies: unit after unit of its own, ahead of the products
-template <typename T, int HD, int TILES, bool SHARED>
+template <typename T, int HD, int TILES>
 struct Feed {
   static constexpr int U = kUnit<HD>, kHalves = U / 16;
-  Piece<HD, TILES, SHARED> pc;
+  Piece<HD, TILES> pc;
   long long x;
   int page[kHalves];       // pages of unit x
   bool more;
   __device__ __forceinline__ void look(const Args& a) {
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
-      const int key = pc.key(x) + 16 * h;
+      const int key = pc.unit(x) * U + 16 * h;
       page[h] = key < pc.len ? __ldg(a.table + (size_t)pc.b * a.width + a.page_of(key)) : -1;
     }
   }
@@ -246,7 +194,7 @@ struct Feed {
       uint32_t ok = 0;
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
-        const int key0 = pc.key(x) + 16 * h, left = pc.len - key0;
+        const int key0 = pc.unit(x) * U + 16 * h, left = pc.len - key0;
         const bool in = page[h] >= 0 && page[h] < a.n_pages;
         if (in) ok |= 1u << h;
         else if (left > 0 && lane == 0) atomicOr(a.err, KF_DEV_BAD_PAGE);
@@ -256,7 +204,7 @@ struct Feed {
 #pragma unroll
         for (int i = 0; i < 16 / RP; ++i) {
           const int r = i * RP + lane / CH, row = 16 * h + r;
-          const int bytes = in && r < left && (!SHARED || r >= pc.f.key - key0) ? 16 : 0;      // (0: zeros, nothing is read)
+          const int bytes = in && r < left ? 16 : 0;      // (0: zeros, nothing is read)
           const uint32_t d = stage + row * (HD * 2) + ((c ^ (row & 7)) << 4);
           mma::cp_async16(d, bytes ? kb + r * HD : static_cast<const T*>(a.pool), bytes);
           mma::cp_async16(d + kUnitBytes / 2, bytes ? vb + r * HD : static_cast<const T*>(a.pool), bytes);
@@ -278,8 +226,8 @@ template <int HD, int TILES> constexpr bool kFits = kCtasPerSm<HD, TILES> * (kSm
 static_assert(sizeof(Part) + NW * sizeof(long long) <= 128, "the static arrays");
 static_assert(kFits<64, 1> && kFits<64, 2> && kFits<128, 1> && kFits<128, 2>, "the CTAs of an SM");
 
-template <typename T, int HD, int TILES, bool SHARED>
-__device__ __forceinline__ void attend(const Args& a) {
+template <typename T, int HD, int TILES>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const Args a) {
   extern __shared__ __align__(128) uint8_t sm[];
   constexpr int ST = kStages<HD, TILES>, ROWS = 16 * TILES, HELD = kHeld<HD, TILES>;
   constexpr int PARTS = kTurns<HD, TILES> ? 2 : 1;      // warps of a piece that hold its rows in the end
@@ -295,24 +243,22 @@ __device__ __forceinline__ void attend(const Args& a) {
       if (n < 0 || n > a.width * a.page) atomicOr(a.err, KF_DEV_BAD_ROW);
     }
   Part part;
-  if (!SHARED && a.direct) {
+  if (a.direct) {
     // this segment's places are the whole list: [0, n + kExtra)
-    First<SHARED> f;
-    f.at(a, 0);
-    const int sb = a.Hkv * a.MT, b = blockIdx.x / sb, n = places_of<HD, TILES>(a, b, f) + kExtra;
+    const int sb = a.Hkv * a.MT, b = blockIdx.x / sb, n = places_of<HD, TILES>(a, b) + kExtra;
     part = Part{n, 0, n, -(long long)(blockIdx.x - b * sb) * n, b, 1};
   } else {
-    if (!SHARED && t == 0) a.split[blockIdx.x].pieces = 0;
-    part = find_part<HD, TILES, SHARED>(a, blockIdx.x, gridDim.x);
+    if (t == 0) a.split[blockIdx.x].pieces = 0;
+    part = find_part<HD, TILES>(a, blockIdx.x, gridDim.x);
   }
   if (part.x0 < part.x1) {
-    Feed<T, HD, TILES, SHARED> feed;
+    Feed<T, HD, TILES> feed;
     feed.start(a, part, warp);
 #pragma unroll
     for (int i = 0; i < ST - 1; ++i) feed.copy(a, part, ring + i * kUnitBytes, open + i, lane);
     int st = 0;
 
-    Piece<HD, TILES, SHARED> pc;
+    Piece<HD, TILES> pc;
     pc.at(a, part);
     do {
       if (pc.xa >= pc.xb) continue;                // (uniform) only places without units
@@ -373,15 +319,15 @@ __device__ __forceinline__ void attend(const Args& a) {
                 mma16816<T>(s[i][n + 1], q[i][k], kb[2], kb[3]);
               }
             }
-          const int key0 = pc.key(x);
-          if (key0 + U - 1 > free_to || (SHARED && key0 < pc.f.key) || ok != (1u << (U / 16)) - 1) {       // (uniform)
+          const int key0 = pc.unit(x) * U;
+          if (key0 + U - 1 > free_to || ok != (1u << (U / 16)) - 1) {       // (uniform)
 #pragma unroll
             for (int i = 0; i < HELD; ++i)
 #pragma unroll
               for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                  if (key0 + 8 * n + 2 * c + (e & 1) > last[i][e >> 1] || (SHARED && key0 + 8 * n + 2 * c + (e & 1) < pc.f.key) || !((ok >> (n >> 1)) & 1u)) s[i][n][e] = -INFINITY;
+                  if (key0 + 8 * n + 2 * c + (e & 1) > last[i][e >> 1] || !((ok >> (n >> 1)) & 1u)) s[i][n][e] = -INFINITY;
           }
 #pragma unroll
           for (int i = 0; i < HELD; ++i) {
@@ -499,25 +445,15 @@ __device__ __forceinline__ void attend(const Args& a) {
         const bool whole = pc.xa == pc.xs && pc.xb == end;
         const int slot = 2 * blockIdx.x + (pc.xa == pc.xs);       // 0: a segment begun elsewhere, 1: one that goes on elsewhere
         // (parts up to the last that begins before the segment's end: total p / parts < end)
-        if ((SHARED || !whole) && pc.xa == pc.xs && j == 0 && lane == 0) {
-          const int pieces = (int)((end * part.parts + part.total - 1) / part.total) - (int)blockIdx.x;
-          if (SHARED) a.part.rec[(int64_t)pc.b * a.Hkv * a.MT + pc.s] = Record{(int)blockIdx.x, pieces};
-          else a.split[blockIdx.x] = Split{pc.b, pc.s, pieces, 0};
-        }
+        if (!whole && pc.xa == pc.xs && j == 0 && lane == 0)
+          a.split[blockIdx.x] = Split{pc.b, pc.s, (int)((end * part.parts + part.total - 1) / part.total) - (int)blockIdx.x, 0};
 #pragma unroll
         for (int i = 0; i < HELD; ++i)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const int rr = 16 * (tile + i) + g + 8 * h, r = seg0 + rr, tok = r / a.G;
             if (r >= R) continue;
-            if constexpr (SHARED) {
-              const bool first = pc.xa == pc.xs;
-              const int64_t at = first ? ((int64_t)pc.b * a.rows + tok) * a.Hq + hk * a.G + r - tok * a.G : (int64_t)blockIdx.x * ROWS + rr;
-              float* op = (first ? a.part.first_o : a.part.more_o) + at * HD;
-#pragma unroll
-              for (int d = 0; d < DT; ++d) *reinterpret_cast<float2*>(op + 8 * d + 2 * c) = make_float2(o[i][d][2 * h], o[i][d][2 * h + 1]);
-              if (c == 0) (first ? a.part.first_ml : a.part.more_ml)[at] = make_float2(m[i][h], l[i][h]);
-            } else if (whole) {
+            if (whole) {
               const float inv = l[i][h] == 0.f ? 0.f : 1.f / l[i][h];     // (no key seen: zeros)
               T* op = static_cast<T*>(a.out) + (((int64_t)pc.b * a.rows + tok) * a.Hq + hk * a.G + r - tok * a.G) * HD;
 #pragma unroll
@@ -534,16 +470,8 @@ __device__ __forceinline__ void attend(const Args& a) {
     } while (pc.next(a, part));
     mma::cp_wait<0>();
   }
-  // (the prefixes' kernel before this one: what comes after is to see both)
-  if (SHARED) asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
-
-template <typename T, int HD, int TILES>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_paged(const __grid_constant__ Args a) { attend<T, HD, TILES, false>(a); }
-// the keys from the groups' prefixes on (kf_shared.cuh)
-template <typename T, int HD, int TILES>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm<HD, TILES>) k_own(const __grid_constant__ Args a) { attend<T, HD, TILES, true>(a); }
 
 // Block (c, y): rows y, y + gridDim.y, ... of the segment that CTA c began and others went on
 // with: its pieces (slot 1 of c, slot 0 of c + 1, c + 2, ...) added in order
@@ -645,23 +573,6 @@ int launch_any(int hd, const Args& a, const Shape& sh, void* work, cudaStream_t 
   if (hd == 128) return sh.tiles == 2 ? launch<T, 128, 2>(a, sh, work, s) : launch<T, 128, 1>(a, sh, work, s);
   return sh.tiles == 2 ? launch<T, 64, 2>(a, sh, work, s) : launch<T, 64, 1>(a, sh, work, s);
 }
-template <typename T, int HD, int TILES>
-void launch_own(const Args& a, int grid, cudaStream_t s) {
-  static PerDevice attr;
-  set_smem_attr(attr, k_own<T, HD, TILES>, kSmem<HD, TILES>);
-  launch_cluster(k_own<T, HD, TILES>, dim3(grid), dim3(kThreads), kSmem<HD, TILES>, 1, true, s, a);
-}
-template <typename T>
-void launch_own_any(int hd, int tiles, const Args& a, int grid, cudaStream_t s) {
-  if (hd == 128) tiles == 2 ? launch_own<T, 128, 2>(a, grid, s) : launch_own<T, 128, 1>(a, grid, s);
-  else tiles == 2 ? launch_own<T, 64, 2>(a, grid, s) : launch_own<T, 64, 1>(a, grid, s);
-}
-int shift_of(int page) {
-  int shift = -1;
-  if ((page & (page - 1)) == 0)
-    for (shift = 0; (1 << shift) < page;) ++shift;
-  return shift;
-}
 // the arguments' sizes; nullptr if they are fine
 const char* sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int width) {
   if (hd != 64 && hd != 128) return "head_dim is 64 or 128";
@@ -674,19 +585,6 @@ const char* sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int 
 }  // namespace
 
 const char* paged_sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int width) { return sizes_fault(B, rows, Hq, Hkv, hd, page, width); }
-
-OwnPlan plan_own(int B, int rows, int G, int Hkv, int hd, int page, int width, int64_t n_pages) {
-  const Shape sh = shape_of(B, rows, G, Hkv, hd, page, width, std::min((int64_t)B * width, n_pages) * page);
-  const int per_sm = hd == 64 && sh.tiles == 1 ? kCtasPerSm<64, 1> : 2;
-  return OwnPlan{(int)std::min<long long>((long long)per_sm * device_sms(), std::max(1ll, sh.segments * (sh.longest + kExtra) / kMinUnits)),
-                 16 * sh.tiles, (int)sh.segments};
-}
-void launch_own(int32_t type, const SharedCall& c, cudaStream_t s) {
-  Args a{c.q, c.q_seq, c.q_row, c.q_head, c.pool, c.table, c.lens, nullptr, nullptr, nullptr, nullptr, c.err, c.n_pages,
-         c.B, c.rows, c.Hq, c.Hkv, c.G, ceil_div(c.rows * c.G, c.own.seg_rows), c.page, shift_of(c.page), c.width, 0, c.scale2, c.sh, c.own};
-  if (type == KF_TYPE_BF16) launch_own_any<__nv_bfloat16>(c.hd, c.own.seg_rows / 16, a, c.own.ctas, s);
-  else launch_own_any<__half>(c.hd, c.own.seg_rows / 16, a, c.own.ctas, s);
-}
 }  // namespace kf
 
 using namespace kf;
@@ -713,9 +611,12 @@ extern "C" int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int3
   if (!aligned(q, 16) || !aligned(pool, 16) || !aligned(out, 16) || !aligned(work, 256) || !aligned(table, 4) || !aligned(lens, 4))
     return refuse(what, "q, pool and out are 16-byte aligned, work 256-byte");
   if (q_seq % 8 || q_row % 8 || q_head % 8) return refuse(what, "q's strides are multiples of 8 elements");
+  int shift = -1;
+  if ((page & (page - 1)) == 0)
+    for (shift = 0; (1 << shift) < page;) ++shift;
   if (!n_pages) pool = q;      // (nothing of it is read)
   const Args a{q, q_seq, q_row, q_head, pool, table, lens, out, nullptr, nullptr, nullptr, serving_error_word(), n_pages,
-               B, rows, Hq, Hkv, G, 0, page, shift_of(page), width, 0, scale * 1.4426950408889634f, {}, {}};
+               B, rows, Hq, Hkv, G, 0, page, shift, width, 0, scale * 1.4426950408889634f};
   if (!a.err) return refuse(what, "no error word", KF_E_CUDA);
   cudaStream_t s = (cudaStream_t)stream;
   return type == KF_TYPE_BF16 ? launch_any<__nv_bfloat16>(hd, a, sh, work, s) : launch_any<__half>(hd, a, sh, work, s);

@@ -1,25 +1,24 @@
-// What the two kernels of shared_attention (kf_op_shared_attention) agree on: the prefixes' keys
-// (kf_shared_prefix.cu) and each sequence's own (kf_paged_attention.cu) leave partial outputs of every
-// query row, which a last kernel adds.
+// What the kernels of shared_attention (kf_op_shared_attention) agree on: segments are query rows that read the
+// same keys, those of a group's sequences its prefix (kf_shared_attention.cu, or with few rows kf_shared_rows.cu), those of a
+// sequence its own keys (kf_shared_rows.cu).  They leave partial outputs, which a last kernel adds.
 //
-// Either kernel takes a list of segments (rows that read the same keys) cut into even parts, one a CTA.
-// The piece that begins a segment leaves its rows' sums at the rows' own places (`first`), a
-// later one, of which a CTA has at most one, at the CTA's (`more`); the segment's record says where they are.
+// The segments form a list that is cut into even parts.  The piece that begins a segment leaves its rows' sums at the rows' own
+// places (`first`), a later one, of which a part has at most one, at the part's (`more`); the
+// segment's record says where they are.
 #pragma once
 
 #include "kf_serving.cuh"
 
 namespace kf {
 
-constexpr int kPrefixRows = 256;            // query rows of a prefix segment
-struct Record { int cta, pieces; };         // the CTA that begins a segment, and how many have pieces of it
+struct Record { int part, pieces; };        // the part that a segment begins in, and how many have pieces of it
 struct Partials {
   float* first_o;                           // [B * rows * Hq][hd], not divided by the sums
   float2* first_ml;                         // [B * rows * Hq]: reference (a raw score) and sum
-  float* more_o;                            // [CTAs][rows of a segment][hd]
-  float2* more_ml;                          // [CTAs][rows of a segment]
+  float* more_o;                            // [parts][rows of a segment][hd]
+  float2* more_ml;                          // [parts][rows of a segment]
   Record* rec;                              // [segments]
-  int ctas, seg_rows, segments;
+  int parts, seg_rows, segments;
 };
 struct Sharing {
   const int32_t *groups, *shared;           // [n + 1] first sequences, [n] tokens of the prefixes
@@ -46,10 +45,24 @@ __device__ __forceinline__ int2 members(const Sharing& s, int g, int B) {
   const int a = min(max(__ldg(s.groups + g), 0), B), b = min(max(__ldg(s.groups + g + 1), 0), B);
   return make_int2(a, max(a, b));
 }
-// the record of a group's pair of sub-tiles under KV head hk (`before`: the rows a head that lie before the group)
-__device__ __forceinline__ int prefix_record(int64_t before, int g, int pair, int hk, int Hkv) {
-  return (int)((before / kPrefixRows + g + pair) * Hkv + hk);
+// the record of a group's tile of `seg_rows` rows under KV head hk (`before`: the rows a head that lie before the group)
+__device__ __forceinline__ int prefix_record(int64_t before, int g, int tile, int seg_rows, int hk, int Hkv) {
+  return (int)((before / seg_rows + g + tile) * Hkv + hk);
 }
+// a list of `total` places in `parts` even parts: the first `more` have one more than the others
+struct Parts {
+  int total, parts, each, more;
+  Parts() = default;
+  __device__ __forceinline__ Parts(int total_, int parts_) : total(total_), parts(parts_) {
+    each = total / parts;
+    more = total - each * parts;
+  }
+  __device__ __forceinline__ int begin(int c) const { return c < parts ? c * each + min(c, more) : total; }
+  __device__ __forceinline__ int part_of(int x) const {
+    const int split = more * (each + 1);
+    return x < split ? x / (each + 1) : more + (x - split) / each;
+  }
+};
 
 struct SharedCall {
   const void* q;
@@ -66,11 +79,11 @@ struct SharedCall {
   Div by_page, by_group, by_seq;            // the page, the heads of a group, a sequence's rows under a KV head
 };
 
-// The kernel of each sequence's own keys (kf_paged_attention.cu): its CTAs, the rows of its segments and its records for
-// these sizes, and its launch, which waits for the kernel before it only at its end
-struct OwnPlan { int ctas, seg_rows, segments; };
-OwnPlan plan_own(int B, int rows, int G, int Hkv, int hd, int page, int width, int64_t n_pages);
-void launch_own(int32_t type, const SharedCall& c, cudaStream_t s);
+// The kernel of kf_shared_rows.cu: how many parts it has and the rows of its segments, and its launch (with the prefixes, or for
+// each sequence's own keys alone, after another kernel)
+struct RowsPlan { int parts, seg_rows; };
+RowsPlan plan_rows(int rows_of_seq, int hd);
+void launch_rows(int32_t type, const SharedCall& c, bool prefixes, cudaStream_t s);
 // what paged attention says to these sizes; nullptr if they are fine
 const char* paged_sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int width);
 

@@ -19,6 +19,7 @@ namespace {
 using namespace pair;
 
 constexpr int kGran = 16, kGrans = kKeys / kGran;    // keys of a box; boxes of a tile
+constexpr int kPrefixRows = 256;                     // query rows of a segment
 constexpr int kExtra = 2;                            // a segment's start and end, in tiles
 constexpr int kMinTiles = 2;                         // places of a CTA, at least
 
@@ -58,22 +59,6 @@ struct Group {
   __device__ __forceinline__ int places(const SharedCall& a) const { return pairs * a.Hkv * (tiles + kExtra); }
 };
 
-// The list of `total` places in `parts` even parts: the first `more` have one more than the others
-struct Parts {
-  int total, parts, each, more;
-  Parts() = default;
-  __device__ __forceinline__ Parts(int total_, int most) : total(total_) {
-    parts = min(most, max(1, total / kMinTiles));
-    each = total / parts;
-    more = total - each * parts;
-  }
-  __device__ __forceinline__ int begin(int c) const { return c < parts ? c * each + min(c, more) : total; }
-  __device__ __forceinline__ int part_of(int x) const {
-    const int split = more * (each + 1);
-    return x < split ? x / (each + 1) : more + (x - split) / each;
-  }
-};
-
 // A CTA's pieces of segments, in order (by the load warp, uniform)
 struct Walk {
   Parts parts;
@@ -84,7 +69,7 @@ struct Walk {
     const int mine = lane < a.sh.n ? Group(a, lane).places(a) : 0;
     int total = __reduce_add_sync(~0u, mine);
     for (int i = 32; i < a.sh.n; i += 32) total += __reduce_add_sync(~0u, i + lane < a.sh.n ? Group(a, i + lane).places(a) : 0);
-    parts = Parts(total, gridDim.x);
+    parts = Parts(total, min((int)gridDim.x, max(1, total / kMinTiles)));
     x = parts.begin(blockIdx.x);
     x1 = parts.begin(blockIdx.x + 1);
     for (int i = 0; x < x1 && i < a.sh.n; i += 32) {
@@ -130,7 +115,7 @@ struct Walk {
       im.n[0] = n;
       im.n[1] = im.rows > kRows ? n : 0;
       im.more = t0 > 0;
-      at = prefix_record(gr.before, g, pair, hk, a.Hkv);
+      at = prefix_record(gr.before, g, pair, kPrefixRows, hk, a.Hkv);
       pieces = parts.part_of(end - 1) - blockIdx.x + 1;      // (parts up to the one of the segment's last tile)
       break;
     }
@@ -366,78 +351,75 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
 }
 
-// The pieces of a query row added: those of its group's prefix and those of its sequence's own keys, by W warps (each
-// every W-th piece; their sums then in order)
-constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+// The pieces of a query row added, those of its group's prefix and those of its sequence's own keys: HD / 4 lanes a row, W rows' worth of
+// lanes share its pieces where there are few rows (each every W-th piece; their sums then in order)
+constexpr int kJoinThreads = 256;
 template <typename T, int HD>
 __global__ void __launch_bounds__(kJoinThreads) k_add(const __grid_constant__ SharedCall a, int W) {
-  constexpr int N = HD / 32;                    // values of a lane
-  using V = typename std::conditional<N == 4, float4, float2>::type;
-  __shared__ V so[kJoinWarps][32];
-  __shared__ float2 sml[kJoinWarps];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % W;
-  const int64_t rows = (int64_t)a.B * a.rows * a.Hq, at = min(rows - 1, (int64_t)blockIdx.x * (kJoinWarps / W) + warp / W);
-  const int64_t bt = at / a.Hq;
-  const int h = (int)(at - bt * a.Hq), b = (int)(bt / a.rows), tok = (int)(bt - (int64_t)b * a.rows), hk = a.by_group.of(h), r = tok * a.G + h - hk * a.G;
+  constexpr int V4 = HD / 4, GR = kJoinThreads / V4;      // lanes of a row; rows' worth of lanes in a block
+  __shared__ float4 so[GR][V4];
+  __shared__ float2 sml[GR];
+  const int v = threadIdx.x % V4, gr = threadIdx.x / V4, part = gr % W;
+  const int64_t rows = (int64_t)a.B * a.rows * a.Hq, at = min(rows - 1, (int64_t)blockIdx.x * (GR / W) + gr / W);
+  const int bt = (int)(at / a.Hq), h = (int)(at - (int64_t)bt * a.Hq), b = bt / a.rows, tok = bt - b * a.rows;
+  const int hk = a.by_group.of(h), r = tok * a.G + h - hk * a.G;
   const int g = group_of(a.sh, b);
   const int2 in = members(a.sh, g, a.B);
   const bool prefixed = b >= in.x && b < in.y && prefix_of(a.sh, g, a.width * a.page) > 0;
-  const int64_t x = (int64_t)(b - in.x) * a.rows * a.G + r;
+  const int x = (b - in.x) * a.rows * a.G + r;
   const int MT = (a.rows * a.G + a.own.seg_rows - 1) / a.own.seg_rows;
   const int own_rec = (b * a.Hkv + hk) * MT + r / a.own.seg_rows;
-  const int pre_rec = prefixed ? min(a.pre.segments - 1, prefix_record((int64_t)in.x * a.rows * a.G, g, (int)(x / kPrefixRows), hk, a.Hkv)) : 0;
+  const int pre_rec = prefixed ? min(a.pre.segments - 1, prefix_record((int64_t)in.x * a.rows * a.G, g, x / a.pre.seg_rows, a.pre.seg_rows, hk, a.Hkv)) : 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   // (written by the kernels before this one: not through the read-only path; a record of groups that are not as they
   // should be may hold anything)
   const int2 own = __ldcg(reinterpret_cast<const int2*>(a.own.rec) + own_rec);
   const int2 pre = prefixed ? __ldcg(reinterpret_cast<const int2*>(a.pre.rec) + pre_rec) : make_int2(0, 0);
-  float m = -INFINITY, l = 0.f, o[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) o[i] = 0.f;
-  auto add = [&](float2 ml, V x) {
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](float2 ml, float4 y) {
     const float mm = fmaxf(m, ml.x);
     const float fa = m == -INFINITY ? 0.f : mma::ex2((m - mm) * a.scale2), fb = ml.x == -INFINITY ? 0.f : mma::ex2((ml.x - mm) * a.scale2);
     m = mm;
     l = l * fa + ml.y * fb;
-    const float* v = reinterpret_cast<const float*>(&x);
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = o[i] * fa + v[i] * fb;
+    o = make_float4(o.x * fa + y.x * fb, o.y * fa + y.y * fb, o.z * fa + y.z * fb, o.w * fa + y.w * fb);
   };
   auto pieces = [&](const Partials& p, int2 rc, int row) {
-    const int c = max(rc.x, 0), n = min(p.ctas - c, rc.y);
+    const int c = max(rc.x, 0), n = min(p.parts - c, rc.y);
 #pragma unroll 4
     for (int i = part; i < n; i += W) {
       const int64_t q = i == 0 ? at : (int64_t)(c + i) * p.seg_rows + row;
-      add(__ldcg((i == 0 ? p.first_ml : p.more_ml) + q), __ldcg(reinterpret_cast<const V*>((i == 0 ? p.first_o : p.more_o) + q * HD) + lane));
+      add(__ldcg((i == 0 ? p.first_ml : p.more_ml) + q), __ldcg(reinterpret_cast<const float4*>((i == 0 ? p.first_o : p.more_o) + q * HD) + v));
     }
   };
   pieces(a.own, own, r % a.own.seg_rows);
-  if (prefixed) pieces(a.pre, pre, (int)(x % kPrefixRows));
+  if (prefixed) pieces(a.pre, pre, x % a.pre.seg_rows);
   if (W > 1) {                                  // (uniform)
-    so[warp][lane] = *reinterpret_cast<V*>(o);
-    if (lane == 0) sml[warp] = make_float2(m, l);
+    so[gr][v] = o;
+    if (v == 0) sml[gr] = make_float2(m, l);
     __syncthreads();
     if (part != 0) return;
-    for (int i = 1; i < W; ++i) add(sml[warp + i], so[warp + i][lane]);
+    for (int i = 1; i < W; ++i) add(sml[gr + i], so[gr + i][v]);
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;   // (no key seen: zeros)
-  T* out = static_cast<T*>(a.out) + at * HD + lane * N;
-  if constexpr (N == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv));
-  else *reinterpret_cast<uint32_t*>(out) = pack2<T>(o[0] * inv, o[1] * inv);
+  reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * HD)[v] = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
 }
 
 // ------------------------------------------------------------------ host
 template <typename T, int HD>
-int launch(int32_t type, const SharedCall& c, const CUtensorMap& map, cudaStream_t s) {
-  static PerDevice attr;
-  set_smem_attr(attr, k_prefix<T, HD>, kSmem<HD>);
-  launch_cluster(k_prefix<T, HD>, dim3(c.pre.ctas), dim3(kThreads), kSmem<HD>, 1, false, s, map, c);
-  launch_own(type, c, s);
-  // as many warps a row as fit the SMs at once
+int launch(int32_t type, const SharedCall& c, bool tiles, const CUtensorMap& map, cudaStream_t s) {
+  if (tiles) {
+    static PerDevice attr;
+    set_smem_attr(attr, k_prefix<T, HD>, kSmem<HD>);
+    launch_cluster(k_prefix<T, HD>, dim3(c.pre.parts), dim3(kThreads), kSmem<HD>, 1, false, s, map, c);
+  }
+  launch_rows(type, c, !tiles, s);
+  // as many lanes a row as fit the SMs at once
   const int64_t rows = (int64_t)c.B * c.rows * c.Hq;
+  constexpr int GR = kJoinThreads / (HD / 4);
   int W = 1;
-  while (W < kJoinWarps && rows * W * 2 <= (int64_t)device_sms() * 64) W *= 2;
-  const int64_t per = kJoinWarps / W;
+  while (W < 8 && rows * (HD / 4) * W * 2 <= (int64_t)device_sms() * 2048) W *= 2;
+  const int64_t per = GR / W;
   launch_cluster(k_add<T, HD>, dim3((unsigned)((rows + per - 1) / per)), dim3(kJoinThreads), 0, 1, true, s, c, W);
   return launched("kf_op_shared_attention");
 }
@@ -450,43 +432,52 @@ bool pool_map(CUtensorMap* m, const void* pool, int64_t n_pages, int Hkv, int pa
   return encode_map_bf16(m, pool, 4, dims, strides, box);      // (fp16 is copied the same way)
 }
 
-// The scratch, in 256-byte pieces; its size where work is NULL
-int64_t layout(SharedCall& c, void* work) {
+// The scratch, in 256-byte pieces; its size where work is NULL.  tiles: the prefixes on tcgen05
+int64_t layout(SharedCall& c, bool tiles, void* work) {
   int64_t at = 0;
   auto take = [&](int64_t bytes) -> void* {
     const int64_t p = at;
     at += (bytes + 255) / 256 * 256;
     return static_cast<uint8_t*>(work) + p;
   };
-  const int64_t rows = (int64_t)c.B * c.rows * c.Hq;
-  const OwnPlan own = plan_own(c.B, c.rows, c.G, c.Hkv, c.hd, c.page, c.width, c.n_pages);
-  // no more CTAs than the longest list that the table could hold fills
-  const int64_t pairs = (int64_t)c.B * c.rows * c.G / kPrefixRows + c.sh.n, tiles = ((int64_t)c.width * c.page + kKeys - 1) / kKeys + kExtra;
-  c.pre.ctas = (int)std::max<int64_t>(1, std::min<int64_t>(device_sms(), pairs * c.Hkv * tiles / kMinTiles));
-  c.pre.seg_rows = kPrefixRows;
-  c.pre.segments = (int)((pairs + 1) * c.Hkv);
-  c.own.ctas = own.ctas;
+  const int64_t rows = (int64_t)c.B * c.rows * c.Hq, per = c.rows * c.G;
+  const RowsPlan own = plan_rows((int)per, c.hd);
+  c.own.parts = own.parts;
   c.own.seg_rows = own.seg_rows;
-  c.own.segments = own.segments;
-  for (Partials* p : {&c.pre, &c.own}) {
+  c.own.segments = (int)((int64_t)c.B * c.Hkv * ceil_div((int)per, own.seg_rows));
+  c.pre.seg_rows = tiles ? kPrefixRows : own.seg_rows;
+  const int64_t pre_tiles = c.B * per / c.pre.seg_rows + c.sh.n;
+  c.pre.segments = (int)((pre_tiles + 1) * c.Hkv);
+  // no more CTAs than the longest list that the table could hold fills
+  const int64_t places = pre_tiles * c.Hkv * (((int64_t)c.width * c.page + kKeys - 1) / kKeys + kExtra);
+  c.pre.parts = tiles ? (int)std::max<int64_t>(1, std::min<int64_t>(device_sms(), places / kMinTiles)) : own.parts;
+  for (Partials* p : {&c.own, &c.pre}) {
     p->first_o = static_cast<float*>(take(rows * c.hd * (int64_t)sizeof(float)));
     p->first_ml = static_cast<float2*>(take(rows * (int64_t)sizeof(float2)));
-    p->more_o = static_cast<float*>(take((int64_t)p->ctas * p->seg_rows * c.hd * (int64_t)sizeof(float)));
-    p->more_ml = static_cast<float2*>(take((int64_t)p->ctas * p->seg_rows * (int64_t)sizeof(float2)));
     p->rec = static_cast<Record*>(take(p->segments * (int64_t)sizeof(Record)));
+    if (p == &c.pre && !tiles) {                // (a part has one later piece, of either kind)
+      p->more_o = c.own.more_o;
+      p->more_ml = c.own.more_ml;
+    } else {
+      p->more_o = static_cast<float*>(take((int64_t)p->parts * p->seg_rows * c.hd * (int64_t)sizeof(float)));
+      p->more_ml = static_cast<float2*>(take((int64_t)p->parts * p->seg_rows * (int64_t)sizeof(float2)));
+    }
   }
   return at;
 }
 const char* sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int width, int n) {
   if (const char* f = paged_sizes_fault(B, rows, Hq, Hkv, hd, page, width)) return f;
-  if (n < 0 || (B > 0 && n < 1)) return "groups out of range";
-  if ((int64_t)B * rows * Hq > (1 << 30) || ((int64_t)B * rows * (Hq / Hkv) / kPrefixRows + n + 1) * Hkv > (1 << 30) || (int64_t)B * Hkv * rows * (Hq / Hkv) > (1 << 30))
-    return "too many rows and heads";
-  if (((int64_t)B * rows * (Hq / Hkv) / kPrefixRows + n + 1) * Hkv * (((int64_t)width * page + kKeys - 1) / kKeys + kExtra) > 0x7fffffff) return "too many keys";
+  if (n < 0 || (B > 0 && n < 1) || n > (1 << 24)) return "groups out of range";
+  const int64_t tiles = 2 * ((int64_t)B * ceil_div(rows * (Hq / Hkv), 16) + n + 1) * Hkv;      // of 16 rows, over prefixes and own keys
+  if ((int64_t)B * rows * Hq > (1 << 30) || tiles > (1 << 30)) return "too many rows and heads";
+  if (tiles * ((int64_t)width * page / 16 + 8) > 0x7fffffff) return "too many keys";
   return nullptr;
 }
 // Nothing to share: each sequence a group, or no pages
 bool plain(int B, int n, int64_t n_pages) { return n >= B || n_pages == 0; }
+// The prefixes on tcgen05
+int g_force_tiles = 1;
+bool on_tiles(const SharedCall& c) { return g_force_tiles; }
 
 }  // namespace
 }  // namespace kf
@@ -508,7 +499,7 @@ extern "C" int64_t kf_op_shared_attention_work(int32_t B, int32_t rows, int32_t 
   c.page = page;
   c.width = width;
   c.sh.n = n;
-  return layout(c, nullptr);
+  return layout(c, on_tiles(c), nullptr);
 }
 
 extern "C" int kf_op_shared_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, const void* q, int64_t q_seq,
@@ -531,10 +522,13 @@ extern "C" int kf_op_shared_attention(int32_t type, int32_t B, int32_t rows, int
   SharedCall c{q, q_seq, q_row, q_head, pool, table, lens, out, n_pages, Sharing{groups, shared, n}, {}, {}, serving_error_word(),
                B, rows, Hq, Hkv, Hq / Hkv, hd, page, width, scale * 1.4426950408889634f, Div(page), Div(Hq / Hkv), Div(rows * (Hq / Hkv))};
   if (!c.err) return refuse(what, "no error word", KF_E_CUDA);
-  layout(c, work);
-  CUtensorMap map;
-  if (!pool_map(&map, pool, n_pages, Hkv, page, hd)) return refuse(what, "a tensor map is refused (the pool)");
+  const bool tiles = on_tiles(c);
+  layout(c, tiles, work);
+  CUtensorMap map{};
+  if (tiles && !pool_map(&map, pool, n_pages, Hkv, page, hd)) return refuse(what, "a tensor map is refused (the pool)");
   cudaStream_t s = (cudaStream_t)stream;
-  if (type == KF_TYPE_BF16) return hd == 64 ? launch<__nv_bfloat16, 64>(type, c, map, s) : launch<__nv_bfloat16, 128>(type, c, map, s);
-  return hd == 64 ? launch<__half, 64>(type, c, map, s) : launch<__half, 128>(type, c, map, s);
+  if (type == KF_TYPE_BF16) return hd == 64 ? launch<__nv_bfloat16, 64>(type, c, tiles, map, s) : launch<__nv_bfloat16, 128>(type, c, tiles, map, s);
+  return hd == 64 ? launch<__half, 64>(type, c, tiles, map, s) : launch<__half, 128>(type, c, tiles, map, s);
 }
+
+extern "C" void kf_force_tiles(int x) { g_force_tiles = x; }
