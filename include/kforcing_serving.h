@@ -137,13 +137,14 @@ int kf_op_paged_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int
  * document): as kf_op_paged_attention, but the keys that a group shares are read once for all of its rows.
  * Sequences groups[g] .. groups[g+1]-1 are group g, and their first shared[g] tokens are the same: groups int32 [n+1] on the
  * device, groups[0] = 0, not falling, groups[n] = B; shared int32 [n], 0 .. width * page, at most the lengths of the group's
- * sequences.  Keys below shared[g] are read through the table row of the group's first sequence, keys from there on
- * through each sequence's own (whose pages below are not looked at; kf_op_pages_fork leaves tables so that both are the same).
- * A group of one, or of none, and a prefix of no tokens are allowed.  Where every sequence is a group by itself (n >= B) the call is
- * kf_op_paged_attention.  What a row sees does not depend on shared: row i keys 0 .. len - rows + i.
+ * sequences.  Every sequence's table row has the prefix, in pages that its group shares or in copies (as kf_op_pages_fork leaves them);
+ * a call reads keys below shared[g] through the group's first sequence's row or through each one's own, which it does
+ * depends on its sizes.  A group of one, or of none, and a prefix of no tokens are allowed.  What a row sees does not
+ * depend on shared: row i keys 0 .. len - rows + i.  A page id outside the pool: KF_DEV_BAD_PAGE, its keys count as unseen by the rows
+ * that are read through it.
  * The same lengths, groups and prefixes in a table of the same width and a pool of the same size give the same bits.
  * A prefix outside 0 .. width * page: KF_DEV_BAD_ROW, and it counts as none.  Groups that are not as said: KF_DEV_BAD_ROW, and
- * out holds anything.
+ * out holds anything.  (Neither is looked at where each sequence is read by itself.)
  * work: kf_op_shared_attention_work bytes of the call's own sizes.  Errors: KF_E_ARG, KF_E_CUDA.
  */
 int64_t kf_op_shared_attention_work(int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, int64_t n_pages, int32_t page,

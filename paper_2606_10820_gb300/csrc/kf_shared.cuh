@@ -76,7 +76,7 @@ struct SharedCall {
   int* err;
   int B, rows, Hq, Hkv, G, hd, page, width;
   float scale2;
-  Div by_page, by_group, by_seq;            // the page, the heads of a group, a sequence's rows under a KV head
+  Div by_page, by_group, by_seq, by_heads, by_rows;      // the page, the heads of a group, a sequence's rows under a KV head; Hq, rows
 };
 
 // The kernel of kf_shared_rows.cu: how many parts it has and the rows of its segments, and its launch (with the prefixes, or for

@@ -351,58 +351,69 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
 }
 
-// The pieces of a query row added, those of its group's prefix and those of its sequence's own keys: HD / 4 lanes a row, W rows' worth of
-// lanes share its pieces where there are few rows (each every W-th piece; their sums then in order)
+// The pieces of a query row added, those of its group's prefix and those of its sequence's own keys: HD / 8 lanes a row, so that
+// many rows are one wave of blocks; of few rows W times as many lanes share the pieces (each every W-th; their sums then in order).
+// What a call takes here is a chain of loads: the first pieces, whose places need no record, come with the records
 constexpr int kJoinThreads = 256;
 template <typename T, int HD>
 __global__ void __launch_bounds__(kJoinThreads) k_add(const __grid_constant__ SharedCall a, int W) {
-  constexpr int V4 = HD / 4, GR = kJoinThreads / V4;      // lanes of a row; rows' worth of lanes in a block
-  __shared__ float4 so[GR][V4];
+  constexpr int LANES = HD / 8, GR = kJoinThreads / LANES;      // of a row; rows' worth of lanes in a block
+  __shared__ float4 so[GR][2][LANES];
   __shared__ float2 sml[GR];
-  const int v = threadIdx.x % V4, gr = threadIdx.x / V4, part = gr % W;
-  const int64_t rows = (int64_t)a.B * a.rows * a.Hq, at = min(rows - 1, (int64_t)blockIdx.x * (GR / W) + gr / W);
-  const int bt = (int)(at / a.Hq), h = (int)(at - (int64_t)bt * a.Hq), b = bt / a.rows, tok = bt - b * a.rows;
+  const int v = threadIdx.x % LANES, gr = threadIdx.x / LANES, part = gr % W;
+  const int rows = a.B * a.rows * a.Hq, at = min(rows - 1, (int)blockIdx.x * (GR / W) + gr / W);
+  const int bt = a.by_heads.of(at), h = at - bt * a.Hq, b = a.by_rows.of(bt), tok = bt - b * a.rows;
   const int hk = a.by_group.of(h), r = tok * a.G + h - hk * a.G;
   const int g = group_of(a.sh, b);
   const int2 in = members(a.sh, g, a.B);
   const bool prefixed = b >= in.x && b < in.y && prefix_of(a.sh, g, a.width * a.page) > 0;
   const int x = (b - in.x) * a.rows * a.G + r;
-  const int MT = (a.rows * a.G + a.own.seg_rows - 1) / a.own.seg_rows;
-  const int own_rec = (b * a.Hkv + hk) * MT + r / a.own.seg_rows;
-  const int pre_rec = prefixed ? min(a.pre.segments - 1, prefix_record((int64_t)in.x * a.rows * a.G, g, x / a.pre.seg_rows, a.pre.seg_rows, hk, a.Hkv)) : 0;
+  // (segments have 16, 32 or 256 rows)
+  const int own_shift = a.own.seg_rows == 16 ? 4 : 5, pre_shift = a.pre.seg_rows == 256 ? 8 : own_shift;
+  const int MT = (a.rows * a.G + a.own.seg_rows - 1) >> own_shift;
+  const int own_rec = (b * a.Hkv + hk) * MT + (r >> own_shift);
+  const int pre_rec = prefixed ? min(a.pre.segments - 1, prefix_record((int64_t)in.x * a.rows * a.G, g, x >> pre_shift, a.pre.seg_rows, hk, a.Hkv)) : 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   // (written by the kernels before this one: not through the read-only path; a record of groups that are not as they
   // should be may hold anything)
   const int2 own = __ldcg(reinterpret_cast<const int2*>(a.own.rec) + own_rec);
   const int2 pre = prefixed ? __ldcg(reinterpret_cast<const int2*>(a.pre.rec) + pre_rec) : make_int2(0, 0);
   float m = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [&](float2 ml, float4 y) {
+  float4 o0 = make_float4(0.f, 0.f, 0.f, 0.f), o1 = o0;
+  auto add = [&](float2 ml, float4 y0, float4 y1) {
     const float mm = fmaxf(m, ml.x);
     const float fa = m == -INFINITY ? 0.f : mma::ex2((m - mm) * a.scale2), fb = ml.x == -INFINITY ? 0.f : mma::ex2((ml.x - mm) * a.scale2);
     m = mm;
     l = l * fa + ml.y * fb;
-    o = make_float4(o.x * fa + y.x * fb, o.y * fa + y.y * fb, o.z * fa + y.z * fb, o.w * fa + y.w * fb);
+    o0 = make_float4(o0.x * fa + y0.x * fb, o0.y * fa + y0.y * fb, o0.z * fa + y0.z * fb, o0.w * fa + y0.w * fb);
+    o1 = make_float4(o1.x * fa + y1.x * fb, o1.y * fa + y1.y * fb, o1.z * fa + y1.z * fb, o1.w * fa + y1.w * fb);
   };
-  auto pieces = [&](const Partials& p, int2 rc, int row) {
+  auto piece = [&](const float* po, const float2* pml, int64_t q) {
+    const float4* y = reinterpret_cast<const float4*>(po + q * HD) + 2 * v;
+    add(__ldcg(pml + q), __ldcg(y), __ldcg(y + 1));
+  };
+  auto later = [&](const Partials& p, int2 rc, int row) {
     const int c = max(rc.x, 0), n = min(p.parts - c, rc.y);
 #pragma unroll 4
-    for (int i = part; i < n; i += W) {
-      const int64_t q = i == 0 ? at : (int64_t)(c + i) * p.seg_rows + row;
-      add(__ldcg((i == 0 ? p.first_ml : p.more_ml) + q), __ldcg(reinterpret_cast<const float4*>((i == 0 ? p.first_o : p.more_o) + q * HD) + v));
-    }
+    for (int i = part > 0 ? part : W; i < n; i += W) piece(p.more_o, p.more_ml, (int64_t)(c + i) * p.seg_rows + row);
   };
-  pieces(a.own, own, r % a.own.seg_rows);
-  if (prefixed) pieces(a.pre, pre, x % a.pre.seg_rows);
+  if (part == 0) {
+    piece(a.own.first_o, a.own.first_ml, at);
+    if (prefixed) piece(a.pre.first_o, a.pre.first_ml, at);
+  }
+  later(a.own, own, r & (a.own.seg_rows - 1));
+  if (prefixed) later(a.pre, pre, x & (a.pre.seg_rows - 1));
   if (W > 1) {                                  // (uniform)
-    so[gr][v] = o;
+    so[gr][0][v] = o0;
+    so[gr][1][v] = o1;
     if (v == 0) sml[gr] = make_float2(m, l);
     __syncthreads();
     if (part != 0) return;
-    for (int i = 1; i < W; ++i) add(sml[gr + i], so[gr + i][v]);
+    for (int i = 1; i < W; ++i) add(sml[gr + i], so[gr + i][0][v], so[gr + i][1][v]);
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;   // (no key seen: zeros)
-  reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * HD)[v] = make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
+  reinterpret_cast<uint4*>(static_cast<T*>(a.out) + (int64_t)at * HD)[v] =
+      make_uint4(pack2<T>(o0.x * inv, o0.y * inv), pack2<T>(o0.z * inv, o0.w * inv), pack2<T>(o1.x * inv, o1.y * inv), pack2<T>(o1.z * inv, o1.w * inv));
 }
 
 // ------------------------------------------------------------------ host
@@ -414,11 +425,12 @@ int launch(int32_t type, const SharedCall& c, bool tiles, const CUtensorMap& map
     launch_cluster(k_prefix<T, HD>, dim3(c.pre.parts), dim3(kThreads), kSmem<HD>, 1, false, s, map, c);
   }
   launch_rows(type, c, !tiles, s);
-  // as many lanes a row as fit the SMs at once
+  // lanes for every second piece that a row may have, as far as they fit the SMs at once
   const int64_t rows = (int64_t)c.B * c.rows * c.Hq;
-  constexpr int GR = kJoinThreads / (HD / 4);
+  constexpr int GR = kJoinThreads / (HD / 8);
+  const int pieces = c.own.parts / c.own.segments + c.pre.parts / c.pre.segments;
   int W = 1;
-  while (W < 8 && rows * (HD / 4) * W * 2 <= (int64_t)device_sms() * 2048) W *= 2;
+  while (W < 8 && W * 4 <= pieces && rows * (HD / 8) * W * 2 <= (int64_t)device_sms() * 2048) W *= 2;
   const int64_t per = GR / W;
   launch_cluster(k_add<T, HD>, dim3((unsigned)((rows + per - 1) / per)), dim3(kJoinThreads), 0, 1, true, s, c, W);
   return launched("kf_op_shared_attention");
@@ -473,11 +485,22 @@ const char* sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int 
   if (tiles * ((int64_t)width * page / 16 + 8) > 0x7fffffff) return "too many keys";
   return nullptr;
 }
-// Nothing to share: each sequence a group, or no pages
-bool plain(int B, int n, int64_t n_pages) { return n >= B || n_pages == 0; }
-// The prefixes on tcgen05
-int g_force_tiles = 1;
-bool on_tiles(const SharedCall& c) { return g_force_tiles; }
+// What reads a call's prefixes.  The lengths are on the device, so the rule takes what the table and the pool could hold:
+//   paged attention, once a sequence, where nothing is shared or the reads of all sequences would be few (they come from L2
+//   at about 10 TB/s, and two launches less); MB of those reads and us, paged and the better of the others:
+//     5: 7.9  10.9   24: 11.2  11.8   44: 9.3  11.8   66: 14.6  13.1   82: 16.2  15.8   120: 19.4  14.5   272: 47.2  37.2
+//   tiles of 16 or 32 rows, each reading the prefix, while those reads are few; MB and us, those and tcgen05:
+//     17: 14.5  17.7   28: 15.3  19.6   204: 38.1  37.2   629: 70.9  71.9   2,200: 252  76
+enum Way { PAGED, ROWS, TILES };
+constexpr double kPagedBytes = 48 << 20, kRowsBytes = 128 << 20;
+Way way_of(int B, int rows, int G, int Hkv, int hd, int64_t n_pages, int page, int width, int n) {
+  if (n >= B || n_pages == 0) return PAGED;
+  const int seg = plan_rows(rows * G, hd).seg_rows;
+  const double keys = (double)std::min((int64_t)width, n_pages) * page * hd * 4 * Hkv;      // bytes of a prefix, at most
+  if ((double)B * ceil_div(rows * G, seg) * keys <= kPagedBytes) return PAGED;
+  const double tiles = (double)(((int64_t)B * rows * G + seg - 1) / seg + n);
+  return tiles * keys <= kRowsBytes ? ROWS : TILES;
+}
 
 }  // namespace
 }  // namespace kf
@@ -487,7 +510,8 @@ using namespace kf;
 extern "C" int64_t kf_op_shared_attention_work(int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, int64_t n_pages, int32_t page,
                                                int32_t width, int32_t n) {
   if (B <= 0 || n_pages < 0 || sizes_fault(B, rows, Hq, Hkv, hd, page, width, n)) return 0;
-  if (plain(B, n, n_pages)) return kf_op_paged_attention_work(B, rows, Hq, Hkv, hd, page, width);
+  const Way way = way_of(B, rows, Hq / Hkv, Hkv, hd, n_pages, page, width, n);
+  if (way == PAGED) return kf_op_paged_attention_work(B, rows, Hq, Hkv, hd, page, width);
   SharedCall c{};
   c.B = B;
   c.rows = rows;
@@ -499,7 +523,7 @@ extern "C" int64_t kf_op_shared_attention_work(int32_t B, int32_t rows, int32_t 
   c.page = page;
   c.width = width;
   c.sh.n = n;
-  return layout(c, on_tiles(c), nullptr);
+  return layout(c, way == TILES, nullptr);
 }
 
 extern "C" int kf_op_shared_attention(int32_t type, int32_t B, int32_t rows, int32_t Hq, int32_t Hkv, int32_t hd, const void* q, int64_t q_seq,
@@ -513,16 +537,17 @@ extern "C" int kf_op_shared_attention(int32_t type, int32_t B, int32_t rows, int
   if (!(scale > 0.f) || std::isinf(scale)) return refuse(what, "scale is a positive number");
   if (B == 0) return KF_OK;
   if (!groups || !shared || !aligned(groups, 4) || !aligned(shared, 4)) return refuse(what, "groups or shared: null or misaligned");
-  if (plain(B, n, n_pages))
+  const Way way = way_of(B, rows, Hq / Hkv, Hkv, hd, n_pages, page, width, n);
+  if (way == PAGED)
     return kf_op_paged_attention(type, B, rows, Hq, Hkv, hd, q, q_seq, q_row, q_head, pool, n_pages, page, table, width, lens, scale, out, work, stream);
   if (!q || !out || !lens || !work || !pool || (width && !table)) return refuse(what, "a null array");
   if (!aligned(q, 16) || !aligned(pool, 16) || !aligned(out, 16) || !aligned(work, 256) || !aligned(table, 4) || !aligned(lens, 4))
     return refuse(what, "q, pool and out are 16-byte aligned, work 256-byte");
   if (q_seq % 8 || q_row % 8 || q_head % 8) return refuse(what, "q's strides are multiples of 8 elements");
   SharedCall c{q, q_seq, q_row, q_head, pool, table, lens, out, n_pages, Sharing{groups, shared, n}, {}, {}, serving_error_word(),
-               B, rows, Hq, Hkv, Hq / Hkv, hd, page, width, scale * 1.4426950408889634f, Div(page), Div(Hq / Hkv), Div(rows * (Hq / Hkv))};
+               B, rows, Hq, Hkv, Hq / Hkv, hd, page, width, scale * 1.4426950408889634f, Div(page), Div(Hq / Hkv), Div(rows * (Hq / Hkv)), Div(Hq), Div(rows)};
   if (!c.err) return refuse(what, "no error word", KF_E_CUDA);
-  const bool tiles = on_tiles(c);
+  const bool tiles = way == TILES;
   layout(c, tiles, work);
   CUtensorMap map{};
   if (tiles && !pool_map(&map, pool, n_pages, Hkv, page, hd)) return refuse(what, "a tensor map is refused (the pool)");
@@ -530,5 +555,3 @@ extern "C" int kf_op_shared_attention(int32_t type, int32_t B, int32_t rows, int
   if (type == KF_TYPE_BF16) return hd == 64 ? launch<__nv_bfloat16, 64>(type, c, tiles, map, s) : launch<__nv_bfloat16, 128>(type, c, tiles, map, s);
   return hd == 64 ? launch<__half, 64>(type, c, tiles, map, s) : launch<__half, 128>(type, c, tiles, map, s);
 }
-
-extern "C" void kf_force_tiles(int x) { g_force_tiles = x; }

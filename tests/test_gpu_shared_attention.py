@@ -26,9 +26,25 @@ def i32(x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
 
 
-def make(groups, rows, Hq, Hkv, hd, dtype=torch.bfloat16, page=16, extra_width=2, seed=0, std=1.0, hide=False, spare=3):
+WAYS = ["paged", "rows", "tiles"]      # what reads the prefixes: paged attention, 16 or 32 rows at a time, 256
+
+
+def room(way, B, n, rows, Hq, Hkv, hd, page):
+    """Pages of a pool and of the table's width that make a call of these sizes choose the way (kf_shared_attention.cu: the reads
+    that they would allow for, 48 MB of all sequences' and 128 MB of all tiles')."""
+    per = rows * Hq // Hkv
+    seg = 32 if hd == 64 and per > 16 else 16
+    bytes_ = page * hd * 4 * Hkv
+    if way == "rows":
+        return (50 << 20) // (B * -(-per // seg) * bytes_) + 1
+    return (135 << 20) // (max(1, B * per // seg) * bytes_) + 1 if way == "tiles" else 0
+
+
+def make(groups, rows, Hq, Hkv, hd, dtype=torch.bfloat16, page=16, extra_width=2, seed=0, std=1.0, hide=False, spare=3, way="paged"):
     """groups: (shared tokens, lengths of the sequences) each.  Full pages of a prefix are in all tables, the rest of it is copied
     (hide: in no table but the first's); pages that nothing uses and slots past the lengths hold NaN."""
+    wide = room(way, sum(len(lens) for _, lens in groups), len(groups), rows, Hq, Hkv, hd, page)
+    spare, extra_width = spare + wide, extra_width + wide
     g = torch.Generator(device="cuda").manual_seed(seed)
     need = sum(n // page + sum(-(-x // page) - n // page for x in lens) for n, lens in groups) + spare
     pool = torch.full((need, 2, Hkv, page, hd), math.nan, device="cuda", dtype=dtype)
@@ -108,28 +124,34 @@ BATCHES = [
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("groups,rows,Hq,Hkv", BATCHES)
-def test_matches_plain(sv, hd, dtype, groups, rows, Hq, Hkv):
-    check(sv, *make(groups, rows, Hq, Hkv, hd, dtype, seed=len(groups) + rows))
+@pytest.mark.parametrize("way", WAYS)
+def test_matches_plain(sv, hd, dtype, groups, rows, Hq, Hkv, way):
+    check(sv, *make(groups, rows, Hq, Hkv, hd, dtype, seed=len(groups) + rows, way=way))
 
 
 @pytest.mark.parametrize("hd", [64, 128])
-def test_own_tables_are_not_looked_at_below_the_prefix(sv, hd):
-    check(sv, *make([(333, [340, 900, 333 + 8]), (48, [56, 57]), (5, [13, 14, 15, 40])], 8, 8, 2, hd, hide=True, seed=5))
+@pytest.mark.parametrize("way", WAYS[1:])
+def test_the_prefix_is_read_through_the_first_table(sv, hd, way):
+    """(What these two ways do beyond what is promised: it shows that they read a prefix once.)"""
+    check(sv, *make([(333, [340, 900, 333 + 8]), (48, [56, 57]), (5, [13, 14, 15, 40])], 8, 8, 2, hd, hide=True, seed=5, way=way))
 
 
 @pytest.mark.parametrize("page", [32, 48, 128])
-def test_page_sizes(sv, page):
-    check(sv, *make([(500, [501, 640, 900]), (47, [48, 49]), (128, [129, 128])], 1, 8, 2, 128, page=page, seed=page))
+@pytest.mark.parametrize("way", WAYS)
+def test_page_sizes(sv, page, way):
+    check(sv, *make([(500, [501, 640, 900]), (47, [48, 49]), (128, [129, 128])], 1, 8, 2, 128, page=page, seed=page, way=way))
 
 
-def test_one_call_over_many_tiles(sv):
+@pytest.mark.parametrize("way", WAYS)
+def test_one_call_over_many_tiles(sv, way):
     """A prefix in more pieces than CTAs take whole, and one of a group's many rows over several pairs of sub-tiles."""
-    check(sv, *make([(32771, [32772 + 100 * i for i in range(6)])], 1, 8, 2, 128, seed=1))
-    check(sv, *make([(700, [710 + i for i in range(150)]), (64, [72] * 9)], 8, 24, 4, 64, torch.float16, seed=2))
+    check(sv, *make([(32771, [32772 + 100 * i for i in range(6)])], 1, 8, 2, 128, seed=1, way=way))
+    check(sv, *make([(700, [710 + i for i in range(150)]), (64, [72] * 9)], 8, 24, 4, 64, torch.float16, seed=2, way=way))
 
 
 @pytest.mark.parametrize("seed", range(6))
-def test_random_groups(sv, seed):
+@pytest.mark.parametrize("way", WAYS)
+def test_random_groups(sv, seed, way):
     g = torch.Generator().manual_seed(seed)
 
     def r(lo, hi):
@@ -142,18 +164,20 @@ def test_random_groups(sv, seed):
         groups.append((n, [n + r(0, [200, 900, 30, 40, 300, 20][seed]) for _ in range(r(0, [5, 6, 9, 30, 12, 4][seed]))]))
     groups.append((4, [9]))
     check(sv, *make(groups, rows, [8, 6, 4, 16, 12, 5][seed], [2, 2, 1, 4, 4, 5][seed], [128, 64, 64, 128, 64, 128][seed],
-                    [torch.bfloat16, torch.float16][seed % 2], seed=seed, hide=seed % 2 == 0))
+                    [torch.bfloat16, torch.float16][seed % 2], seed=seed, hide=seed % 2 == 0 and way != "paged", way=way))
 
 
-def test_rows_that_see_part_of_the_prefix(sv):
+@pytest.mark.parametrize("way", WAYS)
+def test_rows_that_see_part_of_the_prefix(sv, way):
     """A prefix that reaches into the newest rows, to the last token: row i still sees keys 0 .. len - rows + i."""
-    check(sv, *make([(200, [200, 201, 203, 300]), (6, [6, 7]), (3, [3, 3, 4])], 8, 8, 2, 64, seed=3))
-    check(sv, *make([(129, [129, 129, 130])], 140, 2, 1, 128, seed=4))
+    check(sv, *make([(200, [200, 201, 203, 300]), (6, [6, 7]), (3, [3, 3, 4])], 8, 8, 2, 64, seed=3, way=way))
+    check(sv, *make([(129, [129, 129, 130])], 140, 2, 1, 128, seed=4, way=way))
 
 
-def test_shared_with_the_whole_of_paged_attention(sv):
+@pytest.mark.parametrize("way", WAYS)
+def test_shared_with_the_whole_of_paged_attention(sv, way):
     """Tables as a fork leaves them: both attentions give the same rows, within the tolerances of both."""
-    args = make([(400 + 50 * i, [400 + 50 * i + 8 + 13 * j for j in range(9)]) for i in range(7)], 4, 12, 4, 64, torch.float16, seed=6)
+    args = make([(400 + 50 * i, [400 + 50 * i + 8 + 13 * j for j in range(9)]) for i in range(7)], 4, 12, 4, 64, torch.float16, seed=6, way=way)
     got, whole = check(sv, *args), sv.paged_attention(*args[:4])
     assert ((got.double() - whole.double()).abs().max() <= 2 * (2 * 2.0 ** -11 + 2.0 ** -15) * args[1].nan_to_num().abs().max())
     # groups of one are paged attention
@@ -162,14 +186,16 @@ def test_shared_with_the_whole_of_paged_attention(sv):
     assert torch.equal(singles, whole)
 
 
-def test_peaked_and_scaled(sv):
-    check(sv, *make([(700, [701, 790]), (90, [91])], 1, 8, 2, 64, torch.float16, std=30.0, seed=3))
-    check(sv, *make([(700, [701, 790]), (90, [91])], 1, 8, 2, 128, torch.bfloat16, std=30.0, seed=3))
-    check(sv, *make([(700, [701, 790]), (90, [91])], 1, 8, 2, 64, seed=4), scale=0.37)
+@pytest.mark.parametrize("way", WAYS)
+def test_peaked_and_scaled(sv, way):
+    check(sv, *make([(700, [701, 790]), (90, [91])], 1, 8, 2, 64, torch.float16, std=30.0, seed=3, way=way))
+    check(sv, *make([(700, [701, 790]), (90, [91])], 1, 8, 2, 128, torch.bfloat16, std=30.0, seed=3, way=way))
+    check(sv, *make([(700, [701, 790]), (90, [91])], 1, 8, 2, 64, seed=4, way=way), scale=0.37)
 
 
-def test_infinities_stay_in_their_group(sv):
-    args = make([(300, [301, 400]), (300, [305, 310])], 1, 4, 2, 64, seed=7)
+@pytest.mark.parametrize("way", WAYS)
+def test_infinities_stay_in_their_group(sv, way):
+    args = make([(300, [301, 400]), (300, [305, 310])], 1, 4, 2, 64, seed=7, way=way)
     q, pool, table = args[:3]
     want = sv.shared_attention(*args)
     pool[table[0, 3].long(), 1, 0, 5, 7] = math.nan
@@ -181,9 +207,10 @@ def test_infinities_stay_in_their_group(sv):
     assert torch.equal(got, want)
 
 
-def test_same_bits_and_strides(sv):
+@pytest.mark.parametrize("way", WAYS)
+def test_same_bits_and_strides(sv, way):
     """The same call gives the same bits, whatever the pages' order and q's strides."""
-    q, pool, table, lens, starts, shared = make([(900, [901 + 40 * i for i in range(20)]), (77, [100, 2000])], 2, 16, 4, 128, seed=8)
+    q, pool, table, lens, starts, shared = make([(900, [901 + 40 * i for i in range(20)]), (77, [100, 2000])], 2, 16, 4, 128, seed=8, way=way)
     want = sv.shared_attention(q, pool, table, lens, starts, shared)
     perm = torch.randperm(len(pool), device="cuda")
     back = torch.argsort(perm)
@@ -196,8 +223,9 @@ def test_same_bits_and_strides(sv):
     assert torch.equal(sv.shared_attention(q, pool, table, lens, starts, shared), want)
 
 
-def test_bad_pages_and_rows(sv):
-    args = make([(300, [301, 400, 310]), (40, [50, 60])], 1, 4, 2, 64, seed=9)
+@pytest.mark.parametrize("way", WAYS)
+def test_bad_pages_and_rows(sv, way):
+    args = make([(300, [301, 400, 310]), (40, [50, 60])], 1, 4, 2, 64, seed=9, way=way)
     q, pool, table, lens, starts, shared = args
     good = sv.shared_attention(*args)
 
@@ -210,20 +238,24 @@ def test_bad_pages_and_rows(sv):
 
     for bad_id in (-1, len(pool), 1 << 30, -5):
         bad = table.clone()
-        bad[0, 4] = bad_id                                    # of the first group's prefix: unseen by all of it
+        bad[0, 4] = bad_id                                    # of the first group's prefix: unseen by all of it (or by the first)
         got = run(2, table=bad)
-        assert torch.equal(got[3:], good[3:]) and torch.isfinite(got).all() and not torch.equal(got[:3], good[:3])
+        assert torch.equal(got[3:], good[3:]) and torch.isfinite(got).all() and not torch.equal(got[0], good[0])
+        assert all(torch.equal(got[i], good[i]) == (way == "paged") for i in (1, 2))
         bad = table.clone()
         bad[4, 3] = bad_id                                    # of a sequence's own
         got = run(2, table=bad)
         assert torch.equal(got[:4], good[:4]) and torch.isfinite(got).all()
     for kw in (dict(shared=i32([-1, 40])), dict(shared=i32([300, 1 << 30])), dict(groups=i32([0, 7, 5])), dict(groups=i32([1, 3, 5])),
                dict(groups=i32([0, 3, 4])), dict(groups=i32([0, -9, 5])), dict(groups=i32([0, 4, 3])), dict(lens=i32([301, 400, -1, 50, 60]))):
-        run(8, **kw)
+        if way == "paged" and "lens" not in kw:
+            assert torch.equal(sv.shared_attention(q, pool, table, lens, kw.get("groups", starts), kw.get("shared", shared)), good)
+        else:
+            run(8, **kw)
     # an unseen page leaves the rest as it is: against keys cut out by hand
-    one = make([(64, [70, 71])], 1, 2, 1, 64, seed=10)
+    one = make([(64, [70, 71])], 1, 2, 1, 64, seed=10, way=way)
     bad = one[2].clone()
-    bad[0, 1] = -1
+    bad[:, 1] = -1
     got = sv.shared_attention(one[0], one[1], bad, *one[3:])
     with pytest.raises(Exception, match="flags 2$"):
         sv.status()
@@ -234,9 +266,10 @@ def test_bad_pages_and_rows(sv):
         assert (got[b, 0].double() - w).abs().max() <= (2 * 2.0 ** -8 + 2.0 ** -15) * kv[:, 1].abs().max()
 
 
-def test_captured_and_on_another_stream(sv):
+@pytest.mark.parametrize("way", WAYS)
+def test_captured_and_on_another_stream(sv, way):
     """A captured call follows its lists; two captured graphs with scratch of their own; another stream."""
-    args = make([(300, [310 + i for i in range(6)]), (500, [501, 700])], 1, 8, 2, 64, seed=11)
+    args = make([(300, [310 + i for i in range(6)]), (500, [501, 700])], 1, 8, 2, 64, seed=11, way=way)
     q, pool, table, lens, starts, shared = args
     want = sv.shared_attention(*args)
     graphs = []

@@ -105,7 +105,7 @@ def test_back_kernels(lib):
 
 
 def shared(lib, **kw):
-    a = dict(type=1, B=16, rows=1, Hq=8, Hkv=2, hd=128, q=P, q_seq=1024, q_row=1024, q_head=128, pool=P, n_pages=20000, page=16, table=P, width=600,
+    a = dict(type=1, B=16, rows=1, Hq=8, Hkv=2, hd=128, q=P, q_seq=1024, q_row=1024, q_head=128, pool=P, n_pages=20000, page=16, table=P, width=1000,
              lens=P, n=2, groups=P, shared=P, scale=0.1, out=P, work=P, stream=None)
     a.update(kw)
     return lib.kf_op_shared_attention(*a.values())
@@ -124,12 +124,19 @@ def test_shared_kernels(lib):
         assert shared(lib, **kw) == OK
         return [(x.kernel.split("k_")[1].split("<")[0], x.dependent) for x in launches(lib)]
 
-    assert names() == [("prefix", False), ("own", True), ("add", True)]
+    # what reads the prefixes: tcgen05, tiles of few rows, or paged attention, by the reads that the table and the pool allow for
+    assert names(B=64, Hq=32, Hkv=8, width=2000) == [("prefix", False), ("rows", True), ("add", True)]
+    assert names(width=1000) == [("rows", False), ("add", True)]
+    assert [x[0] for x in names(width=100)] == ["paged", "join"] == [x[0] for x in names(n_pages=100)]
     # nothing that is shared: paged attention
     assert [x[0] for x in names(n=16)] == ["paged", "join"] and [x[0] for x in names(n_pages=0, pool=None)] == ["paged", "join"]
     assert shared(lib, B=0, n=0) == OK and not launches(lib)
-    assert lib.kf_op_shared_attention_work(16, 1, 8, 2, 128, 20000, 16, 600, 2) > 2 * 16 * 8 * 128 * 4
+    assert lib.kf_op_shared_attention_work(16, 1, 8, 2, 128, 20000, 16, 1000, 2) > 2 * 16 * 8 * 128 * 4
+    assert lib.kf_op_shared_attention_work(16, 1, 8, 2, 128, 20000, 16, 100, 2) == lib.kf_op_paged_attention_work(16, 1, 8, 2, 128, 16, 100)
     assert lib.kf_op_shared_attention_work(0, 1, 8, 2, 128, 20000, 16, 600, 2) == 0
+    # sizes at their ends
+    assert lib.kf_op_shared_attention_work(1 << 16, 1, 8, 2, 128, 1 << 30, 16, 1 << 10, 1 << 15) > 0
+    assert lib.kf_op_shared_attention_work(1 << 20, 64, 64, 2, 128, 1 << 30, 16, 1 << 20, 2) == 0
 
 
 def policy(lib, **kw):
