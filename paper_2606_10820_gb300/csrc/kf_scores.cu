@@ -29,8 +29,14 @@
 // them is its place.  Where masks close too many groups, the threads' own maxima give the
 // bound; rows where the list would not fit all the same (ties in the hundreds) raise the bound.
 //
+// Policy loss: the gradient's two passes, with a row's loss and its two derivatives between them (every thread
+// computes them: a broadcast would cost a barrier).
+//
 // Measured: 4096 bf16 rows of 50257 in 96 us with eight alternatives (4.3 TB/s), 72 without (5.7); 8 fp32
-// rows 7.5; the gradient of 2048 bf16 rows 86 us (4.8 TB/s).
+// rows 7.5; the gradient of 2048 bf16 rows 86 us (4.8 TB/s); the policy loss of 4096 in 173 us (4.8 TB/s), of 61 fp32 rows in
+// 10 us.  The gradient's passes take 20 instructions an element, 62 % of the issue slots: two rows fill an SM's shared
+// memory, so two CTAs take turns at loads, barriers and arithmetic.  Measured and not kept: the
+// arithmetic on single numbers instead of pairs (fewer moves, more of the fma pipe: 194 us for 179).
 #include <algorithm>
 #include <cooperative_groups.h>
 
@@ -137,10 +143,16 @@ struct Sums {
   }
 };
 
+__device__ __forceinline__ float min3f(float x, float y, float z) {
+  float r;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+  return r;
+}
 // one thread's pass over its elements
 struct Pass {
   Ref r;
   float most = -INFINITY;          // the largest logit
+  float least = INFINITY;          // and the smallest
   uint64_t s = 0ull, t = 0ull;     // S and T, in two lanes each
   __device__ __forceinline__ Pass() : r{-INFINITY, 0.f, -INFINITY, false} {}
   __device__ __forceinline__ void raise(const Args& a, float to) {
@@ -157,15 +169,29 @@ struct Pass {
     s = add_f2(s, e);
     t = fma_f2(e, f2(fmaxf(d.x, kLeast), fmaxf(d.y, kLeast)), t);
   }
+  // (differences above kLeast)
+  __device__ __forceinline__ void pair_of_open(uint64_t d) {
+    const float2 x = f2_split(d);
+    const uint64_t e = f2(ex2(x.x), ex2(x.y));
+    s = add_f2(s, e);
+    t = fma_f2(e, d, t);
+  }
   template <int N>
   __device__ __forceinline__ void add(const Args& a, const float* v) {
-    float top = fmaxf(v[0], v[1]);
+    float top = fmaxf(v[0], v[1]), low = fminf(v[0], v[1]);
 #pragma unroll
-    for (int i = 2; i < N; i += 2) top = max3f(top, v[i], v[i + 1]);
+    for (int i = 2; i < N; i += 2) {
+      top = max3f(top, v[i], v[i + 1]);
+      low = min3f(low, v[i], v[i + 1]);
+    }
     most = fmaxf(most, top);
+    least = fminf(least, low);
     if (top > r.limit) raise(a, top);
     const uint64_t c = f2(a.c2, a.c2), nm = f2(r.nm, r.nm);
-    if (!r.big) {
+    if (!r.big && fmaf(low, a.c2, r.nm) > kLeast) {
+#pragma unroll
+      for (int i = 0; i < N; i += 2) pair_of_open(fma_f2(f2(v[i], v[i + 1]), c, nm));
+    } else if (!r.big) {
 #pragma unroll
       for (int i = 0; i < N; i += 2) pair(f2_split(fma_f2(f2(v[i], v[i + 1]), c, nm)));
     } else {
@@ -310,12 +336,18 @@ __device__ __forceinline__ float2 two_sum(float x, float y) {
 // and its derivatives by lp and H.  The exponents are small differences of numbers of size ten and more, so
 // lp is kept in two parts: in one it would carry 5e-7 of rounding into ratio, and ten times as
 // much of its own size into the KL term.
+// (its inputs: read before the pass over the row)
+struct PolicyIn {
+  float w, old, A, ref;
+  __device__ __forceinline__ PolicyIn(const Policy& p, int64_t r)
+      : w(p.weight ? __ldg(p.weight + r) : 1.f), old(__ldg(p.old_logp + r)), A(__ldg(p.advantage + r)), ref(p.ref_logp ? __ldg(p.ref_logp + r) : 0.f) {}
+};
 struct PolicyRow {
   float logp, ratio, kl, loss, gl, gh;
   bool left_out;                   // no part in the loss: padding, a weight of 0 (or a token outside the vocabulary)
-  __device__ __forceinline__ PolicyRow(const Args& a, const Scores& o, int64_t r, int64_t token, float at_logit) {
+  __device__ __forceinline__ PolicyRow(const Args& a, const Scores& o, const PolicyIn& in, int64_t token, float at_logit) {
     const Policy& p = a.pol;
-    const float w = p.weight ? p.weight[r] : 1.f;
+    const float w = in.w;
     const bool has = token >= 0 && token < a.V;
     left_out = !has || w == 0.f;
     logp = kl = gl = gh = loss = 0.f;
@@ -339,7 +371,9 @@ struct PolicyRow {
         x = make_float2(__fmul_rn(d, a.c2), 0.f);
         lo = fmaf(d, a.c2, -x.x);
       }
-      lo += x.y + fmaf(at_logit - o.ref.raw, p.c2_low, -log2f(f));
+      // (what c2 lost in rounding, of the token's difference and of S: d log2 S / d c = sum p (v - m))
+      const float mean = (o.logs - o.H * kLog2e) / a.c2;
+      lo += x.y + fmaf(at_logit - o.ref.raw - mean, p.c2_low, -log2f(f));
       x = two_sum(x.x, -e);
       x = two_sum(x.x, x.y + lo);
       if (!(fabsf(x.x) < INFINITY)) x = make_float2(o.lp(a, at_logit) * kLog2e, 0.f);
@@ -350,11 +384,11 @@ struct PolicyRow {
       else x = make_float2(h, 0.f);
     }
     logp = x.x + x.y;
-    const float A = p.advantage[r];
-    ratio = expf((x.x - p.old_logp[r]) + x.y);
+    const float A = in.A;
+    ratio = expf((x.x - in.old) + x.y);
     float em1 = 0.f;               // e^u - 1
     if (p.ref_logp) {
-      const float u = (p.ref_logp[r] - x.x) - x.y;
+      const float u = (in.ref - x.x) - x.y;
       if (fabsf(u) < 0.25f) {
         // u^2 / 2 + u^3 / 6 + ... to u^8
         kl = u * u * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, 1.f / 40320, 1.f / 5040), 1.f / 720), 1.f / 120), 1.f / 24), 1.f / 6), 0.5f);
@@ -677,8 +711,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
     const Row<T> next = row_at<T>(a, more ? r + step : r);
     const Extra<T> ex(a, row, r, rank == 0, POLICY);
     const int n = mine.have(row), n_next = mine.have(next);
+    std::conditional_t<POLICY, PolicyIn, int> input = [&] {
+      if constexpr (POLICY) return PolicyIn(a.pol, r);
+      else return 0;
+    }();
     Pass ps;
-#pragma unroll
+#pragma unroll 1
     for (int g = 0; g < kResident; ++g) {
       // this batch's copies are done, later ones may not be
       if (g == 0) mma::cp_wait<kResident - 1>();
@@ -692,6 +730,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
         for (int j = 0; j < kBatch; ++j) Vec16<T>::unpack(s[j * THREADS], v + j * N);
         ps.add<kBatch * N>(a, v);
       } else {
+#pragma unroll 1
         for (int j = 0; g * kBatch + j < n; ++j) {
           float v[N];
           Vec16<T>::unpack(s[j * THREADS], v);
@@ -704,7 +743,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
     float gl, gh;
     bool zeros = false;                   // (uniform) a row that the loss leaves out, whatever it holds
     if constexpr (POLICY) {
-      const PolicyRow p(a, o, r, ex.token, ex.at_logit);
+      const PolicyRow p(a, o, input, ex.token, ex.at_logit);
       gl = p.gl;
       gh = p.gh;
       zeros = p.left_out || o.none;
@@ -727,42 +766,52 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
     const float A = (-gl - gh * o.H) * a.inv_tau, B = -gh * a.inv_tau * kLn2;
     const float at_token = o.none ? 0.f : gl * a.inv_tau;
     T* out = static_cast<T*>(a.grad) + r * a.grad_stride;
-    const uint64_t c2 = f2(a.c2, a.c2), nm = f2(o.ref.nm, o.ref.nm), nlogs = f2(-o.logs, -o.logs), A2 = f2(A, A), B2 = f2(B, B);
-    auto pair = [&](float& x, float& y) {
-      float2 d;
-      if (!o.ref.big) d = f2_split(add_f2(fma_f2(f2(x, y), c2, nm), nlogs));      // (one constant for both would lose log S)
-      else d = f2_split(add_f2(mul_f2(add_f2(f2(x, y), nm), c2), nlogs));
-      d.x = fmaxf(d.x, kLeast);
-      d.y = fmaxf(d.y, kLeast);
-      const float2 g = f2_split(mul_f2(f2(ex2(d.x), ex2(d.y)), fma_f2(B2, f2(d.x, d.y), A2)));
-      x = g.x;
-      y = g.y;
+    // log2 p of a logit (one constant for both would lose log S); `value`: its gradient but for the token's part
+    auto log_p = [&](float v) {
+      return __fadd_rn(o.ref.big ? __fmul_rn(__fadd_rn(v, o.ref.nm), a.c2) : fmaf(v, a.c2, o.ref.nm), -o.logs);
     };
+    auto value = [&](float d) { return __fmul_rn(ex2(d), fmaf(B, d, A)); };
+    // The policy loss takes one constant all the same, and what that loses, the same of all of the row's elements, into A and B:
+    // p (A + B log2 p) = 2^d f (A + B lo + B d), d = log2 p - lo, f = 2^lo
+    const float2 nml = two_sum(o.ref.nm, -o.logs);
+    const float f = ex2(nml.y), B1 = B * f, A1 = fmaf(B, nml.y, A) * f;
+    // (no clamp where none of this thread's elements needs it)
+    const uint64_t c2 = f2(a.c2, a.c2), nm = f2(o.ref.nm, o.ref.nm), nlogs = f2(-o.logs, -o.logs), A2 = f2(A, A), B2 = f2(B, B);
+    const uint64_t nml2 = f2(nml.x, nml.x), A12 = f2(A1, A1), B12 = f2(B1, B1);
+    const bool plain = !o.none && !o.ref.big && fmaf(ps.least, a.c2, nml.x) > kLeast + 1.f;
+    const int token = ex.token >= 0 && ex.token < a.V ? (int)ex.token : -1;
     const bool same = (reinterpret_cast<uintptr_t>(out) & 15) == (reinterpret_cast<uintptr_t>(row.p) & 15);
     if (ex.edge) {
-      float x = ex.edge_logit, y = -INFINITY;
-      pair(x, y);
+      float x = value(fmaxf(log_p(ex.edge_logit), kLeast));
       if (POLICY && zeros) x = 0.f;
-      out[ex.edge_id] = from_f<T>(ex.edge_id == ex.token ? x + at_token : x);
+      out[ex.edge_id] = from_f<T>(ex.edge_id == token ? x + at_token : x);
     }
-#pragma unroll
+#pragma unroll 1
     for (int g = 0; g < kResident; ++g) {
 #pragma unroll
-      for (int j = g * kBatch; j < (g + 1) * kBatch; ++j) {
+      for (int jj = 0; jj < kBatch; ++jj) {
+        const int j = g * kBatch + jj;
         if (j >= n) break;
         float v[N];
         Vec16<T>::unpack(slots[j * THREADS + t], v);
         const int id0 = row.head + (mine.first + j * THREADS) * N;
+        if (plain && !(POLICY && zeros)) {
 #pragma unroll
-        for (int e = 0; e < N; e += 2) pair(v[e], v[e + 1]);
-        if (POLICY && zeros) {
+          for (int e = 0; e < N; e += 2) {
+            const uint64_t x = f2(v[e], v[e + 1]), d = POLICY ? fma_f2(x, c2, nml2) : add_f2(fma_f2(x, c2, nm), nlogs);
+            const float2 ds = f2_split(d);
+            const float2 y = f2_split(mul_f2(f2(ex2(ds.x), ex2(ds.y)), POLICY ? fma_f2(B12, d, A12) : fma_f2(B2, d, A2)));
+            v[e] = y.x;
+            v[e + 1] = y.y;
+          }
+        } else {
 #pragma unroll
-          for (int e = 0; e < N; ++e) v[e] = 0.f;
+          for (int e = 0; e < N; ++e) v[e] = POLICY && zeros ? 0.f : value(fmaxf(log_p(v[e]), kLeast));
         }
-        if (ex.token >= id0 && ex.token < id0 + N) {
+        if ((unsigned)(token - id0) < (unsigned)N) {
 #pragma unroll
           for (int e = 0; e < N; ++e)
-            if (id0 + e == ex.token) v[e] += at_token;
+            if (id0 + e == token) v[e] += at_token;
         }
         if (same) {
           *reinterpret_cast<uint4*>(out + id0) = Vec16<T>::pack(v);

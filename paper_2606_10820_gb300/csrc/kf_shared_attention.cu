@@ -1,14 +1,19 @@
-// The keys that groups of sequences share (kf_op_shared_attention): head_dim 64 or 128, bf16 or fp16,
-// on tcgen05 (kf_attn_pair.cuh).
+// Attention of groups of sequences that begin with the same tokens (kf_op_shared_attention): head_dim 64
+// or 128, bf16 or fp16; the prefixes on tcgen05 (kf_attn_pair.cuh), the sum of all parts, and what reads which call's prefixes.
 //
 // The query rows that read a group's prefix under one KV head are its sequences' rows x group heads: a
 // segment is up to 256 of them, two sub-tiles of 128, over all key tiles of 128 of the prefix.  So
 // a prefix comes from memory once for all of a group's sequences.  The segments' tiles form one list which the
 // CTAs (one a SM) share evenly, kExtra tiles more a segment for its start and end; what a part leaves
-// unfinished the join adds (kf_shared.cuh).  K and V come by TMA, in boxes of the 16 keys that a page is a multiple of;
-// a page outside of the pool is a box outside of the map, which is zeros and closed by the softmax.  Each
-// row sees keys up to its own position.
-// What bounds it: the prefixes' bytes; from about 200 rows a group on the tensor cores and exponentials beside them.
+// unfinished the last kernel adds (kf_shared.cuh).  K and V come by TMA, in boxes of the 16 keys that a page is a multiple of
+// (boxes of 128 rows were no faster); a page outside of the pool is a box outside of the map, which is zeros and closed by the
+// softmax.  Each row sees keys up to its own position.
+// What bounds it: long prefixes their bytes, beside 2,900 clocks of tensor cores and exponentials a tile of 256 rows (64 KB at
+// head_dim 128, for which memory takes 2,800); short ones the first run through the code and the chain of a tile (a single
+// sub-tile 4,300 clocks): the first product starts 5 us after the launch.
+// Measured (GPU time, floor of the bytes): 64 answers about 32,771 tokens, 32 heads over 8 of 128, in 75 us (40); 8 groups of 16
+// after 1,003 to 4,099 tokens 71 us (40); joint steps of eight rows, 16 groups of 16 after 128 to 896, 12 heads over 4 of
+// 64, 36 us (5); 8 candidates of one prompt of 517, by paged attention, 7.4 us.
 #include <algorithm>
 
 #include "kf_attn_pair.cuh"
@@ -20,7 +25,7 @@ using namespace pair;
 
 constexpr int kGran = 16, kGrans = kKeys / kGran;    // keys of a box; boxes of a tile
 constexpr int kPrefixRows = 256;                     // query rows of a segment
-constexpr int kExtra = 2;                            // a segment's start and end, in tiles
+constexpr int kExtra = 3;                            // a segment's start and end, in tiles
 constexpr int kMinTiles = 2;                         // places of a CTA, at least
 
 struct Item {
@@ -538,12 +543,13 @@ extern "C" int kf_op_shared_attention(int32_t type, int32_t B, int32_t rows, int
   if (B == 0) return KF_OK;
   if (!groups || !shared || !aligned(groups, 4) || !aligned(shared, 4)) return refuse(what, "groups or shared: null or misaligned");
   const Way way = way_of(B, rows, Hq / Hkv, Hkv, hd, n_pages, page, width, n);
-  if (way == PAGED)
-    return kf_op_paged_attention(type, B, rows, Hq, Hkv, hd, q, q_seq, q_row, q_head, pool, n_pages, page, table, width, lens, scale, out, work, stream);
-  if (!q || !out || !lens || !work || !pool || (width && !table)) return refuse(what, "a null array");
+  const bool no_work = !work && kf_op_shared_attention_work(B, rows, Hq, Hkv, hd, n_pages, page, width, n) > 0;
+  if (!q || !out || !lens || no_work || (n_pages && !pool) || (width && !table)) return refuse(what, "a null array");
   if (!aligned(q, 16) || !aligned(pool, 16) || !aligned(out, 16) || !aligned(work, 256) || !aligned(table, 4) || !aligned(lens, 4))
     return refuse(what, "q, pool and out are 16-byte aligned, work 256-byte");
   if (q_seq % 8 || q_row % 8 || q_head % 8) return refuse(what, "q's strides are multiples of 8 elements");
+  if (way == PAGED)
+    return kf_op_paged_attention(type, B, rows, Hq, Hkv, hd, q, q_seq, q_row, q_head, pool, n_pages, page, table, width, lens, scale, out, work, stream);
   SharedCall c{q, q_seq, q_row, q_head, pool, table, lens, out, n_pages, Sharing{groups, shared, n}, {}, {}, serving_error_word(),
                B, rows, Hq, Hkv, Hq / Hkv, hd, page, width, scale * 1.4426950408889634f, Div(page), Div(Hq / Hkv), Div(rows * (Hq / Hkv)), Div(Hq), Div(rows)};
   if (!c.err) return refuse(what, "no error word", KF_E_CUDA);

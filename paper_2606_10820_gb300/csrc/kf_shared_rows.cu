@@ -20,7 +20,7 @@ namespace {
 constexpr int NW = 4, kThreads = 32 * NW;        // warps of a CTA
 constexpr int kUnitBytes = 8192;                 // K and V of a unit
 constexpr int kStages = 3;                       // units of a warp's ring
-constexpr int kExtra = 3;                        // a segment's start and end, in units
+constexpr int kExtra = 2;                        // a segment's start and end, in units
 constexpr int kMinPlaces = 4;                    // places of a part, at least
 constexpr int kWhole = 6;                        // units of a segment that is not cut
 constexpr int kCtasPerSm = 2;

@@ -39,7 +39,7 @@ def rotate(lib, **kw):
                                  dict(n=-8), dict(n=12), dict(n=40), dict(eps=float("nan")), dict(eps=float("inf")), dict(eps=-1.0), dict(wq=P + 2),
                                  dict(freq=None), dict(freq=P + 4), dict(pos=None), dict(pos=P + 2), dict(q=None), dict(q=P + 8), dict(k=None),
                                  dict(q_row=510), dict(k_head=-64), dict(oq=None), dict(ok=3 * P + 4), dict(oq_row=1 << 38), dict(oq=P),
-                                 dict(ok=P, ok_row=128)])
+                                 dict(ok=P, ok_row=128), dict(oq_row=0), dict(oq_head=32), dict(ok_head=0), dict(ok_row=8)])
 def test_rotate_refusals(lib, bad):
     assert refused(lib, "kf_op_rotate_heads", rotate(lib, **bad))
 
@@ -53,7 +53,7 @@ def test_rotate_kernels(lib):
 
     assert "k_rotate" in one().kernel and one(T=1 << 16).grid[0] == one(T=1 << 16, eps=-1.0, wq=None, wk=None).grid[0]
     # few tokens: the passes over the heads are split over warps; the heads of a pass stay together
-    assert one(T=1, Hq=32, Hkv=8, hd=128, q_row=8192, k_row=8192).grid[0] * 4 >= 10
+    assert one(T=1, Hq=32, Hkv=8, hd=128, q_row=8192, k_row=8192, oq_head=128, ok_head=128).grid[0] * 4 >= 10
     assert rotate(lib, T=0, q=None, k=None, oq=None, ok=None, pos=None) == OK and not launches(lib)
     assert rotate(lib, n=0, freq=None) == OK
     # over the input itself
@@ -115,8 +115,9 @@ def shared(lib, **kw):
                                  dict(n_pages=-1), dict(n_pages=1 << 31), dict(scale=-1.0), dict(scale=float("nan")), dict(q=None), dict(lens=None),
                                  dict(table=None), dict(pool=None), dict(out=P + 4), dict(q_head=100), dict(work=None), dict(work=P + 64), dict(n=-1),
                                  dict(n=0), dict(groups=None), dict(shared=None), dict(groups=P + 2)])
-def test_shared_refusals(lib, bad):
-    assert refused(lib, "kf_op_shared_attention", shared(lib, **bad))
+@pytest.mark.parametrize("width", [100, 1000])
+def test_shared_refusals(lib, bad, width):
+    assert refused(lib, "kf_op_shared_attention", shared(lib, **{"width": width, **bad}))
 
 
 def test_shared_kernels(lib):
