@@ -18,8 +18,9 @@
 // cost registers; a token's angles are computed once by the warp's lanes and passed on through shared memory.
 // Measured (GPU time, bf16): 16,411 tokens, 32 + 8 heads of 128, norms, in 58 us (5.9 TB/s; with the loads in registers, four
 // passes ahead, 73); 24,361 tokens and V to pages, fp16, in 109 us (5.5 TB/s); eight rows of 256 sequences, 12 + 4 heads of 64, in 5.6 us
-// (the chain of starts, slot, length and page: 7.5 a token at a time); the gradients of 16,384 tokens in 90 us (5.6 TB/s; 127 with the loads
-// in registers); 8 tokens in 2.2 us.
+// (the chain of starts, slot, length and page: 7.5 a token at a time); the gradients of 16,384 tokens in 85 us (5.9 TB/s; 127 with the loads
+// in registers, 92 with the weights read a pass); 8 tokens in 2.2 us.  Not kept: the weights multiplied into the turns (57 -> 61), tokens dealt out
+// in turn instead of in stretches (57 -> 59, the gradients 85 -> 95).
 #include <algorithm>
 #include <climits>
 
@@ -123,24 +124,28 @@ struct Place {
   }
 };
 
-// A token's angles: computed by the warp, 8 pairs handed to each lane
+// A token's angles to the warp's table: cosine and sine of each pair, (1, 0) past the last
+template <int HD>
+__device__ __forceinline__ void fill_table(const Args& a, float2* tab, int pos, int lane) {
+  __syncwarp();                  // (the token before is through with it)
+#pragma unroll
+  for (int i = lane; i < HD / 2; i += 32) {
+    float2 v = make_float2(1.f, 0.f);
+    if (i < a.n) {
+      bool bad;
+      const uint64_t t = turns_of(__ldg(a.freq + i), &bad);
+      v = turn(pos, t, bad);
+      v.y *= a.sign;
+    }
+    tab[i] = v;
+  }
+  __syncwarp();
+}
+// The 8 pairs of a lane
 template <int HD, bool NB>
 struct Angles {
   float c[8], s[8];
-  __device__ __forceinline__ void take(const Args& a, float2* tab, const Place<HD, NB>& pl, int pos, int lane) {
-    __syncwarp();                // (the token before is through with them)
-#pragma unroll
-    for (int i = lane; i < HD / 2; i += 32) {
-      float2 v = make_float2(1.f, 0.f);
-      if (i < a.n) {
-        bool bad;
-        const uint64_t t = turns_of(__ldg(a.freq + i), &bad);
-        v = turn(pos, t, bad);
-        v.y *= a.sign;
-      }
-      tab[i] = v;
-    }
-    __syncwarp();
+  __device__ __forceinline__ void take(const float2* tab, const Place<HD, NB>& pl) {
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
       const int i = NB ? pl.a0 + (e < 4 ? e : HD / 4 + e - 4) : pl.a0 + e;
@@ -153,11 +158,12 @@ struct Angles {
     }
   }
   // x: the lane's 16 elements of a head
+  static constexpr __device__ __forceinline__ int first(int e) { return NB ? 2 * e : e; }
+  static constexpr __device__ __forceinline__ int second(int e) { return NB ? 2 * e + 1 : e + 8; }
   __device__ __forceinline__ void turn_head(float* x) const {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      float& a = x[NB ? 2 * e : e];
-      float& b = x[NB ? 2 * e + 1 : e + 8];
+      float &a = x[first(e)], &b = x[second(e)];
       const float y = fmaf(a, c[e], -b * s[e]);
       b = fmaf(b, c[e], a * s[e]);
       a = y;
@@ -293,7 +299,8 @@ __global__ void __launch_bounds__(kThreads, 6) k_rotate(const __grid_constant__ 
       } else {
         pos = __ldg(a.pos + t);
       }
-      an.take(a, tab[warp], pl, pos, lane);
+      fill_table<HD>(a, tab[warp], pos, lane);
+      an.take(tab[warp], pl);
     }
     mma::cp_wait<kAhead - 2>();
     fill();                      // into the slot of the pass before
@@ -376,8 +383,9 @@ __global__ void __launch_bounds__(kThreads, 3) k_back(const __grid_constant__ Ar
 #pragma unroll
   for (int i = 0; i < kBackAhead - 1; ++i) fill();
   Angles<HD, NB> an;
+  float g[16];                   // the weights, of the query or the key heads (`held`)
   int64_t token = -1;
-  int slot = 0;
+  int slot = 0, held = -1;
 #pragma unroll 1
   for (; now.left > 0; now.next(a)) {
     const int64_t t = now.t;
@@ -386,53 +394,47 @@ __global__ void __launch_bounds__(kThreads, 3) k_back(const __grid_constant__ Ar
     const bool has = j < (k ? a.Hkv : a.Hq);
     if (t != token) {            // (uniform)
       token = t;
-      an.take(a, tab[warp], pl, __ldg(a.pos + t), lane);
+      fill_table<HD>(a, tab[warp], __ldg(a.pos + t), lane);
+      an.take(tab[warp], pl);
+    }
+    if (held != (int)k) {        // (uniform)
+      held = k;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) g[e] = 1.f;
+      if (const uint4* w = static_cast<const uint4*>(k ? a.wk : a.wq)) {
+        const uint4 gw[2] = {__ldg(w + pl.c0), __ldg(w + pl.c1)};
+        unpack16<T>(gw, g);
+      }
     }
     mma::cp_wait<kBackAhead - 2>();
     fill();                      // into the slot of the pass before
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    const uint4 ux[2] = {has ? slots[warp][slot][0][lane] : zero, has ? slots[warp][slot][1][lane] : zero};
-    const uint4 ud[2] = {has ? slots[warp][slot][2][lane] : zero, has ? slots[warp][slot][3][lane] : zero};
+    const uint4 ux[2] = {slots[warp][slot][0][lane], slots[warp][slot][1][lane]}, ud[2] = {slots[warp][slot][2][lane], slots[warp][slot][3][lane]};
     slot = slot + 1 == kBackAhead ? 0 : slot + 1;
     float x[16], d[16];
     unpack16<T>(ux, x);
     unpack16<T>(ud, d);
     an.turn_head(d);
-    // one half of the weights' products at a time (registers): gw = d w
-    const uint4* w = static_cast<const uint4*>(k ? a.wk : a.wq);
     float ss = 0.f, sg = 0.f;
-    uint4 gw[2] = {zero, zero};
-    if (w) {
-      gw[0] = __ldg(w + pl.c0);
-      gw[1] = __ldg(w + pl.c1);
-    }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float g[8];
-      Vec16<T>::unpack(gw[h], g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        ss = fmaf(x[8 * h + e], x[8 * h + e], ss);
-        sg = fmaf(w ? d[8 * h + e] * g[e] : d[8 * h + e], x[8 * h + e], sg);
-      }
+    for (int e = 0; e < 16; ++e) {
+      ss = fmaf(x[e], x[e], ss);
+      sg = fmaf(d[e] * g[e], x[e], sg);
     }
     const float r = rsqrtf(fmaf(sum_head<LANES>(ss), 1.f / HD, a.eps));
     const float m = sum_head<LANES>(sg) * (1.f / HD) * r * r;
+    if (!has) continue;          // (lanes of heads that are not there hold anything)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] *= r;
     if (a.part && !k) {          // (uniform)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[0][e] = fmaf(d[e] * r, x[e], acc[0][e]);
+      for (int e = 0; e < 16; ++e) acc[0][e] = fmaf(d[e], x[e], acc[0][e]);
     } else if (a.part) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[1][e] = fmaf(d[e] * r, x[e], acc[1][e]);
+      for (int e = 0; e < 16; ++e) acc[1][e] = fmaf(d[e], x[e], acc[1][e]);
     }
-    if (!has) continue;
+    // r g w - xh r mean(g w xh)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float g[8];
-      Vec16<T>::unpack(gw[h], g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) d[8 * h + e] = r * fmaf(-m, x[8 * h + e], w ? d[8 * h + e] * g[e] : d[8 * h + e]);
-    }
+    for (int e = 0; e < 16; ++e) d[e] = fmaf(r * g[e], d[e], -m * x[e]);
     const Out& O = k ? a.ok : a.oq;
     T* to = static_cast<T*>(O.p) + t * O.row + j * O.head;
     *reinterpret_cast<uint4*>(to + 8 * pl.c0) = Vec16<T>::pack(d);
