@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
       const int r = sub * kRows + row;
       const Row w(a, im, r);
       const bool mine = r < im.rows;
-      int see = 0;
+      int see = 0x7fffffff;                     // (a row that is not there, of zeros, asks for no mask)
       if (mine) see = min(im.len, min(max(__ldg(a.lens + im.b0 + w.seq), 0), a.width * a.page) - a.rows + w.tok + 1);
       const int32_t* ids = a.table + (int64_t)im.b0 * a.width;
       auto look = [&](int tile) -> int {        // the tile's page of box `lane`
