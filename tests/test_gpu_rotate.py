@@ -339,3 +339,36 @@ def test_refusals(sv):
             sv.rotate_append(**{**fine, **bad})
     with pytest.raises(KfError):
         sv.rotate_append(**{**fine, "slots": i32([]), "starts": i32([0])})
+
+
+def test_append_past_32_bits_and_captured(sv):
+    """Pages past 2^31 elements of a pool; a captured call follows the book that its replay finds."""
+    pool = torch.full((70000, 2, 8, 16, 128), 7.0, device="cuda", dtype=torch.bfloat16)       # 4.6 GB
+    q, k, v, _, freq, how = make(5, 32, 8, 128, 128, torch.bfloat16, seed=4)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    starts, slots, lens = i32([0, 3, 5]), i32([1, 0]), i32([18, 3])
+    table = i32([[69999, 68000], [1, 69000]])
+
+    def expect(lens):
+        n0, n1 = lens.tolist()
+        pos = i32([n1 - 3, n1 - 2, n1 - 1, n0 - 2, n0 - 1])
+        wq, wk = sv.rotate_heads(q, k, pos, freq, **how)
+        at = [(table[s, p // 16].item(), p % 16) for s, p in zip([1, 1, 1, 0, 0], pos.tolist())]
+        return wq, wk, at
+
+    def held(wk, at):
+        return all(torch.equal(pool[p, 0, :, r], wk[i]) and torch.equal(pool[p, 1, :, r], v[i]) for i, (p, r) in enumerate(at))
+
+    got = sv.rotate_append(q, k, v, pool, starts, table, lens, slots, freq, **how)
+    sv.status()
+    wq, wk, at = expect(lens)
+    assert torch.equal(got, wq) and held(wk, at)
+    assert (pool[[1, 68000, 69000, 69999]] != 7).any(-1).any(2).sum() == 2 * 5 and (pool[:1] == 7).all()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = sv.rotate_append(q, k, v, pool, starts, table, lens, slots, freq, **how)
+    lens.copy_(i32([31, 22]))
+    graph.replay()
+    sv.status()
+    wq, wk, at = expect(lens)
+    assert torch.equal(y, wq) and held(wk, at)

@@ -309,3 +309,19 @@ def test_refusals(sv):
         sv.shared_attention(**{**fine, "q": q.clone().requires_grad_()})
     none = sv.shared_attention(q[:0], pool, table[:0], lens[:0], starts[:1], shared[:0])
     assert none.shape == (0, 1, 4, 64)
+
+
+@pytest.mark.parametrize("way", WAYS)
+def test_a_pool_past_32_bits(sv, way):
+    """Pages whose elements lie past 2^31 (and bytes past 2^32) in the pool."""
+    args = list(make([(70, [71, 90, 75]), (33, [40])], 1, 32, 8, 128, seed=12, way=way))
+    small, table = args[1], args[2]
+    big = torch.empty(max(70000, len(small) + 66000), 2, 8, 16, 128, dtype=torch.bfloat16, device="cuda")       # 4.6 GB
+    big[-len(small):] = small
+    if way == "paged":
+        table = table[:, :8].contiguous()
+    args[1], args[2] = big, torch.where(table >= 0, table + (len(big) - len(small)), table)
+    got = sv.shared_attention(*args)
+    sv.status()
+    want, top = plain(*args)
+    assert ((got.double() - want).abs().amax((1, 2, 3)) <= (2 * 2.0 ** -8 + 2.0 ** -15) * top).all()
