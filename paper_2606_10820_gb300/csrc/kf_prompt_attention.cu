@@ -45,6 +45,12 @@ struct Plan {
   PlanItem* item;
 };
 
+// one sub-tile pair, as the load warp hands it to the others
+struct Item {
+  int start, len;
+  int row[2], head[2], n[2];                        // first row, head, key tiles (0: no sub-tile)
+};
+
 struct Args {
   void* out;
   int64_t out_row, out_head;
@@ -128,6 +134,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(int n, int T, int longest
   }
 }
 
+// ------------------------------------------------------------------ the products
 // Cluster launch control: a running CTA cancels one that has not started and does its work (the
 // hardware's queue instead of a counter in memory that a call would have to clear)
 __device__ __forceinline__ void ask_for_cta(uint64_t* answer, uint64_t* bar) {
@@ -151,12 +158,6 @@ __device__ __forceinline__ int cta_taken(const uint64_t* answer) {
       : "l"(lo), "l"(hi));
   return x;
 }
-
-// one sub-tile pair, as the load warp hands it to the others
-struct Item {
-  int start, len;
-  int row[2], head[2], n[2];                        // first row, head, key tiles (0: no sub-tile)
-};
 
 struct Bars : PairBars<Item> {
   uint64_t taken;                                        // a request to take over a CTA is answered
