@@ -13,13 +13,13 @@
 //
 // What bounds it: the heads, read and written once.  A warp's pass takes 4 or 8 heads of a token: hd / 16 lanes a head, two
 // 16-byte vectors a lane, so that both elements of a pair are in one lane.  The passes of all tokens form one list that
-// the warps share evenly.  Each lane streams its vectors through slots of shared memory that are its own (cp.async, kAhead
+// the warps share evenly.  Each lane streams its vectors through slots of shared memory that are its own (cp.async, a few
 // passes ahead, across tokens; no thread waits for another's), so the loads under way do not
 // cost registers; a token's angles are computed once by the warp's lanes and passed on through shared memory.
-// Measured (GPU time, bf16): 16,411 tokens, 32 + 8 heads of 128, norms, in 58 us (5.9 TB/s; with the loads in registers, four
-// passes ahead, 73); 24,361 tokens and V to pages, fp16, in 109 us (5.5 TB/s); eight rows of 256 sequences, 12 + 4 heads of 64, in 5.6 us
-// (the chain of starts, slot, length and page: 7.5 a token at a time); the gradients of 16,384 tokens in 85 us (5.9 TB/s; 127 with the loads
-// in registers, 92 with the weights read a pass); 8 tokens in 2.2 us.  Not kept: the weights multiplied into the turns (57 -> 61), tokens dealt out
+// Measured (GPU time, bf16): 16,411 tokens, 32 + 8 heads of 128, norms, in 58 us (5.8 TB/s; with the loads in registers, four
+// passes ahead, 73); 24,361 tokens and V to pages, fp16, in 104 us (5.8 TB/s); eight rows of 256 sequences, 12 + 4 heads of 64, in 5.9 us
+// (the chain of starts, slot, length and page: 7.5 a token at a time); the gradients of 16,384 tokens in 86 us (5.8 TB/s; 127 with the loads
+// in registers, 92 with the weights read a pass); 8 tokens in 2.1 us.  Not kept: the weights multiplied into the turns (57 -> 61), tokens dealt out
 // in turn instead of in stretches (57 -> 59, the gradients 85 -> 95).
 #include <algorithm>
 #include <climits>
@@ -31,7 +31,9 @@ namespace kf {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;      // of a CTA
-constexpr int kAhead = 5;                   // slots of a warp: one in use, the others' loads under way
+// Slots of a warp: one in use, the others' loads under way (to pages, whose rows are written in no order, eight: 111 -> 104 us at
+// the prompts above; rotation alone 57 with five, 60 with eight)
+template <bool APPEND> constexpr int kAhead = APPEND ? 8 : 5;
 constexpr int kBackAhead = 4;
 constexpr int kJoinThreads = 256;
 
@@ -252,7 +254,8 @@ struct Range {
 template <typename T, int HD, bool NB, bool APPEND>
 __global__ void __launch_bounds__(kThreads, 6) k_rotate(const __grid_constant__ Args a) {
   __shared__ __align__(16) float2 tab[kWarps][HD / 2];
-  __shared__ uint4 slots[kWarps][kAhead][2][32];
+  constexpr int AHEAD = kAhead<APPEND>;
+  __shared__ uint4 slots[kWarps][AHEAD][2][32];
   constexpr int LANES = HD / 16, PER = 32 / LANES;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane / LANES;
   Range now(a, blockIdx.x * kWarps + warp), ahead = now;
@@ -272,10 +275,10 @@ __global__ void __launch_bounds__(kThreads, 6) k_rotate(const __grid_constant__ 
     }
     mma::cp_commit();
     if (ahead.left > 0) ahead.next(a);
-    fslot = fslot + 1 == kAhead ? 0 : fslot + 1;
+    fslot = fslot + 1 == AHEAD ? 0 : fslot + 1;
   };
-#pragma unroll
-  for (int i = 0; i < kAhead - 1; ++i) fill();
+#pragma unroll 1
+  for (int i = 0; i < AHEAD - 1; ++i) fill();
   Angles<HD, NB> an;
   Places places;
   places.base = -32;
@@ -302,10 +305,10 @@ __global__ void __launch_bounds__(kThreads, 6) k_rotate(const __grid_constant__ 
       fill_table<HD>(a, tab[warp], pos, lane);
       an.take(tab[warp], pl);
     }
-    mma::cp_wait<kAhead - 2>();
+    mma::cp_wait<AHEAD - 2>();
     fill();                      // into the slot of the pass before
     uint4 o[2] = {slots[warp][slot][0][lane], slots[warp][slot][1][lane]};
-    slot = slot + 1 == kAhead ? 0 : slot + 1;
+    slot = slot + 1 == AHEAD ? 0 : slot + 1;
     float x[16];
     unpack16<T>(o, x);
     if (a.eps >= 0.f) {
@@ -380,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_back(const __grid_constant__ Ar
     if (ahead.left > 0) ahead.next(a);
     fslot = fslot + 1 == kBackAhead ? 0 : fslot + 1;
   };
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < kBackAhead - 1; ++i) fill();
   Angles<HD, NB> an;
   float g[16];                   // the weights, of the query or the key heads (`held`)
