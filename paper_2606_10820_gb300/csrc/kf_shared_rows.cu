@@ -9,6 +9,8 @@
 // 3 us a segment of three units: 256 sequences of 8 rows and 72 own keys in 16 us of which 2 were copies.)  Segments of up to
 // kWhole units are not cut.
 // What bounds it: the bytes of long stretches; short ones the chain of a segment (Q, pages, K and V, products).
+// Measured: the own keys (1 to 700) of 128 sequences, 32 heads over 8 of 128, 184 MB, in 32 us, 6 of them to the first data; those (1 to
+// 1,024) of 64 sequences, 135 MB, in 20 us from there (6.7 TB/s).
 #include <algorithm>
 
 #include "kf_mma16.cuh"
