@@ -27,6 +27,9 @@ using namespace pair;
 constexpr int kGran = 16, kGrans = kKeys / kGran;    // keys of a box; boxes of a tile
 constexpr int kPrefixRows = 256;                     // query rows of a segment
 constexpr int kExtra = 3;                            // a segment's start and end, in tiles
+constexpr float kAhead = 1.3f;                       // see Walk::ctas
+constexpr float kTileUnits = 9.f;                    // units of own keys (8 KB of K and V) that take as long as a tile of a prefix
+constexpr int kMostCounted = 1024;                   // sequences whose lengths are added up
 constexpr int kMinTiles = 2;                         // places of a CTA, at least
 
 struct Item {
@@ -70,12 +73,29 @@ struct Walk {
   Parts parts;
   int x, x1, base, g;            // the next place, the part's end; the group that it lies in, whose places begin at base
   int at, pieces;                // of the piece: its segment's record, and the CTAs that have pieces of it
+  // The CTAs that take parts; those of the kernel after this one, for each sequence's own keys, start on the SMs of the others.  They have
+  // kAhead of this kernel's share of all work, so that it ends before theirs does
+  static __device__ __forceinline__ int ctas(const SharedCall& a, int lane, int total) {
+    if (a.B > kMostCounted) return gridDim.x;
+    float keys = 0.f;                           // of the sequences after their prefixes
+#pragma unroll 4
+    for (int b = lane; b < a.B; b += 32) keys += (float)min(max(__ldg(a.lens + b), 0), a.width * a.page);
+    for (int i = lane; i < a.sh.n; i += 32) {
+      const Group gr(a, i);
+      keys -= (float)gr.len * a.by_seq.of(gr.rows);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) keys += __shfl_xor_sync(~0u, keys, o);
+    const float tiles = (float)((a.rows * a.G + a.own.seg_rows - 1) / a.own.seg_rows * a.Hkv);
+    const float own = tiles * (fmaxf(keys, 0.f) * (a.hd / 2048.f) + 3.f * a.B) / kTileUnits;      // in tiles of a prefix
+    return min((int)gridDim.x, max((int)gridDim.x / 3, (int)(gridDim.x * (kAhead * total / (total + own)) + 1.f)));
+  }
   __device__ __forceinline__ void start(const SharedCall& a, int lane) {
     base = g = 0;
     const int mine = lane < a.sh.n ? Group(a, lane).places(a) : 0;
     int total = __reduce_add_sync(~0u, mine);
     for (int i = 32; i < a.sh.n; i += 32) total += __reduce_add_sync(~0u, i + lane < a.sh.n ? Group(a, i + lane).places(a) : 0);
-    parts = Parts(total, min((int)gridDim.x, max(1, total / kMinTiles)));
+    parts = Parts(total, min(ctas(a, lane, total), max(1, total / kMinTiles)));
     x = parts.begin(blockIdx.x);
     x1 = parts.begin(blockIdx.x + 1);
     for (int i = 0; x < x1 && i < a.sh.n; i += 32) {
@@ -187,6 +207,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_prefix(const __grid_constant__ 
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = b.tmem;
+  if (blockIdx.x > 0 && b.item[0].n[0] == 0) {      // (uniform) no part: the SM is the next kernel's
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    return;
+  }
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));

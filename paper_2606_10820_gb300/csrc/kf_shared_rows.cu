@@ -374,8 +374,9 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_rows(const __grid_cons
     } while (pc.next(a));
     mma::cp_wait<0>();
   }
-  // (the prefixes' kernel before this one: what comes after is to see both)
-  if (!PREFIX) asm volatile("griddepcontrol.wait;" ::: "memory");
+  // What comes after waits for this kernel alone and is to see the prefixes' kernel before it too: this one does not end before
+  // that.  (One CTA waits; the others leave their SM to those that have not started)
+  if (!PREFIX && blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
