@@ -11,8 +11,8 @@
 // What bounds it: long prefixes their bytes, beside 2,900 clocks of tensor cores and exponentials a tile of 256 rows (64 KB at
 // head_dim 128, for which memory takes 2,800); short ones the first run through the code and the items' starts and ends: the first
 // product starts 5 us after the launch, and an item more in a CTA costs what three tiles do.
-// Measured (GPU time, floor of the bytes): 64 answers about 32,771 tokens, 32 heads over 8 of 128, in 75 us (40); 8 groups of 16
-// after 1,003 to 4,099 tokens 66 us (40); joint steps of eight rows, 16 groups of 16 after 128 to 896, 12 heads over 4 of
+// Measured (GPU time, floor of the bytes): 64 answers about 32,771 tokens, 32 heads over 8 of 128, in 69 us (40; all CTAs on the
+// prefix first 75); 8 groups of 16 after 1,003 to 4,099 tokens 61 us (40; 66); joint steps of eight rows, 16 groups of 16 after 128 to 896, 12 heads over 4 of
 // 64, 37 us (5); 8 candidates of one prompt of 517, by paged attention, 7.4 us.  Not kept: a single sub-tile's scores in both
 // sub-tiles' columns in turn, so that the next S runs under the softmax (66 us both, the document 75 -> 78).
 #include <algorithm>
@@ -73,8 +73,9 @@ struct Walk {
   Parts parts;
   int x, x1, base, g;            // the next place, the part's end; the group that it lies in, whose places begin at base
   int at, pieces;                // of the piece: its segment's record, and the CTAs that have pieces of it
-  // The CTAs that take parts; those of the kernel after this one, for each sequence's own keys, start on the SMs of the others.  They have
-  // kAhead of this kernel's share of all work, so that it ends before theirs does
+  // The CTAs that take parts; those of the kernel after this one, for each sequence's own keys, start on the SMs of the others.  This one
+  // has kAhead of its share of all work, so that it ends before the other does (1.1, 1.3, 1.5: 62.6, 61.8, 66.4 us for the
+  // groups above, 74.1, 69.9, 73.5 for the document)
   static __device__ __forceinline__ int ctas(const SharedCall& a, int lane, int total) {
     if (a.B > kMostCounted) return gridDim.x;
     float keys = 0.f;                           // of the sequences after their prefixes
@@ -520,7 +521,7 @@ const char* sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int 
 //   at about 10 TB/s, and two launches less); MB of those reads and us, paged and the better of the others:
 //     5: 7.9  10.9   24: 11.2  11.8   44: 9.3  11.8   66: 14.6  13.1   82: 16.2  15.8   120: 19.4  14.5   272: 47.2  37.2
 //   tiles of 16 or 32 rows, each reading the prefix, while those reads are few; MB and us, those and tcgen05:
-//     17: 14.5  17.7   28: 15.3  19.6   204: 38.1  36.8   629: 70.9  66.5   2,200: 252  75
+//     17: 14.5  17.7   28: 15.3  19.6   204: 38.1  37.2   629: 70.9  61.2   2,200: 252  69
 enum Way { PAGED, ROWS, TILES };
 constexpr double kPagedBytes = 48 << 20, kRowsBytes = 128 << 20;
 Way way_of(int B, int rows, int G, int Hkv, int hd, int64_t n_pages, int page, int width, int n) {
