@@ -148,7 +148,9 @@ __device__ __forceinline__ float min3f(float x, float y, float z) {
   asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
   return r;
 }
-// one thread's pass over its elements
+// One thread's pass over its elements.  LOW: it keeps the smallest too, and batches without a closed token go without
+// the clamps (the policy loss, 179 -> 173 us; the scores and their gradient, whose registers it costs, are 1.5 % slower so)
+template <bool LOW>
 struct Pass {
   Ref r;
   float most = -INFINITY;          // the largest logit
@@ -178,17 +180,17 @@ struct Pass {
   }
   template <int N>
   __device__ __forceinline__ void add(const Args& a, const float* v) {
-    float top = fmaxf(v[0], v[1]), low = fminf(v[0], v[1]);
+    float top = fmaxf(v[0], v[1]), low = LOW ? fminf(v[0], v[1]) : 0.f;
 #pragma unroll
     for (int i = 2; i < N; i += 2) {
       top = max3f(top, v[i], v[i + 1]);
-      low = min3f(low, v[i], v[i + 1]);
+      if (LOW) low = min3f(low, v[i], v[i + 1]);
     }
     most = fmaxf(most, top);
-    least = fminf(least, low);
+    if (LOW) least = fminf(least, low);
     if (top > r.limit) raise(a, top);
     const uint64_t c = f2(a.c2, a.c2), nm = f2(r.nm, r.nm);
-    if (!r.big && fmaf(low, a.c2, r.nm) > kLeast) {
+    if (LOW && !r.big && fmaf(low, a.c2, r.nm) > kLeast) {
 #pragma unroll
       for (int i = 0; i < N; i += 2) pair_of_open(fma_f2(f2(v[i], v[i + 1]), c, nm));
     } else if (!r.big) {
@@ -258,8 +260,8 @@ struct Scores {
 };
 // The row's sums against its largest reference, added in one fixed order; with `groups` the
 // groups' maxima in sh.group (of every CTA)
-template <int THREADS, int CS, bool GROUPS>
-__device__ __forceinline__ Scores reduce_row(const Args& a, Shared<THREADS>& sh, const Pass& ps) {
+template <int THREADS, int CS, bool GROUPS, bool LOW>
+__device__ __forceinline__ Scores reduce_row(const Args& a, Shared<THREADS>& sh, const Pass<LOW>& ps) {
   constexpr int WARPS = THREADS / 32, LANES = THREADS * CS / kGroups;      // LANES: threads of a group
   static_assert(!GROUPS || (LANES >= 1 && LANES <= 32), "a group lies in a warp");
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -556,7 +558,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
     const Row<T> row = row_at<T>(a, r);
     const Extra<T> ex(a, row, r, rank == 0);
     const int n = mine.have(row);
-    Pass ps;
+    Pass<false> ps;
 #pragma unroll 1
     for (int b = 0; b < batches; ++b) {
       mma::cp_wait<kRing<THREADS> - 2>();          // this batch has landed
@@ -566,12 +568,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores(const Args a
         float v[kBatch * N];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) Vec16<T>::unpack(s[j * THREADS], v + j * N);
-        ps.add<kBatch * N>(a, v);
+        ps.template add<kBatch * N>(a, v);
       } else {
         for (int j = 0; b * kBatch + j < n; ++j) {
           float v[N];
           Vec16<T>::unpack(s[j * THREADS], v);
-          ps.add<N>(a, v);
+          ps.template add<N>(a, v);
         }
       }
       slot = slot + 1 == kRing<THREADS> ? 0 : slot + 1;
@@ -715,8 +717,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
       if constexpr (POLICY) return PolicyIn(a.pol, r);
       else return 0;
     }();
-    Pass ps;
-#pragma unroll 1
+    Pass<POLICY> ps;
+#pragma unroll (POLICY ? 1 : kResident)
     for (int g = 0; g < kResident; ++g) {
       // this batch's copies are done, later ones may not be
       if (g == 0) mma::cp_wait<kResident - 1>();
@@ -728,13 +730,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
         float v[kBatch * N];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) Vec16<T>::unpack(s[j * THREADS], v + j * N);
-        ps.add<kBatch * N>(a, v);
+        ps.template add<kBatch * N>(a, v);
       } else {
-#pragma unroll 1
         for (int j = 0; g * kBatch + j < n; ++j) {
           float v[N];
           Vec16<T>::unpack(s[j * THREADS], v);
-          ps.add<N>(a, v);
+          ps.template add<N>(a, v);
         }
       }
     }
@@ -786,7 +787,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
       if (POLICY && zeros) x = 0.f;
       out[ex.edge_id] = from_f<T>(ex.edge_id == token ? x + at_token : x);
     }
-#pragma unroll 1
+#pragma unroll (POLICY ? 1 : kResident)
     for (int g = 0; g < kResident; ++g) {
 #pragma unroll
       for (int jj = 0; jj < kBatch; ++jj) {
@@ -795,18 +796,31 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
         float v[N];
         Vec16<T>::unpack(slots[j * THREADS + t], v);
         const int id0 = row.head + (mine.first + j * THREADS) * N;
-        if (plain && !(POLICY && zeros)) {
+        if constexpr (!POLICY) {
 #pragma unroll
           for (int e = 0; e < N; e += 2) {
-            const uint64_t x = f2(v[e], v[e + 1]), d = POLICY ? fma_f2(x, c2, nml2) : add_f2(fma_f2(x, c2, nm), nlogs);
+            const uint64_t x = f2(v[e], v[e + 1]);
+            float2 d;
+            if (!o.ref.big) d = f2_split(add_f2(fma_f2(x, c2, nm), nlogs));
+            else d = f2_split(add_f2(mul_f2(add_f2(x, nm), c2), nlogs));
+            d.x = fmaxf(d.x, kLeast);
+            d.y = fmaxf(d.y, kLeast);
+            const float2 y = f2_split(mul_f2(f2(ex2(d.x), ex2(d.y)), fma_f2(B2, f2(d.x, d.y), A2)));
+            v[e] = y.x;
+            v[e + 1] = y.y;
+          }
+        } else if (plain && !zeros) {
+#pragma unroll
+          for (int e = 0; e < N; e += 2) {
+            const uint64_t d = fma_f2(f2(v[e], v[e + 1]), c2, nml2);
             const float2 ds = f2_split(d);
-            const float2 y = f2_split(mul_f2(f2(ex2(ds.x), ex2(ds.y)), POLICY ? fma_f2(B12, d, A12) : fma_f2(B2, d, A2)));
+            const float2 y = f2_split(mul_f2(f2(ex2(ds.x), ex2(ds.y)), fma_f2(B12, d, A12)));
             v[e] = y.x;
             v[e + 1] = y.y;
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < N; ++e) v[e] = POLICY && zeros ? 0.f : value(fmaxf(log_p(v[e]), kLeast));
+          for (int e = 0; e < N; ++e) v[e] = zeros ? 0.f : value(fmaxf(log_p(v[e]), kLeast));
         }
         if ((unsigned)(token - id0) < (unsigned)N) {
 #pragma unroll
