@@ -259,7 +259,8 @@ int kf_op_token_scores_grad(int32_t type, int64_t R, int32_t V, const void* logi
  * as in kf_op_token_scores_grad (it may be the logits themselves).
  * Rows that the loss leaves out have loss 0 and a gradient of zeros, whatever else they hold: a weight of 0, and padding
  * (a negative token), whose logp and kl are 0 and whose ratio is 1.  A weight of a term that is 0
- * leaves that term out.  A row with every logit -inf: a gradient of zeros.  A row with a NaN or +inf: NaN.  A token closed by
+ * leaves that term out.  A row with every logit -inf: a gradient of zeros.  A row with a NaN or +inf: NaN; a NaN in its old_logp,
+ * advantage, weight (or ref_logp, with a KL term): a NaN loss and gradient.  A token closed by
  * -inf: ratio 0 and an infinite kl, which a kl_weight passes on to the loss (and NaN to the gradient).
  * A token >= V: KF_DEV_BAD_TOKEN, NaN numbers, a gradient of zeros.
  * Errors: KF_E_ARG, KF_E_CUDA.

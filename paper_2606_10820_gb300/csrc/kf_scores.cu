@@ -401,12 +401,13 @@ struct PolicyRow {
       }
     }
     if (w == 0.f) return;
-    const float gain = A > 0.f ? fminf(ratio, p.high) * A : fmaxf(ratio, p.low) * A;
-    const bool open = A > 0.f ? ratio <= p.high : ratio >= p.low;
+    // whether the clip decides (comparisons, false of a NaN: fminf and fmaxf would drop it, and the loss be a number)
+    const bool clipped = A > 0.f ? ratio > p.high : A < 0.f && ratio < p.low;
+    const float gain = (!clipped ? ratio : A > 0.f ? p.high : p.low) * A;
     const float k = p.kl_weight == 0.f ? 0.f : p.kl_weight * kl, gk = p.kl_weight == 0.f ? 0.f : p.kl_weight * em1;
     const float c = p.entropy_weight == 0.f ? 0.f : p.entropy_weight * o.H;
     loss = w * (k - gain - c);
-    gl = w * (-gk - (open ? ratio * A : 0.f));
+    gl = w * (-gk - (clipped ? 0.f : ratio * A));
     gh = -w * p.entropy_weight;
   }
 };
