@@ -103,44 +103,43 @@ __device__ __forceinline__ float2 turn(int pos, uint64_t turns, bool bad) {
   return bad ? make_float2(NAN, NAN) : make_float2(c, s);
 }
 
-// Where a lane's two vectors lie in a head, and the first of its angles
+// Where a lane's two vectors lie in a head, the first of its angles, and which of its pairs are turned at all (an angle of 0 would
+// not leave the others as they are: 0 times an infinity is no number)
 template <int HD, bool NB>
 struct Place {
   static constexpr int LANES = HD / 16, PER = 32 / LANES;
-  int c0, c1, a0;                // vectors; angle (NB: of the first vector, the second's are HD / 4 on); < 0: none
+  int c0, c1, a0;                // vectors; angle (NB: of the first vector, the second's are HD / 4 on)
+  bool on[2];                    // the first and the last four of its pairs
   __device__ __forceinline__ Place(int lane, int n) {
     const int l = lane % LANES, n8 = n / 8;
     if (NB) {
       c0 = l;
       c1 = l + LANES;
       a0 = 4 * l;
-    } else if (l < n8) {
-      c0 = l;
-      c1 = l + n8;
-      a0 = 8 * l;
+      on[0] = a0 < n;
+      on[1] = HD / 4 + a0 < n;
     } else {
-      c0 = 2 * n8 + (l - n8);
-      c1 = c0 + (HD - 16 * n8) / 16;
-      a0 = HD / 2;               // past the angles: not turned
+      on[0] = on[1] = l < n8;
+      c0 = on[0] ? l : 2 * n8 + (l - n8);
+      c1 = c0 + (on[0] ? n8 : (HD - 16 * n8) / 16);
+      a0 = on[0] ? 8 * l : 0;
     }
   }
 };
 
-// A token's angles to the warp's table: cosine and sine of each pair, (1, 0) past the last
+// A token's angles to the warp's table: cosine and sine of each pair that is turned
 template <int HD>
 __device__ __forceinline__ void fill_table(const Args& a, float2* tab, int pos, int lane) {
   __syncwarp();                  // (the token before is through with it)
 #pragma unroll
-  for (int i = lane; i < HD / 2; i += 32) {
-    float2 v = make_float2(1.f, 0.f);
+  for (int i = lane; i < HD / 2; i += 32)
     if (i < a.n) {
       bool bad;
       const uint64_t t = turns_of(__ldg(a.freq + i), &bad);
-      v = turn(pos, t, bad);
+      float2 v = turn(pos, t, bad);
       v.y *= a.sign;
+      tab[i] = v;
     }
-    tab[i] = v;
-  }
   __syncwarp();
 }
 // The 8 pairs of a lane
@@ -151,8 +150,7 @@ struct Angles {
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
       const int i = NB ? pl.a0 + (e < 4 ? e : HD / 4 + e - 4) : pl.a0 + e;
-      float4 v = make_float4(1.f, 0.f, 1.f, 0.f);
-      if (i < HD / 2) v = *reinterpret_cast<const float4*>(tab + i);
+      const float4 v = *reinterpret_cast<const float4*>(tab + i);      // (of a pair that is not turned: anything)
       c[e] = v.x;
       s[e] = v.y;
       c[e + 1] = v.z;
@@ -162,13 +160,21 @@ struct Angles {
   // x: the lane's 16 elements of a head
   static constexpr __device__ __forceinline__ int first(int e) { return NB ? 2 * e : e; }
   static constexpr __device__ __forceinline__ int second(int e) { return NB ? 2 * e + 1 : e + 8; }
-  __device__ __forceinline__ void turn_head(float* x) const {
+  __device__ __forceinline__ void turn_pairs(float* x, int from, int to) const {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = from; e < to; ++e) {
       float &a = x[first(e)], &b = x[second(e)];
       const float y = fmaf(a, c[e], -b * s[e]);
       b = fmaf(b, c[e], a * s[e]);
       a = y;
+    }
+  }
+  __device__ __forceinline__ void turn_head(float* x, const Place<HD, NB>& pl) const {
+    if constexpr (NB) {
+      if (pl.on[0]) turn_pairs(x, 0, 4);
+      if (pl.on[1]) turn_pairs(x, 4, 8);
+    } else {
+      if (pl.on[0]) turn_pairs(x, 0, 8);
     }
   }
 };
@@ -328,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, 6) k_rotate(const __grid_constant__ 
         for (int e = 0; e < 16; ++e) x[e] *= r;
       }
     }
-    an.turn_head(x);
+    an.turn_head(x, pl);
     if (!is_v) {
       o[0] = Vec16<T>::pack(x);
       o[1] = Vec16<T>::pack(x + 8);
@@ -416,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_back(const __grid_constant__ Ar
     float x[16], d[16];
     unpack16<T>(ux, x);
     unpack16<T>(ud, d);
-    an.turn_head(d);
+    an.turn_head(d, pl);
     float ss = 0.f, sg = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
