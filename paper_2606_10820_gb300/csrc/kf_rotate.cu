@@ -23,6 +23,7 @@
 // in turn instead of in stretches (57 -> 59, the gradients 85 -> 95).
 #include <algorithm>
 #include <climits>
+#include <cstdlib>
 
 #include "kf_mma.cuh"
 #include "kf_serving.cuh"
@@ -556,6 +557,15 @@ const char* rows_fault(const void* p, int64_t row, int64_t head) {
     if (s % 8 || s < 0 || s > (1ll << 37)) return "strides are multiples of 8 elements";
   return nullptr;
 }
+// whether two of an output's heads share an element: |x row - y head| < hd for some x < T and y < H that are not both 0
+bool heads_meet(int64_t T, int64_t H, int64_t row, int64_t head, int64_t hd) {
+  if ((T > 1 && row < hd) || (H > 1 && head < hd)) return true;
+  if (T == 1 || row >= (H - 1) * head + hd) return false;
+  for (int64_t y = 1; y < H; ++y)
+    for (const int64_t x : {y * head / row, y * head / row + 1})
+      if (x < T && std::abs(x * row - y * head) < hd) return true;
+  return false;
+}
 
 }  // namespace
 }  // namespace kf
@@ -575,8 +585,9 @@ extern "C" int kf_op_rotate_heads(int32_t type, int64_t T, int32_t Hq, int32_t H
   if (const char* f = rows_fault(q_out, q_out_row, q_out_head)) return refuse(what, f);
   if (const char* f = rows_fault(k_out, k_out_row, k_out_head)) return refuse(what, f);
   if (!pos || !aligned(pos, 4)) return refuse(what, "positions: null or misaligned");
-  if ((T > 1 && (q_out_row < hd || k_out_row < hd)) || (Hq > 1 && q_out_head < hd) || (Hkv > 1 && k_out_head < hd))
+  if (heads_meet(T, Hq, q_out_row, q_out_head, hd) || heads_meet(T, Hkv, k_out_row, k_out_head, hd))
     return refuse(what, "an output's heads lie over each other");
+  if (q_out == k_out && !(q_out == q && k_out == k)) return refuse(what, "q_out and k_out are one array");
   if ((q_out == q && (q_out_row != q_row || q_out_head != q_head)) || (k_out == k && (k_out_row != k_row || k_out_head != k_head)))
     return refuse(what, "an output over its input has its strides");
   Args a{};
