@@ -198,10 +198,13 @@ def head_step(model: Model, answer, tau=1.0):
 def policy_step(model: Model, answer, reward, clip=(0.2, 0.28), kl_weight=0.01, entropy_weight=0.0, ref_logp=None, tau=1.0):
     """The clipped policy loss of all answers' tokens under reward [prompts, n], and the LM head's gradient [V, d].
 
-    An answer's advantage is its reward against its prompt's other answers (their mean, in units of their deviation); the tokens'
-    scores as they were drawn are the old policy's, and the reference's where ref_logp [prompts, n, steps] is not given."""
+    An answer's advantage is its reward against its prompt's other answers (their mean, in units of their deviation; 0 where there
+    are none); the tokens' scores as they were drawn are the old policy's, and the reference's where ref_logp [prompts, n, steps] is
+    not given."""
     P, n, steps = answer["tokens"].shape
-    advantage = (reward - reward.mean(1, keepdim=True)) / (reward.std(1, keepdim=True) + 1e-6)
+    advantage = reward - reward.mean(1, keepdim=True)
+    if n > 1:      # (the deviation of one is no number)
+        advantage = advantage / (reward.std(1, keepdim=True) + 1e-6)
     old = answer["logp"].flatten()
     rows = answer["rows"].flatten(0, 1)
     out = serving.policy_loss(rows @ model.head.T, answer["tokens"].flatten(), old, advantage.float().repeat_interleave(steps),
