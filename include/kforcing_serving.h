@@ -45,8 +45,8 @@ extern "C" {
  * then its pairs (y_i, y_i+n), or with neighbours (y_2i, y_2i+1), i < n, turned by the angle pos freq[i]:
  *   (a, b) -> (a cos - b sin, b cos + a sin);  elements 2 n .. hd - 1 stay as they are.
  * n: n_freq, a multiple of 8, at most hd / 2 (0: norms alone).  freq: fp64 [n], on the device, finite and below 2^32
- * in magnitude (NaN heads otherwise); pos: int32 [T], any values.  Angles are exact to 2^-24 of a
- * turn's radius at every position; norms and products are fp32, rounded once to the type.  A head whose squares
+ * in magnitude (NaN heads otherwise); pos: int32 [T], any values.  Angles (less whole quarter turns) are exact to 2^-24 at every
+ * position and frequency; norms and products are fp32, rounded once to the type.  A head whose squares
  * pass fp32's range comes out as zeros or NaN.  Weights: [hd] of the heads' type, 16-byte aligned.
  * q [T][Hq][hd] and k [T][Hkv][hd]: elements of a head contiguous, *_row / *_head the strides of tokens and heads in
  * elements (multiples of 8); q_out and k_out likewise.  An output may be its input itself (same strides), and

@@ -7,7 +7,7 @@
 //   dw = sum g xh,  dx = r (g w - xh mean(g w xh)),  xh = x r.
 //
 // Angles: freq_i / 2 pi turns as a fraction of 64 bits; times the position (mod 2^64) it leaves the
-// fraction of a turn with an error below pos 2^-64, where a product in fp32 would have lost the angle
+// fraction of a turn with an error of at most |pos| 2^-64 (2^-33 of a turn), where a product in fp32 would have lost the angle
 // from positions of a few thousand on.  The nearest quarter turn comes off in whole numbers, so the
 // sine and cosine are taken of |t| <= pi / 4.
 //
@@ -69,16 +69,16 @@ struct Args {
   float eps, sign;               // eps < 0: no norms; sign: -1 turns back
 };
 
-// freq / 2 pi mod 1 as a fraction of 64 bits: the mantissa times 2^66 / 2 pi (2^63 <= it < 2^64), shifted.  NaN,
-// infinities and |freq| >= 2^32: *bad
+// freq / 2 pi mod 1 as a fraction of 64 bits: the mantissa times 2^130 / 2 pi (two words; of one alone a far position of a large frequency
+// would keep little: 1.1e-2 at 2^31 and 4e9), shifted; at most 1 of its last place too small.  NaN, infinities and |freq| >= 2^32: *bad
 __device__ __forceinline__ uint64_t turns_of(double freq, bool* bad) {
-  constexpr uint64_t k = 11743562013128004906ull;      // round(2^66 / 2 pi)
+  constexpr uint64_t k = 11743562013128004905ull, k_low = 18169587780923219392ull;      // 2^130 / 2 pi
   const uint64_t u = (uint64_t)__double_as_longlong(freq);
   const int e = (int)(u >> 52) & 0x7ff;
   const uint64_t m = (u & 0xfffffffffffffull) | (e ? 1ull << 52 : 0ull);
   *bad = e >= 1023 + 32;
-  // m 2^(e - 1075) / 2 pi 2^64 = (m k) 2^(e - 1077): to the right by 22 and more
-  const uint64_t hi = __umul64hi(m, k), lo = m * k;
+  // m 2^(e - 1075) / 2 pi 2^64 = (m k) 2^(e - 1077): to the right by 23 and more
+  const uint64_t lo = m * k + __umul64hi(m, k_low), hi = __umul64hi(m, k) + (lo < m * k);
   const int s = *bad ? 127 : 1077 - max(e, 1);
   uint64_t t;
   if (s < 64) t = (hi << (64 - s)) | (lo >> s);
