@@ -510,22 +510,24 @@ int64_t layout(SharedCall& c, bool tiles, void* work) {
 }
 const char* sizes_fault(int B, int rows, int Hq, int Hkv, int hd, int page, int width, int n) {
   if (const char* f = paged_sizes_fault(B, rows, Hq, Hkv, hd, page, width)) return f;
-  if (n < 0 || (B > 0 && n < 1) || n > (1 << 24)) return "groups out of range";
-  const int64_t tiles = 2 * ((int64_t)B * ceil_div(rows * (Hq / Hkv), 16) + n + 1) * Hkv;      // of 16 rows, over prefixes and own keys
-  if ((int64_t)B * rows * Hq > (1 << 30) || tiles > (1 << 30)) return "too many rows and heads";
-  if (tiles * ((int64_t)width * page / 16 + 8) > 0x7fffffff) return "too many keys";
+  if (n < 0 || (B > 0 && n < 1)) return "groups out of range";
   return nullptr;
 }
+// whether places, records and rows of these sizes can be counted in 31 bits
+bool countable(int B, int rows, int G, int Hkv, int page, int width, int n) {
+  const int64_t tiles = 2 * ((int64_t)B * ceil_div(rows * G, 16) + n + 1) * Hkv;      // of 16 rows, over prefixes and own keys
+  return n <= (1 << 24) && (int64_t)B * rows * G * Hkv <= (1 << 30) && tiles <= (1 << 30) && tiles * ((int64_t)width * page / 16 + 8) <= 0x7fffffff;
+}
 // What reads a call's prefixes.  The lengths are on the device, so the rule takes what the table and the pool could hold:
-//   paged attention, once a sequence, where nothing is shared or the reads of all sequences would be few (they come from L2
-//   at about 10 TB/s, and two launches less); MB of those reads and us, paged and the better of the others:
+//   paged attention, once a sequence, where nothing is shared, sizes pass what the others count in, or the reads of all sequences
+//   would be few (they come from L2 at about 10 TB/s, and two launches less); MB of those reads and us, paged and the better of the others:
 //     5: 7.9  10.9   24: 11.2  11.8   44: 9.3  11.8   66: 14.6  13.1   82: 16.2  15.8   120: 19.4  14.5   272: 47.2  37.2
 //   tiles of 16 or 32 rows, each reading the prefix, while those reads are few; MB and us, those and tcgen05:
 //     17: 14.5  17.7   28: 15.3  19.6   204: 38.1  37.2   629: 70.9  61.2   2,200: 252  69
 enum Way { PAGED, ROWS, TILES };
 constexpr double kPagedBytes = 48 << 20, kRowsBytes = 128 << 20;
 Way way_of(int B, int rows, int G, int Hkv, int hd, int64_t n_pages, int page, int width, int n) {
-  if (n >= B || n_pages == 0) return PAGED;
+  if (n >= B || n_pages == 0 || !countable(B, rows, G, Hkv, page, width, n)) return PAGED;
   const int seg = plan_rows(rows * G, hd).seg_rows;
   const double keys = (double)std::min((int64_t)width, n_pages) * page * hd * 4 * Hkv;      // bytes of a prefix, at most
   if ((double)B * ceil_div(rows * G, seg) * keys <= kPagedBytes) return PAGED;
