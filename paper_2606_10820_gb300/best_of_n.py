@@ -71,22 +71,22 @@ class Model:
         a, b = x[..., :half].float(), x[..., half:].float()
         return torch.cat([a * cos - b * sin, b * cos + a * sin], -1).bfloat16()
 
-    def heads(self, layer, q, k, pos):
-        """The rotated query and key heads."""
-        if self.turn[layer]:
+    def heads(self, layer, q, k, pos, exact=False):
+        """The rotated query and key heads (exact: by rotate_heads also without norms, as rotate_append rotates)."""
+        if exact or self.turn[layer]:
             return serving.rotate_heads(q, k, pos.int(), self.freq, **self.turn[layer])
         return self.rotate(q, pos), self.rotate(k, pos)
 
-    def run(self, tokens, pos, attend, raw=False):
+    def run(self, tokens, pos, attend, raw=False, exact=False):
         """The final hidden rows [T, d] bf16 of tokens at pos; attend(layer, q, k, v) -> [T, heads, hd], of rotated heads
-        (raw: of the projections' own)."""
+        (raw: of the projections' own; exact: see heads)."""
         c = self.cfg
         h = self.emb[tokens].float()
         for i, (wqkv, wo, up, down) in enumerate(self.layers):
             qkv = (self.norm(h) @ wqkv.T).view(len(h), -1, c.hd)
             q, k, v = qkv.split([c.heads, c.kv_heads, c.kv_heads], 1)
             if not raw:
-                q, k = self.heads(i, q, k, pos)
+                q, k = self.heads(i, q, k, pos, exact)
             o = attend(i, q, k, v)
             h = h + (o.reshape(len(h), -1) @ wo.T).float()
             h = h + (torch.nn.functional.gelu(self.norm(h) @ up.T, approximate="tanh") @ down.T).float()
@@ -143,8 +143,9 @@ def best_of_n(model: Model, prompts, n, steps, noise, tau=1.0, shared=False):
         cache.append(layer, k, v, starts, owners)
         return serving.prompt_attention(q, k, v, starts, max(lens))
 
-    # (the prompts' rotated keys are read by their own attention: they are wanted as rows, not in pages alone)
-    rows = model.run(ids, pos, whole)[(starts[1:] - 1).long()]
+    # (the prompts' rotated keys are read by their own attention: they are wanted as rows, not in pages alone; the angles of all
+    # keys of a cache come from one rotation)
+    rows = model.run(ids, pos, whole, exact=shared)[(starts[1:] - 1).long()]
 
     # candidate i of prompt p in slot P + p n + i
     slots = _ints(range(P, P * (1 + n)))
