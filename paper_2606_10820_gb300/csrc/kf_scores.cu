@@ -101,7 +101,9 @@ __device__ __forceinline__ float ex2(float x) {
 // vector; the entropy's cancellation, 2^-24 of kRaise, stays below 2e-6.)  In base-2 units one fused
 // multiply-add gives an element's difference, and what the reference lost in rounding is a factor of S and T alike that
 // cancels; past kLarge (rows at a mask's value, a small tau) that factor would leave fp32's range,
-// so there the logits' difference is formed first and scaled after
+// so there the logits' difference is formed first and scaled after.
+// WHOLE (the policy loss, not where big): references are whole numbers in base-2 units, so that a move from one to another multiplies by a
+// power of two and loses nothing
 struct Ref {
   float raw, nm;                   // nm: minus the reference, base-2 units (a logit where big)
   float limit;                     // a logit past this raises the reference
@@ -110,12 +112,17 @@ struct Ref {
     const float m = fabsf(r * a.inv_tau);
     return m >= kLarge && m < INFINITY;
   }
+  template <bool WHOLE>
+  static __device__ __forceinline__ float units(const Args& a, float r) {
+    return WHOLE ? rintf(__fmul_rn(r, a.c2)) : __fmul_rn(r, a.c2);
+  }
+  template <bool WHOLE>
   __device__ __forceinline__ void set(const Args& a, float r) {
     const float m = r * a.inv_tau;
     raw = r;
     limit = r == -INFINITY ? r : r + a.margin;
     big = large(a, r);
-    nm = m == -INFINITY ? 0.f : big ? -r : -__fmul_rn(r, a.c2);
+    nm = m == -INFINITY ? 0.f : big ? -r : -units<WHOLE>(a, r);
   }
   __device__ __forceinline__ bool open(const Args& a) const { return raw * a.inv_tau != -INFINITY; }
   // log2 of exp(x - m)
@@ -123,9 +130,10 @@ struct Ref {
     return big ? (v + nm) * a.c2 : fmaf(v, a.c2, nm);
   }
   // log2 of exp(m' - m) for an open reference m' of the logit `from`, both as they were rounded
+  template <bool WHOLE>
   __device__ __forceinline__ float less_ref(const Args& a, float from) const {
     if (large(a, from)) return less(a, from);
-    const float was = __fmul_rn(from, a.c2);
+    const float was = units<WHOLE>(a, from);
     return big ? fmaf(nm, a.c2, was) : __fadd_rn(was, nm);      // (no fused multiply-add)
   }
 };
@@ -135,8 +143,9 @@ struct Ref {
 struct Sums {
   float raw, s, t;
   // against the reference r (at or above this one)
+  template <bool WHOLE>
   __device__ __forceinline__ void move_to(const Args& a, const Ref& r) {
-    const float d = raw * a.inv_tau == -INFINITY ? 0.f : fmaxf(r.less_ref(a, raw), kLeast), f = ex2(d);
+    const float d = raw * a.inv_tau == -INFINITY ? 0.f : fmaxf(r.less_ref<WHOLE>(a, raw), kLeast), f = ex2(d);
     t = f * fmaf(d, s, t);
     s *= f;
     raw = r.raw;
@@ -148,8 +157,19 @@ __device__ __forceinline__ float min3f(float x, float y, float z) {
   asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
   return r;
 }
-// One thread's pass over its elements.  LOW: it keeps the smallest too, and batches without a closed token go without
-// the clamps (the policy loss, 179 -> 173 us; the scores and their gradient, whose registers it costs, are 1.5 % slower so)
+// the largest of a warp's numbers (all 32 lanes call it)
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+// One thread's pass over its elements.  LOW, the policy loss: it keeps the smallest too, and batches without a closed token go
+// without the clamps (179 -> 173 us; the scores and their gradient, whose registers it costs, are 1.5 % slower so).  What its S may
+// lose, log p and the ratio do, and kl = e^u - 1 - u twice that over u.  So the references are whole numbers and at first the warp's largest (exponents round at
+// their size), and S is added up a batch at a time: an addition to a sum that holds the row's largest term (a quarter of S, where
+// the logits deviate by four) rounds at that term's size, and one chain of fifty of them lost most.  4096 x 50257 bf16, log p off by
+// (root of the mean) and us: 1.2e-7 and 174.8 with none of it, 9.0e-8 by batches, 7.5e-8 and 176.0 with whole references,
+// 6.6e-8 and 177.7 with the warp's (not kept: with joins in two parts instead 6.1e-8 and 182)
 template <bool LOW>
 struct Pass {
   Ref r;
@@ -159,27 +179,29 @@ struct Pass {
   __device__ __forceinline__ Pass() : r{-INFINITY, 0.f, -INFINITY, false} {}
   __device__ __forceinline__ void raise(const Args& a, float to) {
     const Ref was = r;
-    r.set(a, to);
+    r.template set<LOW>(a, to);
     if (was.open(a)) {
-      const float d = fmaxf(r.less_ref(a, was.raw), kLeast), f = ex2(d);
+      const float d = fmaxf(r.template less_ref<LOW>(a, was.raw), kLeast), f = ex2(d);
       t = mul_f2(f2(f, f), fma_f2(f2(d, d), s, t));
       s = mul_f2(f2(f, f), s);
     }
   }
-  __device__ __forceinline__ void pair(float2 d) {
+  // (to: the sum that S's part goes to)
+  __device__ __forceinline__ void pair(float2 d, uint64_t& to) {
     const uint64_t e = f2(ex2(d.x), ex2(d.y));
-    s = add_f2(s, e);
+    to = add_f2(to, e);
     t = fma_f2(e, f2(fmaxf(d.x, kLeast), fmaxf(d.y, kLeast)), t);
   }
   // (differences above kLeast)
-  __device__ __forceinline__ void pair_of_open(uint64_t d) {
+  __device__ __forceinline__ void pair_of_open(uint64_t d, uint64_t& to) {
     const float2 x = f2_split(d);
     const uint64_t e = f2(ex2(x.x), ex2(x.y));
-    s = add_f2(s, e);
+    to = add_f2(to, e);
     t = fma_f2(e, d, t);
   }
+  // first (uniform over the warp, LOW): the reference is the whole warp's largest
   template <int N>
-  __device__ __forceinline__ void add(const Args& a, const float* v) {
+  __device__ __forceinline__ void add(const Args& a, const float* v, bool first = false) {
     float top = fmaxf(v[0], v[1]), low = LOW ? fminf(v[0], v[1]) : 0.f;
 #pragma unroll
     for (int i = 2; i < N; i += 2) {
@@ -188,23 +210,26 @@ struct Pass {
     }
     most = fmaxf(most, top);
     if (LOW) least = fminf(least, low);
-    if (top > r.limit) raise(a, top);
+    if (LOW && first) raise(a, warp_max(top));
+    else if (top > r.limit) raise(a, top);
     const uint64_t c = f2(a.c2, a.c2), nm = f2(r.nm, r.nm);
+    uint64_t batch = 0ull, &to = LOW ? batch : s;
     if (LOW && !r.big && fmaf(low, a.c2, r.nm) > kLeast) {
 #pragma unroll
-      for (int i = 0; i < N; i += 2) pair_of_open(fma_f2(f2(v[i], v[i + 1]), c, nm));
+      for (int i = 0; i < N; i += 2) pair_of_open(fma_f2(f2(v[i], v[i + 1]), c, nm), to);
     } else if (!r.big) {
 #pragma unroll
-      for (int i = 0; i < N; i += 2) pair(f2_split(fma_f2(f2(v[i], v[i + 1]), c, nm)));
+      for (int i = 0; i < N; i += 2) pair(f2_split(fma_f2(f2(v[i], v[i + 1]), c, nm)), to);
     } else {
 #pragma unroll
-      for (int i = 0; i < N; i += 2) pair(f2_split(mul_f2(add_f2(f2(v[i], v[i + 1]), nm), c)));
+      for (int i = 0; i < N; i += 2) pair(f2_split(mul_f2(add_f2(f2(v[i], v[i + 1]), nm), c)), to);
     }
+    if (LOW) s = add_f2(s, batch);
   }
   __device__ __forceinline__ void add_one(const Args& a, float v) {
     most = fmaxf(most, v);
     if (v > r.limit) raise(a, v);
-    pair(make_float2(r.less(a, v), -INFINITY));
+    pair(make_float2(r.less(a, v), -INFINITY), s);
   }
   __device__ __forceinline__ Sums sums() const {
     const float2 x = f2_split(s), y = f2_split(t);
@@ -288,8 +313,8 @@ __device__ __forceinline__ Scores reduce_row(const Args& a, Shared<THREADS>& sh,
     cl.sync();
     for (int c = 0; c < CS; ++c) m = fmaxf(m, cl.map_shared_rank(&sh, c)->cta_ref);
   }
-  o.ref.set(a, m);
-  su.move_to(a, o.ref);
+  o.ref.template set<LOW>(a, m);
+  su.template move_to<LOW>(a, o.ref);
 #pragma unroll
   for (int i = 16; i; i >>= 1) {
     su.s += __shfl_xor_sync(~0u, su.s, i);
@@ -373,9 +398,9 @@ struct PolicyRow {
         x = make_float2(__fmul_rn(d, a.c2), 0.f);
         lo = fmaf(d, a.c2, -x.x);
       }
-      // (what c2 lost in rounding, of the token's difference and of S: d log2 S / d c = sum p (v - m))
-      const float mean = (o.logs - o.H * kLog2e) / a.c2;
-      lo += x.y + fmaf(at_logit - o.ref.raw - mean, p.c2_low, -log2f(f));
+      // (what c2 lost in rounding, of the token's difference and of S: d log2 S / d c = sum p (v - m), with m the reference as it was rounded)
+      const float mean = o.logs - o.H * kLog2e;
+      lo += x.y + fmaf((x.x - mean) / a.c2, p.c2_low, -log2f(f));
       x = two_sum(x.x, -e);
       x = two_sum(x.x, x.y + lo);
       if (!(fabsf(x.x) < INFINITY)) x = make_float2(o.lp(a, at_logit) * kLog2e, 0.f);
@@ -719,6 +744,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
       else return 0;
     }();
     Pass<POLICY> ps;
+    const bool together = POLICY && __all_sync(~0u, kBatch <= n);      // all lanes have a first batch
 #pragma unroll (POLICY ? 1 : kResident)
     for (int g = 0; g < kResident; ++g) {
       // this batch's copies are done, later ones may not be
@@ -731,7 +757,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_grad(const A
         float v[kBatch * N];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) Vec16<T>::unpack(s[j * THREADS], v + j * N);
-        ps.template add<kBatch * N>(a, v);
+        ps.template add<kBatch * N>(a, v, together && g == 0);
       } else {
         for (int j = 0; g * kBatch + j < n; ++j) {
           float v[N];
