@@ -307,7 +307,7 @@ struct Softmax {
     return true;
   }
   // The same in a third of the code: the scores come from TMEM twice, 64 at a time, for their maximum and for P.  A call of a few
-  // tiles is mostly the first run through its code, at about 15 clocks an instruction: the first tile took 6,000 to 12,000 clocks as above.
+  // tiles is mostly the first run through its code, at 12 to 15 clocks an instruction: the first tile took 6,000 to 12,000 clocks as above.
   // mask(c, s): closed scores among the 64 from 64 c on
   template <typename B, typename M>
   __device__ __forceinline__ bool short_tile(B& b, float sc, bool first, int g, float& m, float& l, int* err, M mask) const {

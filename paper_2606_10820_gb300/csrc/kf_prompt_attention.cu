@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(int n, int T, int longest
 }
 
 // ------------------------------------------------------------------ the products
+// (themselves in kf_attn_pair.cuh; here, how a CTA takes the next ones)
 // Cluster launch control: a running CTA cancels one that has not started and does its work (the
 // hardware's queue instead of a counter in memory that a call would have to clear)
 __device__ __forceinline__ void ask_for_cta(uint64_t* answer, uint64_t* bar) {

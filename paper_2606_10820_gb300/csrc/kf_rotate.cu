@@ -17,9 +17,9 @@
 // passes ahead, across tokens; no thread waits for another's), so the loads under way do not
 // cost registers; a token's angles are computed once by the warp's lanes and passed on through shared memory.
 // Measured (GPU time, bf16): 16,411 tokens, 32 + 8 heads of 128, norms, in 58 us (5.8 TB/s; with the loads in registers, four
-// passes ahead, 73); 24,361 tokens and V to pages, fp16, in 104 us (5.8 TB/s); eight rows of 256 sequences, 12 + 4 heads of 64, in 5.9 us
-// (the chain of starts, slot, length and page: 7.5 a token at a time); the gradients of 16,384 tokens in 86 us (5.8 TB/s; 127 with the loads
-// in registers, 92 with the weights read a pass); 8 tokens in 2.1 us.  Not kept: the weights multiplied into the turns (57 -> 61), tokens dealt out
+// passes ahead, 73); 24,361 tokens and V to pages, fp16, in 105 us (5.7 TB/s); eight rows of 256 sequences, 12 + 4 heads of 64, in 6.1 us
+// (the chain of starts, slot, length and page: 7.5 a token at a time); the gradients of 16,384 tokens in 88 us (5.7 TB/s; 127 with the loads
+// in registers, 92 with the weights read a pass); 8 tokens in 2.0 us.  Not kept: the weights multiplied into the turns (57 -> 61), tokens dealt out
 // in turn instead of in stretches (57 -> 59, the gradients 85 -> 95).
 #include <algorithm>
 #include <climits>

@@ -33,7 +33,7 @@
 // computes them: a broadcast would cost a barrier).
 //
 // Measured: 4096 bf16 rows of 50257 in 96 us with eight alternatives (4.3 TB/s), 72 without (5.7); 8 fp32
-// rows 7.5; the gradient of 2048 bf16 rows 86 us (4.8 TB/s); the policy loss of 4096 in 173 us (4.8 TB/s), of 61 fp32 rows in
+// rows 7.5; the gradient of 2048 bf16 rows 86 us (4.8 TB/s); the policy loss of 4096 in 177 us (4.7 TB/s), of 61 fp32 rows in
 // 10 us.  The gradient's passes take 20 instructions an element, 62 % of the issue slots: two rows fill an SM's shared
 // memory, so two CTAs take turns at loads, barriers and arithmetic.  Measured and not kept: the
 // arithmetic on single numbers instead of pairs (fewer moves, more of the fma pipe: 194 us for 179).

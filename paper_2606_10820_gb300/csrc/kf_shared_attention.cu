@@ -29,7 +29,10 @@ constexpr int kPrefixRows = 256;                     // query rows of a segment
 constexpr int kExtra = 3;                            // a segment's start and end, in tiles
 constexpr float kAhead = 1.3f;                       // see Walk::ctas
 constexpr float kTileUnits = 9.f;                    // units of own keys (8 KB of K and V) that take as long as a tile of a prefix
-constexpr int kMostCounted = 1024;                   // sequences whose lengths are added up
+// Sequences whose lengths are added up (by one warp of each CTA).  Of more there is work for all SMs on either side, and the
+// adding costs more than the split wins: 80 groups of 16 after 1,003 to 4,099 tokens 475 us without and 482 with, 256 of 16 983 and 1,130, 8 of
+// 256 after 4,000 to 16,000 449 and 505; joint steps of 80 groups of 16 134 and 142
+constexpr int kMostCounted = 1024;
 constexpr int kMinTiles = 2;                         // places of a CTA, at least
 
 struct Item {
@@ -518,7 +521,9 @@ bool countable(int B, int rows, int G, int Hkv, int page, int width, int n) {
   const int64_t tiles = 2 * ((int64_t)B * ceil_div(rows * G, 16) + n + 1) * Hkv;      // of 16 rows, over prefixes and own keys
   return n <= (1 << 24) && (int64_t)B * rows * G * Hkv <= (1 << 30) && tiles <= (1 << 30) && tiles * ((int64_t)width * page / 16 + 8) <= 0x7fffffff;
 }
-// What reads a call's prefixes.  The lengths are on the device, so the rule takes what the table and the pool could hold:
+// What reads a call's prefixes.  The lengths are on the device, so the rule takes what the table and the pool could hold.  (Short prefixes in
+// a table of a model's longest context so go a slower way than they could: eight candidates after 517 tokens, 12 heads over 4 of 64, in tables of
+// 592 to 4,096, 8,192 to 32,768 and 131,072 tokens 7.5, 10.4 and 13.0 us; 32 over 8 of 128 in 1,024, 8,192 and 131,072 10.5, 11.1 and 14.5.)
 //   paged attention, once a sequence, where nothing is shared, sizes pass what the others count in, or the reads of all sequences
 //   would be few (they come from L2 at about 10 TB/s, and two launches less); MB of those reads and us, paged and the better of the others:
 //     5: 7.9  10.9   24: 11.2  11.8   44: 9.3  11.8   66: 14.6  13.1   82: 16.2  15.8   120: 19.4  14.5   272: 47.2  37.2

@@ -95,7 +95,8 @@ def shared_attention(q, pool, table, lens, groups, shared, scale=None, out=None)
     """``paged_attention`` of groups of sequences that begin with the same tokens, which are read once a group.
 
     groups [n + 1] int32 on the GPU: sequences groups[g] .. groups[g + 1] - 1 are group g; shared [n] int32: the tokens that
-    they have in common (at most the shortest's), in every one's table row, as ``pages_fork`` leaves them."""
+    they have in common (at most the shortest's), in every one's table row, as ``pages_fork`` leaves them.  What reads a prefix goes by
+    the table's width, so one of the columns that the longest sequence fills is faster for short prefixes than a wider one."""
     return (_m or _load()).shared_attention(q, pool, table, lens, groups, shared, scale, out)
 
 
