@@ -386,7 +386,7 @@ struct PolicyRow {
     if (o.bad) x = make_float2(NAN, 0.f);
     else if (o.none) x = make_float2(-INFINITY, 0.f);
     else {
-      const int bits = __float_as_int(o.s);       // (S is 1 at least: the reference is an element)
+      const int bits = __float_as_int(o.s);       // (S is above a half: the reference is an element to half a unit)
       const float e = (float)((bits >> 23) - 127), f = __int_as_float((bits & 0x7fffff) | 0x3f800000);
       float lo;
       if (!o.ref.big) {
